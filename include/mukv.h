@@ -535,6 +535,113 @@ int mukv_gather_multi(mukv_ctx *const *ctxs, int32_t n_ctx, const int32_t *const
 int mukv_gather_kv(mukv_ctx *ctx, const int32_t *frame_idx, int32_t B, int32_t k_frame, int32_t order,
                    void *k_out, void *v_out, int32_t *n_tokens_out, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The conversation's cache: rows of many sequences in pages.
+ *
+ * Beside the video's cache a program keeps the rows of what is said about it
+ * (questions, answers, chunks just prefilled) for many users at once, whose
+ * lengths all differ and grow token by token.  These calls need no context: the
+ * caller owns the pages, the tables that name them and the lengths, in device
+ * memory, and hands them over with every call.
+ *
+ * Row j of sequence b, KV head g, layer l starts at element
+ *   l * stride_layer + p * stride_page + g * stride_head + (j % page_rows) * stride_row,
+ *   p = table[b][j / page_rows]
+ * of k_pages and of v_pages; its head_dim features are contiguous.  A page number
+ * outside 0 .. n_pages-1 names no rows: what would be read there is seen by no
+ * token, what would be written there is dropped.  Numbers and offsets may
+ * pass 32 bits.
+ *
+ * Every structure is read on the host while the call runs; the arrays it points
+ * to are read on the device.  lengths count a sequence's rows with the new
+ * tokens' own among them: the new tokens of b are its last ones.  Rows past
+ * the table (table_width * page_rows) do not exist; a negative length is none.
+ * ------------------------------------------------------------------------ */
+typedef struct mukv_paged {
+    void *k_pages;          /* device, payload dtype, 16-byte aligned                           */
+    void *v_pages;
+    int64_t stride_layer;   /* element strides, not negative, multiples of 16 bytes             */
+    int64_t stride_page;
+    int64_t stride_head;
+    int64_t stride_row;
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t page_rows;      /* rows of a page, 1 .. 2^24 (any number)                           */
+    int32_t n_q_heads;      /* a multiple of n_kv_heads, at most 1024 times as many             */
+    int32_t n_kv_heads;
+    int32_t head_dim;       /* a power of two in 16..128                                        */
+    int32_t dtype;          /* mukv_dtype of pages, queries, keys, values and outputs           */
+    int32_t device_id;
+} mukv_paged;
+
+typedef struct mukv_seqs {
+    const int32_t *table;   /* device [n_seqs][table_width]; NULL (mukv_paged_attend only): the
+                               sequences are packed without pages, rows and tokens alike: row j of
+                               sequence b is row offsets[b] + j of page 0, lengths is not read     */
+    const int32_t *lengths; /* device [n_seqs]                                                  */
+    const int32_t *offsets; /* device [n_seqs+1]: sequence b owns the new tokens offsets[b] ..
+                               offsets[b+1]-1, ascending from 0 to n_tokens; NULL: n_tokens / n_seqs
+                               tokens each                                                      */
+    int32_t n_seqs;         /* 1 .. 65536                                                       */
+    int32_t table_width;    /* pages a sequence can have                                        */
+    int32_t n_tokens;       /* new tokens of all sequences                                      */
+    int32_t max_new;        /* most new tokens of a sequence (0: not known).  A hint: it chooses
+                               between kernels, nothing is left out if it is wrong              */
+} mukv_seqs;
+
+/* Rotary positions with several axes.  Pair i of a head's first n_rot features is
+ * turned by the angle position[axis[i]] * inv_freq[i]:
+ *   (x, y) -> (x cos - y sin, y cos + x sin)
+ * Features from n_rot on are left as they are.  The angle is reduced to a turn in
+ * 64 bits, so far positions lose nothing; cosine, sine and products are fp32,
+ * rounded once to the payload dtype. */
+enum { MUKV_ROPE_HALVES = 0, MUKV_ROPE_NEIGHBOURS = 1 };
+typedef struct mukv_rope_table {
+    const double *inv_freq; /* device [n_rot / 2]                                               */
+    const int32_t *axis;    /* device [n_rot / 2], 0 .. n_axes-1 (any other number: angle 0);
+                               NULL: all 0                                                      */
+    int32_t n_rot;          /* rotated features: a multiple of 16, 16 .. min(head_dim, 512)     */
+    int32_t n_axes;         /* 1 .. 16                                                          */
+    int32_t pairing;        /* HALVES: pair i is features i and i + n_rot/2; NEIGHBOURS: 2i, 2i+1 */
+    int32_t inverse;        /* 1: turned back (what gradients, and keys to be placed anew, need) */
+} mukv_rope_table;
+
+/*
+ * Rotates n_heads heads of n_tokens tokens.
+ *
+ *   x, out      device, dtype, [n_tokens][n_heads][head_dim] with strides
+ *               (`layer` is ignored); out may be x with the same strides
+ *   positions   device int32 [n_axes][n_tokens]
+ *   head_dim    a multiple of 8 (bf16) or 4 (fp32), at most 1024
+ *
+ * n_tokens = 0 does nothing.
+ * Errors: INVALID_ARG, SHAPE (n_rot > head_dim), UNSUPPORTED (alignment).
+ */
+int mukv_rope(const mukv_rope_table *rope, const void *x, const mukv_strides *x_strides, const int32_t *positions,
+              int32_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t dtype, void *out,
+              const mukv_strides *out_strides, int32_t device_id, void *stream);
+
+/*
+ * Writes the new tokens' keys and values to the pages of one layer, the keys (and
+ * the queries, to q_out) rotated on the way.  Token i of the n_b new ones of
+ * sequence b becomes row lengths[b] - n_b + i; a row that is negative, past the
+ * table, or on a page that does not exist is dropped.  Two tokens must not name the same row.
+ *
+ *   k, v        device, [n_tokens][n_kv_heads][head_dim] with strides (slices of one
+ *               fused projection will do)
+ *   q, q_out    device, [n_tokens][n_q_heads][head_dim] with strides, both or neither;
+ *               q_out may be q with the same strides
+ *   rope        NULL: nothing is rotated, positions is not read
+ *   positions   device int32 [n_axes][n_tokens]
+ *
+ * n_tokens = 0 does nothing.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (alignment, strides).
+ */
+int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *k,
+                      const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides, const void *q,
+                      const mukv_strides *q_strides, void *q_out, const mukv_strides *q_out_strides,
+                      const mukv_rope_table *rope, const int32_t *positions, void *stream);
+
 /* Fills *out (host).  Does not synchronise. */
 int mukv_get_state(const mukv_ctx *ctx, mukv_state *out);
 

@@ -23,6 +23,7 @@ MUKV_SEMI, MUKV_HIER, MUKV_PARALLEL = 0, 1, 2
 MUKV_TEMPORAL, MUKV_AS_GIVEN = 0, 1
 MUKV_ATT_AUTO, MUKV_ATT_GENERIC, MUKV_ATT_MFMA = 0, 1, 2
 MUKV_FREQ_FEATURE, MUKV_FREQ_TOKEN = 0, 1
+MUKV_ROPE_HALVES, MUKV_ROPE_NEIGHBOURS = 0, 1
 
 
 class mukv_config(C.Structure):
@@ -62,6 +63,23 @@ class mukv_state(C.Structure):
     ]
 
 
+class mukv_paged(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("stride_layer", C.c_int64), ("stride_page", C.c_int64),
+                ("stride_head", C.c_int64), ("stride_row", C.c_int64), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
+                ("page_rows", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("device_id", C.c_int32)]
+
+
+class mukv_seqs(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lengths", C.c_void_p), ("offsets", C.c_void_p), ("n_seqs", C.c_int32),
+                ("table_width", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32)]
+
+
+class mukv_rope_table(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("n_rot", C.c_int32), ("n_axes", C.c_int32),
+                ("pairing", C.c_int32), ("inverse", C.c_int32)]
+
+
 KERNEL_NAMES = ("att", "freq", "select", "refine", "compact", "poolq", "score", "rerank", "gather", "copy_freq", "chain")
 
 
@@ -73,7 +91,7 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_retrieve_patches", "mukv_retrieve_at", "mukv_retrieve_units", "mukv_gather_multi", "mukv_gather_kv", "mukv_gather_patches", "mukv_gather_union",
            "mukv_attend", "mukv_prefill_workspace_size", "mukv_prefill_attend", "mukv_prefill_attend_static",
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
-           "mukv_plain_copy", "mukv_get_state", "mukv_strerror")
+           "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append", "mukv_strerror")
 
 _lib = None
 
@@ -114,6 +132,10 @@ def load():
     lib.mukv_plain_copy.argtypes = [vp, vp, C.c_int64, vp]
     lib.mukv_profile_begin.argtypes = [vp]
     lib.mukv_profile_end.argtypes = [vp, C.POINTER(mukv_profile)]
+    strides, paged, seqs = C.POINTER(mukv_strides), C.POINTER(mukv_paged), C.POINTER(mukv_seqs)
+    lib.mukv_rope.argtypes = [C.POINTER(mukv_rope_table), vp, strides, vp, i32, i32, i32, i32, vp, strides, i32, vp]
+    lib.mukv_paged_append.argtypes = [paged, i32, seqs, vp, strides, vp, strides, vp, strides, vp, strides,
+                                      C.POINTER(mukv_rope_table), vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -277,6 +299,17 @@ def mukv_get_state(h) -> mukv_state:
     s = mukv_state()
     _check((_lib or load()).mukv_get_state(h, C.byref(s)), "mukv_get_state")
     return s
+
+
+def mukv_rope(rope, x_ptr, x_strides, pos_ptr, n_tokens, n_heads, head_dim, dtype, out_ptr, out_strides, device_id, stream):
+    _check((_lib or load()).mukv_rope(rope, x_ptr, x_strides, pos_ptr, n_tokens, n_heads, head_dim, dtype, out_ptr, out_strides,
+                                      device_id, stream), "mukv_rope")
+
+
+def mukv_paged_append(pages, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, q_ptr, q_strides, q_out_ptr, q_out_strides, rope,
+                      pos_ptr, stream):
+    _check((_lib or load()).mukv_paged_append(pages, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, q_ptr, q_strides, q_out_ptr,
+                                              q_out_strides, rope, pos_ptr, stream), "mukv_paged_append")
 
 
 # ---- convenience object ----------------------------------------------------------------------
@@ -618,3 +651,99 @@ class MuKV:
                     if rc != 0:
                         raise RuntimeError(f"hipMemcpyAsync failed ({rc})")
         return k, v
+
+
+# ---- the conversation's cache ----------------------------------------------------------------
+_STRIDES = {}   # C form of the strides met so far
+
+
+def _rows(t):
+    """Strides of [token][head][feature] as the C ABI takes them."""
+    key = t.stride()
+    st = _STRIDES.get(key)
+    if st is None:
+        assert len(key) == 3 and key[2] == 1
+        if len(_STRIDES) > 256:
+            _STRIDES.clear()
+        st = _STRIDES[key] = mukv_strides(0, key[1], key[0])
+    return st
+
+
+def _dtype(t):
+    assert t.dtype in (torch.bfloat16, torch.float32), t.dtype
+    return MUKV_BF16 if t.dtype == torch.bfloat16 else MUKV_F32
+
+
+class Rope:
+    """Rotary positions with several axes: pair i turns by positions[axis[i]] * inv_freq[i].  inv_freq float64 [n_rot/2] and axis
+    int32 [n_rot/2] (None: one axis) on the device."""
+
+    def __init__(self, inv_freq, axis=None, *, n_axes=1, pairing="halves"):
+        assert inv_freq.dtype == torch.float64 and inv_freq.is_contiguous()
+        assert axis is None or (axis.dtype == torch.int32 and axis.is_contiguous() and axis.numel() == inv_freq.numel())
+        self._held = inv_freq, axis
+        self.n_axes = n_axes
+        kind = {"halves": MUKV_ROPE_HALVES, "neighbours": MUKV_ROPE_NEIGHBOURS}[pairing]
+        self.table = mukv_rope_table(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.numel(), n_axes, kind, 0)
+        self.back = mukv_rope_table(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.numel(), n_axes, kind, 1)
+
+    def positions_of(self, positions, n_tokens):
+        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (self.n_axes, n_tokens)
+        return positions.data_ptr()
+
+    def rotate(self, x, positions, *, inverse=False, out=None):
+        """x [n_tokens][n_heads][head_dim] (any token and head strides), positions int32 [n_axes][n_tokens].  `out` may be x."""
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        assert x.dim() == 3 and out.shape == x.shape and out.dtype == x.dtype
+        mukv_rope(self.back if inverse else self.table, _ptr(x), _rows(x), self.positions_of(positions, x.shape[0]), x.shape[0],
+                  x.shape[1], x.shape[2], _dtype(x), _ptr(out), _rows(out), x.device.index or 0, _stream())
+        return out
+
+
+class PagedKV:
+    """The conversation's cache: keys and values of many sequences in pages.  k_pages, v_pages: [layer][page][KV head][row][feature],
+    any strides but the last (a cache laid out [layer][page][row][KV head][feature] is passed permuted).  Tables are int32
+    [sequence][page], lengths int32 [sequence], both on the device and the caller's."""
+
+    def __init__(self, k_pages, v_pages, *, n_q_heads):
+        assert k_pages.dim() == 5 and v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
+        assert v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device and k_pages.stride(4) == 1
+        L, n, hkv, R, D = k_pages.shape
+        sl, sp, sh, sr, _ = k_pages.stride()
+        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self._held = k_pages, v_pages
+        self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, _dtype(k_pages),
+                                 k_pages.device.index or 0)
+        self._seqs = mukv_seqs()
+
+    def _sequences(self, table, lengths, offsets, n_tokens, max_new):
+        assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
+        assert lengths.dtype == torch.int32 and lengths.is_contiguous() and lengths.numel() == table.shape[0]
+        s = self._seqs
+        s.table, s.lengths = table.data_ptr(), lengths.data_ptr()
+        s.n_seqs, s.table_width = table.shape
+        if offsets is None:
+            s.offsets = None
+        else:
+            assert offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.numel() == s.n_seqs + 1
+            s.offsets = offsets.data_ptr()
+        s.n_tokens, s.max_new = n_tokens, max_new
+        return s
+
+    def append(self, layer, table, lengths, k, v, *, q=None, offsets=None, rope=None, positions=None, q_out=None):
+        """New tokens' keys and values [n_tokens][n_kv_heads][head_dim] become the last rows of their sequences (lengths count
+        them already); with `rope` the keys, and q [n_tokens][n_q_heads][head_dim], are rotated on the way.  Returns q_out."""
+        p, T = self._pages, k.shape[0]
+        assert k.shape == v.shape == (T, p.n_kv_heads, p.head_dim) and k.dtype == v.dtype == self.dtype
+        s = self._sequences(table, lengths, offsets, T, 0)
+        qp = op = qs = os_ = None
+        if q is not None:
+            assert q.shape == (T, p.n_q_heads, p.head_dim) and q.dtype == self.dtype
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            assert q_out.shape == q.shape and q_out.dtype == q.dtype
+            qp, qs, op, os_ = q.data_ptr(), _rows(q), q_out.data_ptr(), _rows(q_out)
+        mukv_paged_append(p, layer, s, k.data_ptr(), _rows(k), v.data_ptr(), _rows(v), qp, qs, op, os_,
+                          None if rope is None else rope.table, None if rope is None else rope.positions_of(positions, T), _stream())
+        return q_out

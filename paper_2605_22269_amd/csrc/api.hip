@@ -10,6 +10,7 @@
 #include "mukv_internal.h"
 
 using mukv::Ctx;
+using mukv::DeviceScope;
 
 struct mukv_ctx {
     Ctx c;
@@ -20,19 +21,6 @@ namespace {
 constexpr double kDefaultRefineMargin = 1e-5;
 
 bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
-
-// Makes the context's device current for the duration of a call and gives the caller's back.
-struct DeviceScope {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceScope(int device) {
-        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-        ok = hipSetDevice(device) == hipSuccess;
-    }
-    ~DeviceScope() {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
 
 template <typename T>
 hipError_t dalloc(T **p, size_t count) {

@@ -258,6 +258,19 @@ __host__ __device__ inline size_t att64_key_bytes(int P, int D, size_t key_size)
     return ((size_t)P * (D + 16 / key_size) * key_size + 7) & ~(size_t)7;
 }
 
+// Makes a device current for the duration of a call and gives the caller's back.
+struct DeviceScope {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceScope(int device) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        ok = hipSetDevice(device) == hipSuccess;
+    }
+    ~DeviceScope() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
 // ---- small device helpers ----
 __device__ __forceinline__ float to_float(uint16_t bits) { return __uint_as_float((uint32_t)bits << 16); }
 __device__ __forceinline__ float to_float(float x) { return x; }

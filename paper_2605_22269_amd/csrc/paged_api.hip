@@ -1,0 +1,180 @@
+// C ABI of the conversation's paged cache (declared in include/mukv.h): argument validation and dispatch.  Nothing here is kept
+// between calls.
+#include "paged_internal.h"
+
+using mukv::DeviceScope;
+using mukv::PagedView;
+using mukv::RopeArgs;
+
+namespace {
+
+bool aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+int elem_size(int dtype) { return dtype == MUKV_BF16 ? 2 : 4; }
+int finished(hipError_t e) { return e == hipSuccess ? MUKV_OK : MUKV_ERR_HIP; }
+
+// Strides of `count` steps: not negative, whole pieces of 16 bytes, and so small that bytes stay within 63 bits.
+int check_stride(int64_t stride, int64_t count, int esz) {
+    if (stride < 0) return MUKV_ERR_INVALID_ARG;
+    if (stride * esz % 16 || stride > (INT64_MAX >> 4) / (count > 0 ? count : 1)) return MUKV_ERR_UNSUPPORTED;
+    return MUKV_OK;
+}
+
+int check_pages(const mukv_paged *p) {
+    if (!p || !p->k_pages || !p->v_pages) return MUKV_ERR_INVALID_ARG;
+    if (p->n_layers < 1 || p->n_pages < 1 || p->page_rows < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->device_id < 0)
+        return MUKV_ERR_INVALID_ARG;
+    if (p->dtype != MUKV_BF16 && p->dtype != MUKV_F32) return MUKV_ERR_INVALID_ARG;
+    if (p->n_q_heads % p->n_kv_heads) return MUKV_ERR_SHAPE;
+    if (p->head_dim < 16 || p->head_dim > 128 || (p->head_dim & (p->head_dim - 1))) return MUKV_ERR_UNSUPPORTED;
+    if (p->n_q_heads / p->n_kv_heads > 1024 || p->n_q_heads > 65535) return MUKV_ERR_UNSUPPORTED;
+    const int esz = elem_size(p->dtype);
+    const int64_t strides[4] = {p->stride_layer, p->stride_page, p->stride_head, p->stride_row};
+    const int64_t counts[4] = {p->n_layers, p->n_pages, p->n_kv_heads, p->page_rows};
+    for (int i = 0; i < 4; ++i)
+        if (const int rc = check_stride(strides[i], counts[i], esz)) return rc;
+    if (!aligned(p->k_pages) || !aligned(p->v_pages)) return MUKV_ERR_UNSUPPORTED;
+    return MUKV_OK;
+}
+
+int check_seqs(const mukv_paged *p, const mukv_seqs *s, bool may_be_packed, bool has_tokens) {
+    if (!s) return MUKV_ERR_INVALID_ARG;
+    if (s->n_seqs < 1) return MUKV_ERR_INVALID_ARG;
+    if (s->n_seqs > 65536) return MUKV_ERR_UNSUPPORTED;
+    if (has_tokens) {
+        if (s->n_tokens < 0 || s->max_new < 0) return MUKV_ERR_INVALID_ARG;
+        if (!s->offsets && s->n_tokens % s->n_seqs) return MUKV_ERR_SHAPE;
+        if ((int64_t)s->n_tokens * p->n_q_heads > 0x7fffffff) return MUKV_ERR_UNSUPPORTED;
+    }
+    if (!s->table) {
+        if (!may_be_packed) return MUKV_ERR_INVALID_ARG;
+        return s->offsets ? MUKV_OK : MUKV_ERR_INVALID_ARG;
+    }
+    if (!s->lengths || s->table_width < 1) return MUKV_ERR_INVALID_ARG;
+    if (p->page_rows > 1 << 24 || (int64_t)s->table_width * p->page_rows > 0x7ffffff0 || (int64_t)s->table_width * s->n_seqs > 0x7fffffff)
+        return MUKV_ERR_UNSUPPORTED; // row and entry numbers are 32-bit in the kernels
+    return MUKV_OK;
+}
+
+PagedView view_of(const mukv_paged &p, int layer, const mukv_seqs &s) {
+    const int esz = elem_size(p.dtype);
+    PagedView v;
+    v.k = static_cast<unsigned char *>(p.k_pages) + layer * p.stride_layer * esz;
+    v.v = static_cast<unsigned char *>(p.v_pages) + layer * p.stride_layer * esz;
+    v.stride_page = p.stride_page * esz;
+    v.stride_head = p.stride_head * esz;
+    v.stride_row = p.stride_row * esz;
+    v.table = s.table;
+    v.lengths = s.lengths;
+    v.offsets = s.offsets;
+    v.n_pages = p.n_pages;
+    v.page_rows = p.page_rows;
+    v.n_seqs = s.n_seqs;
+    v.table_width = s.table_width;
+    v.n_tokens = s.n_tokens;
+    v.per_seq = s.n_tokens / s.n_seqs;
+    v.Hq = p.n_q_heads;
+    v.Hkv = p.n_kv_heads;
+    v.G = p.n_q_heads / p.n_kv_heads;
+    return v;
+}
+
+// [token][head][head_dim] with strides
+int check_rows(const void *x, const mukv_strides *st, int n_tokens, int n_heads, int esz) {
+    if (!x || !st) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_stride(st->token, n_tokens, esz)) return rc;
+    if (const int rc = check_stride(st->head, n_heads, esz)) return rc;
+    return aligned(x) ? MUKV_OK : MUKV_ERR_UNSUPPORTED;
+}
+RopeArgs::Rows rows_in(const void *x, const mukv_strides *st, void *out, const mukv_strides *out_st, int heads, int esz) {
+    RopeArgs::Rows r = {};
+    if (!x) return r;
+    r.x = static_cast<const unsigned char *>(x);
+    r.token = st->token * esz;
+    r.head = st->head * esz;
+    r.out = static_cast<unsigned char *>(out);
+    if (out) {
+        r.out_token = out_st->token * esz;
+        r.out_head = out_st->head * esz;
+    }
+    r.heads = heads;
+    return r;
+}
+
+int check_rope(const mukv_rope_table *r, bool have_positions, int head_dim) {
+    if (!r || !r->inv_freq || !have_positions) return MUKV_ERR_INVALID_ARG;
+    if (r->n_rot < 1 || r->n_axes < 1 || r->n_axes > 16 || (r->inverse != 0 && r->inverse != 1)) return MUKV_ERR_INVALID_ARG;
+    if (r->pairing != MUKV_ROPE_HALVES && r->pairing != MUKV_ROPE_NEIGHBOURS) return MUKV_ERR_INVALID_ARG;
+    if (r->n_rot > head_dim) return MUKV_ERR_SHAPE;
+    if (r->n_rot % 16 || r->n_rot > 512) return MUKV_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(r->inv_freq) & 7) return MUKV_ERR_UNSUPPORTED;
+    return MUKV_OK;
+}
+void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
+    a.rotate = r != nullptr;
+    if (!r) return;
+    a.inv_freq = r->inv_freq;
+    a.axis = r->axis;
+    a.positions = positions;
+    a.n_rot = r->n_rot;
+    a.n_axes = r->n_axes;
+    a.neighbours = r->pairing == MUKV_ROPE_NEIGHBOURS;
+    a.inverse = r->inverse != 0;
+}
+
+} // namespace
+
+extern "C" {
+
+int mukv_rope(const mukv_rope_table *rope, const void *x, const mukv_strides *x_strides, const int32_t *positions,
+              int32_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t dtype, void *out,
+              const mukv_strides *out_strides, int32_t device_id, void *stream) {
+    if (n_tokens < 0 || n_heads < 1 || head_dim < 1 || device_id < 0) return MUKV_ERR_INVALID_ARG;
+    if (dtype != MUKV_BF16 && dtype != MUKV_F32) return MUKV_ERR_INVALID_ARG;
+    const int esz = elem_size(dtype);
+    if (const int rc = check_rope(rope, n_tokens == 0 || positions, head_dim)) return rc;
+    if (head_dim * esz % 16 || head_dim > 1024 || n_heads > 65535) return MUKV_ERR_UNSUPPORTED;
+    if (n_tokens == 0) return MUKV_OK;
+    if (const int rc = check_rows(x, x_strides, n_tokens, n_heads, esz)) return rc;
+    if (const int rc = check_rows(out, out_strides, n_tokens, n_heads, esz)) return rc;
+    RopeArgs a = {};
+    a.q = rows_in(x, x_strides, out, out_strides, n_heads, esz);
+    a.n_tokens = n_tokens;
+    a.D = head_dim;
+    set_rope(a, rope, positions);
+    DeviceScope dev(device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    return finished(mukv::launch_rope(a, dtype, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *k,
+                      const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides, const void *q,
+                      const mukv_strides *q_strides, void *q_out, const mukv_strides *q_out_strides,
+                      const mukv_rope_table *rope, const int32_t *positions, void *stream) {
+    if (const int rc = check_pages(pages)) return rc;
+    if (layer < 0 || layer >= pages->n_layers) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
+    const int esz = elem_size(pages->dtype), T = seqs->n_tokens;
+    if (rope)
+        if (const int rc = check_rope(rope, T == 0 || positions, pages->head_dim)) return rc;
+    if (T == 0) return MUKV_OK; // (empty tensors need not have an address)
+    if ((q != nullptr) != (q_out != nullptr)) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_rows(k, k_strides, T, pages->n_kv_heads, esz)) return rc;
+    if (const int rc = check_rows(v, v_strides, T, pages->n_kv_heads, esz)) return rc;
+    if (q) {
+        if (const int rc = check_rows(q, q_strides, T, pages->n_q_heads, esz)) return rc;
+        if (const int rc = check_rows(q_out, q_out_strides, T, pages->n_q_heads, esz)) return rc;
+    }
+    RopeArgs a = {};
+    a.q = rows_in(q, q_strides, q_out, q_out_strides, pages->n_q_heads, esz);
+    a.k = rows_in(k, k_strides, nullptr, nullptr, pages->n_kv_heads, esz);
+    a.v = rows_in(v, v_strides, nullptr, nullptr, pages->n_kv_heads, esz);
+    a.view = view_of(*pages, layer, *seqs);
+    a.n_tokens = T;
+    a.D = pages->head_dim;
+    set_rope(a, rope, positions);
+    DeviceScope dev(pages->device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    return finished(mukv::launch_rope(a, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
+}
+
+} // extern "C"

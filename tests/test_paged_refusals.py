@@ -1,0 +1,85 @@
+"""What the paged cache's calls refuse, on the host, before anything is launched (no GPU here: pointers are never followed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2605_22269_amd import binding as mk
+
+P = 1 << 20  # stands for device memory
+
+
+def pages(**kw):
+    base = dict(k_pages=P, v_pages=P, stride_layer=4096 * 100, stride_page=4096, stride_head=1024, stride_row=64, n_layers=2, n_pages=100,
+                page_rows=16, n_q_heads=8, n_kv_heads=4, head_dim=64, dtype=mk.MUKV_BF16, device_id=0)
+    return mk.mukv_paged(**{**base, **kw})
+
+
+def seqs(**kw):
+    base = dict(table=P, lengths=P, offsets=P, n_seqs=3, table_width=10, n_tokens=5, max_new=0)
+    return mk.mukv_seqs(**{**base, **kw})
+
+
+def rope(**kw):
+    return mk.mukv_rope_table(**{**dict(inv_freq=P, axis=P, n_rot=64, n_axes=3, pairing=0, inverse=0), **kw})
+
+
+ST = mk.mukv_strides(0, 64, 64 * 16)
+BAD, SHAPE, UNSUP = mk.MUKV_ERR_INVALID_ARG, mk.MUKV_ERR_SHAPE, mk.MUKV_ERR_UNSUPPORTED
+PAGES = [({"k_pages": None}, BAD), ({"v_pages": None}, BAD), ({"n_layers": 0}, BAD), ({"n_pages": 0}, BAD), ({"page_rows": 0}, BAD),
+         ({"n_kv_heads": 0}, BAD), ({"device_id": -1}, BAD), ({"dtype": 2}, BAD), ({"n_q_heads": 6}, SHAPE), ({"head_dim": 48}, UNSUP),
+         ({"head_dim": 256}, UNSUP), ({"n_q_heads": 4 * 1025}, UNSUP), ({"stride_row": -64}, BAD), ({"stride_row": 68}, UNSUP),
+         ({"stride_head": 4}, UNSUP), ({"stride_page": 1 << 60}, UNSUP), ({"k_pages": P + 8}, UNSUP), ({"page_rows": (1 << 24) + 1}, UNSUP)]
+SEQS = [({"n_seqs": 0}, BAD), ({"n_seqs": 65537}, UNSUP), ({"table": None}, BAD), ({"lengths": None}, BAD), ({"table_width": 0}, BAD),
+        ({"n_tokens": -1}, BAD), ({"max_new": -1}, BAD), ({"offsets": None}, SHAPE), ({"n_tokens": 1 << 29}, UNSUP),
+        ({"table_width": 1 << 28}, UNSUP)]
+
+
+def append(p=None, layer=0, s=None, k=P, ks=ST, v=P, vs=ST, q=P, qs=ST, qo=P, qos=ST, r=None, pos=P):
+    ref = lambda x: None if x is None else C.byref(x)
+    return mk.load().mukv_paged_append(ref(p or pages()), layer, ref(s or seqs()), k, ref(ks), v, ref(vs), q, ref(qs), qo, ref(qos), ref(r),
+                                       pos, None)
+
+
+@pytest.mark.parametrize("kw,status", PAGES)
+def test_append_refuses_pages(kw, status):
+    assert append(p=pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", SEQS)
+def test_append_refuses_sequences(kw, status):
+    assert append(s=seqs(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({"layer": -1}, BAD), ({"layer": 2}, BAD), ({"k": None}, BAD), ({"v": None}, BAD), ({"ks": None}, BAD), ({"q": None}, BAD),
+    ({"qo": None}, BAD), ({"qs": None}, BAD), ({"k": P + 2}, UNSUP), ({"ks": mk.mukv_strides(0, 65, 1024)}, UNSUP),
+    ({"vs": mk.mukv_strides(0, 64, -1024)}, BAD), ({"r": rope(), "pos": None}, BAD)])
+def test_append_refuses_tensors(kw, status):
+    assert append(**kw) == status
+
+
+ROPES = [({"inv_freq": None}, BAD), ({"n_rot": 0}, BAD), ({"n_rot": 24}, UNSUP), ({"n_rot": 80}, SHAPE), ({"n_axes": 0}, BAD),
+         ({"n_axes": 17}, BAD), ({"pairing": 2}, BAD), ({"inverse": 2}, BAD), ({"inv_freq": P + 4}, UNSUP)]
+
+
+@pytest.mark.parametrize("kw,status", ROPES)
+def test_rotations_are_refused_alike(kw, status):
+    assert append(r=rope(**kw)) == status
+    call = lambda r: mk.load().mukv_rope(C.byref(r), P, C.byref(ST), P, 4, 8, 64, mk.MUKV_BF16, P, C.byref(ST), 0, None)
+    assert call(rope(**kw)) == status
+
+
+@pytest.mark.parametrize("args,status", [
+    (dict(T=-1), BAD), (dict(H=0), BAD), (dict(D=0), BAD), (dict(dtype=5), BAD), (dict(dev=-1), BAD), (dict(x=None), BAD), (dict(out=None), BAD),
+    (dict(pos=None), BAD), (dict(D=68), UNSUP), (dict(D=1032), UNSUP), (dict(H=65536), UNSUP), (dict(x=P + 4), UNSUP)])
+def test_rope_refuses(args, status):
+    a = {**dict(T=4, H=8, D=64, dtype=mk.MUKV_BF16, dev=0, x=P, out=P, pos=P), **args}
+    assert mk.load().mukv_rope(C.byref(rope()), a["x"], C.byref(ST), a["pos"], a["T"], a["H"], a["D"], a["dtype"], a["out"], C.byref(ST),
+                               a["dev"], None) == status
+
+
+def test_nothing_to_do_is_no_error():
+    assert append(s=seqs(n_tokens=0)) == mk.MUKV_OK
+    assert mk.load().mukv_rope(C.byref(rope()), P, C.byref(ST), P, 0, 8, 64, mk.MUKV_BF16, P, C.byref(ST), 0, None) == mk.MUKV_OK
+    assert mk.load().mukv_paged_append(None, 0, C.byref(seqs()), P, None, P, None, None, None, None, None, None, None, None) == BAD
+    assert mk.load().mukv_rope(None, P, C.byref(ST), P, 4, 8, 64, 0, P, C.byref(ST), 0, None) == BAD
