@@ -560,7 +560,8 @@ int mukv_gather_kv(mukv_ctx *ctx, const int32_t *frame_idx, int32_t B, int32_t k
 typedef struct mukv_paged {
     void *k_pages;          /* device, payload dtype, 16-byte aligned                           */
     void *v_pages;
-    int64_t stride_layer;   /* element strides, not negative, multiples of 16 bytes             */
+    int64_t stride_layer;   /* element strides, not negative, multiples of 16 bytes (that of
+                               a dimension of one is not read)                                  */
     int64_t stride_page;
     int64_t stride_head;
     int64_t stride_row;
@@ -641,6 +642,50 @@ int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
                       const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides, const void *q,
                       const mukv_strides *q_strides, void *q_out, const mukv_strides *q_out_strides,
                       const mukv_rope_table *rope, const int32_t *positions, void *stream);
+
+/* What rows have received of the softmax weights, device float: row j of layer l,
+ * sequence b, KV head g at l * stride_layer + b * stride_seq + g * stride_head + j, for j < rows. */
+typedef struct mukv_row_weights {
+    const float *in;      /* NULL: zeros                                                        */
+    float *out;           /* may be `in`                                                        */
+    int64_t stride_layer; /* element strides, not negative                                      */
+    int64_t stride_seq;
+    int64_t stride_head;
+    int32_t rows;         /* rows a head has room for                                           */
+    float decay;          /* finite, not negative; mukv_paged_attend: out = decay * in + received
+                             (1: weights accumulate)                                            */
+} mukv_row_weights;
+
+/*
+ * Attention of the new tokens over their sequences' rows at one layer: scores
+ * q.k / sqrt(D), softmax over the rows a token sees, head h on KV head
+ * h / (n_q_heads / n_kv_heads).  With causal = 1 token i of the n_b new ones sees the
+ * rows j <= lengths[b] - n_b + i, with 0 all of its sequence's rows.  One token per
+ * sequence and whole prompts, with or without rows before them, mixed as they come.
+ * A token that sees no row gets zeros; one that sees a NaN or +inf score gets NaN;
+ * what rows hold that it does not see never reaches it.
+ *
+ *   q          device, [n_tokens][n_q_heads][head_dim] with strides (NULL: contiguous)
+ *   out        device, [n_tokens][n_q_heads][head_dim] contiguous
+ *   weights    NULL, or where the rows' weights go: `out` receives, for every row of
+ *              every sequence, decay * in + the sum of its softmax weights over the
+ *              sequence's new tokens and the heads of its KV head's group (rows on pages
+ *              that do not exist: 0).  Rows past a sequence's length are left as they are;
+ *              stride_layer is not read (the arrays are this layer's).
+ *   workspace  device scratch of at least mukv_paged_workspace_size() bytes, 16-byte
+ *              aligned.  It must have been zero-filled once before its first use;
+ *              every call leaves it fit for the next one, of any shape.  Calls that share a
+ *              workspace must not overlap on the device.
+ *
+ * Arithmetic in fp32, sums in an order that does not depend on timing; `out` is rounded to
+ * the payload dtype.
+ * n_tokens = 0 does nothing, except that weights are brought from in to out.
+ * Errors: INVALID_ARG, SHAPE, CAPACITY (workspace too small), UNSUPPORTED.
+ */
+int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, int32_t with_weights, int64_t *bytes_out);
+int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *q,
+                      const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
+                      void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Fills *out (host).  Does not synchronise. */
 int mukv_get_state(const mukv_ctx *ctx, mukv_state *out);

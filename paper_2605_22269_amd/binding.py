@@ -75,6 +75,11 @@ class mukv_seqs(C.Structure):
                 ("table_width", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32)]
 
 
+class mukv_row_weights(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("stride_layer", C.c_int64), ("stride_seq", C.c_int64),
+                ("stride_head", C.c_int64), ("rows", C.c_int32), ("decay", C.c_float)]
+
+
 class mukv_rope_table(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("n_rot", C.c_int32), ("n_axes", C.c_int32),
                 ("pairing", C.c_int32), ("inverse", C.c_int32)]
@@ -91,7 +96,8 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_retrieve_patches", "mukv_retrieve_at", "mukv_retrieve_units", "mukv_gather_multi", "mukv_gather_kv", "mukv_gather_patches", "mukv_gather_union",
            "mukv_attend", "mukv_prefill_workspace_size", "mukv_prefill_attend", "mukv_prefill_attend_static",
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
-           "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append", "mukv_strerror")
+           "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append",
+           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_strerror")
 
 _lib = None
 
@@ -136,6 +142,8 @@ def load():
     lib.mukv_rope.argtypes = [C.POINTER(mukv_rope_table), vp, strides, vp, i32, i32, i32, i32, vp, strides, i32, vp]
     lib.mukv_paged_append.argtypes = [paged, i32, seqs, vp, strides, vp, strides, vp, strides, vp, strides,
                                       C.POINTER(mukv_rope_table), vp, vp]
+    lib.mukv_paged_workspace_size.argtypes = [paged, seqs, i32, C.POINTER(C.c_int64)]
+    lib.mukv_paged_attend.argtypes = [paged, i32, seqs, vp, strides, i32, vp, C.POINTER(mukv_row_weights), vp, C.c_int64, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -310,6 +318,17 @@ def mukv_paged_append(pages, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, q_
                       pos_ptr, stream):
     _check((_lib or load()).mukv_paged_append(pages, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, q_ptr, q_strides, q_out_ptr,
                                               q_out_strides, rope, pos_ptr, stream), "mukv_paged_append")
+
+
+def mukv_paged_workspace_size(pages, seqs, with_weights):
+    n = C.c_int64(0)
+    _check((_lib or load()).mukv_paged_workspace_size(pages, seqs, with_weights, C.byref(n)), "mukv_paged_workspace_size")
+    return n.value
+
+
+def mukv_paged_attend(pages, layer, seqs, q_ptr, q_strides, causal, out_ptr, weights, ws_ptr, ws_bytes, stream):
+    _check((_lib or load()).mukv_paged_attend(pages, layer, seqs, q_ptr, q_strides, causal, out_ptr, weights, ws_ptr, ws_bytes, stream),
+           "mukv_paged_attend")
 
 
 # ---- convenience object ----------------------------------------------------------------------
@@ -662,6 +681,8 @@ def _rows(t):
     key = t.stride()
     st = _STRIDES.get(key)
     if st is None:
+        if t.numel() == 0:
+            return mukv_strides(0, 0, 0)   # (an empty tensor's strides are anything)
         assert len(key) == 3 and key[2] == 1
         if len(_STRIDES) > 256:
             _STRIDES.clear()
@@ -715,7 +736,10 @@ class PagedKV:
         self._held = k_pages, v_pages
         self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, _dtype(k_pages),
                                  k_pages.device.index or 0)
-        self._seqs = mukv_seqs()
+        self._seqs, self._space = mukv_seqs(), _Workspace(k_pages.device)
+
+    def _workspace(self, s, with_weights):
+        return self._space.get(self._pages, s, with_weights)
 
     def _sequences(self, table, lengths, offsets, n_tokens, max_new):
         assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
@@ -747,3 +771,73 @@ class PagedKV:
         mukv_paged_append(p, layer, s, k.data_ptr(), _rows(k), v.data_ptr(), _rows(v), qp, qs, op, os_,
                           None if rope is None else rope.table, None if rope is None else rope.positions_of(positions, T), _stream())
         return q_out
+
+    def attend(self, layer, table, lengths, q, *, offsets=None, max_new=0, causal=True, out=None, weights=None, weights_out=None,
+               decay=1.0):
+        """q [n_tokens][n_q_heads][head_dim]: every sequence's new tokens (lengths count them) attend to its rows.  With
+        weights_out, float32 [sequence][KV head][row], it becomes decay * weights + what every row received (weights None: zeros;
+        weights_out may be weights).  Returns out."""
+        p, T = self._pages, q.shape[0]
+        assert q.shape == (T, p.n_q_heads, p.head_dim) and q.dtype == self.dtype
+        s = self._sequences(table, lengths, offsets, T, max_new)
+        return _attend(self, s, layer, q, causal, out, weights, weights_out, decay)
+
+
+def _attend(cache, s, layer, q, causal, out, weights, weights_out, decay):
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
+    w = None
+    if weights_out is not None:
+        assert weights_out.dtype == torch.float32 and weights_out.dim() == 3 and weights_out.stride(2) == 1
+        assert weights_out.shape[:2] == (s.n_seqs, cache._pages.n_kv_heads)
+        if weights is not None:
+            assert weights.dtype == torch.float32 and weights.shape == weights_out.shape and weights.stride() == weights_out.stride()
+        w = mukv_row_weights(_ptr(weights), weights_out.data_ptr(), 0, weights_out.stride(0), weights_out.stride(1), weights_out.shape[2], decay)
+    else:
+        assert weights is None
+    ws = cache._workspace(s, w is not None)
+    mukv_paged_attend(cache._pages, layer, s, q.data_ptr(), _rows(q), int(causal), out.data_ptr(), w, ws.data_ptr(), ws.numel(), _stream())
+    return out
+
+
+class _Workspace:
+    """Scratch of the attention calls of one cache, a piece for every stream that calls: calls on different streams may overlap."""
+
+    def __init__(self, device):
+        self.device, self.by_stream, self.need = device, {}, (None, 0)
+
+    def get(self, pages, s, with_weights):
+        key = (s.n_tokens, with_weights)   # (what else it takes is the cache's own)
+        if self.need[0] != key:
+            self.need = key, mukv_paged_workspace_size(pages, s, int(with_weights))
+        ws = self.by_stream.get(st := _stream())
+        if ws is None or ws.numel() < self.need[1]:
+            ws = self.by_stream[st] = torch.zeros(self.need[1], dtype=torch.uint8, device=self.device)
+        return ws
+
+
+class PackedKV:
+    """Attention over packed sequences without pages: q [n_tokens][n_q_heads][head_dim] and k, v [n_tokens][n_kv_heads][head_dim],
+    sequence b the tokens offsets[b] .. offsets[b+1]-1 of all three (slices of one fused projection will do)."""
+
+    def __init__(self, *, n_q_heads):
+        self._pages, self._seqs, self._space = mukv_paged(), mukv_seqs(), None
+        self._pages.n_q_heads = n_q_heads
+
+    def _workspace(self, s, with_weights):
+        return self._space.get(self._pages, s, with_weights)
+
+    def attend(self, q, k, v, offsets, *, max_new=0, causal=True, out=None, weights=None, weights_out=None, decay=1.0):
+        p, s, T = self._pages, self._seqs, q.shape[0]
+        assert k.dim() == 3 and v.shape == k.shape and v.stride() == k.stride() and k.stride(2) == 1 and k.shape[0] == T
+        assert q.shape == (T, p.n_q_heads, k.shape[2]) and q.dtype == k.dtype == v.dtype
+        assert offsets.dtype == torch.int32 and offsets.is_contiguous()
+        p.k_pages, p.v_pages, p.stride_row, p.stride_head = k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1)
+        p.n_layers, p.n_pages, p.page_rows, p.n_kv_heads, p.head_dim = 1, 1, max(T, 1), k.shape[1], k.shape[2]
+        p.dtype, p.device_id = _dtype(k), k.device.index or 0
+        s.offsets, s.n_seqs, s.n_tokens, s.max_new = offsets.data_ptr(), offsets.numel() - 1, T, max_new
+        if self._space is None or self._space.device != q.device or self._space.kind != (p.dtype, p.n_kv_heads, p.head_dim):
+            self._space = _Workspace(q.device)
+            self._space.kind = p.dtype, p.n_kv_heads, p.head_dim
+        return _attend(self, s, 0, q, causal, out, weights, weights_out, decay)

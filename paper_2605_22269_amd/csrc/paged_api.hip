@@ -1,5 +1,7 @@
 // C ABI of the conversation's paged cache (declared in include/mukv.h): argument validation and dispatch.  Nothing here is kept
 // between calls.
+#include <cmath>
+
 #include "paged_internal.h"
 
 using mukv::DeviceScope;
@@ -12,12 +14,16 @@ bool aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 int elem_size(int dtype) { return dtype == MUKV_BF16 ? 2 : 4; }
 int finished(hipError_t e) { return e == hipSuccess ? MUKV_OK : MUKV_ERR_HIP; }
 
-// Strides of `count` steps: not negative, whole pieces of 16 bytes, and so small that bytes stay within 63 bits.
+// Strides of `count` places: not negative, whole pieces of 16 bytes, and so small that bytes stay within 63 bits.  That of a single
+// place is never walked and may be anything.
 int check_stride(int64_t stride, int64_t count, int esz) {
+    if (count <= 1) return MUKV_OK;
     if (stride < 0) return MUKV_ERR_INVALID_ARG;
-    if (stride * esz % 16 || stride > (INT64_MAX >> 4) / (count > 0 ? count : 1)) return MUKV_ERR_UNSUPPORTED;
+    if (stride * esz % 16 || stride > (INT64_MAX >> 4) / count) return MUKV_ERR_UNSUPPORTED;
     return MUKV_OK;
 }
+
+int64_t in_bytes(int64_t stride, int64_t count, int esz) { return count > 1 ? stride * esz : 0; }
 
 int check_pages(const mukv_paged *p) {
     if (!p || !p->k_pages || !p->v_pages) return MUKV_ERR_INVALID_ARG;
@@ -58,11 +64,11 @@ int check_seqs(const mukv_paged *p, const mukv_seqs *s, bool may_be_packed, bool
 PagedView view_of(const mukv_paged &p, int layer, const mukv_seqs &s) {
     const int esz = elem_size(p.dtype);
     PagedView v;
-    v.k = static_cast<unsigned char *>(p.k_pages) + layer * p.stride_layer * esz;
-    v.v = static_cast<unsigned char *>(p.v_pages) + layer * p.stride_layer * esz;
-    v.stride_page = p.stride_page * esz;
-    v.stride_head = p.stride_head * esz;
-    v.stride_row = p.stride_row * esz;
+    v.k = static_cast<unsigned char *>(p.k_pages) + layer * in_bytes(p.stride_layer, p.n_layers, esz);
+    v.v = static_cast<unsigned char *>(p.v_pages) + layer * in_bytes(p.stride_layer, p.n_layers, esz);
+    v.stride_page = in_bytes(p.stride_page, p.n_pages, esz);
+    v.stride_head = in_bytes(p.stride_head, p.n_kv_heads, esz);
+    v.stride_row = in_bytes(p.stride_row, p.page_rows, esz);
     v.table = s.table;
     v.lengths = s.lengths;
     v.offsets = s.offsets;
@@ -85,16 +91,16 @@ int check_rows(const void *x, const mukv_strides *st, int n_tokens, int n_heads,
     if (const int rc = check_stride(st->head, n_heads, esz)) return rc;
     return aligned(x) ? MUKV_OK : MUKV_ERR_UNSUPPORTED;
 }
-RopeArgs::Rows rows_in(const void *x, const mukv_strides *st, void *out, const mukv_strides *out_st, int heads, int esz) {
+RopeArgs::Rows rows_in(const void *x, const mukv_strides *st, void *out, const mukv_strides *out_st, int tokens, int heads, int esz) {
     RopeArgs::Rows r = {};
     if (!x) return r;
     r.x = static_cast<const unsigned char *>(x);
-    r.token = st->token * esz;
-    r.head = st->head * esz;
+    r.token = in_bytes(st->token, tokens, esz);
+    r.head = in_bytes(st->head, heads, esz);
     r.out = static_cast<unsigned char *>(out);
     if (out) {
-        r.out_token = out_st->token * esz;
-        r.out_head = out_st->head * esz;
+        r.out_token = in_bytes(out_st->token, tokens, esz);
+        r.out_head = in_bytes(out_st->head, heads, esz);
     }
     r.heads = heads;
     return r;
@@ -121,6 +127,28 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
     a.inverse = r->inverse != 0;
 }
 
+// The workspace of an attention call: counts, records, then (with weights) a pair per query.
+struct Space {
+    int64_t counts, records, pairs, bytes; // offsets
+};
+Space space_of(const mukv_paged &p, const mukv_seqs &s, bool with_weights) {
+    const mukv::PlanShape plan = mukv::paged_plan(p.dtype);
+    const int64_t n = mukv::records_bound(plan);
+    Space x;
+    x.counts = 0;
+    x.records = (4 * n + 255) & ~(int64_t)255;
+    x.pairs = x.records + 4 * n * plan.queries * (p.head_dim + 2);
+    x.bytes = x.pairs + (with_weights ? 8 * (int64_t)s.n_tokens * p.n_q_heads : 0);
+    return x;
+}
+
+int check_weights(const mukv_row_weights *w) {
+    if (!w->out || w->rows < 1 || w->stride_layer < 0 || w->stride_seq < 0 || w->stride_head < 0) return MUKV_ERR_INVALID_ARG;
+    if (!(w->decay >= 0.f) || !(w->decay <= 3.4e38f)) return MUKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(w->in) & 3) || (reinterpret_cast<uintptr_t>(w->out) & 3)) return MUKV_ERR_UNSUPPORTED;
+    return MUKV_OK;
+}
+
 } // namespace
 
 extern "C" {
@@ -137,7 +165,7 @@ int mukv_rope(const mukv_rope_table *rope, const void *x, const mukv_strides *x_
     if (const int rc = check_rows(x, x_strides, n_tokens, n_heads, esz)) return rc;
     if (const int rc = check_rows(out, out_strides, n_tokens, n_heads, esz)) return rc;
     RopeArgs a = {};
-    a.q = rows_in(x, x_strides, out, out_strides, n_heads, esz);
+    a.q = rows_in(x, x_strides, out, out_strides, n_tokens, n_heads, esz);
     a.n_tokens = n_tokens;
     a.D = head_dim;
     set_rope(a, rope, positions);
@@ -165,9 +193,9 @@ int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
         if (const int rc = check_rows(q_out, q_out_strides, T, pages->n_q_heads, esz)) return rc;
     }
     RopeArgs a = {};
-    a.q = rows_in(q, q_strides, q_out, q_out_strides, pages->n_q_heads, esz);
-    a.k = rows_in(k, k_strides, nullptr, nullptr, pages->n_kv_heads, esz);
-    a.v = rows_in(v, v_strides, nullptr, nullptr, pages->n_kv_heads, esz);
+    a.q = rows_in(q, q_strides, q_out, q_out_strides, T, pages->n_q_heads, esz);
+    a.k = rows_in(k, k_strides, nullptr, nullptr, T, pages->n_kv_heads, esz);
+    a.v = rows_in(v, v_strides, nullptr, nullptr, T, pages->n_kv_heads, esz);
     a.view = view_of(*pages, layer, *seqs);
     a.n_tokens = T;
     a.D = pages->head_dim;
@@ -175,6 +203,61 @@ int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     DeviceScope dev(pages->device_id);
     if (!dev.ok) return MUKV_ERR_HIP;
     return finished(mukv::launch_rope(a, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, int32_t with_weights, int64_t *bytes_out) {
+    if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_pages(pages)) return rc;
+    if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
+    *bytes_out = space_of(*pages, *seqs, with_weights != 0).bytes;
+    return MUKV_OK;
+}
+
+int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *q,
+                      const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
+                      void *workspace, int64_t workspace_bytes, void *stream) {
+    if (const int rc = check_pages(pages)) return rc;
+    if (layer < 0 || layer >= pages->n_layers || (causal != 0 && causal != 1)) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
+    if (weights)
+        if (const int rc = check_weights(weights)) return rc;
+    const int T = seqs->n_tokens, D = pages->head_dim, esz = elem_size(pages->dtype);
+    if (T == 0 && !weights) return MUKV_OK;
+    const mukv_strides dense = {0, D, (int64_t)D * pages->n_q_heads};
+    const mukv_strides *qs = q_strides ? q_strides : &dense;
+    if (T > 0) { // (empty tensors need not have an address)
+        if (const int rc = check_rows(q, qs, T, pages->n_q_heads, esz)) return rc;
+        if (!out) return MUKV_ERR_INVALID_ARG;
+        if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
+    }
+    if (!workspace) return MUKV_ERR_INVALID_ARG;
+    const Space x = space_of(*pages, *seqs, weights != nullptr);
+    if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
+    if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
+    mukv::PagedAttendArgs a = {};
+    a.view = view_of(*pages, layer, *seqs);
+    a.plan = mukv::paged_plan(pages->dtype);
+    a.q = static_cast<const unsigned char *>(q);
+    a.q_token = in_bytes(qs->token, T, esz);
+    a.q_head = in_bytes(qs->head, pages->n_q_heads, esz);
+    a.out = out;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    a.counts = reinterpret_cast<int *>(ws + x.counts);
+    a.records = reinterpret_cast<float *>(ws + x.records);
+    a.pairs = weights ? reinterpret_cast<float *>(ws + x.pairs) : nullptr;
+    a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
+    a.causal = causal;
+    if (weights) {
+        a.weights_in = weights->in;
+        a.weights_out = weights->out;
+        a.weights_seq = weights->stride_seq;
+        a.weights_head = weights->stride_head;
+        a.weights_rows = weights->rows;
+        a.decay = weights->decay;
+    }
+    DeviceScope dev(pages->device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    return finished(mukv::launch_paged_attend(a, D, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
 }
 
 } // extern "C"

@@ -1,0 +1,630 @@
+// Attention of new tokens over the rows of a paged cache (or of packed sequences), for any number of tokens a sequence, any payload type
+// and head size.
+//
+//   out[token][h] = sum_j p_j v_j / sum_j p_j,  p_j = 2^(s_j - m),  s_j = log2(e) / sqrt(D) q.k_j,  m = max_j s_j
+//
+// over the rows j of the token's sequence that it sees.  One pass over the rows with the running maximum and sum; rows shared by
+// chunks of a sequence are joined by the last of its workgroups to finish.
+#include <climits>
+#include <type_traits>
+
+#include "attend_dev.h"
+#include "paged_internal.h"
+
+namespace mukv {
+
+namespace {
+
+constexpr int kPQ = 16, kPWaves = 4; // queries and waves of a workgroup
+
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_prefix(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false); // within the 16 lanes of a row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false); // the row before, in rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false); // the half before, in the upper half
+    return v;
+}
+
+struct Unit {
+    SeqShape s;
+    int b, g, tile, chunk, chunks, per; // per: blocks of a chunk
+    int record;                         // of the tile's first chunk
+};
+
+// The unit of this workgroup, the same in all lanes; false: there is none.
+__device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p, int id, Unit *u) {
+    const int lane = threadIdx.x & 63;
+    if (v.n_seqs == 1) {
+        u->s = shape_of(v, p, 0);
+        u->b = 0;
+        u->per = chunk_of(p, u->s, chunk_of(p, blocks_of(v, u->s)));
+        u->chunks = (int)div_up(u->s.blocks, u->per);
+        u->record = 0;
+        if (id >= u->s.tiles * v.Hkv * u->chunks) return false;
+    } else {
+        const SeqShape none = {0, 0, 0, 0, 0, 1};
+        SeqShape s = none;
+        double all = 0.0;
+        for (int b0 = 0; b0 < v.n_seqs; b0 += 64) {
+            s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
+            all += blocks_of(v, s);
+        }
+        const int per = chunk_of(p, wave_sum(all));
+        int units0 = 0, records0 = 0, b0 = 0;
+        for (;; b0 += 64) {
+            if (b0 >= v.n_seqs) return false;
+            if (v.n_seqs > 64) s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
+            const int chunks = chunks_of(p, s, per), units = s.tiles * v.Hkv * chunks, records = chunks > 1 ? units : 0;
+            const int units1 = units0 + wave_prefix(units), records1 = records0 + wave_prefix(records);
+            const uint64_t here = __builtin_amdgcn_ballot_w64(id < units1);
+            if (here) {
+                const int at = __builtin_ctzll(here);
+                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+                u->s = SeqShape{of(s.first), of(s.n_new), of(s.length), of(s.rows), of(s.tiles), of(s.blocks)};
+                u->b = b0 + at;
+                u->per = chunk_of(p, u->s, per);
+                u->chunks = of(chunks);
+                u->record = of(records1 - records);
+                id -= of(units1 - units);
+                break;
+            }
+            units0 = __builtin_amdgcn_readlane(units1, 63);
+            records0 = __builtin_amdgcn_readlane(records1, 63);
+        }
+    }
+    // KV heads next to each other: workgroups go to the eight XCDs in turn, so an XCD meets few heads' rows
+    u->g = id % v.Hkv;
+    id /= v.Hkv;
+    u->chunk = id % u->chunks;
+    const int rank = id / u->chunks;
+    u->record += (rank * v.Hkv + u->g) * u->chunks;
+    u->tile = u->s.tiles - 1 - rank; // under the mask the last ones have the most to do: they start first
+    return true;
+}
+
+// The rows of a tile, in blocks of 32 (bf16) or 16 (fp32), dealt to the waves in turn; nothing crosses the waves until the end.
+//   rows     a lane works out where one row lives, from a table entry that was requested a block earlier; the others fetch that by
+//            lane permutes.  Keys and values go straight to registers, the next block's requested as soon as this one's are used up.
+//   scores   S^T = K Q^T (16x16x32 bf16, 16x16x4 fp32): a lane holds ONE query (lane % 16) and the rows 4 (lane / 16) + r of every 16.
+//   values   O^T += V^T P^T: the weights are the B operand as they stand in the lane.  bf16: pairs hi + lo, nothing of the fp32
+//            weight is lost; the value rows pass through LDS the wave has to itself and the transpose read.  fp32: no transpose needed.
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attend_kernel(PagedAttendArgs a) {
+    constexpr int W = kPWaves;
+    constexpr bool kBf16 = sizeof(T) == 2;
+    constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
+    constexpr int kRows = kBf16 ? 32 : 16;             // rows of a block
+    constexpr int kTiles = kRows / 16;                 // 16-row tiles of the scores
+    constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16; // 16-byte pieces of a key row (and of a query) per lane
+    constexpr int NF = D / 16;                         // 16-feature tiles of the output
+    // bf16: value pieces per lane, each load of the wave kRowsPerLoad whole rows.  fp32: per 4-row step D / 16 floats
+    constexpr int kRowsPerLoad = 64 / kPieces, NV = kBf16 ? kRows / kRowsPerLoad : 4;
+    constexpr int kVW = kBf16 ? 4 : (D >= 64 ? 4 : D / 16), kVH = kBf16 ? 1 : (D == 128 ? 2 : 1); // dwords per load, loads per row
+    typedef __attribute__((ext_vector_type(kVW))) unsigned int raw_v;
+    // per wave: staged value rows (bf16), at the end its outputs [16 queries][D]
+    __shared__ __align__(1024) unsigned char s_buf[W][64 * D];
+    __shared__ float s_m[W][kPQ], s_l[W][kPQ];
+    constexpr bool kQueryLds = !kBf16 && D == 128; // fp32, 128 features: the queries' operands wait in LDS
+    __shared__ raw16 s_q[kQueryLds ? KK : 1][kQueryLds ? 64 : 1];
+    const PagedView &v = a.view;
+    Unit u;
+    if (!find_unit(v, a.plan, blockIdx.x, &u)) return;
+    const int g = u.g, b = u.b, G = v.G, n_new = u.s.n_new;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int n_queries = n_new * G; // of this KV head: (token, head in group), token-major
+    const float scale = a.scale_log2e * (1.f / query_factor<T, D>());
+    // the lane's query as a matrix operand: 16-byte pieces lg, lg + 4, ... of its row
+    const int my_q = u.tile * kPQ + lr;
+    const bool q_ok = my_q < n_queries;
+    const int my_tok = q_ok ? my_q / G : 0;
+    raw16 qb[kQueryLds ? 1 : KK];
+    const bool has_piece = kPieces >= 4 || lg < kPieces; // (rows of 32 bytes have two pieces)
+    const int my_piece = kPieces >= 4 ? lg : lg & (kPieces - 1);
+    {
+        const unsigned char *qp = a.q + (int64_t)(u.s.first + my_tok) * a.q_token + (int64_t)(g * G + (q_ok ? my_q - my_tok * G : 0)) * a.q_head;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            if (kQueryLds && wave != 0) break; // the same in all waves
+            raw16 x = *reinterpret_cast<const raw16 *>(qp + 16 * (my_piece + 4 * kk));
+            x = q_ok && has_piece ? brought_down<T, D>(x) : raw16{0u, 0u, 0u, 0u};
+            if constexpr (kQueryLds)
+                s_q[kk][lane] = x;
+            else
+                qb[kk] = x;
+        }
+    }
+    const int first_tok = u.tile * kPQ / G;
+    const int last_q = u.tile * kPQ + kPQ - 1 < n_queries ? u.tile * kPQ + kPQ - 1 : n_queries - 1, last_tok = last_q / G;
+    const int past = u.s.length - n_new; // token i sees row j iff j <= past + i (it may be negative)
+    int n_rows = u.s.rows;               // up to the last one that a query of the tile sees
+    if (a.causal && past + last_tok + 1 < n_rows) n_rows = past + last_tok + 1 > 0 ? past + last_tok + 1 : 0;
+    // the workgroup's blocks of rows, dealt to its waves
+    constexpr int kBlocks = 4; // to one of the plan's
+    const int n_blk = (n_rows + kRows - 1) / kRows;
+    const int64_t lo = (int64_t)u.chunk * u.per * kBlocks, hi = lo + (int64_t)u.per * kBlocks;
+    const int b_lo = lo < n_blk ? (int)lo : n_blk, b_hi = hi < n_blk ? (int)hi : n_blk;
+    const unsigned char *const kb = v.k + g * v.stride_head, *const vb = v.v + g * v.stride_head;
+
+    // Row lane % kRows of a block: the page it is on, requested early, where it lives, and the first token that sees it (INT_MAX: it
+    // lives nowhere).  Loads are unconditional: a row that lives nowhere reads the first page's first row; what was read instead
+    // of a value row becomes zeros (its weights are zero, but zero times anything must stay zero).
+    auto page_at = [&](int blk) __attribute__((always_inline)) {
+        const int r = blk * kRows + (lane & (kRows - 1));
+        return v.table && blk < b_hi && r < n_rows ? v.table[entry_of(v, b, r)] : 0;
+    };
+    auto find = [&](int blk, int page, int64_t *off, int *ft) __attribute__((always_inline)) {
+        const int r = blk * kRows + (lane & (kRows - 1));
+        const bool there = blk < b_hi && r < n_rows && is_page(v, page);
+        *off = !there ? 0 : v.table ? offset_of(v, page, r) : (int64_t)(u.s.first + r) * v.stride_row;
+        *ft = there ? (a.causal ? r - past : 0) : INT_MAX;
+    };
+    auto from_lane = [&](int64_t x, int from) __attribute__((always_inline)) {
+        return (int64_t)((uint64_t)(unsigned)__shfl((int)(x >> 32), from) << 32 | (unsigned)__shfl((int)x, from));
+    };
+    auto value_row = [&](int i) { return kBf16 ? i * kRowsPerLoad + lane / kPieces : 4 * lg + i; }; // of the lane's load i
+    raw16 kx[kTiles][KK];
+    raw_v vx[NV][kVH];
+    auto request_keys = [&](int64_t off) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const unsigned char *p = kb + from_lane(off, 16 * t + lr) + 16 * my_piece;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) kx[t][kk] = *reinterpret_cast<const raw16 *>(p + 64 * kk);
+        }
+    };
+    auto request_values = [&](int64_t off) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const unsigned char *p = vb + from_lane(off, value_row(i)) + (kBf16 ? lane % kPieces : lr) * 4 * kVW;
+#pragma unroll
+            for (int h = 0; h < kVH; ++h) vx[i][h] = *reinterpret_cast<const raw_v *>(p + 256 * h);
+        }
+    };
+
+    float m_run = -INFINITY, l_run = 0.f; // of query lr; l_run: over the rows this lane holds
+    f32x4 acc[NF]; // of query lr.  bf16: tile f, features 16 f + 4 lg + r.  fp32: tile (h, e), features 64 h + kVW (4 lg + r) + e
+#pragma unroll
+    for (int f = 0; f < NF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+    unsigned char *const buf = s_buf[wave];
+    int64_t off; // of the block in hand
+    int ft, page_next = 0;
+    if constexpr (kQueryLds) __syncthreads(); // the queries are there
+    // One block; the next one's keys and values are requested as soon as the registers of this one's are free.
+    auto step = [&](auto more, int next) __attribute__((always_inline)) {
+        // ---- scores S^T = K Q^T: query lr, rows 16 t + 4 lg + r ----
+        f32x4 sc[kTiles];
+        if constexpr (kQueryLds) asm volatile("" ::: "memory"); // (the queries are read again, not held)
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    if (!has_piece) kx[t][kk] = raw16{0u, 0u, 0u, 0u};
+                    sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[t][kk]),
+                                                                    __builtin_bit_cast(bf16x8, qb[kk]), sc[t], 0, 0, 0);
+                }
+            }
+        } else { // sums of four terms each, joined pair by pair: nearer to 64 bits than one sum of D terms
+            f32x4 part[KK];
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                f32x4 c[4];
+                const raw16 qk = kQueryLds ? s_q[kk][lane] : qb[kQueryLds ? 0 : kk];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[0][kk][e]), __uint_as_float(qk[e]),
+                                                                f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                part[kk] = (c[0] + c[1]) + (c[2] + c[3]);
+            }
+#pragma unroll
+            for (int n = KK; n > 1; n /= 2)
+#pragma unroll
+                for (int i = 0; i < n / 2; ++i) part[i] = part[2 * i] + part[2 * i + 1];
+            sc[0] = part[0];
+        }
+        int64_t off_next = 0;
+        int ft_next = 0;
+        if constexpr (more.value) {
+            __builtin_amdgcn_sched_barrier(0);
+            find(next, page_next, &off_next, &ft_next);
+            request_keys(off_next);
+            page_next = page_at(next + W);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const bool late = __builtin_amdgcn_ballot_w64(ft > first_tok) != 0; // somebody does not see some row
+        auto first_to_see = [&](int e) { return __shfl(ft, 16 * (e / 4) + 4 * lg + e % 4); }; // row 16 t + 4 lg + r, e = 4 t + r
+        if (late) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sc[t][r] = my_tok >= first_to_see(4 * t + r) ? sc[t][r] : -INFINITY;
+        }
+        // ---- statistics and weights, all of query lr (a NaN score is in no maximum and makes the sum one).  What the
+        // exponents subtract is a whole number, so that bringing sums from one to another multiplies by a power of two ----
+        float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
+        if constexpr (kTiles == 2) mx = fmaxf(mx, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+        mx = ceilf(xrow_max(mx) * scale);
+        if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) { // a maximum moved: bring what was summed to it
+            const float m_new = fmaxf(m_run, mx);
+            const float corr = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= corr;
+#pragma unroll
+            for (int f = 0; f < NF; ++f) acc[f] *= corr;
+        }
+        const float ref = m_run == -INFINITY ? 0.f : m_run;
+        float p[4 * kTiles];
+        if (__builtin_amdgcn_ballot_w64(fabsf(ref) > kLargeRef) != 0) { // somebody's is so large that its rounding shows
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if constexpr (kBf16)
+                        p[4 * t + r] = __builtin_amdgcn_exp2f(fabsf(ref) > kLargeRef ? scaled_apart(sc[t][r], scale, ref) : fmaf(sc[t][r], scale, -ref));
+                    else
+                        p[4 * t + r] = weight_of_any(sc[t][r], scale, ref);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) // (bf16 payloads: the output's own rounding is four orders above the difference's)
+                    p[4 * t + r] = kBf16 ? __builtin_amdgcn_exp2f(fmaf(sc[t][r], scale, -ref)) : weight_of(sc[t][r], scale, ref);
+        }
+        float sum = (p[0] + p[1]) + (p[2] + p[3]);
+        if constexpr (kTiles == 2) sum += (p[4] + p[5]) + (p[6] + p[7]);
+        l_run += sum;
+        // A value that is no number, in a row that a token of the tile does not see, must not reach that token: its weight is zero,
+        // the product is not.  Such blocks (rare) are multiplied token by token, hidden rows as zeros.
+        bool apart = false;
+        if (late) {
+            unsigned worst = 0; // (only whether it reaches the exponent of infinities)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const bool nowhere = __shfl(ft, value_row(i)) == INT_MAX; // zeros in the place of what was read
+#pragma unroll
+                for (int h = 0; h < kVH; ++h)
+#pragma unroll
+                    for (int e = 0; e < kVW; ++e) {
+                        const unsigned x = nowhere ? 0u : vx[i][h][e];
+                        vx[i][h][e] = x;
+                        const unsigned upper = x & 0x7F800000u, lower = kBf16 ? (x & 0x7F80u) << 16 : 0u;
+                        worst = worst > upper ? worst : upper;
+                        worst = worst > lower ? worst : lower;
+                    }
+            }
+            apart = first_tok != last_tok && __builtin_amdgcn_ballot_w64(worst == 0x7F800000u) != 0;
+        }
+        // ---- O^T += V^T P^T: the weights are the B operand as they stand in the lane ----
+        if constexpr (kBf16) {
+            raw16 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                hi[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
+                lo[e] = bf16_pair(p[2 * e] - __uint_as_float(hi[e] << 16), p[2 * e + 1] - __uint_as_float(hi[e] & 0xFFFF0000u));
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int row = value_row(i);
+                *reinterpret_cast<raw_v *>(buf + row * kRowB + 16 * ((lane % kPieces) ^ row_swizzle<D>(row))) = vx[i][0];
+            }
+            if constexpr (more.value) request_values(off_next);
+            asm volatile("" ::: "memory"); // a wave's LDS accesses keep their order; no other wave reads these rows
+            const int q4 = lr >> 2, piece = (lane & 3) >> 1, sub = 8 * (lane & 1);
+            auto values_of = [&](int f) __attribute__((always_inline)) { // rows 4 lg + t and 16 + 4 lg + t of feature 16 f + lr
+                const int r0 = 4 * lg + q4, r1 = r0 + 16;
+                const i16x4 v0 = lds_read_tr16(buf + r0 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r0)) + sub);
+                const i16x4 v1 = lds_read_tr16(buf + r1 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r1)) + sub);
+                return i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            };
+            if (__builtin_expect(!apart, 1)) {
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    const bf16x8 av = __builtin_bit_cast(bf16x8, values_of(f));
+                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi), acc[f], 0, 0, 0);
+                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo), acc[f], 0, 0, 0);
+                }
+            } else {
+#pragma unroll 1
+                for (int tok = first_tok; tok <= last_tok; ++tok)
+#pragma unroll
+                    for (int f = 0; f < NF; ++f) {
+                        i16x8 x = values_of(f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = tok >= first_to_see(e) ? x[e] : (short)0;
+                        f32x4 c = acc[f];
+                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
+                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[f][r] = tok == my_tok ? c[r] : acc[f][r];
+                    }
+            }
+            asm volatile("" ::: "memory"); // the next block's rows take their place
+        } else {
+            __builtin_amdgcn_sched_barrier(0);
+            auto product = [&](int h, int e, auto seen) __attribute__((always_inline)) { // four rows at a time, joined pair by pair
+                f32x4 d[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    d[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(seen(i) ? __uint_as_float(vx[i][h][e]) : 0.f, p[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                return (d[0] + d[1]) + (d[2] + d[3]);
+            };
+            if (__builtin_expect(!apart, 1)) {
+#pragma unroll
+                for (int h = 0; h < kVH; ++h)
+#pragma unroll
+                    for (int e = 0; e < kVW; ++e) acc[kVW * h + e] += product(h, e, [](int) { return true; });
+            } else {
+#pragma unroll 1
+                for (int tok = first_tok; tok <= last_tok; ++tok)
+#pragma unroll
+                    for (int h = 0; h < kVH; ++h)
+#pragma unroll
+                        for (int e = 0; e < kVW; ++e) {
+                            const f32x4 d = product(h, e, [&](int i) { return tok >= first_to_see(i); });
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[kVW * h + e][r] += tok == my_tok ? d[r] : 0.f;
+                        }
+            }
+            if constexpr (more.value) {
+                __builtin_amdgcn_sched_barrier(0);
+                request_values(off_next);
+            }
+        }
+        off = off_next;
+        ft = ft_next;
+    };
+    if (b_lo + wave < b_hi) {
+        int blk = b_lo + wave;
+        page_next = page_at(blk + W);
+        find(blk, page_at(blk), &off, &ft);
+        request_keys(off);
+        request_values(off);
+        // the last block apart: a branch around the loads would make every wait in the loop one for all of them
+        for (; blk + W < b_hi; blk += W) step(std::true_type{}, blk + W);
+        step(std::false_type{}, 0);
+    }
+    // ---- the waves' results join in LDS ----
+    const float l_sum = xrow_sum(l_run);
+    if (lg == 0) {
+        // (maxima leave NaN scores out: where there was nothing else the sum is still to be looked at)
+        s_m[wave][lr] = m_run == -INFINITY && l_sum != 0.f ? 0.f : m_run;
+        s_l[wave][lr] = l_sum;
+    }
+    constexpr int kQuads = D / 4; // 4-feature pieces of an output row, piece c of query n at c ^ (n % kQuads)
+    f32x4(*const s_o)[kQuads] = reinterpret_cast<f32x4(*)[kQuads]>(buf);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+        if constexpr (kBf16) {
+            s_o[lr][(4 * f + lg) ^ (lr & (kQuads - 1))] = acc[f];
+        } else if constexpr (kVW == 4) { // register r of the four tiles of h: features 64 h + 16 lg + 4 r ..
+            const int h = f / 4, r = f % 4;
+            s_o[lr][(16 * h + 4 * lg + r) ^ (lr & (kQuads - 1))] =
+                f32x4{acc[4 * h][r], acc[4 * h + 1][r], acc[4 * h + 2][r], acc[4 * h + 3][r]};
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = kVW * (4 * lg + r) + f;
+                s_o[lr][(d / 4) ^ (lr & (kQuads - 1))][d % 4] = acc[f][r];
+            }
+        }
+    }
+    __syncthreads();
+    T *const out = static_cast<T *>(a.out);
+    const int n_q_here = n_queries - u.tile * kPQ < kPQ ? n_queries - u.tile * kPQ : kPQ;
+    auto row_of = [&](int n) { // of the tile's query n among the outputs
+        const int qq = u.tile * kPQ + n, tok = qq / G;
+        return (int64_t)(u.s.first + tok) * v.Hq + g * G + (qq - tok * G);
+    };
+    auto finish = [&](int n, int c, float m, float l, f32x4 o) {
+        const int64_t row = row_of(n);
+        const bool seen = l != 0.f; // no row that the query sees: zeros (a NaN or +inf score makes l a NaN, and the output with it)
+        o = seen ? o / l : f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (kBf16)
+            *reinterpret_cast<u32x2 *>(out + row * D + 4 * c) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
+        else
+            *reinterpret_cast<f32x4 *>(out + row * D + 4 * c) = o;
+        if (a.pairs && c == 0) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = seen ? f32x2{m, 1.f / l} : f32x2{0.f, 0.f};
+    };
+    for (int i = tid; i < n_q_here * kQuads; i += 64 * W) {
+        const int n = i / kQuads, c = i - n * kQuads;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) m = fmaxf(m, s_m[w][n]);
+        float l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float lw = s_l[w][n];
+            if (lw != 0.f) { // a wave none of whose rows the query sees has nothing to add (a NaN has)
+                const float x = __builtin_amdgcn_exp2f(s_m[w][n] - m);
+                l = fmaf(lw, x, l);
+                const f32x4 ow = reinterpret_cast<const f32x4(*)[kQuads]>(s_buf[w])[n][c ^ (n & (kQuads - 1))];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(ow[e], x, o[e]);
+            }
+        }
+        if (u.chunks > 1) { // the chunk's record: [0] maximum, [1] normaliser, [2..] unnormalised output
+            float *rec = a.records + ((int64_t)(u.record + u.chunk) * kPQ + n) * (D + 2);
+            if (c == 0) store_far(rec, m, l);
+            store_far(rec + 2 + 4 * c, o[0], o[1]);
+            store_far(rec + 4 + 4 * c, o[2], o[3]);
+        } else {
+            finish(n, c, m, l, o);
+        }
+    }
+    if (u.chunks == 1) return;
+    // ---- the chunks' records: the last workgroup of the tile to get here joins them, in their order ----
+    __shared__ int s_last;
+    if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
+    for (int i = tid; i < n_q_here * kQuads; i += 64 * W) {
+        const int n = i / kQuads, c = i - n * kQuads;
+        const float *rec = a.records + ((int64_t)u.record * kPQ + n) * (D + 2);
+        constexpr int64_t kNext = (int64_t)kPQ * (D + 2);
+        constexpr int kAhead = 8; // records requested together
+        float m = -INFINITY, l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int s0 = 0; s0 < u.chunks; s0 += kAhead) {
+            f32x2 st[kAhead], x0[kAhead], x1[kAhead];
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+                if (s0 + s >= u.chunks) break;
+                st[s] = load_far(rec + (s0 + s) * kNext);
+                x0[s] = load_far(rec + (s0 + s) * kNext + 2 + 4 * c);
+                x1[s] = load_far(rec + (s0 + s) * kNext + 4 + 4 * c);
+            }
+            float m_new = m;
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s)
+                if (s0 + s < u.chunks) m_new = fmaxf(m_new, st[s][0]);
+            const float corr = l != 0.f ? __builtin_amdgcn_exp2f(m - m_new) : 0.f;
+            l *= corr;
+            o *= corr;
+            m = m_new;
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+                if (s0 + s >= u.chunks) break;
+                if (st[s][1] == 0.f) continue; // none of its rows is seen
+                const float x = __builtin_amdgcn_exp2f(st[s][0] - m);
+                l = fmaf(st[s][1], x, l);
+                o = f32x4{fmaf(x0[s][0], x, o[0]), fmaf(x0[s][1], x, o[1]), fmaf(x1[s][0], x, o[2]), fmaf(x1[s][1], x, o[3])};
+            }
+        }
+        finish(n, c, m, l, o);
+    }
+}
+
+// What each row receives: weights_out[b][g][j] = decay * weights_in[b][g][j] + sum over the tokens and the group's heads of p_j / sum p.
+// Grid (64 rows, sequence, KV head).  A wave keeps the keys of 16 rows (the A operand) in registers and the sequence's queries stream past it, 16 at
+// a time, with what their weights subtract and the sum they are divided by: S^T leaves a lane one query and four rows, so the sums
+// over the queries run in the lane until the end, where 16 lanes join.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_weights_kernel(PagedAttendArgs a, int n_groups) {
+    constexpr bool kBf16 = sizeof(T) == 2;
+    constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
+    constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16;
+    const PagedView &v = a.view;
+    const int g = blockIdx.z, b = blockIdx.y;
+    const SeqShape s = shape_of(v, a.plan, b);
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, G = v.G;
+    const int n_w = s.rows < a.weights_rows ? s.rows : a.weights_rows; // rows that have a weight
+    const int past = s.length - s.n_new, n_queries = s.n_new * G;
+    const float scale = a.scale_log2e * (1.f / query_factor<T, D>());
+    const bool has_piece = kPieces >= 4 || lg < kPieces;
+    const int my_piece = kPieces >= 4 ? lg : lg & (kPieces - 1);
+    for (int r0 = 16 * ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)); r0 < n_w; r0 += 64 * n_groups) {
+        const int r = r0 + lr;
+        const int page = r < n_w ? (v.table ? v.table[entry_of(v, b, r)] : 0) : -1;
+        const bool there = is_page(v, page);
+        const int64_t off = !there ? 0 : v.table ? offset_of(v, page, r) : (int64_t)(s.first + r) * v.stride_row;
+        const unsigned char *kp = v.k + g * v.stride_head + off + 16 * my_piece;
+        raw16 kx[KK];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            kx[kk] = *reinterpret_cast<const raw16 *>(kp + 64 * kk);
+            if (!has_piece) kx[kk] = raw16{0u, 0u, 0u, 0u};
+        }
+        const int ft = there ? (a.causal ? r - past : 0) : INT_MAX;
+        int from[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) from[e] = __shfl(ft, 4 * lg + e);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // queries before the first row's first token see none of these rows
+        int q0 = a.causal && r0 - past > 0 ? (r0 - past < s.n_new ? (r0 - past) * G & ~15 : n_queries) : 0;
+        for (; q0 < n_queries; q0 += 16) {
+            const int qq = q0 + lr < n_queries ? q0 + lr : n_queries - 1, tok = qq / G, h = g * G + (qq - tok * G);
+            const unsigned char *qp = a.q + (int64_t)(s.first + tok) * a.q_token + (int64_t)h * a.q_head + 16 * my_piece;
+            const f32x2 pair = *reinterpret_cast<const f32x2 *>(a.pairs + 2 * ((int64_t)(s.first + tok) * v.Hq + h));
+            raw16 qx[KK];
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                qx[kk] = *reinterpret_cast<const raw16 *>(qp + 64 * kk);
+                qx[kk] = has_piece ? brought_down<T, D>(qx[kk]) : raw16{0u, 0u, 0u, 0u};
+            }
+            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (kBf16) {
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[kk]), __builtin_bit_cast(bf16x8, qx[kk]), sc, 0, 0, 0);
+            } else { // (in the attention's own order: the same scores)
+                f32x4 part[KK];
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    f32x4 c[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[kk][e]), __uint_as_float(qx[kk][e]),
+                                                                    f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                    part[kk] = (c[0] + c[1]) + (c[2] + c[3]);
+                }
+#pragma unroll
+                for (int n = KK; n > 1; n /= 2)
+#pragma unroll
+                    for (int i = 0; i < n / 2; ++i) part[i] = part[2 * i] + part[2 * i + 1];
+                sc = part[0];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float w = weight_of_any(sc[e], scale, pair[0]) * pair[1];
+                sum[e] += q0 + lr < n_queries && tok >= from[e] ? w : 0.f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = row16_sum(sum[e]);
+        const int row = r0 + 4 * lg + (lr & 3);
+        if (lr < 4 && row < n_w) {
+            const int64_t at = b * a.weights_seq + g * a.weights_head + row;
+            const float got = lr == 0 ? sum[0] : lr == 1 ? sum[1] : lr == 2 ? sum[2] : sum[3];
+            a.weights_out[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], got) : got;
+        }
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_typed(const PagedAttendArgs &a, hipStream_t st) {
+    const unsigned grid = (unsigned)units_bound(a.view, a.plan);
+    if (grid > 0) {
+        hipLaunchKernelGGL((paged_attend_kernel<T, D>), dim3(grid), dim3(64 * kPWaves), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!a.weights_out) return hipSuccess;
+    const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
+    int64_t groups = (rows + 63) / 64, most = 8192 / ((int64_t)a.view.Hkv * a.view.n_seqs);
+    if (most < 16) most = 16;
+    if (groups > most) groups = most; // (a workgroup goes round: a table is often wider than its sequences)
+    if (groups < 1) return hipSuccess;
+    hipLaunchKernelGGL((paged_weights_kernel<T, D>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, (int)groups);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_by_dim(const PagedAttendArgs &a, int D, hipStream_t st) {
+    switch (D) {
+    case 16: return launch_typed<T, 16>(a, st);
+    case 32: return launch_typed<T, 32>(a, st);
+    case 64: return launch_typed<T, 64>(a, st);
+    default: return launch_typed<T, 128>(a, st);
+    }
+}
+
+} // namespace
+
+PlanShape paged_plan(int dtype) {
+    PlanShape p;
+    p.queries = kPQ;
+    p.rows = dtype == MUKV_BF16 ? 128 : 64; // a block of every wave
+    p.target = 512;                         // two workgroups per compute unit, as many as are resident
+    p.most = 64;
+    return p;
+}
+
+hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st) {
+    return dtype == MUKV_BF16 ? launch_by_dim<uint16_t>(a, D, st) : launch_by_dim<float>(a, D, st);
+}
+
+} // namespace mukv

@@ -22,4 +22,27 @@ struct RopeArgs {
 };
 hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
 
+// The plan's measures for a call: which kernel takes it follows from types and sizes that the host knows.
+PlanShape paged_plan(int dtype);
+
+struct PagedAttendArgs {
+    PagedView view;
+    PlanShape plan;
+    const unsigned char *q; // strides in bytes
+    int64_t q_token, q_head;
+    void *out;     // [n_tokens][Hq][D]
+    int *counts;   // [records_bound], zero between calls
+    float *records; // [records_bound][queries of a tile][D + 2]
+    float *pairs;  // [n_tokens * Hq][2]: what a query's weights' exponents subtract, 1 / their sum (0: no row seen); or null
+    float scale_log2e;
+    int causal;
+    // with pairs: weights_out[b][g][j] = decay * weights_in[b][g][j] + what row j received; weights_in may be null
+    const float *weights_in;
+    float *weights_out;
+    int64_t weights_seq, weights_head; // strides in elements
+    int weights_rows;                  // rows a head has room for
+    float decay;
+};
+hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st);
+
 } // namespace mukv

@@ -77,3 +77,51 @@ def near(got, want, err, dtype, rounded=True):
     tol = err + h * (np.abs(want) + err) + 1e-40
     bad = ~(np.abs(got - want) <= tol)
     assert not bad.any(), (int(bad.sum()), got[bad][:5], want[bad][:5], tol[bad][:5] if np.ndim(tol) else tol)
+
+
+def gathered(pages, layer, table, lengths, R, b, n):
+    """Rows 0..n-1 of sequence b as [n][head][D], and which of them are there."""
+    page, r, ok = places(table, lengths, R, pages.shape[1], b, np.arange(n))
+    return pages[layer][page, :, r], ok
+
+
+def attention(q, rows_of, lengths, offsets, hkv, causal, room):
+    """q [T][Hq][D]; rows_of(b, n) -> k, v [n][Hkv][D] and which rows are there.  Returns out, the weights every row received
+    [B][Hkv][n], and for each output the mean of |v| under its weights and the largest sum |q_i k_i| of the rows it sees."""
+    T, Hq, D = q.shape
+    G = Hq // hkv
+    out, amean, reach = np.zeros_like(q), np.zeros_like(q), np.zeros((T, Hq, 1))
+    received = []
+    for b in range(len(lengths)):
+        lo, hi = offsets[b], offsets[b + 1]
+        n = min(max(int(lengths[b]), 0), room)
+        k, v, there = rows_of(b, n)
+        got = np.zeros((hkv, n))
+        for i in range(hi - lo):
+            seen = there & (np.arange(n) <= max(int(lengths[b]), 0) - (hi - lo) + i) if causal else there
+            if not seen.any():
+                continue
+            for h in range(Hq):
+                kk, vv = k[seen, h // G], v[seen, h // G]
+                with np.errstate(invalid="ignore", over="ignore"):
+                    s = kk @ q[lo + i, h] / np.sqrt(D)
+                    w = np.exp(s - s.max())
+                    w = w / w.sum()
+                    out[lo + i, h] = w @ vv
+                    amean[lo + i, h] = w @ np.abs(vv)
+                    reach[lo + i, h] = (np.abs(kk) @ np.abs(q[lo + i, h])).max()
+                got[h // G, seen] += w
+        received.append(got)
+    return out, received, amean, reach
+
+
+def attention_error(amean, reach, n, D, dtype, single_weights=False):
+    """What an output may be off before its last rounding.  A score: its products add up in fp32 (bf16 payloads: D terms in an order of
+    the matrix core's; fp32: sums of four joined pair by pair), a weight is off by that and the exponential's own two steps, in numerator and
+    denominator; sums over n rows, 16 at a time and more; bf16 payloads: the weight as a pair of bf16 (2^-16), or as one (2^-8)."""
+    terms = D if dtype == torch.bfloat16 else 12
+    score = (terms + 4) * 2.0**-24 * reach / np.sqrt(D)
+    rel = 2 * score + (n / 16 + 20) * 2.0**-24
+    if dtype == torch.bfloat16:
+        rel = rel + (2.0**-8 if single_weights else 2.0**-16)
+    return amean * rel

@@ -83,3 +83,51 @@ def test_nothing_to_do_is_no_error():
     assert mk.load().mukv_rope(C.byref(rope()), P, C.byref(ST), P, 0, 8, 64, mk.MUKV_BF16, P, C.byref(ST), 0, None) == mk.MUKV_OK
     assert mk.load().mukv_paged_append(None, 0, C.byref(seqs()), P, None, P, None, None, None, None, None, None, None, None) == BAD
     assert mk.load().mukv_rope(None, P, C.byref(ST), P, 4, 8, 64, 0, P, C.byref(ST), 0, None) == BAD
+
+
+# ---- attention ----
+def attend(p=None, layer=0, s=None, q=P, qs=ST, causal=1, out=P, w=None, ws=P, n=1 << 40):
+    ref = lambda x: None if x is None else C.byref(x)
+    return mk.load().mukv_paged_attend(ref(p or pages()), layer, ref(s or seqs()), q, ref(qs), causal, out, ref(w), ws, n, None)
+
+
+def weights(**kw):
+    return mk.mukv_row_weights(**{**dict(in_=P, out=P, stride_layer=0, stride_seq=400, stride_head=100, rows=100, decay=1.0), **kw})
+
+
+WEIGHTS = [({"out": None}, BAD), ({"rows": 0}, BAD), ({"stride_seq": -1}, BAD), ({"stride_head": -1}, BAD), ({"stride_layer": -1}, BAD),
+           ({"decay": -0.5}, BAD), ({"decay": float("nan")}, BAD), ({"decay": float("inf")}, BAD), ({"out": P + 2}, UNSUP), ({"in_": P + 1}, UNSUP)]
+
+
+@pytest.mark.parametrize("kw,status", PAGES)
+def test_attend_refuses_pages(kw, status):
+    assert attend(p=pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [(k, s) for k, s in SEQS if k not in ({"table": None}, {"offsets": None})] + [
+    ({"table": None, "offsets": None, "n_tokens": 6}, BAD), ({"offsets": None}, SHAPE)])
+def test_attend_refuses_sequences(kw, status):
+    assert attend(s=seqs(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", WEIGHTS)
+def test_attend_refuses_weights(kw, status):
+    assert attend(w=weights(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({"layer": -1}, BAD), ({"layer": 2}, BAD), ({"causal": 2}, BAD), ({"q": None}, BAD), ({"out": None}, BAD), ({"ws": None}, BAD),
+    ({"n": 1000}, mk.MUKV_ERR_CAPACITY), ({"q": P + 8}, UNSUP), ({"out": P + 8}, UNSUP), ({"ws": P + 8}, UNSUP),
+    ({"qs": mk.mukv_strides(0, 60, 1024)}, UNSUP), ({"qs": mk.mukv_strides(0, -64, 1024)}, BAD)])
+def test_attend_refuses_tensors(kw, status):
+    assert attend(**kw) == status
+
+
+def test_workspace_size():
+    call = lambda p, s, w, out: mk.load().mukv_paged_workspace_size(C.byref(p), C.byref(s), w, out)
+    n, m = C.c_int64(), C.c_int64()
+    assert call(pages(), seqs(), 0, C.byref(n)) == call(pages(), seqs(), 1, C.byref(m)) == mk.MUKV_OK
+    assert m.value == n.value + 8 * 5 * 8 and n.value > 0
+    assert call(pages(), seqs(), 2, C.byref(n)) == call(pages(), seqs(), 0, None) == BAD
+    assert call(pages(n_pages=0), seqs(), 0, C.byref(n)) == BAD
+    assert attend(s=seqs(n_tokens=0)) == mk.MUKV_OK
