@@ -652,7 +652,7 @@ typedef struct mukv_row_weights {
     int64_t stride_seq;
     int64_t stride_head;
     int32_t rows;         /* rows a head has room for                                           */
-    float decay;          /* finite, not negative; mukv_paged_attend: out = decay * in + received
+    float decay;          /* finite, not negative: mukv_paged_attend gives decay * in + received
                              (1: weights accumulate)                                            */
 } mukv_row_weights;
 
@@ -686,6 +686,31 @@ int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, in
 int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *q,
                       const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
                       void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Eviction by accumulated weight, all layers at once: of every (layer, sequence, KV
+ * head) `budget` rows stay -- the first n_sink, the last n_recent and, of the others,
+ * those with the largest weights->in (equal weights: the lower row; NaN below everything;
+ * rows past weights->rows weigh 0) -- in their order, packed to rows 0, 1, ..., their
+ * weights to weights->out.  A sequence with no more rows keeps all of them.  Rows on pages
+ * that do not exist are never kept, so the rows of a sequence that stay number the same in
+ * all layers and heads.  Keys were rotated where they stood and stay as they are.
+ *
+ *   weights      in (required) and out; out may be in.  Entries of out from the rows that
+ *                stay up to the former length become 0; decay is not read
+ *   into_table   device int32 [n_seqs][into_width]: pages to pack the rows into, none of them
+ *                in `table` (the former pages are then free); NULL: in place.  A row whose
+ *                page there does not exist is lost
+ *   kept_out     device int32 [n_layers][n_seqs][n_kv_heads][budget]: the former row of every
+ *                row that stays, padded with -1
+ *   lengths_out  device int32 [n_seqs], may be seqs->lengths
+ *
+ * A page must belong to one sequence.  offsets, n_tokens and max_new of seqs are not read.
+ * Errors: INVALID_ARG (budget < 1, n_sink + n_recent > budget), UNSUPPORTED.
+ */
+int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,
+                     int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
+                     int32_t *kept_out, int32_t *lengths_out, void *stream);
 
 /* Fills *out (host).  Does not synchronise. */
 int mukv_get_state(const mukv_ctx *ctx, mukv_state *out);

@@ -97,7 +97,7 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_attend", "mukv_prefill_workspace_size", "mukv_prefill_attend", "mukv_prefill_attend_static",
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
            "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append",
-           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_strerror")
+           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_strerror")
 
 _lib = None
 
@@ -144,6 +144,7 @@ def load():
                                       C.POINTER(mukv_rope_table), vp, vp]
     lib.mukv_paged_workspace_size.argtypes = [paged, seqs, i32, C.POINTER(C.c_int64)]
     lib.mukv_paged_attend.argtypes = [paged, i32, seqs, vp, strides, i32, vp, C.POINTER(mukv_row_weights), vp, C.c_int64, vp]
+    lib.mukv_paged_evict.argtypes = [paged, seqs, C.POINTER(mukv_row_weights), i32, i32, i32, vp, i32, vp, vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -329,6 +330,11 @@ def mukv_paged_workspace_size(pages, seqs, with_weights):
 def mukv_paged_attend(pages, layer, seqs, q_ptr, q_strides, causal, out_ptr, weights, ws_ptr, ws_bytes, stream):
     _check((_lib or load()).mukv_paged_attend(pages, layer, seqs, q_ptr, q_strides, causal, out_ptr, weights, ws_ptr, ws_bytes, stream),
            "mukv_paged_attend")
+
+
+def mukv_paged_evict(pages, seqs, weights, budget, n_sink, n_recent, into_ptr, into_width, kept_ptr, lengths_ptr, stream):
+    _check((_lib or load()).mukv_paged_evict(pages, seqs, weights, budget, n_sink, n_recent, into_ptr, into_width, kept_ptr, lengths_ptr,
+                                             stream), "mukv_paged_evict")
 
 
 # ---- convenience object ----------------------------------------------------------------------
@@ -781,6 +787,32 @@ class PagedKV:
         assert q.shape == (T, p.n_q_heads, p.head_dim) and q.dtype == self.dtype
         s = self._sequences(table, lengths, offsets, T, max_new)
         return _attend(self, s, layer, q, causal, out, weights, weights_out, decay)
+
+    def evict(self, table, lengths, weights, budget, *, sink=0, recent=0, into=None, weights_out=None, kept=None, lengths_out=None):
+        """Brings every sequence down to `budget` rows per layer and KV head: the first `sink`, the last `recent`, and the others
+        by weights, float32 [layer][sequence][KV head][row].  The rows that stay are packed in their order, in place or into the
+        pages of the table `into`, and so are their weights (weights_out None: in place).  Returns the rows kept, int32
+        [layer][sequence][KV head][budget] padded with -1, and the new lengths (lengths_out may be lengths)."""
+        p = self._pages
+        s = self._sequences(table, lengths, None, 0, 0)
+        if weights_out is None:
+            weights_out = weights
+        assert weights.dtype == weights_out.dtype == torch.float32 and weights.dim() == 4 and weights.stride(3) == 1
+        assert weights.shape[:3] == (p.n_layers, s.n_seqs, p.n_kv_heads)
+        assert weights_out.shape == weights.shape and weights_out.stride() == weights.stride()
+        if into is not None:
+            assert into.dtype == torch.int32 and into.is_contiguous() and into.dim() == 2 and into.shape[0] == s.n_seqs
+        shape = (p.n_layers, s.n_seqs, p.n_kv_heads, budget)
+        if kept is None:
+            kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+        if lengths_out is None:
+            lengths_out = torch.empty_like(lengths)
+        assert kept.dtype == lengths_out.dtype == torch.int32 and kept.shape == shape and lengths_out.shape == lengths.shape
+        assert kept.is_contiguous() and lengths_out.is_contiguous()
+        w = mukv_row_weights(weights.data_ptr(), weights_out.data_ptr(), *weights.stride()[:3], weights.shape[3], 0.0)
+        mukv_paged_evict(p, s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1], kept.data_ptr(),
+                         lengths_out.data_ptr(), _stream())
+        return kept, lengths_out
 
 
 def _attend(cache, s, layer, q, causal, out, weights, weights_out, decay):

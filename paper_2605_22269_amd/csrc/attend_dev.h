@@ -142,4 +142,15 @@ __device__ __forceinline__ int val_slot(int piece, int row) {
     return D == 128 ? piece ^ (((row & 3) << 2) | ((row >> 2) & 3)) : piece ^ (((row >> 1) & 1) << 2);
 }
 
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_prefix(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false); // within the 16 lanes of a row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false); // the row before, in rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false); // the half before, in the upper half
+    return v;
+}
+
 } // namespace mukv

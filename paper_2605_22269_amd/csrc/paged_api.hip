@@ -49,14 +49,14 @@ int check_seqs(const mukv_paged *p, const mukv_seqs *s, bool may_be_packed, bool
     if (has_tokens) {
         if (s->n_tokens < 0 || s->max_new < 0) return MUKV_ERR_INVALID_ARG;
         if (!s->offsets && s->n_tokens % s->n_seqs) return MUKV_ERR_SHAPE;
-        if ((int64_t)s->n_tokens * p->n_q_heads > 0x7fffffff) return MUKV_ERR_UNSUPPORTED;
+        if ((int64_t)s->n_tokens * p->n_q_heads > 0x7ff00000) return MUKV_ERR_UNSUPPORTED;
     }
     if (!s->table) {
         if (!may_be_packed) return MUKV_ERR_INVALID_ARG;
         return s->offsets ? MUKV_OK : MUKV_ERR_INVALID_ARG;
     }
     if (!s->lengths || s->table_width < 1) return MUKV_ERR_INVALID_ARG;
-    if (p->page_rows > 1 << 24 || (int64_t)s->table_width * p->page_rows > 0x7ffffff0 || (int64_t)s->table_width * s->n_seqs > 0x7fffffff)
+    if (p->page_rows > 1 << 24 || (int64_t)s->table_width * p->page_rows > 0x7ff00000 || (int64_t)s->table_width * s->n_seqs > 0x7fffffff)
         return MUKV_ERR_UNSUPPORTED; // row and entry numbers are 32-bit in the kernels
     return MUKV_OK;
 }
@@ -258,6 +258,44 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     DeviceScope dev(pages->device_id);
     if (!dev.ok) return MUKV_ERR_HIP;
     return finished(mukv::launch_paged_attend(a, D, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,
+                     int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
+                     int32_t *kept_out, int32_t *lengths_out, void *stream) {
+    if (const int rc = check_pages(pages)) return rc;
+    if (const int rc = check_seqs(pages, seqs, false, false)) return rc;
+    if (!weights || !weights->in || !kept_out || !lengths_out) return MUKV_ERR_INVALID_ARG;
+    mukv_row_weights w = *weights;
+    w.decay = 0.f; // not read
+    if (const int rc = check_weights(&w)) return rc;
+    if (budget < 1 || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > budget) return MUKV_ERR_INVALID_ARG;
+    if (into_table && into_width < 1) return MUKV_ERR_INVALID_ARG;
+    const int64_t lists = (int64_t)pages->n_layers * seqs->n_seqs * pages->n_kv_heads;
+    if (lists > 0x7fffffff || (int64_t)into_width * seqs->n_seqs > 0x7fffffff || budget > 1 << 30) return MUKV_ERR_UNSUPPORTED;
+    mukv::EvictArgs a = {};
+    mukv_seqs s = *seqs;
+    s.offsets = nullptr;
+    s.n_tokens = s.max_new = 0;
+    const int esz = elem_size(pages->dtype);
+    a.view = view_of(*pages, 0, s);
+    a.stride_layer = in_bytes(pages->stride_layer, pages->n_layers, esz);
+    a.w_in = w.in;
+    a.w_out = w.out;
+    a.w_layer = w.stride_layer;
+    a.w_seq = w.stride_seq;
+    a.w_head = w.stride_head;
+    a.w_rows = w.rows;
+    a.budget = budget;
+    a.n_sink = n_sink;
+    a.n_recent = n_recent;
+    a.into = into_table;
+    a.into_width = into_width;
+    a.kept = kept_out;
+    a.lengths_out = lengths_out;
+    DeviceScope dev(pages->device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    return finished(mukv::launch_paged_evict(a, pages->n_layers, pages->head_dim * esz, pages->device_id, reinterpret_cast<hipStream_t>(stream)));
 }
 
 } // extern "C"

@@ -45,4 +45,17 @@ struct PagedAttendArgs {
 };
 hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st);
 
+struct EvictArgs {
+    PagedView view; // of layer 0
+    int64_t stride_layer; // bytes
+    const float *w_in;
+    float *w_out;
+    int64_t w_layer, w_seq, w_head; // elements
+    int w_rows, budget, n_sink, n_recent;
+    const int32_t *into; // [n_seqs][into_width], or null: in place
+    int into_width;
+    int32_t *kept, *lengths_out; // [layer][n_seqs][Hkv][budget], [n_seqs]
+};
+hipError_t launch_paged_evict(const EvictArgs &a, int n_layers, int row_bytes, int device, hipStream_t st);
+
 } // namespace mukv

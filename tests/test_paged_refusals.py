@@ -131,3 +131,33 @@ def test_workspace_size():
     assert call(pages(), seqs(), 2, C.byref(n)) == call(pages(), seqs(), 0, None) == BAD
     assert call(pages(n_pages=0), seqs(), 0, C.byref(n)) == BAD
     assert attend(s=seqs(n_tokens=0)) == mk.MUKV_OK
+
+
+# ---- eviction ----
+def evict(p=None, s=None, w=None, budget=50, sink=4, recent=10, into=P, width=5, kept=P, lengths=P):
+    w = weights() if w is None else w
+    return mk.load().mukv_paged_evict(C.byref(p or pages()), C.byref(s or seqs()), C.byref(w) if w else None, budget, sink, recent, into, width,
+                                      kept, lengths, None)
+
+
+@pytest.mark.parametrize("kw,status", PAGES)
+def test_evict_refuses_pages(kw, status):
+    assert evict(p=pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [({"n_seqs": 0}, BAD), ({"table": None}, BAD), ({"lengths": None}, BAD), ({"table_width": 0}, BAD),
+                                       ({"table_width": 1 << 28}, UNSUP)])
+def test_evict_refuses_sequences(kw, status):
+    assert evict(s=seqs(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [x for x in WEIGHTS if "decay" not in x[0]] + [({"in_": None}, BAD)])
+def test_evict_refuses_weights(kw, status):
+    assert evict(w=weights(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({"budget": 0}, BAD), ({"sink": -1}, BAD), ({"recent": -1}, BAD), ({"sink": 41}, BAD), ({"width": 0}, BAD), ({"kept": None}, BAD),
+    ({"lengths": None}, BAD), ({"w": 0}, BAD), ({"budget": (1 << 30) + 1}, UNSUP)])
+def test_evict_refuses(kw, status):
+    assert evict(**kw) == status
