@@ -840,7 +840,7 @@ class _Workspace:
         self.device, self.by_stream, self.need = device, {}, (None, 0)
 
     def get(self, pages, s, with_weights):
-        key = (s.n_tokens, with_weights)   # (what else it takes is the cache's own)
+        key = (s.n_tokens, s.n_seqs, s.max_new, with_weights)   # (what else it takes is the cache's own)
         if self.need[0] != key:
             self.need = key, mukv_paged_workspace_size(pages, s, int(with_weights))
         ws = self.by_stream.get(st := _stream())

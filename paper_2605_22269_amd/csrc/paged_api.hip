@@ -127,17 +127,19 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
     a.inverse = r->inverse != 0;
 }
 
-// The workspace of an attention call: counts, records, then (with weights) a pair per query.
+// Which kernel takes an attention call, and its workspace: counts, records, then (with weights) a pair per query.
 struct Space {
-    int64_t counts, records, pairs, bytes; // offsets
+    bool flash;
+    mukv::PlanShape plan;
+    int64_t records, pairs, bytes; // offsets; the counts are at 0
 };
 Space space_of(const mukv_paged &p, const mukv_seqs &s, bool with_weights) {
-    const mukv::PlanShape plan = mukv::paged_plan(p.dtype);
-    const int64_t n = mukv::records_bound(plan);
+    const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
     Space x;
-    x.counts = 0;
-    x.records = (4 * n + 255) & ~(int64_t)255;
-    x.pairs = x.records + 4 * n * plan.queries * (p.head_dim + 2);
+    x.flash = mukv::paged_takes_flash(p.dtype, p.head_dim, p.n_q_heads / p.n_kv_heads, hint, with_weights);
+    x.plan = mukv::paged_plan(p.dtype, x.flash);
+    x.records = 4 * mukv::kPlanRecords;
+    x.pairs = x.records + 4 * (int64_t)mukv::records_bound(x.plan) * x.plan.queries * (p.head_dim + 2);
     x.bytes = x.pairs + (with_weights ? 8 * (int64_t)s.n_tokens * p.n_q_heads : 0);
     return x;
 }
@@ -236,13 +238,13 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
     mukv::PagedAttendArgs a = {};
     a.view = view_of(*pages, layer, *seqs);
-    a.plan = mukv::paged_plan(pages->dtype);
+    a.plan = x.plan;
     a.q = static_cast<const unsigned char *>(q);
     a.q_token = in_bytes(qs->token, T, esz);
     a.q_head = in_bytes(qs->head, pages->n_q_heads, esz);
     a.out = out;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
-    a.counts = reinterpret_cast<int *>(ws + x.counts);
+    a.counts = reinterpret_cast<int *>(ws);
     a.records = reinterpret_cast<float *>(ws + x.records);
     a.pairs = weights ? reinterpret_cast<float *>(ws + x.pairs) : nullptr;
     a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
@@ -257,7 +259,7 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     }
     DeviceScope dev(pages->device_id);
     if (!dev.ok) return MUKV_ERR_HIP;
-    return finished(mukv::launch_paged_attend(a, D, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
+    return finished(mukv::launch_paged_attend(a, D, pages->dtype, x.flash, reinterpret_cast<hipStream_t>(stream)));
 }
 
 int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,

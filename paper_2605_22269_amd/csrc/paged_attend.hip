@@ -9,70 +9,13 @@
 #include <type_traits>
 
 #include "attend_dev.h"
-#include "paged_internal.h"
+#include "paged_dev.h"
 
 namespace mukv {
 
 namespace {
 
 constexpr int kPQ = 16, kPWaves = 4; // queries and waves of a workgroup
-
-struct Unit {
-    SeqShape s;
-    int b, g, tile, chunk, chunks, per; // per: blocks of a chunk
-    int record;                         // of the tile's first chunk
-};
-
-// The unit of this workgroup, the same in all lanes; false: there is none.
-__device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p, int id, Unit *u) {
-    const int lane = threadIdx.x & 63;
-    if (v.n_seqs == 1) {
-        u->s = shape_of(v, p, 0);
-        u->b = 0;
-        u->per = chunk_of(p, u->s, chunk_of(p, blocks_of(v, u->s)));
-        u->chunks = (int)div_up(u->s.blocks, u->per);
-        u->record = 0;
-        if (id >= u->s.tiles * v.Hkv * u->chunks) return false;
-    } else {
-        const SeqShape none = {0, 0, 0, 0, 0, 1};
-        SeqShape s = none;
-        double all = 0.0;
-        for (int b0 = 0; b0 < v.n_seqs; b0 += 64) {
-            s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
-            all += blocks_of(v, s);
-        }
-        const int per = chunk_of(p, wave_sum(all));
-        int units0 = 0, records0 = 0, b0 = 0;
-        for (;; b0 += 64) {
-            if (b0 >= v.n_seqs) return false;
-            if (v.n_seqs > 64) s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
-            const int chunks = chunks_of(p, s, per), units = s.tiles * v.Hkv * chunks, records = chunks > 1 ? units : 0;
-            const int units1 = units0 + wave_prefix(units), records1 = records0 + wave_prefix(records);
-            const uint64_t here = __builtin_amdgcn_ballot_w64(id < units1);
-            if (here) {
-                const int at = __builtin_ctzll(here);
-                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-                u->s = SeqShape{of(s.first), of(s.n_new), of(s.length), of(s.rows), of(s.tiles), of(s.blocks)};
-                u->b = b0 + at;
-                u->per = chunk_of(p, u->s, per);
-                u->chunks = of(chunks);
-                u->record = of(records1 - records);
-                id -= of(units1 - units);
-                break;
-            }
-            units0 = __builtin_amdgcn_readlane(units1, 63);
-            records0 = __builtin_amdgcn_readlane(records1, 63);
-        }
-    }
-    // KV heads next to each other: workgroups go to the eight XCDs in turn, so an XCD meets few heads' rows
-    u->g = id % v.Hkv;
-    id /= v.Hkv;
-    u->chunk = id % u->chunks;
-    const int rank = id / u->chunks;
-    u->record += (rank * v.Hkv + u->g) * u->chunks;
-    u->tile = u->s.tiles - 1 - rank; // under the mask the last ones have the most to do: they start first
-    return true;
-}
 
 // The rows of a tile, in blocks of 32 (bf16) or 16 (fp32), dealt to the waves in turn; nothing crosses the waves until the end.
 //   rows     a lane works out where one row lives, from a table entry that was requested a block earlier; the others fetch that by
@@ -603,16 +546,21 @@ hipError_t launch_by_dim(const PagedAttendArgs &a, int D, hipStream_t st) {
 
 } // namespace
 
-PlanShape paged_plan(int dtype) {
+bool paged_takes_flash(int dtype, int D, int G, int64_t new_hint, bool with_weights) {
+    return dtype == MUKV_BF16 && D >= 64 && !with_weights && new_hint * G > 64;
+}
+
+PlanShape paged_plan(int dtype, bool flash) {
     PlanShape p;
-    p.queries = kPQ;
-    p.rows = dtype == MUKV_BF16 ? 128 : 64; // a block of every wave
-    p.target = 512;                         // two workgroups per compute unit, as many as are resident
+    p.queries = flash ? 256 : kPQ;
+    p.rows = flash ? 64 : dtype == MUKV_BF16 ? 128 : 64; // a step of the workgroup; a block of every wave
+    p.target = flash ? 256 : 512;                        // as many workgroups as are resident
     p.most = 64;
     return p;
 }
 
-hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st) {
+hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, bool flash, hipStream_t st) {
+    if (flash) return launch_paged_flash(a, D, st);
     return dtype == MUKV_BF16 ? launch_by_dim<uint16_t>(a, D, st) : launch_by_dim<float>(a, D, st);
 }
 

@@ -22,8 +22,11 @@ struct RopeArgs {
 };
 hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
 
-// The plan's measures for a call: which kernel takes it follows from types and sizes that the host knows.
-PlanShape paged_plan(int dtype);
+// The plan's measures for a call: which kernel takes it follows from types and sizes that the host knows (paged_attend.hip).
+// new_hint: new tokens of a sequence, as far as that is known.
+bool paged_takes_flash(int dtype, int D, int G, int64_t new_hint, bool with_weights);
+PlanShape paged_plan(int dtype, bool flash);
+constexpr int kPlanRecords = 1024; // most that any plan's records_bound is: the counts at a workspace's start
 
 struct PagedAttendArgs {
     PagedView view;
@@ -43,7 +46,8 @@ struct PagedAttendArgs {
     int weights_rows;                  // rows a head has room for
     float decay;
 };
-hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st);
+hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, bool flash, hipStream_t st);
+hipError_t launch_paged_flash(const PagedAttendArgs &a, int D, hipStream_t st);
 
 struct EvictArgs {
     PagedView view; // of layer 0

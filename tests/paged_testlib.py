@@ -118,10 +118,11 @@ def attention(q, rows_of, lengths, offsets, hkv, causal, room):
 def attention_error(amean, reach, n, D, dtype, single_weights=False):
     """What an output may be off before its last rounding.  A score: its products add up in fp32 (bf16 payloads: D terms in an order of
     the matrix core's; fp32: sums of four joined pair by pair), a weight is off by that and the exponential's own two steps, in numerator and
-    denominator; sums over n rows, 16 at a time and more; bf16 payloads: the weight as a pair of bf16 (2^-16), or as one (2^-8)."""
+    denominator; sums over n rows, 16 at a time and more; bf16 payloads: the weight as a pair of bf16 (2^-16), or as one (2^-8), in numerator
+    and denominator."""
     terms = D if dtype == torch.bfloat16 else 12
     score = (terms + 4) * 2.0**-24 * reach / np.sqrt(D)
     rel = 2 * score + (n / 16 + 20) * 2.0**-24
     if dtype == torch.bfloat16:
-        rel = rel + (2.0**-8 if single_weights else 2.0**-16)
+        rel = rel + (2.0**-7 if single_weights else 2.0**-16)
     return amean * rel

@@ -37,7 +37,9 @@ class Case:
 
         return attention(f64(self.q), rows, self.lengths, self.off, self.hkv, causal, self.table.shape[1] * self.R)
 
-    def check(self, got, causal=True, single_weights=False):
+    def check(self, got, causal=True):
+        # more than a token or two a sequence: rows of 64 and 128 bf16 features are multiplied by weights of 8 bits
+        single_weights = self.dtype == BF16 and self.D >= 64 and -(-int(self.off[-1]) // len(self.news)) * (self.hq // self.hkv) > 64
         want, received, amean, reach = self.wanted(causal)
         near(f64(got), want, attention_error(amean, reach, max(self.lengths.max(), 1), self.D, self.dtype, single_weights), self.dtype)
         return received
@@ -64,6 +66,37 @@ def test_attention_over_pages(D, hq, hkv, R, dtype, seqs):
     c = Case(seqs, D, hq, hkv, R, dtype, seed=D + R + len(seqs))
     c.check(c.attend())
     c.check(c.attend(causal=False), causal=False)
+
+
+@pytest.mark.parametrize("D,hq,hkv,R", [(128, 28, 4, 16), (64, 14, 2, 7), (128, 4, 4, 64), (64, 8, 1, 1), (128, 12, 1, 24)])
+@pytest.mark.parametrize("seqs", [[(300, 300)], [(37, 1000), (256, 257), (0, 10), (60, 31), (129, 129)], [(100, 6001)], [(70, 64), (64, 2000), (500, 500)]],
+                         ids=["whole", "mixed", "past", "edges"])
+def test_prompts(D, hq, hkv, R, seqs):
+    c = Case(seqs, D, hq, hkv, R, BF16, seed=D + R + len(seqs))
+    first = c.attend()
+    c.check(first)
+    assert torch.equal(c.attend(), first)
+    c.check(c.attend(causal=False), causal=False)
+
+
+def test_prompts_over_pages_that_are_none():
+    c = Case([(200, 300), (90, 90), (150, 64)], 128, 8, 2, 16, BF16, seed=14)
+    c.table[0, 3], c.table[0, 17] = -1, 2**31 - 1
+    c.table[2, :] = -5
+    c.check(c.attend())
+    c.check(c.attend(causal=False), causal=False)
+
+
+def test_prompts_with_scores_of_any_size():
+    c = Case([(100, 100), (70, 900)], 64, 4, 2, 16, BF16, seed=16, q_scale=1e17)
+    got, want = f64(c.attend()), c.wanted()[0]
+    # (one row each, but for scores nearer than 64 terms' rounding of themselves)
+    assert (np.abs(got - want).max(-1) <= 2.0**-6 * np.abs(want).max()).mean() > 0.999
+    c = Case([(100, 100)], 64, 4, 2, 16, BF16, seed=17)
+    c.q[3, 1, 7], c.q[50, 2] = float("nan"), -float("inf")
+    got = f64(c.attend())
+    bad = ~np.isfinite(got).all(-1)
+    assert np.isnan(got[3, 1]).all() and np.isnan(got[50, 2]).all() and bad.sum() == 2
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -134,7 +167,7 @@ def test_lengths_that_make_no_sense_are_brought_in_range(dtype):
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("D,news,rows", [(64, 6, 50), (128, 16, 40), (16, 3, 3), (64, 200, 230)])
+@pytest.mark.parametrize("D,news,rows", [(64, 6, 50), (128, 16, 40), (16, 3, 3), (64, 200, 230), (128, 130, 140), (128, 33, 33)])
 def test_hidden_rows_never_reach_a_token(D, news, rows, dtype, bad):
     """The last row's key and value are no numbers: only the last token sees it.  So is what lies past the last row, and on the first
     page of the layer, where rows that live nowhere are read."""
