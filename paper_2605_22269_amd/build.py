@@ -11,9 +11,6 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmukv.so")
 SOURCES = ["api.hip", "compress.hip", "att_mfma.hip", "retrieve.hip", "attend.hip", "paged_api.hip", "rope.hip", "paged_attend.hip",
            "paged_flash.hip", "paged_evict.hip"]
-# paged_flash.hip: a wave has 512 registers, of which vector instructions reach 256.  Matrix results are in those unless they do not fit;
-# the compiler's default puts all of them in the others, and moves every score over (its kernel 6000 such moves and spills, this way 1000).
-EXTRA = {"paged_flash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 OBJ = os.path.join(PKG, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -31,7 +28,7 @@ def build_lib(verbose: bool = False) -> str:
 
     def compile_one(src):
         obj = os.path.join(OBJ, src + ".o")
-        cmd = [HIPCC, *FLAGS, *EXTRA.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.check_call(cmd)

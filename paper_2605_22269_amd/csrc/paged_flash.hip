@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kFQ = 256, kFRows = 64, kQB = 2; // queries of a workgroup, rows of a step, blocks of 32 queries of a wave
 constexpr int kRing = 8;                       // steps whose rows' places are held
-constexpr float kLag = 8.f;                    // how far (in log2 units) the running maximum may be ahead of what exponents subtract
+constexpr float kMostSum = 18446744073709551616.f; // 2^64: sums of weights past this are worked out again (see below)
 
 // sum of two bf16 and x, in fp32
 __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
@@ -30,12 +30,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     __shared__ int64_t s_off[kRing][kFRows];                 // byte offset of a row
     __shared__ __align__(16) int s_ft[kRing][kFRows];        // first token that sees it
     __shared__ int s_masked[kRing][2];                       // some query of the tile may not see some row of that half of the step
-    __shared__ int s_bad[2], s_any;
+    __shared__ int s_bad[2], s_any, s_again;
     __shared__ unsigned s_inf[2][kFQ][D / 32]; // outputs that a value of +inf, of -inf reaches (both: NaN), where s_any says so
     __shared__ int s_last;
     const PagedView &v = a.view;
     Unit u;
     if (!find_unit(v, a.plan, blockIdx.x, &u)) return;
+    if (threadIdx.x == 0) s_again = 0;
     const int g = u.g, b = u.b, G = v.G, n_new = u.s.n_new;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lq = lane & 31, half = lane >> 5;
     const int n_queries = n_new * G;
@@ -64,11 +65,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     int n_rows = u.s.rows;
     if (a.causal && past + last_tok + 1 < n_rows) n_rows = past + last_tok + 1 > 0 ? past + last_tok + 1 : 0;
     // the unit's steps (a step is one of the plan's blocks)
+    n_rows = __builtin_amdgcn_readfirstlane(n_rows); // (the same in all lanes: scalar registers, and branches that are)
     const int all_steps = (n_rows + kFRows - 1) / kFRows;
     const int64_t lo = (int64_t)u.chunk * u.per, hi = lo + u.per;
-    const int t_lo = lo < all_steps ? (int)lo : all_steps, n_steps = (hi < all_steps ? (int)hi : all_steps) - t_lo;
+    const int t_lo = __builtin_amdgcn_readfirstlane(lo < all_steps ? (int)lo : all_steps);
+    const int n_steps = __builtin_amdgcn_readfirstlane((hi < all_steps ? (int)hi : all_steps) - t_lo);
     const int row0 = t_lo * kFRows;                                                     // the unit's first row
     const int n_halves = n_steps == 0 ? 0 : ((row0 + n_steps * kFRows < n_rows ? row0 + n_steps * kFRows : n_rows) - row0 + 31) / 32;
+    const int all_halves = (n_halves + 1) & ~1;
     const unsigned char *const kb = v.k + g * v.stride_head, *const vb = v.v + g * v.stride_head;
 
     // ---- where rows live ----
@@ -90,11 +94,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     // A wave brings rows 16 wave .. 16 wave + 15 of a step, kRowsPerLoad at a time.  A row's 16-byte pieces are stored permuted, so
     // that neither the reads of key operands nor the transpose reads of values meet in a bank.
     const int ld_row = 16 * wave + lane / kPieces, ld_piece = lane % kPieces;
-    const unsigned char *k_from[kLoads], *v_from[kLoads];
+    unsigned k_piece = 0, v_piece = 0; // where in its row the lane's piece of load i comes from, a byte each
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        k_from[i] = kb + 16 * key_slot<D>(ld_piece, ld_row + i * kRowsPerLoad);
-        v_from[i] = vb + 16 * val_slot<D>(ld_piece, ld_row + i * kRowsPerLoad);
+        k_piece |= 16u * key_slot<D>(ld_piece, ld_row + i * kRowsPerLoad) << (8 * i);
+        v_piece |= 16u * val_slot<D>(ld_piece, ld_row + i * kRowsPerLoad) << (8 * i);
     }
     auto request = [&](int t) __attribute__((always_inline)) { // the rows of step t
         if (t >= n_steps) return;
@@ -103,8 +107,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         for (int i = 0; i < kLoads; ++i) {
             const int64_t off = s_off[t & (kRing - 1)][ld_row + i * kRowsPerLoad];
             const int lds = (16 * wave + i * kRowsPerLoad) * kRowB; // the wave's 1024 bytes, lane order
-            load_to_lds(k_from[i] + off, dk + lds);
-            load_to_lds(v_from[i] + off, dv + lds);
+            load_to_lds(kb + (off + (k_piece >> (8 * i) & 255u)), dk + lds);
+            load_to_lds(vb + (off + (v_piece >> (8 * i) & 255u)), dv + lds);
         }
     };
 
@@ -112,101 +116,113 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     float ref[kQB], l_run[kQB]; // what exponents subtract; sum of the weights over the rows this lane holds
     f32x16 o[kQB][NF];          // features 32 f + 8 (j / 4) + 4 half + j % 4 of query lq
     f32x16 sc[2][kQB];          // scores of two halves of a step: rows 8 (j / 4) + 4 half + j % 4
-    float s_scale[kQB], s_ref[kQB]; // a weight is 2^(score * s_scale - s_ref)
+    float s_scale = scale, s_ref[kQB]; // a weight is 2^(score * s_scale - s_ref)
+    bool large = false;             // some ref is so large that the product's rounding shows
+    bf16x8 ak[KK], av[2][NF];       // operands on their way: keys of a half, values of its two 16 rows
+    // Where this lane reads its operands of a step's first half: keys of 16-feature step kk, values of feature block f (rows 4 half +
+    // (lane % 16) / 4 and 8 later of every 16, 4 features).  The walkers go from step to step with the buffers.
+    unsigned k_at[KK], v_at[NF][2];
+    auto first_operands = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kQB; ++i) {
-        ref[i] = -INFINITY;
-        l_run[i] = 0.f;
+        for (int kk = 0; kk < KK; ++kk) k_at[kk] = lq * kRowB + 16 * key_slot<D>(2 * kk + half, lq);
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
-    }
-    int koff[KK]; // this lane's key operand of 16-feature step kk in a half of a staged step
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) koff[kk] = lq * kRowB + 16 * key_slot<D>(2 * kk + half, lq);
-    // its value operand of feature block f: rows 4 half + (lane % 16) / 4 and 8 later of every 16, 4 features
-    int voff[NF][2];
-#pragma unroll
-    for (int f = 0; f < NF; ++f) {
-        const int row = 4 * half + ((lane & 15) >> 2), piece = 4 * f + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), sub = 8 * (lane & 1);
-        voff[f][0] = row * kRowB + 16 * val_slot<D>(piece, row) + sub;
-        voff[f][1] = (row + 8) * kRowB + 16 * val_slot<D>(piece, row + 8) + sub;
-    }
-    auto keys_of = [&](int h) { return s_kv + (h >> 1 & 1) * kBuf + (h & 1) * 32 * kRowB; };
-    auto values_of = [&](int h) { return s_kv + (2 + (h >> 1) % 3) * kBuf + (h & 1) * 32 * kRowB; };
-    auto load_k = [&](const unsigned char *ks, int kk) { return *reinterpret_cast<const bf16x8 *>(ks + koff[kk]); };
-    auto load_v = [&](const unsigned char *vs, int grp, int f) { // of 16 rows
-        const i16x4 x = lds_read_tr16(vs + grp * 16 * kRowB + voff[f][0]), y = lds_read_tr16(vs + grp * 16 * kRowB + voff[f][1]);
-        return i16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        for (int f = 0; f < NF; ++f) {
+            const int row = 4 * half + ((lane & 15) >> 2), piece = 4 * f + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), sub = 8 * (lane & 1);
+            v_at[f][0] = 2 * kBuf + row * kRowB + 16 * val_slot<D>(piece, row) + sub;
+            v_at[f][1] = 2 * kBuf + (row + 8) * kRowB + 16 * val_slot<D>(piece, row + 8) + sub;
+        }
     };
+    auto next_keys = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) k_at[kk] ^= kBuf;
+    };
+    auto next_values = [&](int t) __attribute__((always_inline)) { // from those of step t
+        const unsigned by = t % 3 == 2 ? 0u - 2u * kBuf : (unsigned)kBuf;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            v_at[f][0] += by;
+            v_at[f][1] += by;
+        }
+    };
+    auto load_k = [&](auto second, int kk) { return *reinterpret_cast<const bf16x8 *>(s_kv + k_at[kk] + second.value * 32 * kRowB); };
+    auto load_v = [&](auto second, int grp, int f) { // of 16 rows
+        const int at = (second.value * 32 + grp * 16) * kRowB;
+        const i16x4 x = lds_read_tr16(s_kv + v_at[f][0] + at), y = lds_read_tr16(s_kv + v_at[f][1] + at);
+        return __builtin_bit_cast(bf16x8, i16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+    };
+    auto values_of = [&](int h) { return s_kv + (2 + (h >> 1) % 3) * kBuf + (h & 1) * 32 * kRowB; };
     // weights of query block i and 16 rows as a matrix operand
     auto weights_of = [&](const f32x16 &s, int i, int grp, float *sum) __attribute__((always_inline)) {
         raw16 w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e], s_scale[i], -s_ref[i]));
-            const float y = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e + 1], s_scale[i], -s_ref[i]));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e], s_scale, -s_ref[i]));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e + 1], s_scale, -s_ref[i]));
             w[e] = bf16_pair(x, y);
             *sum = add_pair(w[e], *sum); // (the weights as they enter the product: a row that has nearly all of it keeps its value)
         }
         return __builtin_bit_cast(bf16x8, w);
     };
 
-    // ---- the scores of half h are there: mask, maximum, what the exponents subtract ----
-    auto look = [&](auto par, int h) __attribute__((always_inline)) {
+    auto scores_of = [&](auto second, f32x16 *s) __attribute__((always_inline)) { // of a half of the step that k_at is at
+#pragma unroll
+        for (int i = 0; i < kQB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[i][j] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            const bf16x8 x = load_k(second, kk);
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qb[i][kk], s[i], 0, 0, 0);
+        }
+    };
+    auto is_masked = [&](int h) { return __builtin_amdgcn_readfirstlane(s_masked[(h >> 1) & (kRing - 1)][h & 1]) != 0; };
+    auto hide = [&](int h, f32x16 *s) __attribute__((always_inline)) { // scores of rows that the query does not see: -inf
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+            const i32x4 ft = *reinterpret_cast<const i32x4 *>(&s_ft[(h >> 1) & (kRing - 1)][32 * (h & 1) + 8 * jj + 4 * half]);
+#pragma unroll
+            for (int i = 0; i < kQB; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[i][4 * jj + r] = my_tok[i] >= ft[r] ? s[i][4 * jj + r] : -INFINITY;
+        }
+    };
+    auto largest = [&](const f32x16 &s) __attribute__((always_inline)) { // over both halves of the lanes, scaled
+        float m4[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) m4[c] = fmaxf(fmaxf(s[c], s[4 + c]), fmaxf(s[8 + c], s[12 + c]));
+        return half_max(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]))) * scale;
+    };
+    auto base_of = [&](int i) { return ref[i] == -INFINITY ? 0.f : ref[i]; };
+    auto set_ref = [&]() __attribute__((always_inline)) {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) any |= fabsf(base_of(i)) > kLargeRef;
+        large = __builtin_amdgcn_ballot_w64(any) != 0;
+        s_scale = large ? 1.f : scale;
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) s_ref[i] = large ? 0.f : base_of(i);
+    };
+    // For step(h), with v_at at h's step and k_at at that of half h + 1.
+    auto load_ahead = [&](auto par) __attribute__((always_inline)) {
+        using Here = std::integral_constant<int, par.value>;
+        using There = std::integral_constant<int, 1 - par.value>;
+#pragma unroll
+        for (int kk = 0; kk < KK / 2; ++kk) ak[kk] = load_k(There{}, kk);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) av[0][f] = load_v(Here{}, 0, f);
+    };
+    // The scores of half h, before their weights are taken.
+    auto look = [&](auto par, int h, int flag) __attribute__((always_inline)) { // flag: s_masked of the half
         constexpr int P = par.value;
         const int slot = (h >> 1) & (kRing - 1);
-        const bool masked = __builtin_amdgcn_readfirstlane(s_masked[slot][h & 1]) != 0;
-        if (masked) {
+        const bool masked = h < all_halves && __builtin_amdgcn_readfirstlane(flag) != 0;
+        if (masked) hide(h, sc[P]);
+        if (__builtin_expect(large, 0)) {
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) {
-                const i32x4 ft = *reinterpret_cast<const i32x4 *>(&s_ft[slot][32 * (h & 1) + 8 * jj + 4 * half]);
+            for (int i = 0; i < kQB; ++i)
 #pragma unroll
-                for (int i = 0; i < kQB; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[P][i][4 * jj + r] = my_tok[i] >= ft[r] ? sc[P][i][4 * jj + r] : -INFINITY;
-            }
-        }
-        float mx[kQB];
-        bool ahead = false, large = false;
-#pragma unroll
-        for (int i = 0; i < kQB; ++i) {
-            float m4[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) m4[c] = fmaxf(fmaxf(sc[P][i][c], sc[P][i][4 + c]), sc[P][i][8 + c]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) m4[c] = fmaxf(m4[c], sc[P][i][12 + c]);
-            mx[i] = half_max(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]))) * scale;
-            ahead |= mx[i] > ref[i] + kLag;
-        }
-        if (__builtin_amdgcn_ballot_w64(ahead) != 0) { // bring what was summed to the new maximum
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) {
-                const float to = mx[i] > ref[i] + kLag ? mx[i] : ref[i];
-                const float corr = __builtin_amdgcn_exp2f(ref[i] - (to == -INFINITY ? 0.f : to));
-                ref[i] = to;
-                l_run[i] *= corr;
-#pragma unroll
-                for (int f = 0; f < NF; ++f)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[i][f][j] *= corr;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kQB; ++i) {
-            s_scale[i] = scale;
-            s_ref[i] = ref[i] == -INFINITY ? 0.f : ref[i];
-            large |= fabsf(s_ref[i]) > kLargeRef;
-        }
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(large) != 0, 0)) { // so large that the product's rounding shows
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) sc[P][i][j] = scaled_apart(sc[P][i][j], s_scale[i], s_ref[i]);
-                s_scale[i] = 1.f;
-                s_ref[i] = 0.f;
-            }
+                for (int j = 0; j < 16; ++j) sc[P][i][j] = scaled_apart(sc[P][i][j], scale, base_of(i));
         }
         // A value that is no number must not reach a token that does not see its row: the weight is zero, the product is not.
         if (masked) {
@@ -235,7 +251,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                     sees[i] = weighs[i] = 0;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const float w = __builtin_amdgcn_exp2f(fmaf(sc[P][i][j], s_scale[i], -s_ref[i]));
+                        const float w = __builtin_amdgcn_exp2f(fmaf(sc[P][i][j], s_scale, -s_ref[i]));
                         sees[i] |= (unsigned)(my_tok[i] >= s_ft[slot][32 * (h & 1) + 8 * (j / 4) + 4 * half + j % 4]) << j;
                         weighs[i] |= (unsigned)(w != 0.f) << j;
                     }
@@ -267,105 +283,178 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                     s_any = 1;
                 }
                 __syncthreads();
+                load_ahead(par); // (they were there already)
             }
         }
     };
 
-    // Half h: its weights and values, and the scores of half h + 1 between them.
+    // Half h: its weights and values, and the scores of half h + 1 between them.  Operands are in registers a section before their products.
+    constexpr int K1 = KK * 3 / 4; // products of the scores in the first section
     auto step = [&](auto par, int h) __attribute__((always_inline)) {
         constexpr int P = par.value;
-        if constexpr (P == 1) { // the rows of the next step are there; the next but one's take the place of this one's keys
-            rows_landed();
-            __syncthreads();
-            const int t = h >> 1;
-            request(t + 2);
-        }
-        const unsigned char *const ks = keys_of(h + 1), *const vs = values_of(h); // (past the last half: whatever is there)
-        f32x16 *const cur = sc[P], *const nxt = sc[1 - P];
+        using Here = std::integral_constant<int, P>;
+        using There = std::integral_constant<int, 1 - P>;
+        f32x16 *const nxt = sc[1 - P];
+        bf16x8 pw[2][kQB];
+        const int flag = s_masked[((h + 1) >> 1) & (kRing - 1)][1 - P];
+        // ---- most of the scores; weights of the first 16 rows ----
 #pragma unroll
         for (int i = 0; i < kQB; ++i)
 #pragma unroll
             for (int j = 0; j < 16; ++j) nxt[i][j] = 0.f;
-        bf16x8 pw[2][kQB], ak[2], av[2][NF];
-        ak[0] = load_k(ks, 0);
 #pragma unroll
-        for (int kk = 0; kk < KK / 2; ++kk) { // weights of the first 16 rows beside the first features of the scores
-            ak[(kk + 1) & 1] = load_k(ks, kk + 1);
-            if (kk >= KK / 2 - 2) {
+        for (int kk = KK / 2; kk < KK; ++kk) ak[kk] = load_k(There{}, kk);
 #pragma unroll
-                for (int f = 0; f < NF / 2; ++f) av[0][NF / 2 * (kk - KK / 2 + 2) + f] = __builtin_bit_cast(bf16x8, load_v(vs, 0, NF / 2 * (kk - KK / 2 + 2) + f));
-            }
-            __builtin_amdgcn_sched_barrier(0);
+        for (int f = 0; f < NF; ++f) av[1][f] = load_v(Here{}, 1, f);
 #pragma unroll
-            for (int i = 0; i < kQB; ++i) nxt[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[kk & 1], qb[i][kk], nxt[i], 0, 0, 0);
-            if (kk % (KK / 4) == 0) pw[0][kk / (KK / 4)] = weights_of(cur[kk / (KK / 4)], kk / (KK / 4), 0, &l_run[kk / (KK / 4)]);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int kk = 0; kk < K1; ++kk)
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) nxt[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[kk], qb[i][kk], nxt[i], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) pw[0][i] = weights_of(sc[P][i], i, 0, &l_run[i]);
+#pragma unroll
+        for (int n = 0; n < K1 * kQB; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0); // reads of LDS
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);   // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x402, D == 128 ? 5 : 10, 0); // vector instructions beside it
         }
+        __builtin_amdgcn_sched_barrier(0);
+        // ---- the rest of the scores; values of the first 16 rows, weights of the others ----
 #pragma unroll
-        for (int kk = KK / 2; kk < KK; ++kk) { // weights of the other 16 beside the other features and the first rows' values
-            if (kk + 1 < KK) ak[(kk + 1) & 1] = load_k(ks, kk + 1);
-            const int s = kk - KK / 2;
-            if (s >= KK / 2 - 2) {
+        for (int kk = K1; kk < KK; ++kk)
 #pragma unroll
-                for (int f = 0; f < NF / 2; ++f) av[1][NF / 2 * (s - KK / 2 + 2) + f] = __builtin_bit_cast(bf16x8, load_v(vs, 1, NF / 2 * (s - KK / 2 + 2) + f));
-            }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) nxt[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[kk & 1], qb[i][kk], nxt[i], 0, 0, 0);
-            {
-                const int f = s; // KK / 2 == NF
-#pragma unroll
-                for (int i = 0; i < kQB; ++i) o[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[0][f], pw[0][i], o[i][f], 0, 0, 0);
-            }
-            if (s % (KK / 4) == 0) pw[1][s / (KK / 4)] = weights_of(cur[s / (KK / 4)], s / (KK / 4), 1, &l_run[s / (KK / 4)]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+            for (int i = 0; i < kQB; ++i) nxt[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[kk], qb[i][kk], nxt[i], 0, 0, 0);
 #pragma unroll
         for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int i = 0; i < kQB; ++i) o[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[1][f], pw[1][i], o[i][f], 0, 0, 0);
+            for (int i = 0; i < kQB; ++i) o[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[0][f], pw[0][i], o[i][f], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) pw[1][i] = weights_of(sc[P][i], i, 1, &l_run[i]);
+#pragma unroll
+        for (int n = 0; n < (KK - K1 + NF) * kQB; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, D == 128 ? 5 : 10, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (P == 0) { // the rows of the next step are there; the next but one's take the place of this one's keys
+            rows_landed();
+            __syncthreads();
+            request((h >> 1) + 2);
+            next_keys();
+        } else {
+            next_values(h >> 1);
+        }
+        // ---- values of the other 16 rows; the scores go to where vector instructions reach them ----
+        load_ahead(There{});
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) {
+                o[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[1][f], pw[1][i], o[i][f], 0, 0, 0);
+                if (f == NF / 2) asm volatile("" : "+v"(nxt[i]));
+            }
+        return flag;
     };
 
-    if (n_halves > 0) {
-        if (tid < 2) s_bad[tid] = 0;
-        if (tid == 0) s_any = 0;
-        for (int i = tid; i < 2 * kFQ * (D / 32); i += 256) (&s_inf[0][0][0])[i] = 0u;
-        {
-            const int p0 = page_at(wave), p1 = page_at(wave + 4);
-            tabulate(wave, p0);
-            tabulate(wave + 4, p1);
-        }
-        int page = page_at(wave + 8);
+    int page;
+    auto stage = [&]() __attribute__((always_inline)) { // the first two steps' rows
+        const int p0 = page_at(wave), p1 = page_at(wave + 4);
+        page = page_at(wave + 8);
+        __syncthreads(); // everybody is done with what was there
+        tabulate(wave, p0);
+        tabulate(wave + 4, p1);
         __syncthreads();
         request(0);
         request(1);
+        first_operands();
         rows_landed();
         __syncthreads();
-        {
-            const unsigned char *const ks = keys_of(0);
-#pragma unroll
-            for (int i = 0; i < kQB; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) sc[0][i][j] = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-                for (int i = 0; i < kQB; ++i) sc[0][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load_k(ks, kk), qb[i][kk], sc[0][i], 0, 0, 0);
+    };
+    auto next_places = [&](int h) __attribute__((always_inline)) {
+        // places of the steps up to this one are free: four new ones every four steps (which are read from two steps on)
+        if ((h & 7) == 7) {
+            tabulate((h >> 1) + 5 + wave, page);
+            page = page_at((h >> 1) + 9 + wave);
         }
-        look(std::integral_constant<int, 0>{}, 0);
-        for (int h = 0; h < n_halves; h += 2) {
-            step(std::integral_constant<int, 0>{}, h);
-            if (h + 1 >= n_halves) break;
-            look(std::integral_constant<int, 1>{}, h + 1);
-            step(std::integral_constant<int, 1>{}, h + 1);
-            if (h + 2 >= n_halves) break;
-            look(std::integral_constant<int, 0>{}, h + 2);
-            // places of the steps up to this one are free: four new ones every four steps (which are read from two steps on)
-            const int t = h >> 1;
-            if ((t & 3) == 3) {
-                tabulate(t + 5 + wave, page);
-                page = page_at(t + 9 + wave);
+    };
+    // What exponents subtract is the largest score of the unit's first half, and stays: weights then are what they are, not at most
+    // 1, and floating point holds them as well, so nothing in the loop waits for a maximum or brings sums to another one.  Sums that
+    // leave the range (a later score larger by 64 log2 units or so) are worked out again with the largest score of all rows.
+    if (n_halves > 0)
+    for (bool again = false;; again = true) {
+        if (__builtin_expect(again, 0)) {
+            stage();
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) ref[i] = -INFINITY;
+            auto max_of = [&](auto par, int h) __attribute__((always_inline)) {
+                scores_of(par, sc[0]);
+                if (is_masked(h)) hide(h, sc[0]);
+#pragma unroll
+                for (int i = 0; i < kQB; ++i) ref[i] = fmaxf(ref[i], largest(sc[0][i]));
+            };
+#pragma unroll 1
+            for (int h = 0; h < n_halves; h += 2) {
+                max_of(std::integral_constant<int, 0>{}, h);
+                max_of(std::integral_constant<int, 1>{}, h + 1);
+                rows_landed(); // of the next step; this one's keys are done with
+                __syncthreads();
+                request((h >> 1) + 2);
+                next_keys();
+                next_places(h + 1);
             }
+        }
+        stage();
+        if (tid < 2) s_bad[tid] = 0;
+        if (tid == 0) s_any = 0;
+        for (int i = tid; i < 2 * kFQ * (D / 32); i += 256) (&s_inf[0][0][0])[i] = 0u;
+        scores_of(std::integral_constant<int, 0>{}, sc[0]);
+        if (!again) {
+            f32x16 s[kQB];
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) s[i] = sc[0][i];
+            if (is_masked(0)) hide(0, s);
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) ref[i] = largest(s[i]);
+        }
+        set_ref();
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            l_run[i] = 0.f;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
+        }
+        __syncthreads(); // the flags are cleared
+        load_ahead(std::integral_constant<int, 0>{});
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) asm volatile("" : "+v"(sc[0][i]));
+        look(std::integral_constant<int, 0>{}, 0, s_masked[0][0]);
+#pragma unroll 1
+        for (int h = 0; h < n_halves; h += 2) { // (an odd half out is joined by one whose rows nobody sees)
+            const int odd = step(std::integral_constant<int, 0>{}, h);
+            look(std::integral_constant<int, 1>{}, h + 1, odd);
+            const int even = step(std::integral_constant<int, 1>{}, h + 1);
+            next_places(h + 1);
+            look(std::integral_constant<int, 0>{}, h + 2, even);
+        }
+        if (again) break;
+        bool out_of_range = false;
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) // (no row of the first half seen, but perhaps others: not with all pages there)
+            out_of_range |= l_run[i] > kMostSum || (ref[i] == -INFINITY && n_halves > 1 && my_tok[i] >= (a.causal ? row0 + 32 - past : 0));
+        if (__builtin_amdgcn_ballot_w64(out_of_range) != 0 && lane == 0) s_again = 1;
+        __syncthreads();
+        if (__builtin_expect(s_again == 0, 1)) break;
+    }
+    if (n_halves == 0) {
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            ref[i] = l_run[i] = 0.f;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
         }
     }
     // ---- results ----

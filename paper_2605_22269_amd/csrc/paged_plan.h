@@ -87,9 +87,9 @@ MUKV_HD int chunk_of(const PlanShape &p, double all_blocks) {
     const int64_t per = div_up((int64_t)all_blocks, p.target);
     return per < 1 ? 1 : per > 0x40000000 ? 0x40000000 : (int)per;
 }
-MUKV_HD int chunk_of(const PlanShape &p, const SeqShape &s, int per) {
+MUKV_HD int chunk_of(const PlanShape &p, const SeqShape &s, int per) { // of one sequence: as many chunks, all about the same
     const int least = (int)div_up(s.blocks, p.most);
-    return per > least ? per : least;
+    return (int)div_up(s.blocks, div_up(s.blocks, per > least ? per : least));
 }
 MUKV_HD int chunks_of(const PlanShape &p, const SeqShape &s, int per) { return (int)div_up(s.blocks, chunk_of(p, s, per)); }
 // Workgroups that cover every unit, and records: sum over sequences of tiles * ceil(blocks / per) is at most target + tiles, and where

@@ -100,6 +100,35 @@ def test_prompts_with_scores_of_any_size():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("low,high,at", [(0.02, 60.0, 150), (60.0, 0.02, 150), (1.0, 400.0, 299), (1e-3, 1e4, 40)])
+def test_scores_that_grow_or_fall_by_much_along_the_rows(low, high, at, D, dtype):
+    """Rows from `at` on have keys of another size: what exponents subtract at first is far from the largest score of all."""
+    c = Case([(200, 300), (40, 200)], D, 8, 2, 16, dtype, seed=D + at)
+    for b in range(2):
+        for j in range(int(c.lengths[b])):
+            c.kp[:, c.table[b][j // 16], :, j % 16] *= low if j < at else high
+    want, _, amean, reach = c.wanted()
+    got = c.attend()
+    # a score this large is known to its own rounding only: where that is less than a sixteenth
+    err = attention_error(amean, reach, 300, D, dtype, dtype == BF16)
+    sure = (D + 4) * 2.0**-24 * reach[..., 0] / np.sqrt(D) < 2.0**-4
+    assert sure.any() or high > 1e3   # (there only that the outputs are numbers)
+    near(f64(got)[sure], want[sure], err[sure], dtype)
+    assert np.isfinite(f64(got)).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompts_whose_first_page_is_none(causal):
+    c = Case([(150, 400), (150, 150)], 128, 8, 2, 64, BF16, seed=18)
+    c.table[:, 0] = -1
+    c.kp[:] *= 40.0     # scores of a few hundred, either sign: the rows that are there decide what exponents subtract
+    want, _, amean, reach = c.wanted(causal)
+    err = attention_error(amean, reach, 400, 128, BF16, True)
+    near(f64(c.attend(causal=causal)), want, err, BF16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_long_rows_are_shared_out_and_joined(dtype):
     c = Case([(1, 20011)], 128, 8, 1, 16, dtype, seed=1)
     first = c.attend()
