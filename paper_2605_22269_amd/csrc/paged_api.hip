@@ -131,15 +131,17 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
 struct Space {
     bool flash;
     mukv::PlanShape plan;
-    int64_t records, pairs, bytes; // offsets; the counts are at 0
+    int64_t stats, values, pairs, bytes; // offsets; the counts are at 0
 };
-Space space_of(const mukv_paged &p, const mukv_seqs &s, bool with_weights) {
+Space space_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool with_weights) {
     const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
     Space x;
     x.flash = mukv::paged_takes_flash(p.dtype, p.head_dim, p.n_q_heads / p.n_kv_heads, hint, with_weights);
-    x.plan = mukv::paged_plan(p.dtype, x.flash);
-    x.records = 4 * mukv::kPlanRecords;
-    x.pairs = x.records + 4 * (int64_t)mukv::records_bound(x.plan) * x.plan.queries * (p.head_dim + 2);
+    x.plan = mukv::paged_plan(p.dtype, x.flash, causal);
+    const int64_t rows = (int64_t)x.plan.records * x.plan.queries;
+    x.stats = 4 * mukv::kPlanRecords;
+    x.values = x.stats + 8 * rows;
+    x.pairs = x.values + 4 * rows * p.head_dim;
     x.bytes = x.pairs + (with_weights ? 8 * (int64_t)s.n_tokens * p.n_q_heads : 0);
     return x;
 }
@@ -211,7 +213,7 @@ int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, in
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_pages(pages)) return rc;
     if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
-    *bytes_out = space_of(*pages, *seqs, with_weights != 0).bytes;
+    *bytes_out = space_of(*pages, *seqs, true, with_weights != 0).bytes;
     return MUKV_OK;
 }
 
@@ -233,7 +235,7 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
         if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
     }
     if (!workspace) return MUKV_ERR_INVALID_ARG;
-    const Space x = space_of(*pages, *seqs, weights != nullptr);
+    const Space x = space_of(*pages, *seqs, causal != 0, weights != nullptr);
     if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
     if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
     mukv::PagedAttendArgs a = {};
@@ -245,7 +247,8 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     a.out = out;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.counts = reinterpret_cast<int *>(ws);
-    a.records = reinterpret_cast<float *>(ws + x.records);
+    a.records.stats = reinterpret_cast<float *>(ws + x.stats);
+    a.records.values = reinterpret_cast<float *>(ws + x.values);
     a.pairs = weights ? reinterpret_cast<float *>(ws + x.pairs) : nullptr;
     a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
     a.causal = causal;

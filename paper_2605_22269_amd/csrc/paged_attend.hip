@@ -379,55 +379,18 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(ow[e], x, o[e]);
             }
         }
-        if (u.chunks > 1) { // the chunk's record: [0] maximum, [1] normaliser, [2..] unnormalised output
-            float *rec = a.records + ((int64_t)(u.record + u.chunk) * kPQ + n) * (D + 2);
-            if (c == 0) store_far(rec, m, l);
-            store_far(rec + 2 + 4 * c, o[0], o[1]);
-            store_far(rec + 4 + 4 * c, o[2], o[3]);
+        if (u.chunks > 1) {
+            if (c == 0) store_far(a.records.stats + ((int64_t)(u.record + u.chunk) * kPQ + n) * 2, m, l);
+            store_far4(chunk_values<kPQ, D>(a.records, u.record + u.chunk), n * D + 4 * c, o);
         } else {
             finish(n, c, m, l, o);
         }
     }
     if (u.chunks == 1) return;
-    // ---- the chunks' records: the last workgroup of the tile to get here joins them, in their order ----
     __shared__ int s_last;
     if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
-    for (int i = tid; i < n_q_here * kQuads; i += 64 * W) {
-        const int n = i / kQuads, c = i - n * kQuads;
-        const float *rec = a.records + ((int64_t)u.record * kPQ + n) * (D + 2);
-        constexpr int64_t kNext = (int64_t)kPQ * (D + 2);
-        constexpr int kAhead = 8; // records requested together
-        float m = -INFINITY, l = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-        for (int s0 = 0; s0 < u.chunks; s0 += kAhead) {
-            f32x2 st[kAhead], x0[kAhead], x1[kAhead];
-#pragma unroll
-            for (int s = 0; s < kAhead; ++s) {
-                if (s0 + s >= u.chunks) break;
-                st[s] = load_far(rec + (s0 + s) * kNext);
-                x0[s] = load_far(rec + (s0 + s) * kNext + 2 + 4 * c);
-                x1[s] = load_far(rec + (s0 + s) * kNext + 4 + 4 * c);
-            }
-            float m_new = m;
-#pragma unroll
-            for (int s = 0; s < kAhead; ++s)
-                if (s0 + s < u.chunks) m_new = fmaxf(m_new, st[s][0]);
-            const float corr = l != 0.f ? __builtin_amdgcn_exp2f(m - m_new) : 0.f;
-            l *= corr;
-            o *= corr;
-            m = m_new;
-#pragma unroll
-            for (int s = 0; s < kAhead; ++s) {
-                if (s0 + s >= u.chunks) break;
-                if (st[s][1] == 0.f) continue; // none of its rows is seen
-                const float x = __builtin_amdgcn_exp2f(st[s][0] - m);
-                l = fmaf(st[s][1], x, l);
-                o = f32x4{fmaf(x0[s][0], x, o[0]), fmaf(x0[s][1], x, o[1]), fmaf(x1[s][0], x, o[2]), fmaf(x1[s][1], x, o[3])};
-            }
-        }
-        finish(n, c, m, l, o);
-    }
+    __shared__ float s_join[join_scratch(kPlanChunks, kPQ)];
+    join_chunks<kPQ, D, 64 * W, kPlanChunks, 1, 16>(a.records, u.record, u.chunks, n_q_here, s_join, finish);
 }
 
 // What each row receives: weights_out[b][g][j] = decay * weights_in[b][g][j] + sum over the tokens and the group's heads of p_j / sum p.
@@ -550,12 +513,26 @@ bool paged_takes_flash(int dtype, int D, int G, int64_t new_hint, bool with_weig
     return dtype == MUKV_BF16 && D >= 64 && !with_weights && new_hint * G > 64;
 }
 
-PlanShape paged_plan(int dtype, bool flash) {
+PlanShape paged_plan(int dtype, bool flash, bool causal) {
     PlanShape p;
-    p.queries = flash ? 256 : kPQ;
-    p.rows = flash ? 64 : dtype == MUKV_BF16 ? 128 : 64; // a step of the workgroup; a block of every wave
-    p.target = flash ? 256 : 512;                        // as many workgroups as are resident
-    p.most = 64;
+    p.causal = causal;
+    p.most = kPlanChunks;
+    if (flash) {
+        p.queries = 256;
+        p.rows = 64; // a step of the workgroup
+        p.records = 704;
+        p.places = 256;
+        p.start = 3;
+        p.join = 0.8f;
+        p.record = 0.06f;
+    } else {
+        p.queries = kPQ;
+        p.rows = dtype == MUKV_BF16 ? 128 : 64; // a block of every wave
+        p.records = 1024;                       // two workgroups per compute unit, as many as are resident, and the odd ones
+        p.places = 512;
+        p.start = 0;
+        p.join = p.record = 0.f;
+    }
     return p;
 }
 

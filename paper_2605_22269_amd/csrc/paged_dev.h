@@ -12,25 +12,48 @@ struct Unit {
     int record;                         // of the tile's first chunk
 };
 
+// Blocks of a chunk: the number of chunks that costs least, a lane a number.
+__device__ __forceinline__ int chunk_by_cost(const PlanShape &p, const PlanSums &x, bool one_sequence) {
+    const int chunks = (threadIdx.x & 63) + 1;
+    const float cost = chunks <= p.most ? cost_of(p, x, one_sequence, chunks) : 1e30f;
+    const int best = 1 + (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == -wave_max(-cost)));
+    return best == 1 ? kWhole : (int)((x.longest + best - 1) / best);
+}
+
 // The unit of this workgroup, the same in all lanes; false: there is none.
 __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p, int id, Unit *u) {
     const int lane = threadIdx.x & 63;
     if (v.n_seqs == 1) {
         u->s = shape_of(v, p, 0);
         u->b = 0;
-        u->per = chunk_of(p, u->s, chunk_of(p, blocks_of(v, u->s)));
-        u->chunks = (int)div_up(u->s.blocks, u->per);
+        const PlanSums x = sums_of(v, p, u->s);
+        const int per = p.start ? chunk_by_cost(p, x, true) : chunk_by_room(p, x.blocks);
+        u->chunks = chunks_of(p, u->s, per);
+        u->per = per >= kWhole ? u->s.blocks : chunk_of(p, u->s, per);
         u->record = 0;
         if (id >= u->s.tiles * v.Hkv * u->chunks) return false;
     } else {
         const SeqShape none = {0, 0, 0, 0, 0, 1};
         SeqShape s = none;
-        double all = 0.0;
+        PlanSums all = {0.0, 0.0, 0.0, 0.0};
         for (int b0 = 0; b0 < v.n_seqs; b0 += 64) {
             s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
-            all += blocks_of(v, s);
+            const PlanSums x = sums_of(v, p, s);
+            all.tiles += x.tiles;
+            all.blocks += x.blocks;
+            all.seen += x.seen;
+            all.longest = fmax(all.longest, x.longest);
         }
-        const int per = chunk_of(p, wave_sum(all));
+        all.blocks = wave_sum(all.blocks);
+        int per;
+        if (p.start) {
+            all.tiles = wave_sum(all.tiles);
+            all.seen = wave_sum(all.seen);
+            all.longest = wave_max(all.longest);
+            per = chunk_by_cost(p, all, false);
+        } else {
+            per = chunk_by_room(p, all.blocks);
+        }
         int units0 = 0, records0 = 0, b0 = 0;
         for (;; b0 += 64) {
             if (b0 >= v.n_seqs) return false;
@@ -43,7 +66,7 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
                 auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
                 u->s = SeqShape{of(s.first), of(s.n_new), of(s.length), of(s.rows), of(s.tiles), of(s.blocks)};
                 u->b = b0 + at;
-                u->per = chunk_of(p, u->s, per);
+                u->per = per >= kWhole ? u->s.blocks : chunk_of(p, u->s, per);
                 u->chunks = of(chunks);
                 u->record = of(records1 - records);
                 id -= of(units1 - units);
@@ -61,6 +84,101 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
     u->record += (rank * v.Hkv + u->g) * u->chunks;
     u->tile = u->s.tiles - 1 - rank; // under the mask the last ones have the most to do: they start first
     return true;
+}
+
+// ---- joining a tile's chunks ----
+// Records are written through to, and read from, the memory that all XCDs share.
+constexpr int kFar = 16; // cache policy of a buffer access: the scope of the whole GPU (sc1)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t far_buffer(float *p, int64_t floats) {
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, (int)(4 * floats), 0x00027000);
+}
+__device__ __forceinline__ f32x4 load_far4(__amdgpu_buffer_rsrc_t r, int floats) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, 4 * floats, 0, kFar));
+}
+__device__ __forceinline__ void store_far4(__amdgpu_buffer_rsrc_t r, int floats, f32x4 x) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw16, x), r, 4 * floats, 0, kFar);
+}
+// the values of one chunk of a tile
+template <int kQueries, int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_values(const ChunkRecords &r, int record) {
+    return far_buffer(r.values + (int64_t)record * kQueries * D, kQueries * D);
+}
+
+// LDS that join_chunks wants, in floats
+constexpr int join_scratch(int chunks, int queries) { return (chunks + 2) * queries; }
+
+// The last workgroup of a tile joins its chunks, in their order.  put(n, c, m, l, x): features 4 c .. 4 c + 3 of query n, x the sum of
+// the outputs that belongs to the reference m and the sum of weights l.  kAhead chunks of kItems pieces of 16 bytes are requested
+// together, the first of them before anything else is known; there are at most kChunks.
+template <int kQueries, int D, int kThreads, int kChunks, int kItems, int kAhead, typename Put>
+__device__ __forceinline__ void join_chunks(const ChunkRecords &r, int record, int chunks, int n_q, float *scratch, Put put) {
+    const int tid = threadIdx.x;
+    float(*const s_by)[kQueries] = reinterpret_cast<float(*)[kQueries]>(scratch); // what a chunk's output is multiplied by, -1: nothing seen
+    float *const s_m = s_by[chunks], *const s_l = s_by[chunks + 1];
+    constexpr int kQuads = D / 4;
+    const int n_items = n_q * kQuads;
+    const auto values = far_buffer(r.values + (int64_t)record * kQueries * D, (int64_t)chunks * kQueries * D);
+    f32x4 y[kItems][kAhead];
+    auto request = [&](int i0, int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kItems; ++u)
+#pragma unroll
+            for (int c = 0; c < kAhead; ++c)
+                if (c0 + c < chunks && i0 + u * kThreads < n_items) y[u][c] = load_far4(values, (c0 + c) * kQueries * D + 4 * (i0 + u * kThreads));
+    };
+    request(tid, 0);
+    const float *stats = r.stats + (int64_t)record * kQueries * 2;
+    constexpr int kLanes = kThreads / kQueries, kEach = (kChunks + kLanes - 1) / kLanes; // lanes of a query, chunks of a lane
+    static_assert(kLanes == 16 || kLanes == 1, "a row of lanes, or one");
+    const int n_here = tid / kLanes, first = tid % kLanes;
+    f32x2 st[kEach]; // the lane's chunks: reference, sum of weights
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int c = first + k * kLanes;
+        st[k] = f32x2{-INFINITY, 0.f};
+        if (c < chunks && n_here < n_q) st[k] = load_far(stats + 2 * (c * kQueries + n_here));
+    }
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+        if (st[k][1] != 0.f) m = fmaxf(m, st[k][0]); // (else none of the chunk's rows is seen; a NaN is)
+    if constexpr (kLanes == 16) m = row16_max(m);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int c = first + k * kLanes;
+        const float by = st[k][1] != 0.f ? __builtin_amdgcn_exp2f(st[k][0] - m) : -1.f;
+        if (st[k][1] != 0.f) l = fmaf(st[k][1], by, l);
+        if (c < chunks && n_here < n_q) s_by[c][n_here] = by;
+    }
+    if constexpr (kLanes == 16) l = row16_sum(l);
+    if (first == 0) {
+        s_m[n_here] = m;
+        s_l[n_here] = l;
+    }
+    __syncthreads();
+    for (int i0 = tid; i0 < n_items; i0 += kItems * kThreads) {
+        f32x4 x[kItems];
+#pragma unroll
+        for (int u = 0; u < kItems; ++u) x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < chunks; c0 += kAhead) {
+            if (i0 != tid || c0 != 0) request(i0, c0);
+#pragma unroll
+            for (int u = 0; u < kItems; ++u)
+#pragma unroll
+                for (int c = 0; c < kAhead; ++c) {
+                    if (c0 + c >= chunks || i0 + u * kThreads >= n_items) continue;
+                    const float by = s_by[c0 + c][(i0 + u * kThreads) / kQuads];
+                    if (by < 0.f) continue;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[u][e] = fmaf(y[u][c][e], by, x[u][e]);
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < kItems; ++u) {
+            const int i = i0 + u * kThreads, n = i / kQuads;
+            if (i < n_items) put(n, i - n * kQuads, s_m[n], s_l[n], x[u]);
+        }
+    }
 }
 
 } // namespace mukv

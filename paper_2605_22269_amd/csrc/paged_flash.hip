@@ -458,13 +458,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         }
     }
     // ---- results ----
-    T *const out = static_cast<T *>(a.out);
+    if (n_halves > 0 && __builtin_expect(s_any != 0, 0)) {
 #pragma unroll
-    for (int i = 0; i < kQB; ++i) {
-        const float l_sum = half_sum(l_run[i]);
-        const int qq = q0 + 32 * i + lq;
-        const bool ok = qq < n_queries;
-        if (n_halves > 0 && __builtin_expect(s_any != 0, 0)) {
+        for (int i = 0; i < kQB; ++i)
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 const unsigned up = s_inf[0][32 * (kQB * wave + i) + lq][f], down = s_inf[1][32 * (kQB * wave + i) + lq][f];
@@ -475,82 +471,93 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                     if (down >> d & 1) o[i][f][j] -= INFINITY;
                 }
             }
+    }
+    float l_sum[kQB];
+#pragma unroll
+    for (int i = 0; i < kQB; ++i) l_sum[i] = half_sum(l_run[i]);
+    if (u.chunks > 1) {
+        // The chunk's record: values as they stand in the lanes, so that every access is a kilobyte in a row (query by query they were
+        // 16-byte pieces of lines: a call of 220 tiles in two chunks 122 us, unsplit 70).  The last workgroup of the tile to get here
+        // joins them, in their order.
+        auto piece = [&](int i, int f, int jj) { return (((wave * kQB + i) * NF + f) * 4 + jj) * 256 + 4 * lane; };
+        {
+            const auto values = chunk_values<kFQ, D>(a.records, u.record + u.chunk);
+            float *const stats = a.records.stats + (int64_t)(u.record + u.chunk) * kFQ * 2;
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) {
+                if (half == 0) store_far(stats + 2 * (32 * (kQB * wave + i) + lq), base_of(i), l_sum[i]);
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int jj = 0; jj < 4; ++jj)
+                        store_far4(values, piece(i, f, jj), f32x4{o[i][f][4 * jj], o[i][f][4 * jj + 1], o[i][f][4 * jj + 2], o[i][f][4 * jj + 3]});
+            }
         }
-        if (u.chunks > 1) { // the chunk's record: [0] what exponents subtracted, [1] sum of the weights, [2..] unnormalised output
-            if (!ok) continue;
-            float *rec = a.records + ((int64_t)(u.record + u.chunk) * kFQ + (qq - u.tile * kFQ)) * (D + 2);
-            if (half == 0) store_far(rec, ref[i] == -INFINITY ? 0.f : ref[i], l_sum);
+        if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
+        const float *const stats = a.records.stats + ((int64_t)u.record * kFQ + 32 * kQB * wave + lq) * 2;
+        float m[kQB];
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            m[i] = -INFINITY;
+            l_sum[i] = 0.f;
+#pragma unroll 8
+            for (int c = 0; c < u.chunks; ++c) {
+                const f32x2 st = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
+                m[i] = st[1] != 0.f ? fmaxf(m[i], st[0]) : m[i]; // (else none of the chunk's rows is seen; a NaN is)
+            }
 #pragma unroll
             for (int f = 0; f < NF; ++f)
 #pragma unroll
-                for (int jj = 0; jj < 4; ++jj)
+                for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
+        }
+#pragma unroll 1
+        for (int c = 0; c < u.chunks; ++c) {
+            const auto values = chunk_values<kFQ, D>(a.records, u.record + c);
+            f32x2 st[kQB];
 #pragma unroll
-                    for (int r = 0; r < 4; r += 2) store_far(rec + 2 + 32 * f + 8 * jj + 4 * half + r, o[i][f][4 * jj + r], o[i][f][4 * jj + r + 1]);
-        } else {
-            const bool seen = l_sum != 0.f; // a query that saw nothing gets zeros; NaN stays NaN
-            const float inv = 1.f / l_sum;
-            const int tok = ok ? my_tok[i] : 0;
-            T *const op = out + ((int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0)) * D + 8 * half;
+            for (int i = 0; i < kQB; ++i) st[i] = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
 #pragma unroll
-            for (int f = 0; f < NF; ++f)
+            for (int i = 0; i < kQB; ++i) {
+                f32x4 x[NF][4];
 #pragma unroll
-                for (int jj = 0; jj < 4; jj += 2) { // a lane holds features 8 jj + 4 half .. + 3: the halves swap, and it stores 16 bytes
-                    raw16 w;
+                for (int f = 0; f < NF; ++f)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t pk[2];
+                    for (int jj = 0; jj < 4; ++jj) x[f][jj] = load_far4(values, piece(i, f, jj));
+                const bool some = st[i][1] != 0.f;
+                const float by = some ? __builtin_amdgcn_exp2f(st[i][0] - m[i]) : 0.f;
+                if (some) l_sum[i] = fmaf(st[i][1], by, l_sum[i]);
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) pk[x] = bf16_pair(o[i][f][4 * (jj + x) + 2 * e] * inv, o[i][f][4 * (jj + x) + 2 * e + 1] * inv);
-                        auto sw = __builtin_amdgcn_permlane32_swap(pk[0], pk[1], false, false);
-                        w[e] = sw[0];
-                        w[2 + e] = sw[1];
-                    }
-                    if (!seen) w = raw16{0u, 0u, 0u, 0u};
-                    if (ok) *reinterpret_cast<raw16 *>(op + 32 * f + 8 * jj) = w;
-                }
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][f][j] = some ? fmaf(x[f][j / 4][j % 4], by, o[i][f][j]) : o[i][f][j];
+            }
         }
     }
-    if (u.chunks == 1) return;
-    // ---- the chunks' records: the last workgroup of the tile to get here joins them, in their order ----
-    if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
-    constexpr int kQuads = D / 4;
-    const int n_q_here = n_queries - u.tile * kFQ < kFQ ? n_queries - u.tile * kFQ : kFQ;
-    for (int i = tid; i < n_q_here * kQuads; i += 256) {
-        const int n = i / kQuads, c = i - n * kQuads, qq = u.tile * kFQ + n, tok = qq / G;
-        const float *rec = a.records + ((int64_t)u.record * kFQ + n) * (D + 2);
-        constexpr int64_t kNext = (int64_t)kFQ * (D + 2);
-        constexpr int kAhead = 4; // records requested together
-        float m = -INFINITY, l = 0.f;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-        for (int s0 = 0; s0 < u.chunks; s0 += kAhead) {
-            f32x2 st[kAhead], x0[kAhead], x1[kAhead];
+    T *const out = static_cast<T *>(a.out);
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s) {
-                if (s0 + s >= u.chunks) break;
-                st[s] = load_far(rec + (s0 + s) * kNext);
-                x0[s] = load_far(rec + (s0 + s) * kNext + 2 + 4 * c);
-                x1[s] = load_far(rec + (s0 + s) * kNext + 4 + 4 * c);
+    for (int i = 0; i < kQB; ++i) {
+        const int qq = q0 + 32 * i + lq;
+        const bool ok = qq < n_queries, seen = l_sum[i] != 0.f; // a query that saw nothing gets zeros; NaN stays NaN
+        const float inv = 1.f / l_sum[i];
+        const int tok = ok ? my_tok[i] : 0;
+        T *const op = out + ((int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0)) * D + 8 * half;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int jj = 0; jj < 4; jj += 2) { // a lane holds features 8 jj + 4 half .. + 3: the halves swap, and it stores 16 bytes
+                raw16 w;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t pk[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) pk[x] = bf16_pair(o[i][f][4 * (jj + x) + 2 * e] * inv, o[i][f][4 * (jj + x) + 2 * e + 1] * inv);
+                    auto sw = __builtin_amdgcn_permlane32_swap(pk[0], pk[1], false, false);
+                    w[e] = sw[0];
+                    w[2 + e] = sw[1];
+                }
+                if (!seen) w = raw16{0u, 0u, 0u, 0u};
+                if (ok) *reinterpret_cast<raw16 *>(op + 32 * f + 8 * jj) = w;
             }
-            float m_new = m;
-#pragma unroll
-            for (int s = 0; s < kAhead; ++s)
-                if (s0 + s < u.chunks && st[s][1] != 0.f) m_new = fmaxf(m_new, st[s][0]);
-            const float corr = l != 0.f ? __builtin_amdgcn_exp2f(m - m_new) : 0.f;
-            l *= corr;
-            x *= corr;
-            m = m_new;
-#pragma unroll
-            for (int s = 0; s < kAhead; ++s) {
-                if (s0 + s >= u.chunks) break;
-                if (st[s][1] == 0.f) continue; // none of its rows is seen
-                const float y = __builtin_amdgcn_exp2f(st[s][0] - m);
-                l = fmaf(st[s][1], y, l);
-                x = f32x4{fmaf(x0[s][0], y, x[0]), fmaf(x0[s][1], y, x[1]), fmaf(x1[s][0], y, x[2]), fmaf(x1[s][1], y, x[3])};
-            }
-        }
-        x = l != 0.f ? x / l : f32x4{0.f, 0.f, 0.f, 0.f};
-        *reinterpret_cast<u32x2 *>(out + ((int64_t)(u.s.first + tok) * v.Hq + g * G + (qq - tok * G)) * D + 4 * c) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
     }
 }
 

@@ -25,8 +25,16 @@ hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
 // The plan's measures for a call: which kernel takes it follows from types and sizes that the host knows (paged_attend.hip).
 // new_hint: new tokens of a sequence, as far as that is known.
 bool paged_takes_flash(int dtype, int D, int G, int64_t new_hint, bool with_weights);
-PlanShape paged_plan(int dtype, bool flash);
-constexpr int kPlanRecords = 1024; // most that any plan's records_bound is: the counts at a workspace's start
+PlanShape paged_plan(int dtype, bool flash, bool causal);
+constexpr int kPlanChunks = 64;     // most chunks of a sequence
+constexpr int kPlanRecords = 1024;  // most that any plan has: the counts at a workspace's start
+
+// What a chunk of a tile's rows leaves for whoever joins them: per query, what its exponents subtracted and the sum of its weights, and its
+// unnormalised output.
+struct ChunkRecords {
+    float *stats;  // [record][queries][2]
+    float *values; // [record][queries][D]
+};
 
 struct PagedAttendArgs {
     PagedView view;
@@ -34,8 +42,8 @@ struct PagedAttendArgs {
     const unsigned char *q; // strides in bytes
     int64_t q_token, q_head;
     void *out;     // [n_tokens][Hq][D]
-    int *counts;   // [records_bound], zero between calls
-    float *records; // [records_bound][queries of a tile][D + 2]
+    int *counts;   // [kPlanRecords], zero between calls
+    ChunkRecords records; // room for the plan's
     float *pairs;  // [n_tokens * Hq][2]: what a query's weights' exponents subtract, 1 / their sum (0: no row seen); or null
     float scale_log2e;
     int causal;

@@ -1,6 +1,7 @@
 // Where the rows of a paged cache live: plain C++, the same on the device and on the host (where the tests walk through it).
 #pragma once
 
+#include <math.h>
 #include <stdint.h>
 
 #if defined(__HIP__)
@@ -62,8 +63,12 @@ MUKV_HD bool is_page(const PagedView &v, int page) { return (unsigned)page < (un
 // about them has to be known on the host.
 struct PlanShape {
     int queries, rows; // of a tile, of a block
-    int target;        // units that are wanted; tiles come on top, since each has one unit at least
-    int most;          // chunks of a sequence
+    int records;       // chunks that there is room for, of tiles with more than one
+    int most;          // chunks of a tile
+    int places;        // workgroups that are resident at once
+    int start;         // what a unit costs before its first block, in blocks; 0: as many chunks as there is room for
+    float join, record; // what joining a chunk of a tile costs, and a chunk of any tile, in blocks
+    int causal;
 };
 MUKV_HD int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -80,28 +85,56 @@ MUKV_HD SeqShape shape_of(const PagedView &v, const PlanShape &p, int b) {
     s.blocks = s.rows > 0 ? (int)div_up(s.rows, p.rows) : 1; // (without rows a tile still has zeros to write)
     return s;
 }
-// Blocks of all tiles, what the chunks share out.
-MUKV_HD double blocks_of(const PagedView &v, const SeqShape &s) { return (double)s.tiles * v.Hkv * s.blocks; }
-// Blocks of a chunk, given those of the whole call.
-MUKV_HD int chunk_of(const PlanShape &p, double all_blocks) {
-    const int64_t per = div_up((int64_t)all_blocks, p.target);
-    return per < 1 ? 1 : per > 0x40000000 ? 0x40000000 : (int)per;
+
+// Of all sequences: tiles (times KV heads), their blocks, those of them that are seen, and the most that a tile has.
+struct PlanSums {
+    double tiles, blocks, seen, longest;
+};
+MUKV_HD PlanSums sums_of(const PagedView &v, const PlanShape &p, const SeqShape &s) {
+    PlanSums x;
+    x.tiles = (double)s.tiles * v.Hkv;
+    x.blocks = x.tiles * s.blocks;
+    const double late = p.causal ? 0.5 * s.n_new / p.rows : 0.0; // under the mask a tile misses half of the new rows in the mean
+    x.seen = x.tiles * (late < s.blocks - 1 ? s.blocks - late : 1.0);
+    x.longest = s.tiles > 0 ? s.blocks : 0.0;
+    return x;
+}
+// What the call takes, in blocks, if the longest tile's rows are `chunks` chunks (1e30: there is no room for them).  Units of about
+// the same size run `places` at a time.
+MUKV_HD float cost_of(const PlanShape &p, const PlanSums &x, bool one_sequence, int chunks) {
+    const float per = ceilf((float)x.longest / (float)chunks);
+    const float tiles = (float)x.tiles, seen = (float)x.seen;
+    float units = tiles;
+    if (chunks > 1) {
+        units = one_sequence ? tiles * (float)chunks : (float)x.blocks / per + tiles;
+        if (units > (float)p.records || (float)chunks > (float)x.longest) return 1e30f;
+    }
+    const float rounds = ceilf(units / (float)p.places) * (seen / units + (float)p.start), last = per + (float)p.start;
+    return (rounds > last ? rounds : last) + (chunks > 1 ? p.join * (float)chunks + p.record * units : 0.f);
+}
+constexpr int kWhole = 0x40000000; // blocks of a chunk: more than any tile has
+MUKV_HD int chunk_by_room(const PlanShape &p, double all_blocks) { // room: sum of ceil(blocks / per) is at most twice blocks / per where there are two chunks or more
+    const int64_t per = div_up((int64_t)all_blocks, p.records / 2);
+    return per < 1 ? 1 : per > kWhole ? kWhole : (int)per;
 }
 MUKV_HD int chunk_of(const PlanShape &p, const SeqShape &s, int per) { // of one sequence: as many chunks, all about the same
     const int least = (int)div_up(s.blocks, p.most);
     return (int)div_up(s.blocks, div_up(s.blocks, per > least ? per : least));
 }
-MUKV_HD int chunks_of(const PlanShape &p, const SeqShape &s, int per) { return (int)div_up(s.blocks, chunk_of(p, s, per)); }
-// Workgroups that cover every unit, and records: sum over sequences of tiles * ceil(blocks / per) is at most target + tiles, and where
-// there are two chunks or more, at most twice target.
+MUKV_HD int chunks_of(const PlanShape &p, const SeqShape &s, int per) {
+    if (per >= kWhole) return 1;
+    return (int)div_up(s.blocks, chunk_of(p, s, per));
+}
+// Workgroups that cover every unit.
 MUKV_HD int64_t units_bound(const PagedView &v, const PlanShape &p) {
     const int64_t with = v.n_seqs < v.n_tokens ? v.n_seqs : v.n_tokens;
     const int64_t tiles = ((int64_t)v.n_tokens * v.G / p.queries + with) * v.Hkv;
     const int64_t room = v.table ? room_of(v) : v.n_tokens; // (packed: a sequence has no more rows than there are tokens)
     int64_t chunks = div_up(room, p.rows);
     chunks = chunks > p.most ? p.most : chunks < 1 ? 1 : chunks;
-    return tiles * chunks < tiles + p.target ? tiles * chunks : tiles + p.target;
+    // with start: all units are within the records if any tile has two chunks; without: tiles of one chunk come on top
+    const int64_t split = p.start ? (tiles > p.records ? tiles : p.records) : tiles + p.records;
+    return tiles * chunks < split ? tiles * chunks : split;
 }
-MUKV_HD int records_bound(const PlanShape &p) { return 2 * p.target; }
 
 } // namespace mukv
