@@ -129,15 +129,13 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
 
 // Which kernel takes an attention call, and its workspace: counts, records, then (with weights) a pair per query.
 struct Space {
-    bool flash;
     mukv::PlanShape plan;
     int64_t stats, values, pairs, bytes; // offsets; the counts are at 0
 };
 Space space_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool with_weights) {
     const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
     Space x;
-    x.flash = mukv::paged_takes_flash(p.dtype, p.head_dim, p.n_q_heads / p.n_kv_heads, hint, with_weights);
-    x.plan = mukv::paged_plan(p.dtype, x.flash, causal);
+    x.plan = mukv::paged_plan(p.dtype, mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint), causal);
     const int64_t rows = (int64_t)x.plan.records * x.plan.queries;
     x.stats = 4 * mukv::kPlanRecords;
     x.values = x.stats + 8 * rows;
@@ -262,7 +260,7 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     }
     DeviceScope dev(pages->device_id);
     if (!dev.ok) return MUKV_ERR_HIP;
-    return finished(mukv::launch_paged_attend(a, D, pages->dtype, x.flash, reinterpret_cast<hipStream_t>(stream)));
+    return finished(mukv::launch_paged_attend(a, D, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
 }
 
 int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,

@@ -394,10 +394,10 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
 }
 
 // What each row receives: weights_out[b][g][j] = decay * weights_in[b][g][j] + sum over the tokens and the group's heads of p_j / sum p.
-// Grid (64 rows, sequence, KV head).  A wave keeps the keys of 16 rows (the A operand) in registers and the sequence's queries stream past it, 16 at
-// a time, with what their weights subtract and the sum they are divided by: S^T leaves a lane one query and four rows, so the sums
-// over the queries run in the lane until the end, where 16 lanes join.
-template <typename T, int D>
+// Grid (rows, sequence, KV head).  A wave keeps the keys of kTiles times 16 rows (the A operand) in registers and the sequence's queries
+// stream past it, 16 at a time and requested one tile ahead, with what their weights subtract and the sum they are divided by: S^T
+// leaves a lane one query and four rows of every 16, so the sums over the queries run in the lane until the end, where 16 lanes join.
+template <typename T, int D, int kTiles>
 __global__ __launch_bounds__(256) void paged_weights_kernel(PagedAttendArgs a, int n_groups) {
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
@@ -411,90 +411,134 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedAttendArgs a, i
     const float scale = a.scale_log2e * (1.f / query_factor<T, D>());
     const bool has_piece = kPieces >= 4 || lg < kPieces;
     const int my_piece = kPieces >= 4 ? lg : lg & (kPieces - 1);
-    for (int r0 = 16 * ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)); r0 < n_w; r0 += 64 * n_groups) {
-        const int r = r0 + lr;
-        const int page = r < n_w ? (v.table ? v.table[entry_of(v, b, r)] : 0) : -1;
-        const bool there = is_page(v, page);
-        const int64_t off = !there ? 0 : v.table ? offset_of(v, page, r) : (int64_t)(s.first + r) * v.stride_row;
-        const unsigned char *kp = v.k + g * v.stride_head + off + 16 * my_piece;
-        raw16 kx[KK];
+    constexpr int kRows = 16 * kTiles; // of a wave
+    for (int r0 = kRows * ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)); r0 < n_w; r0 += 4 * kRows * n_groups) {
+        raw16 kx[kTiles][KK];
+        int from[kTiles][4]; // first token that sees row 16 t + 4 lg + e
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            kx[kk] = *reinterpret_cast<const raw16 *>(kp + 64 * kk);
-            if (!has_piece) kx[kk] = raw16{0u, 0u, 0u, 0u};
-        }
-        const int ft = there ? (a.causal ? r - past : 0) : INT_MAX;
-        int from[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) from[e] = __shfl(ft, 4 * lg + e);
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        // queries before the first row's first token see none of these rows
-        int q0 = a.causal && r0 - past > 0 ? (r0 - past < s.n_new ? (r0 - past) * G & ~15 : n_queries) : 0;
-        for (; q0 < n_queries; q0 += 16) {
-            const int qq = q0 + lr < n_queries ? q0 + lr : n_queries - 1, tok = qq / G, h = g * G + (qq - tok * G);
-            const unsigned char *qp = a.q + (int64_t)(s.first + tok) * a.q_token + (int64_t)h * a.q_head + 16 * my_piece;
-            const f32x2 pair = *reinterpret_cast<const f32x2 *>(a.pairs + 2 * ((int64_t)(s.first + tok) * v.Hq + h));
-            raw16 qx[KK];
+        for (int t = 0; t < kTiles; ++t) {
+            const int r = r0 + 16 * t + lr;
+            const int page = r < n_w ? (v.table ? v.table[entry_of(v, b, r)] : 0) : -1;
+            const bool there = is_page(v, page);
+            const int64_t off = !there ? 0 : v.table ? offset_of(v, page, r) : (int64_t)(s.first + r) * v.stride_row;
+            const unsigned char *kp = v.k + g * v.stride_head + off + 16 * my_piece;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                qx[kk] = *reinterpret_cast<const raw16 *>(qp + 64 * kk);
-                qx[kk] = has_piece ? brought_down<T, D>(qx[kk]) : raw16{0u, 0u, 0u, 0u};
+                kx[t][kk] = *reinterpret_cast<const raw16 *>(kp + 64 * kk);
+                if (!has_piece) kx[t][kk] = raw16{0u, 0u, 0u, 0u};
             }
-            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (kBf16) {
+            const int ft = there ? (a.causal ? r - past : 0) : INT_MAX;
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[kk]), __builtin_bit_cast(bf16x8, qx[kk]), sc, 0, 0, 0);
-            } else { // (in the attention's own order: the same scores)
-                f32x4 part[KK];
+            for (int e = 0; e < 4; ++e) from[t][e] = __shfl(ft, 4 * lg + e);
+        }
+        float sum[kTiles][4];
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    f32x4 c[4];
+        for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[kk][e]), __uint_as_float(qx[kk][e]),
-                                                                    f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                    part[kk] = (c[0] + c[1]) + (c[2] + c[3]);
+            for (int e = 0; e < 4; ++e) sum[t][e] = 0.f;
+        raw16 qx[2][KK];
+        f32x2 pair[2];
+        int tok[2];
+        auto request = [&](int q0, int at) __attribute__((always_inline)) {
+            const int qq = q0 + lr < n_queries ? q0 + lr : n_queries - 1, h = g * G + qq % G;
+            tok[at] = qq / G;
+            const unsigned char *qp = a.q + (int64_t)(s.first + tok[at]) * a.q_token + (int64_t)h * a.q_head + 16 * my_piece;
+            pair[at] = *reinterpret_cast<const f32x2 *>(a.pairs + 2 * ((int64_t)(s.first + tok[at]) * v.Hq + h));
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) qx[at][kk] = *reinterpret_cast<const raw16 *>(qp + 64 * kk);
+            if (q0 + lr >= n_queries) tok[at] = -1; // sees nothing
+        };
+        auto add = [&](int at) __attribute__((always_inline)) {
+            raw16 q[KK];
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) q[kk] = has_piece ? brought_down<T, D>(qx[at][kk]) : raw16{0u, 0u, 0u, 0u};
+            const float ref = pair[at][0], inv = pair[at][1];
+            const bool large = __builtin_amdgcn_ballot_w64(fabsf(ref) > kLargeRef) != 0; // (its rounding shows)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (kBf16) {
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk)
+                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[t][kk]), __builtin_bit_cast(bf16x8, q[kk]), sc, 0, 0, 0);
+                } else { // (in the attention's own order: the same scores)
+                    f32x4 part[KK];
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) {
+                        f32x4 c[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[t][kk][e]), __uint_as_float(q[kk][e]),
+                                                                        f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                        part[kk] = (c[0] + c[1]) + (c[2] + c[3]);
+                    }
+#pragma unroll
+                    for (int n = KK; n > 1; n /= 2)
+#pragma unroll
+                        for (int i = 0; i < n / 2; ++i) part[i] = part[2 * i] + part[2 * i + 1];
+                    sc = part[0];
                 }
 #pragma unroll
-                for (int n = KK; n > 1; n /= 2)
-#pragma unroll
-                    for (int i = 0; i < n / 2; ++i) part[i] = part[2 * i] + part[2 * i + 1];
-                sc = part[0];
+                for (int e = 0; e < 4; ++e) {
+                    // (bf16 payloads: rounded at the size of the difference, 2^-21 of a weight that matters)
+                    const float w = large ? weight_of_any(sc[e], scale, ref) : kBf16 ? __builtin_amdgcn_exp2f(fmaf(sc[e], scale, -ref)) : weight_of(sc[e], scale, ref);
+                    sum[t][e] += tok[at] >= from[t][e] && tok[at] >= 0 ? w * inv : 0.f;
+                }
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float w = weight_of_any(sc[e], scale, pair[0]) * pair[1];
-                sum[e] += q0 + lr < n_queries && tok >= from[e] ? w : 0.f;
-            }
+        };
+        // queries before the first row's first token see none of these rows
+        int q0 = a.causal && r0 - past > 0 ? (r0 - past < s.n_new ? (r0 - past) * G & ~15 : n_queries) : 0;
+        if (q0 < n_queries) request(q0, 0);
+        for (; q0 < n_queries; q0 += 32) {
+            if (q0 + 16 < n_queries) request(q0 + 16, 1);
+            add(0);
+            if (q0 + 32 < n_queries) request(q0 + 32, 0);
+            if (q0 + 16 < n_queries) add(1);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = row16_sum(sum[e]);
-        const int row = r0 + 4 * lg + (lr & 3);
-        if (lr < 4 && row < n_w) {
-            const int64_t at = b * a.weights_seq + g * a.weights_head + row;
-            const float got = lr == 0 ? sum[0] : lr == 1 ? sum[1] : lr == 2 ? sum[2] : sum[3];
-            a.weights_out[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], got) : got;
+        for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[t][e] = row16_sum(sum[t][e]);
+            const int row = r0 + 16 * t + 4 * lg + (lr & 3);
+            if (lr < 4 && row < n_w) {
+                const int64_t at = b * a.weights_seq + g * a.weights_head + row;
+                const float got = lr == 0 ? sum[t][0] : lr == 1 ? sum[t][1] : lr == 2 ? sum[t][2] : sum[t][3];
+                a.weights_out[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], got) : got;
+            }
         }
     }
+}
+
+template <typename T, int D, int kTiles>
+hipError_t launch_weights(const PagedAttendArgs &a, hipStream_t st) {
+    constexpr int kRows = 4 * 16 * kTiles; // of a workgroup
+    const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
+    int64_t groups = (rows + kRows - 1) / kRows, most = 8192 / ((int64_t)a.view.Hkv * a.view.n_seqs);
+    if (most < 16) most = 16;
+    if (groups > most) groups = most; // (a workgroup goes round: a table is often wider than its sequences)
+    if (groups < 1) return hipSuccess;
+    hipLaunchKernelGGL((paged_weights_kernel<T, D, kTiles>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, (int)groups);
+    return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_typed(const PagedAttendArgs &a, hipStream_t st) {
     const unsigned grid = (unsigned)units_bound(a.view, a.plan);
     if (grid > 0) {
-        hipLaunchKernelGGL((paged_attend_kernel<T, D>), dim3(grid), dim3(64 * kPWaves), 0, st, a);
-        const hipError_t e = hipGetLastError();
+        hipError_t e;
+        if (a.plan.queries != kPQ) {
+            e = launch_paged_flash(a, D, st);
+        } else {
+            hipLaunchKernelGGL((paged_attend_kernel<T, D>), dim3(grid), dim3(64 * kPWaves), 0, st, a);
+            e = hipGetLastError();
+        }
         if (e != hipSuccess) return e;
     }
     if (!a.weights_out) return hipSuccess;
-    const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
-    int64_t groups = (rows + 63) / 64, most = 8192 / ((int64_t)a.view.Hkv * a.view.n_seqs);
-    if (most < 16) most = 16;
-    if (groups > most) groups = most; // (a workgroup goes round: a table is often wider than its sequences)
-    if (groups < 1) return hipSuccess;
-    hipLaunchKernelGGL((paged_weights_kernel<T, D>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, (int)groups);
-    return hipGetLastError();
+    // Queries that stream past are shared by the rows a wave holds; where there are few of them it is more waves that count (us a
+    // call, 16 / 64 rows a wave: 64 users, one token, 2000 rows, 64/8 heads 62 / 85; 6 users, 16 tokens, 36000 rows in all, 28/4 heads 35 / 20).
+    if ((int64_t)a.view.n_tokens * a.view.G <= 32 * (int64_t)a.view.n_seqs) return launch_weights<T, D, 1>(a, st);
+    return launch_weights<T, D, sizeof(T) == 2 ? 4 : 2>(a, st);
 }
 
 template <typename T>
@@ -509,16 +553,29 @@ hipError_t launch_by_dim(const PagedAttendArgs &a, int D, hipStream_t st) {
 
 } // namespace
 
-bool paged_takes_flash(int dtype, int D, int G, int64_t new_hint, bool with_weights) {
-    return dtype == MUKV_BF16 && D >= 64 && !with_weights && new_hint * G > 64;
+// Which kernel takes a call, by what is known on the host; us a launch, 28/4 heads of 128.
+// The kernel for any shape reads a sequence's rows once for every 16 queries of a KV head, the one for prompts once for 128 or 256, but its
+// units are large and start slowly: it takes calls with more queries than that (any / prompts: one user, 16 tokens over 8000 rows
+// 24* / 35, over 32000 51* / 60, 32 tokens over 8000 30* / 36, 64 tokens 58 / 37*, over 1000 15.8* / 19.9; 8 users over 8000 rows, 4 tokens
+// 34* / 46, 8 tokens 53 / 46*, 16 tokens 94 / 48*).
+// Tiles of 128 or of 256 queries: the wide ones read operands for twice the products, so they are faster where there is enough to
+// do for every compute unit, and slower where a tile is half empty or the last tiles' rows are what the call waits for (128 / 256: 6
+// users, 16 tokens over 3000 to 9000 rows 41* / 60; 300 tokens 15* / 20; 2000 tokens 58* / 71; 8192 tokens 712 / 560*; 1568 over 6272 rows
+// 312 / 263*; 8 users, 64 tokens over 8000 rows 148 / 109*).
+int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint) {
+    if (dtype != MUKV_BF16 || D < 64) return 0;
+    const int64_t queries = new_hint * v.G; // of a sequence and KV head
+    if (queries < 48 || (int64_t)v.n_tokens * v.Hq < 1500) return 0;
+    const int64_t room = v.table ? room_of(v) : new_hint, tiles = div_up(queries, 256) * v.n_seqs * v.Hkv;
+    return queries <= 128 || (tiles <= 256 && room <= 4096) ? 128 : 256;
 }
 
-PlanShape paged_plan(int dtype, bool flash, bool causal) {
+PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
     PlanShape p;
     p.causal = causal;
     p.most = kPlanChunks;
-    if (flash) {
-        p.queries = 256;
+    if (prompt_tile) {
+        p.queries = prompt_tile;
         p.rows = 64; // a step of the workgroup
         p.records = 704;
         p.places = 256;
@@ -536,8 +593,7 @@ PlanShape paged_plan(int dtype, bool flash, bool causal) {
     return p;
 }
 
-hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, bool flash, hipStream_t st) {
-    if (flash) return launch_paged_flash(a, D, st);
+hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st) {
     return dtype == MUKV_BF16 ? launch_by_dim<uint16_t>(a, D, st) : launch_by_dim<float>(a, D, st);
 }
 

@@ -9,7 +9,7 @@ namespace mukv {
 
 namespace {
 
-constexpr int kFQ = 256, kFRows = 64, kQB = 2; // queries of a workgroup, rows of a step, blocks of 32 queries of a wave
+constexpr int kFRows = 64; // rows of a step
 constexpr int kRing = 8;                       // steps whose rows' places are held
 constexpr float kMostSum = 18446744073709551616.f; // 2^64: sums of weights past this are worked out again (see below)
 
@@ -19,13 +19,14 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
 }
 
 // One workgroup of four waves per unit; a wave owns 64 queries from the scores to the output.
-template <int D>
+template <int D, int kQB, bool PAIRS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_flash_kernel(PagedAttendArgs a) {
     using T = uint16_t;
     constexpr int kRowB = D * 2, kPieces = kRowB / 16, kRowsPerLoad = 64 / kPieces; // rows one load of a wave brings
     constexpr int kLoads = kFRows / 4 / kRowsPerLoad;                               // such loads per wave and step
     constexpr int KK = D / 16, NF = D / 32; // 16-feature steps of the scores, 32-feature blocks of the output
     constexpr int kBuf = kFRows * kRowB;
+    constexpr int kFQ = 128 * kQB; // queries of the workgroup, kQB blocks of 32 a wave
     __shared__ __align__(1024) unsigned char s_kv[5 * kBuf]; // keys of two steps, values of three
     __shared__ int64_t s_off[kRing][kFRows];                 // byte offset of a row
     __shared__ __align__(16) int s_ft[kRing][kFRows];        // first token that sees it
@@ -159,7 +160,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e], s_scale, -s_ref[i]));
             const float y = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e + 1], s_scale, -s_ref[i]));
             w[e] = bf16_pair(x, y);
-            *sum = add_pair(w[e], *sum); // (the weights as they enter the product: a row that has nearly all of it keeps its value)
+            // (the weights as they enter the product: a row that has nearly all of it keeps its value; where the weights of rows are
+            // asked for, the sum is theirs, before the rounding)
+            *sum = PAIRS ? *sum + (x + y) : add_pair(w[e], *sum);
         }
         return __builtin_bit_cast(bf16x8, w);
     };
@@ -472,9 +475,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                 }
             }
     }
-    float l_sum[kQB];
+    float l_sum[kQB], at[kQB]; // sum of the weights, and what they are relative to
 #pragma unroll
-    for (int i = 0; i < kQB; ++i) l_sum[i] = half_sum(l_run[i]);
+    for (int i = 0; i < kQB; ++i) {
+        l_sum[i] = half_sum(l_run[i]);
+        at[i] = base_of(i);
+    }
     if (u.chunks > 1) {
         // The chunk's record: values as they stand in the lanes, so that every access is a kilobyte in a row (query by query they were
         // 16-byte pieces of lines: a call of 220 tiles in two chunks 122 us, unsplit 70).  The last workgroup of the tile to get here
@@ -485,7 +491,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             float *const stats = a.records.stats + (int64_t)(u.record + u.chunk) * kFQ * 2;
 #pragma unroll
             for (int i = 0; i < kQB; ++i) {
-                if (half == 0) store_far(stats + 2 * (32 * (kQB * wave + i) + lq), base_of(i), l_sum[i]);
+                if (half == 0) store_far(stats + 2 * (32 * (kQB * wave + i) + lq), at[i], l_sum[i]);
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -495,15 +501,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         }
         if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
         const float *const stats = a.records.stats + ((int64_t)u.record * kFQ + 32 * kQB * wave + lq) * 2;
-        float m[kQB];
 #pragma unroll
         for (int i = 0; i < kQB; ++i) {
-            m[i] = -INFINITY;
+            at[i] = -INFINITY;
             l_sum[i] = 0.f;
 #pragma unroll 8
             for (int c = 0; c < u.chunks; ++c) {
                 const f32x2 st = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
-                m[i] = st[1] != 0.f ? fmaxf(m[i], st[0]) : m[i]; // (else none of the chunk's rows is seen; a NaN is)
+                at[i] = st[1] != 0.f ? fmaxf(at[i], st[0]) : at[i]; // (else none of the chunk's rows is seen; a NaN is)
             }
 #pragma unroll
             for (int f = 0; f < NF; ++f)
@@ -524,7 +529,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 #pragma unroll
                     for (int jj = 0; jj < 4; ++jj) x[f][jj] = load_far4(values, piece(i, f, jj));
                 const bool some = st[i][1] != 0.f;
-                const float by = some ? __builtin_amdgcn_exp2f(st[i][0] - m[i]) : 0.f;
+                const float by = some ? __builtin_amdgcn_exp2f(st[i][0] - at[i]) : 0.f;
                 if (some) l_sum[i] = fmaf(st[i][1], by, l_sum[i]);
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
@@ -540,7 +545,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         const bool ok = qq < n_queries, seen = l_sum[i] != 0.f; // a query that saw nothing gets zeros; NaN stays NaN
         const float inv = 1.f / l_sum[i];
         const int tok = ok ? my_tok[i] : 0;
-        T *const op = out + ((int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0)) * D + 8 * half;
+        const int64_t row = (int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0);
+        T *const op = out + row * D + 8 * half;
+        if (PAIRS && ok && half == 0) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = seen ? f32x2{at[i], inv} : f32x2{0.f, 0.f};
 #pragma unroll
         for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -563,13 +570,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 
 } // namespace
 
-hipError_t launch_paged_flash(const PagedAttendArgs &a, int D, hipStream_t st) {
+template <int D, int kQB>
+static hipError_t launch_flash(const PagedAttendArgs &a, hipStream_t st) {
     const unsigned grid = (unsigned)units_bound(a.view, a.plan);
-    if (D == 128)
-        hipLaunchKernelGGL((paged_flash_kernel<128>), dim3(grid), dim3(256), 0, st, a);
+    if (a.pairs)
+        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, true>), dim3(grid), dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((paged_flash_kernel<64>), dim3(grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, false>), dim3(grid), dim3(256), 0, st, a);
     return hipGetLastError();
+}
+
+hipError_t launch_paged_flash(const PagedAttendArgs &a, int D, hipStream_t st) {
+    const bool wide = a.plan.queries == 256;
+    if (D == 128) return wide ? launch_flash<128, 2>(a, st) : launch_flash<128, 1>(a, st);
+    return wide ? launch_flash<64, 2>(a, st) : launch_flash<64, 1>(a, st);
 }
 
 } // namespace mukv

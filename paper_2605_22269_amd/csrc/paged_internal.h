@@ -22,10 +22,10 @@ struct RopeArgs {
 };
 hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
 
-// The plan's measures for a call: which kernel takes it follows from types and sizes that the host knows (paged_attend.hip).
-// new_hint: new tokens of a sequence, as far as that is known.
-bool paged_takes_flash(int dtype, int D, int G, int64_t new_hint, bool with_weights);
-PlanShape paged_plan(int dtype, bool flash, bool causal);
+// Which kernel takes an attention call follows from types and sizes that the host knows (paged_attend.hip): 0 that for any shape, otherwise
+// the one for prompts, with tiles of so many queries.  new_hint: new tokens of a sequence, as far as that is known.
+int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint);
+PlanShape paged_plan(int dtype, int prompt_tile, bool causal);
 constexpr int kPlanChunks = 64;     // most chunks of a sequence
 constexpr int kPlanRecords = 1024;  // most that any plan has: the counts at a workspace's start
 
@@ -54,7 +54,7 @@ struct PagedAttendArgs {
     int weights_rows;                  // rows a head has room for
     float decay;
 };
-hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, bool flash, hipStream_t st);
+hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st);
 hipError_t launch_paged_flash(const PagedAttendArgs &a, int D, hipStream_t st);
 
 struct EvictArgs {

@@ -39,7 +39,7 @@ class Case:
 
     def check(self, got, causal=True):
         # more than a token or two a sequence: rows of 64 and 128 bf16 features are multiplied by weights of 8 bits
-        single_weights = self.dtype == BF16 and self.D >= 64 and -(-int(self.off[-1]) // len(self.news)) * (self.hq // self.hkv) > 64
+        single_weights = self.dtype == BF16 and self.D >= 64 and -(-int(self.off[-1]) // len(self.news)) * (self.hq // self.hkv) >= 48
         want, received, amean, reach = self.wanted(causal)
         near(f64(got), want, attention_error(amean, reach, max(self.lengths.max(), 1), self.D, self.dtype, single_weights), self.dtype)
         return received
@@ -287,6 +287,28 @@ def test_weights_that_rows_receive(D, hq, hkv, R, seqs, dtype):
     for b, n in enumerate(c.lengths):
         near(f64(short)[b][:, : min(n, 40)], received[b][:, :40], (1 + received[b][:, :40]) * tol, F32)
     assert (short[:, :, 40:] == 5.0).all()
+
+
+@pytest.mark.parametrize("D,hq,hkv,R,new", [(128, 28, 4, 16, 16), (64, 64, 8, 7, 16), (128, 8, 1, 64, 60)])
+def test_weights_of_windows_of_many_users(D, hq, hkv, R, new):
+    c = Case([(new, 300), (new, new), (new, new - 5), (new, 1700), (new, 90), (new, 64)], D, hq, hkv, R, BF16, seed=R + D)
+    c.table[0, 2] = -1
+    N = int(c.lengths.max()) + 5
+    got = torch.full((6, hkv, N), -3.0, device="cuda")
+    received = c.check(c.attend(weights_out=got, max_new=new))
+    again = torch.zeros_like(got)
+    c.attend(weights_out=again, max_new=new)
+    tol = weights_error(c, received)
+    for b, n in enumerate(c.lengths):
+        near(f64(got)[b][:, :n], received[b], (1 + received[b]) * tol, F32)
+        assert (got[b, :, n:] == -3.0).all() and torch.equal(again[b, :, :n], got[b, :, :n])
+
+
+def test_hints_choose_kernels_and_nothing_else():
+    """The longest sequence is longer than the hint says, or far shorter."""
+    c = Case([(1, 500), (40, 700), (0, 3), (300, 310)], 128, 28, 4, 16, BF16, seed=20)
+    for hint in (0, 1, 5, 1000):
+        c.check(c.attend(max_new=hint))
 
 
 def test_no_new_tokens():
