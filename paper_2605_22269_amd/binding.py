@@ -11,6 +11,7 @@ from __future__ import annotations
 import collections
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -138,13 +139,13 @@ def load():
     lib.mukv_plain_copy.argtypes = [vp, vp, C.c_int64, vp]
     lib.mukv_profile_begin.argtypes = [vp]
     lib.mukv_profile_end.argtypes = [vp, C.POINTER(mukv_profile)]
-    strides, paged, seqs = C.POINTER(mukv_strides), C.POINTER(mukv_paged), C.POINTER(mukv_seqs)
-    lib.mukv_rope.argtypes = [C.POINTER(mukv_rope_table), vp, strides, vp, i32, i32, i32, i32, vp, strides, i32, vp]
+    paged = seqs = strides = vp   # (structures go by address: the callers keep them)
+    lib.mukv_rope.argtypes = [vp, vp, strides, vp, i32, i32, i32, i32, vp, strides, i32, vp]
     lib.mukv_paged_append.argtypes = [paged, i32, seqs, vp, strides, vp, strides, vp, strides, vp, strides,
-                                      C.POINTER(mukv_rope_table), vp, vp]
+                                      vp, vp, vp]
     lib.mukv_paged_workspace_size.argtypes = [paged, seqs, i32, C.POINTER(C.c_int64)]
-    lib.mukv_paged_attend.argtypes = [paged, i32, seqs, vp, strides, i32, vp, C.POINTER(mukv_row_weights), vp, C.c_int64, vp]
-    lib.mukv_paged_evict.argtypes = [paged, seqs, C.POINTER(mukv_row_weights), i32, i32, i32, vp, i32, vp, vp, vp]
+    lib.mukv_paged_attend.argtypes = [paged, i32, seqs, vp, strides, i32, vp, vp, vp, C.c_int64, vp]
+    lib.mukv_paged_evict.argtypes = [paged, seqs, vp, i32, i32, i32, vp, i32, vp, vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -679,26 +680,37 @@ class MuKV:
 
 
 # ---- the conversation's cache ----------------------------------------------------------------
-_STRIDES = {}   # C form of the strides met so far
+# A generated token is two of these calls a layer, of a few microseconds each on the device, so what Python does for one is kept short: every
+# attribute of a tensor is asked for once, a structure is filled by one pack, strides keep their C form.
+_STRIDES = {}   # address of the C form of the strides met so far
+_STRIDES_KEPT = []
+_SEQS = struct.Struct("@QQQiiii")   # mukv_seqs
+_I32 = torch.int32
 
 
 def _rows(t):
-    """Strides of [token][head][feature] as the C ABI takes them."""
+    """Strides of [token][head][feature] as the C ABI takes them: the address of a structure that stays."""
     key = t.stride()
-    st = _STRIDES.get(key)
-    if st is None:
-        if t.numel() == 0:
-            return mukv_strides(0, 0, 0)   # (an empty tensor's strides are anything)
+    at = _STRIDES.get(key)
+    if at is None:
+        if t.numel() == 0:   # (its strides are anything, and not read)
+            key = (0, 0, 1)
+            if key in _STRIDES:
+                return _STRIDES[key]
         assert len(key) == 3 and key[2] == 1
-        if len(_STRIDES) > 256:
-            _STRIDES.clear()
-        st = _STRIDES[key] = mukv_strides(0, key[1], key[0])
-    return st
+        _STRIDES_KEPT.append(mukv_strides(0, key[1], key[0]))
+        at = _STRIDES[key] = C.addressof(_STRIDES_KEPT[-1])
+    return at
 
 
 def _dtype(t):
     assert t.dtype in (torch.bfloat16, torch.float32), t.dtype
     return MUKV_BF16 if t.dtype == torch.bfloat16 else MUKV_F32
+
+
+def _stream_of(index):
+    """Handle of the current stream of that device."""
+    return torch.cuda.current_stream(index).cuda_stream if _raw_stream is None else _raw_stream(index)
 
 
 class Rope:
@@ -707,86 +719,129 @@ class Rope:
 
     def __init__(self, inv_freq, axis=None, *, n_axes=1, pairing="halves"):
         assert inv_freq.dtype == torch.float64 and inv_freq.is_contiguous()
-        assert axis is None or (axis.dtype == torch.int32 and axis.is_contiguous() and axis.numel() == inv_freq.numel())
+        assert axis is None or (axis.dtype == _I32 and axis.is_contiguous() and axis.numel() == inv_freq.numel())
         self._held = inv_freq, axis
         self.n_axes = n_axes
         kind = {"halves": MUKV_ROPE_HALVES, "neighbours": MUKV_ROPE_NEIGHBOURS}[pairing]
-        self.table = mukv_rope_table(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.numel(), n_axes, kind, 0)
-        self.back = mukv_rope_table(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.numel(), n_axes, kind, 1)
-
-    def positions_of(self, positions, n_tokens):
-        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (self.n_axes, n_tokens)
-        return positions.data_ptr()
+        self._tables = [mukv_rope_table(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.numel(), n_axes, kind, back) for back in (0, 1)]
+        self.table, self.back = (C.addressof(t) for t in self._tables)
 
     def rotate(self, x, positions, *, inverse=False, out=None):
         """x [n_tokens][n_heads][head_dim] (any token and head strides), positions int32 [n_axes][n_tokens].  `out` may be x."""
         if out is None:
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        assert x.dim() == 3 and out.shape == x.shape and out.dtype == x.dtype
-        mukv_rope(self.back if inverse else self.table, _ptr(x), _rows(x), self.positions_of(positions, x.shape[0]), x.shape[0],
-                  x.shape[1], x.shape[2], _dtype(x), _ptr(out), _rows(out), x.device.index or 0, _stream())
+        T, H, D = x.shape
+        assert out.shape == x.shape and out.dtype == x.dtype
+        assert positions.dtype is _I32 and positions.shape == (self.n_axes, T) and positions.is_contiguous()
+        dev = x.device.index or 0
+        mukv_rope(self.back if inverse else self.table, x.data_ptr(), _rows(x), positions.data_ptr(), T, H, D, _dtype(x), out.data_ptr(),
+                  _rows(out), dev, _stream_of(dev))
         return out
 
 
-class PagedKV:
+class _Sequences:
+    """What the caches share: the C structures, and scratch of the attention calls, a piece for every stream that calls (calls on
+    different streams may overlap)."""
+
+    def __init__(self):
+        self._pages, self._seqs = mukv_paged(), mukv_seqs()
+        self._pages_at, self._seqs_at = C.addressof(self._pages), C.addressof(self._seqs)
+        self._seqs_memory = memoryview(self._seqs).cast("B")
+        self._scratch, self._need = {}, (None, 0)
+
+    def _attend(self, s, key, layer, q, causal, out, weights, weights_out, decay):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous()
+        w = None
+        if weights_out is not None:
+            st = weights_out.stride()
+            assert weights_out.dtype is torch.float32 and len(st) == 3 and st[2] == 1
+            assert weights_out.shape[:2] == (self._seqs.n_seqs, self._pages.n_kv_heads)
+            if weights is not None:
+                assert weights.dtype is torch.float32 and weights.shape == weights_out.shape and weights.stride() == st
+            w = mukv_row_weights(_ptr(weights), weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
+        else:
+            assert weights is None
+        stream = _stream_of(self._index)
+        if self._need[0] != key:
+            self._need = key, mukv_paged_workspace_size(self._pages_at, s, int(w is not None))
+        need = self._need[1]
+        ws = self._scratch.get(stream)
+        if ws is None or ws[1] < need or ws[3] != self._index:   # (zeros, as every call finds and leaves the part that counts)
+            t = torch.zeros(need, dtype=torch.uint8, device=q.device)
+            ws = self._scratch[stream] = t.data_ptr(), need, t, self._index
+        mukv_paged_attend(self._pages_at, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
+                          None if w is None else C.addressof(w), ws[0], ws[1], stream)
+        return out
+
+
+class PagedKV(_Sequences):
     """The conversation's cache: keys and values of many sequences in pages.  k_pages, v_pages: [layer][page][KV head][row][feature],
     any strides but the last (a cache laid out [layer][page][row][KV head][feature] is passed permuted).  Tables are int32
     [sequence][page], lengths int32 [sequence], both on the device and the caller's."""
 
     def __init__(self, k_pages, v_pages, *, n_q_heads):
+        super().__init__()
         assert k_pages.dim() == 5 and v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
         assert v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device and k_pages.stride(4) == 1
         L, n, hkv, R, D = k_pages.shape
         sl, sp, sh, sr, _ = k_pages.stride()
-        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self.dtype, self.device, self._index = k_pages.dtype, k_pages.device, k_pages.device.index or 0
         self._held = k_pages, v_pages
-        self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, _dtype(k_pages),
-                                 k_pages.device.index or 0)
-        self._seqs, self._space = mukv_seqs(), _Workspace(k_pages.device)
-
-    def _workspace(self, s, with_weights):
-        return self._space.get(self._pages, s, with_weights)
+        self._kv_row, self._q_row = (hkv, D), (n_q_heads, D)
+        self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, _dtype(k_pages), self._index)
+        self._pages_at = C.addressof(self._pages)
 
     def _sequences(self, table, lengths, offsets, n_tokens, max_new):
-        assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
-        assert lengths.dtype == torch.int32 and lengths.is_contiguous() and lengths.numel() == table.shape[0]
-        s = self._seqs
-        s.table, s.lengths = table.data_ptr(), lengths.data_ptr()
-        s.n_seqs, s.table_width = table.shape
-        if offsets is None:
-            s.offsets = None
-        else:
-            assert offsets.dtype == torch.int32 and offsets.is_contiguous() and offsets.numel() == s.n_seqs + 1
-            s.offsets = offsets.data_ptr()
-        s.n_tokens, s.max_new = n_tokens, max_new
-        return s
+        n, width = table.shape
+        assert table.dtype is _I32 and table.is_contiguous()
+        assert lengths.dtype is _I32 and lengths.shape == (n,) and lengths.is_contiguous()
+        off = 0
+        if offsets is not None:
+            assert offsets.dtype is _I32 and offsets.shape == (n + 1,) and offsets.is_contiguous()
+            off = offsets.data_ptr()
+        _SEQS.pack_into(self._seqs_memory, 0, table.data_ptr(), lengths.data_ptr(), off, n, width, n_tokens, max_new)
+        return self._seqs_at
 
     def append(self, layer, table, lengths, k, v, *, q=None, offsets=None, rope=None, positions=None, q_out=None):
         """New tokens' keys and values [n_tokens][n_kv_heads][head_dim] become the last rows of their sequences (lengths count
         them already); with `rope` the keys, and q [n_tokens][n_q_heads][head_dim], are rotated on the way.  Returns q_out."""
-        p, T = self._pages, k.shape[0]
-        assert k.shape == v.shape == (T, p.n_kv_heads, p.head_dim) and k.dtype == v.dtype == self.dtype
+        shape, dt = k.shape, self.dtype
+        T = shape[0]
+        assert shape[1:] == self._kv_row and v.shape == shape and k.dtype is dt and v.dtype is dt
         s = self._sequences(table, lengths, offsets, T, 0)
-        qp = op = qs = os_ = None
+        qp = op = qs = os_ = turn = pos = None
+        known = _STRIDES.get
         if q is not None:
-            assert q.shape == (T, p.n_q_heads, p.head_dim) and q.dtype == self.dtype
+            shape = q.shape
+            assert shape[0] == T and shape[1:] == self._q_row and q.dtype is dt
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            assert q_out.shape == q.shape and q_out.dtype == q.dtype
-            qp, qs, op, os_ = q.data_ptr(), _rows(q), q_out.data_ptr(), _rows(q_out)
-        mukv_paged_append(p, layer, s, k.data_ptr(), _rows(k), v.data_ptr(), _rows(v), qp, qs, op, os_,
-                          None if rope is None else rope.table, None if rope is None else rope.positions_of(positions, T), _stream())
+                q_out = torch.empty(shape, dtype=dt, device=q.device)
+            else:
+                assert q_out.shape == shape and q_out.dtype is dt
+            qp, qs = q.data_ptr(), known(q.stride()) or _rows(q)
+            op, os_ = q_out.data_ptr(), known(q_out.stride()) or _rows(q_out)
+        if rope is not None:
+            assert positions.dtype is _I32 and positions.shape == (rope.n_axes, T) and positions.is_contiguous()
+            turn, pos = rope.table, positions.data_ptr()
+        mukv_paged_append(self._pages_at, layer, s, k.data_ptr(), known(k.stride()) or _rows(k), v.data_ptr(),
+                          known(v.stride()) or _rows(v), qp, qs, op, os_, turn, pos,
+                          _stream_of(self._index))
         return q_out
 
     def attend(self, layer, table, lengths, q, *, offsets=None, max_new=0, causal=True, out=None, weights=None, weights_out=None,
                decay=1.0):
         """q [n_tokens][n_q_heads][head_dim]: every sequence's new tokens (lengths count them) attend to its rows.  With
         weights_out, float32 [sequence][KV head][row], it becomes decay * weights + what every row received (weights None: zeros;
-        weights_out may be weights).  Returns out."""
-        p, T = self._pages, q.shape[0]
-        assert q.shape == (T, p.n_q_heads, p.head_dim) and q.dtype == self.dtype
+        weights_out may be weights).  max_new: most new tokens of a sequence, as a hint.  Returns out."""
+        shape = q.shape
+        T = shape[0]
+        assert shape[1:] == self._q_row and q.dtype is self.dtype
         s = self._sequences(table, lengths, offsets, T, max_new)
-        return _attend(self, s, layer, q, causal, out, weights, weights_out, decay)
+        key = T, self._seqs.n_seqs, self._seqs.table_width, max_new, weights_out is None   # (what else scratch depends on is the cache's)
+        return self._attend(s, key, layer, q, causal, out, weights, weights_out, decay)
 
     def evict(self, table, lengths, weights, budget, *, sink=0, recent=0, into=None, weights_out=None, kept=None, lengths_out=None):
         """Brings every sequence down to `budget` rows per layer and KV head: the first `sink`, the last `recent`, and the others
@@ -795,81 +850,51 @@ class PagedKV:
         [layer][sequence][KV head][budget] padded with -1, and the new lengths (lengths_out may be lengths)."""
         p = self._pages
         s = self._sequences(table, lengths, None, 0, 0)
+        n = table.shape[0]
         if weights_out is None:
             weights_out = weights
-        assert weights.dtype == weights_out.dtype == torch.float32 and weights.dim() == 4 and weights.stride(3) == 1
-        assert weights.shape[:3] == (p.n_layers, s.n_seqs, p.n_kv_heads)
-        assert weights_out.shape == weights.shape and weights_out.stride() == weights.stride()
+        st = weights.stride()
+        assert weights.dtype is torch.float32 and weights_out.dtype is torch.float32 and len(st) == 4 and st[3] == 1
+        assert weights.shape[:3] == (p.n_layers, n, p.n_kv_heads)
+        assert weights_out.shape == weights.shape and weights_out.stride() == st
         if into is not None:
-            assert into.dtype == torch.int32 and into.is_contiguous() and into.dim() == 2 and into.shape[0] == s.n_seqs
-        shape = (p.n_layers, s.n_seqs, p.n_kv_heads, budget)
+            assert into.dtype is _I32 and into.is_contiguous() and into.dim() == 2 and into.shape[0] == n
+        shape = (p.n_layers, n, p.n_kv_heads, budget)
         if kept is None:
-            kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+            kept = torch.empty(shape, dtype=_I32, device=self.device)
         if lengths_out is None:
             lengths_out = torch.empty_like(lengths)
-        assert kept.dtype == lengths_out.dtype == torch.int32 and kept.shape == shape and lengths_out.shape == lengths.shape
+        assert kept.dtype is _I32 and lengths_out.dtype is _I32 and kept.shape == shape and lengths_out.shape == lengths.shape
         assert kept.is_contiguous() and lengths_out.is_contiguous()
-        w = mukv_row_weights(weights.data_ptr(), weights_out.data_ptr(), *weights.stride()[:3], weights.shape[3], 0.0)
-        mukv_paged_evict(p, s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1], kept.data_ptr(),
-                         lengths_out.data_ptr(), _stream())
+        w = mukv_row_weights(weights.data_ptr(), weights_out.data_ptr(), st[0], st[1], st[2], weights.shape[3], 0.0)
+        mukv_paged_evict(self._pages_at, s, C.addressof(w), budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1], kept.data_ptr(),
+                         lengths_out.data_ptr(), _stream_of(self._index))
         return kept, lengths_out
 
 
-def _attend(cache, s, layer, q, causal, out, weights, weights_out, decay):
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
-    w = None
-    if weights_out is not None:
-        assert weights_out.dtype == torch.float32 and weights_out.dim() == 3 and weights_out.stride(2) == 1
-        assert weights_out.shape[:2] == (s.n_seqs, cache._pages.n_kv_heads)
-        if weights is not None:
-            assert weights.dtype == torch.float32 and weights.shape == weights_out.shape and weights.stride() == weights_out.stride()
-        w = mukv_row_weights(_ptr(weights), weights_out.data_ptr(), 0, weights_out.stride(0), weights_out.stride(1), weights_out.shape[2], decay)
-    else:
-        assert weights is None
-    ws = cache._workspace(s, w is not None)
-    mukv_paged_attend(cache._pages, layer, s, q.data_ptr(), _rows(q), int(causal), out.data_ptr(), w, ws.data_ptr(), ws.numel(), _stream())
-    return out
-
-
-class _Workspace:
-    """Scratch of the attention calls of one cache, a piece for every stream that calls: calls on different streams may overlap."""
-
-    def __init__(self, device):
-        self.device, self.by_stream, self.need = device, {}, (None, 0)
-
-    def get(self, pages, s, with_weights):
-        key = (s.n_tokens, s.n_seqs, s.max_new, with_weights)   # (what else it takes is the cache's own)
-        if self.need[0] != key:
-            self.need = key, mukv_paged_workspace_size(pages, s, int(with_weights))
-        ws = self.by_stream.get(st := _stream())
-        if ws is None or ws.numel() < self.need[1]:
-            ws = self.by_stream[st] = torch.zeros(self.need[1], dtype=torch.uint8, device=self.device)
-        return ws
-
-
-class PackedKV:
+class PackedKV(_Sequences):
     """Attention over packed sequences without pages: q [n_tokens][n_q_heads][head_dim] and k, v [n_tokens][n_kv_heads][head_dim],
     sequence b the tokens offsets[b] .. offsets[b+1]-1 of all three (slices of one fused projection will do)."""
 
     def __init__(self, *, n_q_heads):
-        self._pages, self._seqs, self._space = mukv_paged(), mukv_seqs(), None
+        super().__init__()
         self._pages.n_q_heads = n_q_heads
-
-    def _workspace(self, s, with_weights):
-        return self._space.get(self._pages, s, with_weights)
+        self._kind = None
 
     def attend(self, q, k, v, offsets, *, max_new=0, causal=True, out=None, weights=None, weights_out=None, decay=1.0):
-        p, s, T = self._pages, self._seqs, q.shape[0]
-        assert k.dim() == 3 and v.shape == k.shape and v.stride() == k.stride() and k.stride(2) == 1 and k.shape[0] == T
-        assert q.shape == (T, p.n_q_heads, k.shape[2]) and q.dtype == k.dtype == v.dtype
-        assert offsets.dtype == torch.int32 and offsets.is_contiguous()
-        p.k_pages, p.v_pages, p.stride_row, p.stride_head = k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1)
-        p.n_layers, p.n_pages, p.page_rows, p.n_kv_heads, p.head_dim = 1, 1, max(T, 1), k.shape[1], k.shape[2]
-        p.dtype, p.device_id = _dtype(k), k.device.index or 0
-        s.offsets, s.n_seqs, s.n_tokens, s.max_new = offsets.data_ptr(), offsets.numel() - 1, T, max_new
-        if self._space is None or self._space.device != q.device or self._space.kind != (p.dtype, p.n_kv_heads, p.head_dim):
-            self._space = _Workspace(q.device)
-            self._space.kind = p.dtype, p.n_kv_heads, p.head_dim
-        return _attend(self, s, 0, q, causal, out, weights, weights_out, decay)
+        """As PagedKV.attend; weights are [sequence][KV head][token of the sequence]."""
+        p, (T, hkv, D), st = self._pages, k.shape, k.stride()
+        assert v.shape == k.shape and v.stride() == st and (st[2] == 1 or T == 0)
+        assert q.shape == (T, p.n_q_heads, D) and q.dtype is k.dtype and k.dtype is v.dtype
+        assert offsets.dtype is _I32 and offsets.is_contiguous()
+        p.k_pages, p.v_pages, p.stride_row, p.stride_head = k.data_ptr(), v.data_ptr(), st[0], st[1]
+        kind = k.dtype, hkv, D, k.device
+        if self._kind != kind:
+            self._kind, self._need, self._index = kind, (None, 0), k.device.index or 0
+            p.n_layers, p.n_pages, p.n_kv_heads, p.head_dim, p.dtype, p.device_id = 1, 1, hkv, D, _dtype(k), self._index
+        p.page_rows = T if T > 0 else 1
+        n = offsets.numel() - 1
+        _SEQS.pack_into(self._seqs_memory, 0, 0, 0, offsets.data_ptr(), n, 0, T, max_new)
+        if T == 0 and weights_out is None:
+            return q if out is None else out
+        return self._attend(self._seqs_at, (T, n, max_new, weights_out is None), 0, q, causal, out, weights, weights_out, decay)

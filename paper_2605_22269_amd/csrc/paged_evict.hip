@@ -2,8 +2,8 @@
 //
 // evict_select_kernel ranks the rows, evict_move_kernel packs the chosen rows' keys and values.  A row's rank is a 32-bit key: 0 for
 // rows that do not exist (never kept), 1 for NaN weights, the weight's bits in an order that compares as the weights do, all ones
-// for the rows that stay whatever they weigh.  The m-th largest key is found digit by digit (8 bits, counts in LDS); of the rows
-// that equal it the first ones stay.
+// for the rows that stay whatever they weigh.  The m-th largest key is found by its digits (8 bits, counts in LDS); once the rows that
+// share its upper half are few, by counting among them.  Of the rows that equal it the first ones stay.
 #include "attend_dev.h"
 #include "paged_internal.h"
 
@@ -11,9 +11,10 @@ namespace mukv {
 
 namespace {
 
-constexpr int kSelThreads = 512, kSelRows = 4, kSelWaves = kSelThreads / 64; // rows a thread takes at a time when the list is written
+constexpr int kSelRows = 4;      // rows a thread takes at a time when the list is written
 constexpr int kSelCache = 32768; // keys that wait in LDS; those of further rows are worked out again on every pass
 constexpr int kSelCopies = 4;    // of the counts: lanes that count the same digit at once share an address less often
+constexpr int kSelCand = 512;    // rows that share the upper half of the key and are ranked by counting
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
     if (w != w) return 1u;
@@ -22,11 +23,15 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 // One workgroup per (layer, sequence, KV head).  What bounds it: with a few thousand rows the barriers of the four digits.
+template <int kSelThreads>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, int cache_keys) {
+    constexpr int kSelWaves = kSelThreads / 64;
     extern __shared__ __align__(16) uint32_t s_key[]; // [cache_keys]
     __shared__ int s_hist[kSelCopies][256];
     __shared__ int s_found[3]; // the digit, how many keys are above it, how many share it
     __shared__ int s_sum[2][kSelWaves];
+    __shared__ uint32_t s_cand_key[kSelCand];
+    __shared__ int s_cand_row[kSelCand], s_n_cand, s_last_row;
     const PagedView &v = a.view;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int g = blockIdx.x % v.Hkv, b = blockIdx.x / v.Hkv % v.n_seqs, layer = blockIdx.x / v.Hkv / v.n_seqs;
@@ -45,20 +50,29 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
     // ---- the m-th largest key, digit by digit ----
     uint32_t prefix = 0; // of the digits found
     int m = 0, need = 0;
+    int last_row = -1;   // counted among few: the last row that stays of those that equal the m-th
+    if (tid == 0) s_n_cand = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = tid; i < kSelCopies * 256; i += kSelThreads) (&s_hist[0][0])[i] = 0;
         __syncthreads();
         int there = 0;
-        for (int j = tid; j < n; j += kSelThreads) {
-            uint32_t k;
-            if (shift == 24) {
-                k = key_of(j);
-                if (j < cache_keys) s_key[j] = k;
-                there += k != 0u;
-            } else {
-                k = get(j);
+        constexpr int kAhead = 4; // rows a thread asks for together
+        for (int j0 = tid; j0 < n; j0 += kAhead * kSelThreads) {
+            uint32_t k[kAhead];
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const int j = j0 + e * kSelThreads;
+                k[e] = j >= n ? 0u : shift == 24 ? key_of(j) : get(j);
             }
-            if (k != 0u && (shift == 24 || k >> (shift + 8) == prefix)) atomicAdd(&s_hist[lane & (kSelCopies - 1)][k >> shift & 255u], 1);
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const int j = j0 + e * kSelThreads;
+                if (shift == 24) {
+                    if (j < n && j < cache_keys) s_key[j] = k[e];
+                    there += k[e] != 0u;
+                }
+                if (k[e] != 0u && (shift == 24 || k[e] >> (shift + 8) == prefix)) atomicAdd(&s_hist[lane & (kSelCopies - 1)][k[e] >> shift & 255u], 1);
+            }
         }
         if (shift == 24) {
             there = wave_sum(there);
@@ -105,11 +119,38 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
             need = -1;
             break;
         }
+        if (shift == 16 && s_found[2] <= kSelCand) { // (the same in all threads)
+            for (int j = tid; j < n; j += kSelThreads) {
+                const uint32_t k = get(j);
+                if (k >> 16 != prefix) continue;
+                const int at = atomicAdd(&s_n_cand, 1);
+                s_cand_key[at] = k;
+                s_cand_row[at] = j;
+            }
+            __syncthreads();
+            const int n_cand = s_n_cand;
+            if (tid < n_cand) {
+                const uint32_t k = s_cand_key[tid];
+                const int j = s_cand_row[tid];
+                int ahead = 0;
+                for (int i = 0; i < n_cand; ++i) ahead += s_cand_key[i] > k || (s_cand_key[i] == k && s_cand_row[i] < j);
+                if (ahead == need - 1) {
+                    s_found[0] = (int)k;
+                    s_last_row = j;
+                }
+            }
+            __syncthreads();
+            prefix = (uint32_t)s_found[0];
+            last_row = s_last_row;
+            need = 0;
+            break;
+        }
     }
     // Rows above `prefix` stay, and the first `need` of those that equal it (-1: all that are not below it).  (Rows that stay whatever
     // they weigh are no more than the budget: where their key is the m-th largest, all of them are within it, and need is -1.)
     const uint32_t least = need < 0 ? prefix : prefix + 1;
-    const int quota = need < 0 ? 0 : need;
+    const int quota = need > 0 ? need : 0;
+    auto stays = [&](uint32_t k, int j) { return k >= least || (k == prefix && j <= last_row); };
     // ---- the list, ascending: kSelRows neighbouring rows a thread ----
     int over0 = 0, equal0 = 0; // before this round
     for (int base = 0; m > 0 && base < n; base += kSelThreads * kSelRows) {
@@ -122,8 +163,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
             k[e] = j0 + e < n ? get(j0 + e) : 0u;
             w[e] = j0 + e < n && j0 + e < a.w_rows ? w_in[j0 + e] : 0.f;
             if (k[e] == 0u) continue;
-            over += k[e] >= least;
-            equal += need >= 0 && k[e] == prefix;
+            over += stays(k[e], j0 + e);
+            equal += need > 0 && k[e] == prefix;
         }
         const int both = wave_prefix(over | equal << 16);
         if (lane == 63) s_sum[1][wave] = both;
@@ -140,7 +181,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
 #pragma unroll
         for (int e = 0; e < kSelRows; ++e) {
             if (k[e] == 0u) continue;
-            const bool is_equal = need >= 0 && k[e] == prefix, is_over = k[e] >= least;
+            const bool is_equal = need > 0 && k[e] == prefix, is_over = stays(k[e], j0 + e);
             if (is_over || (is_equal && q < quota)) {
                 const int pos = o + (q < quota ? q : quota);
                 kept[pos] = j0 + e;
@@ -207,7 +248,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
                 const int rr = r + u * rows_at_once;
                 if (rr >= kMoveRows || s_from[rr] < 0) continue;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) *reinterpret_cast<raw16 *>(bases[t] + s_to[rr]) = x[u][t];
+                for (int t = 0; t < 2; ++t) __builtin_nontemporal_store(x[u][t], reinterpret_cast<raw16 *>(bases[t] + s_to[rr]));
             }
         }
         __syncthreads(); // the next rows' places take these ones'
@@ -261,19 +302,26 @@ __global__ __launch_bounds__(kMoveThreads) void evict_pack_kernel(EvictArgs a, i
     if (blockIdx.y == 0 && blockIdx.z == 0 && layer == 0 && g == 0) write_length(a, kept, b);
 }
 
+template <int kSelThreads>
+hipError_t launch_select(const EvictArgs &a, int lists, int keys, int device, hipStream_t st) {
+    static bool allowed[kMaxDevices];
+    if (keys * sizeof(uint32_t) > 32 * 1024) {
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(&evict_select_kernel<kSelThreads>), kSelCache * sizeof(uint32_t), device, allowed);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((evict_select_kernel<kSelThreads>), dim3(lists), dim3(kSelThreads), keys * sizeof(uint32_t), st, a, keys);
+    return hipGetLastError();
+}
+
 } // namespace
 
 hipError_t launch_paged_evict(const EvictArgs &a, int n_layers, int row_bytes, int device, hipStream_t st) {
     const int lists = n_layers * a.view.n_seqs * a.view.Hkv;
     const int64_t room = room_of(a.view);
     const int keys = (int)(room < kSelCache ? room : kSelCache);
-    static bool allowed[kMaxDevices];
-    if (keys * sizeof(uint32_t) > 48 * 1024) {
-        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(&evict_select_kernel), kSelCache * sizeof(uint32_t), device, allowed);
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(evict_select_kernel, dim3(lists), dim3(kSelThreads), keys * sizeof(uint32_t), st, a, keys);
-    hipError_t e = hipGetLastError();
+    // Few lists: a workgroup each has a compute unit to itself.  (us a launch, 1024 / 512 threads: 112 lists of 8200 rows 24 / 30, 768 of 900
+    // to 6000 rows 45 / 28.)
+    hipError_t e = lists <= 256 ? launch_select<1024>(a, lists, keys, device, st) : launch_select<512>(a, lists, keys, device, st);
     if (e != hipSuccess) return e;
     const int chunks = (a.budget + kMoveRows - 1) / kMoveRows;
     if (a.into) {

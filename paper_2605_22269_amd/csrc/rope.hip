@@ -33,6 +33,10 @@ __device__ __forceinline__ void piece_put(raw16 &x, int e, float y0, float y1) {
     }
 }
 
+// Past the caches: what is written here is read by other launches, on other XCDs (1568 tokens, 28/4 heads of 128: 7.6 us a launch, 8.8
+// without; 24 prompts of 64/8 heads, 0.45 GB: 90, 95).
+__device__ __forceinline__ void put_piece(unsigned char *p, raw16 x) { __builtin_nontemporal_store(x, reinterpret_cast<raw16 *>(p)); }
+
 template <typename T, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_wg) {
     constexpr int E = 16 / (int)sizeof(T); // elements of a piece
@@ -51,17 +55,29 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
     auto worked_out = [&]() {
         for (int i = tid; i < nt * n_pairs; i += kRopeThreads) {
             const int t = i / n_pairs, p = i - t * n_pairs;
+            // (up to three axes: all positions of the token, so that nothing waits for which one it is)
             const int ax = a.axis ? a.axis[p] : 0;
-            const int pos = (unsigned)ax < (unsigned)a.n_axes ? a.positions[(int64_t)ax * a.n_tokens + t0 + t] : 0;
+            const int32_t *at = a.positions + t0 + t;
+            int pos = at[0];
+            if (a.n_axes <= 3) {
+                const int second = a.n_axes > 1 ? at[a.n_tokens] : 0, third = a.n_axes > 2 ? at[2 * (int64_t)a.n_tokens] : 0;
+                pos = ax == 0 ? pos : ax == 1 ? second : ax == 2 ? third : 0;
+            } else {
+                pos = (unsigned)ax < (unsigned)a.n_axes ? at[(int64_t)ax * a.n_tokens] : 0;
+            }
             double turns = (double)pos * a.inv_freq[p] * 0.15915494309189533577; // 1 / 2 pi
             turns -= rint(turns);
             float s, c;
             sincospif((float)(2.0 * turns), &s, &c);
             s_turn[t][p] = float2{c, a.inverse ? -s : s};
         }
-        if (tid < nt && a.v.heads) {
+    };
+    // by the last wave, beside the first one's cosines
+    auto placed = [&]() {
+        const int mine = tid - (kRopeThreads - 64);
+        if (mine >= 0 && mine < nt && a.v.heads) {
             const PagedView &v = a.view;
-            const int tok = t0 + tid;
+            const int tok = t0 + mine;
             int b;
             if (v.offsets) { // the last sequence that starts at or before the token
                 int lo = 0, hi = v.n_seqs - 1;
@@ -84,7 +100,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
                 const int page = v.table[entry_of(v, b, row)];
                 if (is_page(v, page)) place = offset_of(v, page, row);
             }
-            s_place[tid] = place;
+            s_place[mine] = place;
         }
     };
 
@@ -107,6 +123,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
             if (pair) y[u] = *reinterpret_cast<const raw16 *>(p + 16 * (my_item + joint));
         }
         if (r0 == 0) {
+            placed();
             worked_out();
             __syncthreads();
         }
@@ -128,8 +145,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
                     piece_put<T>(x[u], e, x0 * c0.x - y0 * c0.y, x1 * c1.x - y1 * c1.y);
                     piece_put<T>(y[u], e, y0 * c0.x + x0 * c0.y, y1 * c1.x + x1 * c1.y);
                 }
-                *reinterpret_cast<raw16 *>(p + 16 * my_item) = x[u];
-                *reinterpret_cast<raw16 *>(p + 16 * (my_item + joint)) = y[u];
+                put_piece(p + 16 * my_item, x[u]);
+                put_piece(p + 16 * (my_item + joint), y[u]);
             } else {
                 if (NEIGHBOURS && E * my_item < 2 * n_pairs) {
 #pragma unroll
@@ -139,7 +156,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
                         piece_put<T>(x[u], e, x0 * c.x - y0 * c.y, y0 * c.x + x0 * c.y);
                     }
                 }
-                *reinterpret_cast<raw16 *>(p + 16 * (my_item + joint)) = x[u];
+                put_piece(p + 16 * (my_item + joint), x[u]);
             }
         }
         if (r0 + kRopeAhead * at_once >= n_rows) break;
@@ -147,13 +164,14 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
     for (int r = v_first; r < n_v; r += v_at_once) {
         const int t = r / a.v.heads, h = r - t * a.v.heads;
         if (r != v_first) vx = *reinterpret_cast<const raw16 *>(a.v.x + (t0 + t) * a.v.token + h * a.v.head + 16 * v_item);
-        if (s_place[t] >= 0) *reinterpret_cast<raw16 *>(a.view.v + s_place[t] + h * a.view.stride_head + 16 * v_item) = vx;
+        if (s_place[t] >= 0) put_piece(a.view.v + s_place[t] + h * a.view.stride_head + 16 * v_item, vx);
     }
 }
 
 template <typename T>
 hipError_t launch_rope_typed(const RopeArgs &a, hipStream_t st) {
-    int per_wg = a.n_tokens / 1024;
+    // 1568 tokens: 10.0 us a launch with a token a workgroup, 8.8 with two, 9.2 with three
+    int per_wg = a.n_tokens / 768;
     per_wg = per_wg < 1 ? 1 : per_wg > kRopeTokens ? kRopeTokens : per_wg;
     const unsigned grid = (unsigned)((a.n_tokens + per_wg - 1) / per_wg);
     if (a.neighbours || !a.rotate)

@@ -120,6 +120,13 @@ def test_lengths_past_the_table_and_fewer_weights_than_rows():
     c.check(150, 4, 30, in_place=True, weights_in_place=True)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_many_lists(in_place):
+    rng = np.random.default_rng(9)
+    c = Case([int(x) for x in rng.integers(0, 700, 40)], 16, 16, 4, 2, BF16, seed=10)
+    c.check(200, 4, 50, in_place=in_place, weights_in_place=in_place)
+
+
 def test_again_and_again():
     """A cache that grows by 20 rows and is cut back, five times, in place: the rows that survive are those of the plain form."""
     c = Case([300], 16, 32, 2, 2, BF16, seed=7)
