@@ -585,7 +585,7 @@ PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
     } else {
         p.queries = kPQ;
         p.rows = dtype == MUKV_BF16 ? 128 : 64; // a block of every wave
-        p.records = 1024;                       // two workgroups per compute unit, as many as are resident, and the odd ones
+        p.records = 2048;
         p.places = 512;
         p.start = 0;
         p.join = p.record = 0.f;

@@ -27,7 +27,7 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
         u->s = shape_of(v, p, 0);
         u->b = 0;
         const PlanSums x = sums_of(v, p, u->s);
-        const int per = p.start ? chunk_by_cost(p, x, true) : chunk_by_room(p, x.blocks);
+        const int per = p.start ? chunk_by_cost(p, x, true) : chunk_by_room(p, x);
         u->chunks = chunks_of(p, u->s, per);
         u->per = per >= kWhole ? u->s.blocks : chunk_of(p, u->s, per);
         u->record = 0;
@@ -45,14 +45,14 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
             all.longest = fmax(all.longest, x.longest);
         }
         all.blocks = wave_sum(all.blocks);
+        all.tiles = wave_sum(all.tiles);
+        all.longest = wave_max(all.longest);
         int per;
         if (p.start) {
-            all.tiles = wave_sum(all.tiles);
             all.seen = wave_sum(all.seen);
-            all.longest = wave_max(all.longest);
             per = chunk_by_cost(p, all, false);
         } else {
-            per = chunk_by_room(p, all.blocks);
+            per = chunk_by_room(p, all);
         }
         int units0 = 0, records0 = 0, b0 = 0;
         for (;; b0 += 64) {

@@ -27,7 +27,7 @@ hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
 int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint);
 PlanShape paged_plan(int dtype, int prompt_tile, bool causal);
 constexpr int kPlanChunks = 64;     // most chunks of a sequence
-constexpr int kPlanRecords = 1024;  // most that any plan has: the counts at a workspace's start
+constexpr int kPlanRecords = 2048;  // most that any plan has: the counts at a workspace's start
 
 // What a chunk of a tile's rows leaves for whoever joins them: per query, what its exponents subtracted and the sum of its weights, and its
 // unnormalised output.

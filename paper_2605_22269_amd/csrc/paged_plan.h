@@ -66,7 +66,7 @@ struct PlanShape {
     int records;       // chunks that there is room for, of tiles with more than one
     int most;          // chunks of a tile
     int places;        // workgroups that are resident at once
-    int start;         // what a unit costs before its first block, in blocks; 0: as many chunks as there is room for
+    int start;         // what a unit costs before its first block, in blocks; 0: rows are all that has to move (chunk_by_room)
     float join, record; // what joining a chunk of a tile costs, and a chunk of any tile, in blocks
     int causal;
 };
@@ -113,9 +113,24 @@ MUKV_HD float cost_of(const PlanShape &p, const PlanSums &x, bool one_sequence, 
     return (rounds > last ? rounds : last) + (chunks > 1 ? p.join * (float)chunks + p.record * units : 0.f);
 }
 constexpr int kWhole = 0x40000000; // blocks of a chunk: more than any tile has
-MUKV_HD int chunk_by_room(const PlanShape &p, double all_blocks) { // room: sum of ceil(blocks / per) is at most twice blocks / per where there are two chunks or more
-    const int64_t per = div_up((int64_t)all_blocks, p.records / 2);
-    return per < 1 ? 1 : per > kWhole ? kWhole : (int)per;
+// Blocks of a chunk where rows are all that has to move (start: 0).  Few tiles: eight blocks, which is enough to hide how a unit starts,
+// or less where that leaves compute units without one; many: whole, unless they differ much, when the long ones are cut to half
+// the mean.  (us a launch, blocks of 128 rows a chunk: 8 users of 8000 rows, 28/4 heads, 8 blocks 26.9, 4 28.1, 2 37; 64 users of
+// 2000, 64/8 heads, whole 93, 8 blocks 104; 64 users of 200 to 12000, 30 blocks 199, 15 188, 8 187.)
+// Room: the sum of ceil(blocks / per) over tiles with two chunks or more is at most twice that of blocks / per.
+MUKV_HD int chunk_by_room(const PlanShape &p, const PlanSums &x) {
+    const double least = ceil(x.blocks / (p.records / 2));
+    double per;
+    if (x.tiles < 256.0) {
+        per = ceil(x.blocks / 256.0);
+        per = per < 8.0 ? per : 8.0;
+    } else {
+        if (x.longest * x.tiles <= 1.5 * x.blocks) return kWhole;
+        per = ceil(0.5 * x.blocks / x.tiles);
+        per = per > 8.0 ? per : 8.0;
+    }
+    per = per > least ? per : least;
+    return per < 1.0 ? 1 : per > kWhole ? kWhole : (int)per;
 }
 MUKV_HD int chunk_of(const PlanShape &p, const SeqShape &s, int per) { // of one sequence: as many chunks, all about the same
     const int least = (int)div_up(s.blocks, p.most);

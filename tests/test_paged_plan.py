@@ -22,7 +22,7 @@ int main() {
     for (int trial = 0; trial < 3000; ++trial) {
         PagedView v = {};
         PlanShape p;
-        const int kinds[3][7] = {{16, 128, 1024, 64, 512, 0, 0}, {16, 64, 1024, 64, 512, 0, 0}, {in(0, 1) ? 256 : 128, 64, 704, 64, 256, 3, 1}};
+        const int kinds[3][7] = {{16, 128, 2048, 64, 512, 0, 0}, {16, 64, 2048, 64, 512, 0, 0}, {in(0, 1) ? 256 : 128, 64, 704, 64, 256, 3, 1}};
         const int *k = kinds[in(0, 2)];
         p.queries = k[0]; p.rows = k[1]; p.records = k[2]; p.most = k[3]; p.places = k[4]; p.start = k[5]; p.join = 0.8f * k[6]; p.record = 0.06f * k[6]; p.causal = in(0, 1);
         v.n_seqs = in(1, in(0, 3) ? 5 : 150);
@@ -49,7 +49,7 @@ int main() {
             all.tiles += x.tiles; all.blocks += x.blocks; all.seen += x.seen;
             if (x.longest > all.longest) all.longest = x.longest;
         }
-        int per = chunk_by_room(p, all.blocks);
+        int per = chunk_by_room(p, all);
         if (p.start) { // the least cost, as the lanes find it
             int best = 1;
             for (int c = 2; c <= p.most; ++c)
