@@ -590,6 +590,8 @@ PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
         p.start = 0;
         p.join = p.record = 0.f;
     }
+    p.log_queries = p.queries == 256 ? 8 : p.queries == 128 ? 7 : 4;
+    p.log_rows = p.rows == 128 ? 7 : 6;
     return p;
 }
 

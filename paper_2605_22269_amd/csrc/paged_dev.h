@@ -17,7 +17,7 @@ __device__ __forceinline__ int chunk_by_cost(const PlanShape &p, const PlanSums 
     const int chunks = (threadIdx.x & 63) + 1;
     const float cost = chunks <= p.most ? cost_of(p, x, one_sequence, chunks) : 1e30f;
     const int best = 1 + (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == -wave_max(-cost)));
-    return best == 1 ? kWhole : (int)((x.longest + best - 1) / best);
+    return best == 1 ? kWhole : div_up32((int)x.longest, best);
 }
 
 // The unit of this workgroup, the same in all lanes; false: there is none.
@@ -29,20 +29,20 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
         const PlanSums x = sums_of(v, p, u->s);
         const int per = p.start ? chunk_by_cost(p, x, true) : chunk_by_room(p, x);
         u->chunks = chunks_of(p, u->s, per);
-        u->per = per >= kWhole ? u->s.blocks : chunk_of(p, u->s, per);
+        u->per = chunk_of(p, u->s, per);
         u->record = 0;
         if (id >= u->s.tiles * v.Hkv * u->chunks) return false;
     } else {
         const SeqShape none = {0, 0, 0, 0, 0, 1};
         SeqShape s = none;
-        PlanSums all = {0.0, 0.0, 0.0, 0.0};
+        PlanSums all = {0.f, 0.f, 0.f, 0.f};
         for (int b0 = 0; b0 < v.n_seqs; b0 += 64) {
             s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
             const PlanSums x = sums_of(v, p, s);
             all.tiles += x.tiles;
             all.blocks += x.blocks;
             all.seen += x.seen;
-            all.longest = fmax(all.longest, x.longest);
+            all.longest = fmaxf(all.longest, x.longest);
         }
         all.blocks = wave_sum(all.blocks);
         all.tiles = wave_sum(all.tiles);
@@ -66,7 +66,7 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
                 auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
                 u->s = SeqShape{of(s.first), of(s.n_new), of(s.length), of(s.rows), of(s.tiles), of(s.blocks)};
                 u->b = b0 + at;
-                u->per = per >= kWhole ? u->s.blocks : chunk_of(p, u->s, per);
+                u->per = chunk_of(p, u->s, per);
                 u->chunks = of(chunks);
                 u->record = of(records1 - records);
                 id -= of(units1 - units);

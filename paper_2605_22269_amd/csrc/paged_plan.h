@@ -62,7 +62,8 @@ MUKV_HD bool is_page(const PagedView &v, int page) { return (unsigned)page < (un
 // rows, a whole number of blocks of `rows` each.  Every workgroup works the plan out for itself from lengths and offsets, so nothing
 // about them has to be known on the host.
 struct PlanShape {
-    int queries, rows; // of a tile, of a block
+    int queries, rows; // of a tile, of a block: powers of two, 1 << log_queries and 1 << log_rows
+    int log_queries, log_rows;
     int records;       // chunks that there is room for, of tiles with more than one
     int most;          // chunks of a tile
     int places;        // workgroups that are resident at once
@@ -71,6 +72,8 @@ struct PlanShape {
     int causal;
 };
 MUKV_HD int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// (Numbers here stay so far below 2^31 that 32 bits hold the sums; a division of 64 bits is a quarter of a microsecond of instructions.)
+MUKV_HD int div_up32(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
 struct SeqShape {
     int first, n_new, length, rows; // its first new token, how many, its length as its tokens count it, rows that exist
@@ -81,35 +84,34 @@ MUKV_HD SeqShape shape_of(const PagedView &v, const PlanShape &p, int b) {
     tokens_of(v, b, &s.first, &s.n_new);
     s.length = length_of(v, b, s.n_new);
     s.rows = rows_of(v, s.first, s.length);
-    s.tiles = (int)div_up((int64_t)s.n_new * v.G, p.queries);
-    s.blocks = s.rows > 0 ? (int)div_up(s.rows, p.rows) : 1; // (without rows a tile still has zeros to write)
+    s.tiles = (s.n_new * v.G + p.queries - 1) >> p.log_queries;
+    s.blocks = s.rows > 0 ? (int)(((unsigned)s.rows + p.rows - 1) >> p.log_rows) : 1; // (without rows a tile still has zeros to write)
     return s;
 }
 
 // Of all sequences: tiles (times KV heads), their blocks, those of them that are seen, and the most that a tile has.
-struct PlanSums {
-    double tiles, blocks, seen, longest;
+struct PlanSums { // (32 bits: 10^-5 of a sum may be missing, which the room for records allows for)
+    float tiles, blocks, seen, longest;
 };
 MUKV_HD PlanSums sums_of(const PagedView &v, const PlanShape &p, const SeqShape &s) {
     PlanSums x;
-    x.tiles = (double)s.tiles * v.Hkv;
-    x.blocks = x.tiles * s.blocks;
-    const double late = p.causal ? 0.5 * s.n_new / p.rows : 0.0; // under the mask a tile misses half of the new rows in the mean
-    x.seen = x.tiles * (late < s.blocks - 1 ? s.blocks - late : 1.0);
-    x.longest = s.tiles > 0 ? s.blocks : 0.0;
+    x.tiles = (float)s.tiles * (float)v.Hkv;
+    x.blocks = x.tiles * (float)s.blocks;
+    const float late = p.causal ? 0.5f * (float)s.n_new / (float)p.rows : 0.f; // under the mask a tile misses half of the new rows in the mean
+    x.seen = x.tiles * (late < (float)s.blocks - 1.f ? (float)s.blocks - late : 1.f);
+    x.longest = s.tiles > 0 ? (float)s.blocks : 0.f;
     return x;
 }
 // What the call takes, in blocks, if the longest tile's rows are `chunks` chunks (1e30: there is no room for them).  Units of about
 // the same size run `places` at a time.
 MUKV_HD float cost_of(const PlanShape &p, const PlanSums &x, bool one_sequence, int chunks) {
-    const float per = ceilf((float)x.longest / (float)chunks);
-    const float tiles = (float)x.tiles, seen = (float)x.seen;
-    float units = tiles;
+    const float per = ceilf(x.longest / (float)chunks);
+    float units = x.tiles;
     if (chunks > 1) {
-        units = one_sequence ? tiles * (float)chunks : (float)x.blocks / per + tiles;
-        if (units > (float)p.records || (float)chunks > (float)x.longest) return 1e30f;
+        units = one_sequence ? x.tiles * (float)chunks : x.blocks / per + x.tiles;
+        if (units * 1.001f > (float)p.records || (float)chunks > x.longest) return 1e30f;
     }
-    const float rounds = ceilf(units / (float)p.places) * (seen / units + (float)p.start), last = per + (float)p.start;
+    const float rounds = ceilf(units / (float)p.places) * (x.seen / units + (float)p.start), last = per + (float)p.start;
     return (rounds > last ? rounds : last) + (chunks > 1 ? p.join * (float)chunks + p.record * units : 0.f);
 }
 constexpr int kWhole = 0x40000000; // blocks of a chunk: more than any tile has
@@ -119,26 +121,27 @@ constexpr int kWhole = 0x40000000; // blocks of a chunk: more than any tile has
 // 2000, 64/8 heads, whole 93, 8 blocks 104; 64 users of 200 to 12000, 30 blocks 199, 15 188, 8 187.)
 // Room: the sum of ceil(blocks / per) over tiles with two chunks or more is at most twice that of blocks / per.
 MUKV_HD int chunk_by_room(const PlanShape &p, const PlanSums &x) {
-    const double least = ceil(x.blocks / (p.records / 2));
-    double per;
-    if (x.tiles < 256.0) {
-        per = ceil(x.blocks / 256.0);
-        per = per < 8.0 ? per : 8.0;
+    const float least = ceilf(x.blocks * (2.002f / (float)p.records));
+    float per;
+    if (x.tiles < 256.f) {
+        per = ceilf(x.blocks * (1.f / 256.f));
+        per = per < 8.f ? per : 8.f;
     } else {
-        if (x.longest * x.tiles <= 1.5 * x.blocks) return kWhole;
-        per = ceil(0.5 * x.blocks / x.tiles);
-        per = per > 8.0 ? per : 8.0;
+        if (x.longest * x.tiles <= 1.5f * x.blocks) return kWhole;
+        per = ceilf(0.5f * x.blocks / x.tiles);
+        per = per > 8.f ? per : 8.f;
     }
     per = per > least ? per : least;
-    return per < 1.0 ? 1 : per > kWhole ? kWhole : (int)per;
+    return per < 1.f ? 1 : per > (float)kWhole ? kWhole : (int)per;
 }
 MUKV_HD int chunk_of(const PlanShape &p, const SeqShape &s, int per) { // of one sequence: as many chunks, all about the same
-    const int least = (int)div_up(s.blocks, p.most);
-    return (int)div_up(s.blocks, div_up(s.blocks, per > least ? per : least));
+    if (per >= s.blocks) return s.blocks;
+    const int least = div_up32(s.blocks, p.most);
+    return div_up32(s.blocks, div_up32(s.blocks, per > least ? per : least));
 }
 MUKV_HD int chunks_of(const PlanShape &p, const SeqShape &s, int per) {
-    if (per >= kWhole) return 1;
-    return (int)div_up(s.blocks, chunk_of(p, s, per));
+    if (per >= s.blocks) return 1;
+    return div_up32(s.blocks, chunk_of(p, s, per));
 }
 // Workgroups that cover every unit.
 MUKV_HD int64_t units_bound(const PagedView &v, const PlanShape &p) {

@@ -71,8 +71,9 @@ def test_attention_over_pages(D, hq, hkv, R, dtype, seqs):
 @pytest.mark.parametrize("D,hq,hkv,R", [(128, 28, 4, 16), (64, 14, 2, 7), (128, 4, 4, 64), (64, 8, 1, 1), (128, 12, 1, 24)])
 @pytest.mark.parametrize("seqs", [[(300, 300)], [(37, 1000), (256, 257), (0, 10), (60, 31), (129, 129)], [(100, 6001)], [(70, 64), (64, 2000), (500, 500)]],
                          ids=["whole", "mixed", "past", "edges"])
-def test_prompts(D, hq, hkv, R, seqs):
-    c = Case(seqs, D, hq, hkv, R, BF16, seed=D + R + len(seqs))
+@pytest.mark.parametrize("room", [0, 9000])   # how many rows the table has room for decides between tiles of 128 and 256 queries
+def test_prompts(D, hq, hkv, R, seqs, room):
+    c = Case(seqs, D, hq, hkv, R, BF16, seed=D + R + len(seqs), width=-(-room // R) if room else None)
     first = c.attend()
     c.check(first)
     assert torch.equal(c.attend(), first)
@@ -104,7 +105,7 @@ def test_prompts_with_scores_of_any_size():
 @pytest.mark.parametrize("low,high,at", [(0.02, 60.0, 150), (60.0, 0.02, 150), (1.0, 400.0, 299), (1e-3, 1e4, 40)])
 def test_scores_that_grow_or_fall_by_much_along_the_rows(low, high, at, D, dtype):
     """Rows from `at` on have keys of another size: what exponents subtract at first is far from the largest score of all."""
-    c = Case([(200, 300), (40, 200)], D, 8, 2, 16, dtype, seed=D + at)
+    c = Case([(200, 300), (40, 200)], D, 8, 2, 16, dtype, seed=D + at, width=300 if at == 150 else None)
     for b in range(2):
         for j in range(int(c.lengths[b])):
             c.kp[:, c.table[b][j // 16], :, j % 16] *= low if j < at else high
@@ -120,7 +121,7 @@ def test_scores_that_grow_or_fall_by_much_along_the_rows(low, high, at, D, dtype
 
 @pytest.mark.parametrize("causal", [True, False])
 def test_prompts_whose_first_page_is_none(causal):
-    c = Case([(150, 400), (150, 150)], 128, 8, 2, 64, BF16, seed=18)
+    c = Case([(150, 400), (150, 150)], 128, 8, 2, 64, BF16, seed=18, width=100)
     c.table[:, 0] = -1
     c.kp[:] *= 40.0     # scores of a few hundred, either sign: the rows that are there decide what exponents subtract
     want, _, amean, reach = c.wanted(causal)
@@ -196,11 +197,12 @@ def test_lengths_that_make_no_sense_are_brought_in_range(dtype):
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("D,news,rows", [(64, 6, 50), (128, 16, 40), (16, 3, 3), (64, 200, 230), (128, 130, 140), (128, 33, 33)])
-def test_hidden_rows_never_reach_a_token(D, news, rows, dtype, bad):
+@pytest.mark.parametrize("D,news,rows,room", [(64, 6, 50, 0), (128, 16, 40, 0), (16, 3, 3, 0), (64, 200, 230, 0), (128, 130, 140, 0), (128, 33, 33, 0),
+                                              (64, 400, 401, 5000), (128, 230, 260, 5000)])
+def test_hidden_rows_never_reach_a_token(D, news, rows, room, dtype, bad):
     """The last row's key and value are no numbers: only the last token sees it.  So is what lies past the last row, and on the first
     page of the layer, where rows that live nowhere are read."""
-    c = Case([(news, rows), (news, rows)], D, 4, 2, 16, dtype, seed=D + news)
+    c = Case([(news, rows), (news, rows)], D, 4, 2, 16, dtype, seed=D + news, width=-(-room // 16) if room else None)
     c.lengths[1] = rows - 1
     c.table[1, 0] = -1
     clean = c.attend()

@@ -25,6 +25,8 @@ int main() {
         const int kinds[3][7] = {{16, 128, 2048, 64, 512, 0, 0}, {16, 64, 2048, 64, 512, 0, 0}, {in(0, 1) ? 256 : 128, 64, 704, 64, 256, 3, 1}};
         const int *k = kinds[in(0, 2)];
         p.queries = k[0]; p.rows = k[1]; p.records = k[2]; p.most = k[3]; p.places = k[4]; p.start = k[5]; p.join = 0.8f * k[6]; p.record = 0.06f * k[6]; p.causal = in(0, 1);
+        for (p.log_queries = 0; 1 << p.log_queries < p.queries;) ++p.log_queries;
+        for (p.log_rows = 0; 1 << p.log_rows < p.rows;) ++p.log_rows;
         v.n_seqs = in(1, in(0, 3) ? 5 : 150);
         v.page_rows = in(1, 70); v.table_width = in(1, in(0, 4) ? 40 : 3000); v.n_pages = in(1, 500);
         v.G = in(1, 9); v.Hkv = in(1, 8); v.Hq = v.G * v.Hkv;
@@ -54,7 +56,7 @@ int main() {
             int best = 1;
             for (int c = 2; c <= p.most; ++c)
                 if (cost_of(p, all, v.n_seqs == 1, c) < cost_of(p, all, v.n_seqs == 1, best)) best = c;
-            per = best == 1 ? kWhole : (int)((all.longest + best - 1) / best);
+            per = best == 1 ? kWhole : div_up32((int)all.longest, best);
         }
         int64_t units = 0, records = 0, tokens = 0;
         for (int b = 0; b < v.n_seqs; ++b) {
@@ -71,7 +73,7 @@ int main() {
                     CHECK(offset_of(v, v.n_pages - 1, j) == (int64_t)(v.n_pages - 1) * (1 << 20) + 16 * (j % v.page_rows));
                 }
             CHECK((int64_t)s.tiles * p.queries >= (int64_t)s.n_new * v.G && (int64_t)(s.tiles - 1) * p.queries < (int64_t)s.n_new * v.G);
-            const int n = chunks_of(p, s, per), c = per >= kWhole ? s.blocks : chunk_of(p, s, per);
+            const int n = chunks_of(p, s, per), c = chunk_of(p, s, per);
             CHECK(c >= 1 && n >= 1 && n <= p.most && (int64_t)n * c >= s.blocks && (int64_t)(n - 1) * c < s.blocks);
             units += (int64_t)s.tiles * v.Hkv * n;
             if (n > 1) records += (int64_t)s.tiles * v.Hkv * n;
