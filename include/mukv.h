@@ -673,15 +673,16 @@ typedef struct mukv_row_weights {
  *              that do not exist: 0).  Rows past a sequence's length are left as they are;
  *              stride_layer is not read (the arrays are this layer's).
  *   workspace  device scratch of at least mukv_paged_workspace_size() bytes, 16-byte
- *              aligned.  It must have been zero-filled once before its first use;
- *              every call leaves it fit for the next one, of any shape.  Calls that share a
- *              workspace must not overlap on the device.
+ *              aligned.  Its first MUKV_PAGED_CLEAR bytes must have been zero-filled once
+ *              before its first use; every call leaves it fit for the next one, of any shape.
+ *              Calls that share a workspace must not overlap on the device.
  *
  * Arithmetic in fp32, sums in an order that does not depend on timing; `out` is rounded to
  * the payload dtype.
  * n_tokens = 0 does nothing, except that weights are brought from in to out.
  * Errors: INVALID_ARG, SHAPE, CAPACITY (workspace too small), UNSUPPORTED.
  */
+enum { MUKV_PAGED_CLEAR = 8192 };
 int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, int32_t with_weights, int64_t *bytes_out);
 int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *q,
                       const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
@@ -711,6 +712,14 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
 int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,
                      int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
                      int32_t *kept_out, int32_t *lengths_out, void *stream);
+
+/*
+ * The graph capture that `stream` is in: a number that no other capture of the
+ * process has, 0 if there is none.  Scratch that a capture clears is fit for the
+ * calls of that capture alone: nothing has run when the capture ends.
+ * Errors: INVALID_ARG (id_out NULL), HIP.
+ */
+int mukv_stream_capture(void *stream, uint64_t *id_out);
 
 /* Fills *out (host).  Does not synchronise. */
 int mukv_get_state(const mukv_ctx *ctx, mukv_state *out);

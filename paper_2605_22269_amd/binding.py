@@ -98,7 +98,7 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_attend", "mukv_prefill_workspace_size", "mukv_prefill_attend", "mukv_prefill_attend_static",
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
            "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append",
-           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_strerror")
+           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_stream_capture", "mukv_strerror")
 
 _lib = None
 
@@ -146,6 +146,7 @@ def load():
     lib.mukv_paged_workspace_size.argtypes = [paged, seqs, i32, C.POINTER(C.c_int64)]
     lib.mukv_paged_attend.argtypes = [paged, i32, seqs, vp, strides, i32, vp, vp, vp, C.c_int64, vp]
     lib.mukv_paged_evict.argtypes = [paged, seqs, vp, i32, i32, i32, vp, i32, vp, vp, vp]
+    lib.mukv_stream_capture.argtypes = [vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
     for name in EXPORTS[:-1]:
@@ -326,6 +327,10 @@ def mukv_paged_workspace_size(pages, seqs, with_weights):
     n = C.c_int64(0)
     _check((_lib or load()).mukv_paged_workspace_size(pages, seqs, with_weights, C.byref(n)), "mukv_paged_workspace_size")
     return n.value
+
+
+def mukv_stream_capture(stream, id_out_ptr):
+    _check((_lib or load()).mukv_stream_capture(stream, id_out_ptr), "mukv_stream_capture")
 
 
 def mukv_paged_attend(pages, layer, seqs, q_ptr, q_strides, causal, out_ptr, weights, ws_ptr, ws_bytes, stream):
@@ -686,6 +691,7 @@ _STRIDES = {}   # address of the C form of the strides met so far
 _STRIDES_KEPT = []
 _SEQS = struct.Struct("@QQQiiii")   # mukv_seqs
 _I32 = torch.int32
+MUKV_PAGED_CLEAR = 8192
 
 
 def _rows(t):
@@ -741,13 +747,16 @@ class Rope:
 
 class _Sequences:
     """What the caches share: the C structures, and scratch of the attention calls, a piece for every stream that calls (calls on
-    different streams may overlap)."""
+    different streams may overlap).  A graph that is being captured has a piece of its own, in the graph's memory, and clears what has
+    to be clear itself: its replays may come before, after or beside anything else."""
 
     def __init__(self):
         self._pages, self._seqs = mukv_paged(), mukv_seqs()
         self._pages_at, self._seqs_at = C.addressof(self._pages), C.addressof(self._seqs)
         self._seqs_memory = memoryview(self._seqs).cast("B")
         self._scratch, self._need = {}, (None, 0)
+        self._capture = C.c_uint64(0)
+        self._capture_at = C.addressof(self._capture)
 
     def _attend(self, s, key, layer, q, causal, out, weights, weights_out, decay):
         if out is None:
@@ -768,10 +777,14 @@ class _Sequences:
         if self._need[0] != key:
             self._need = key, mukv_paged_workspace_size(self._pages_at, s, int(w is not None))
         need = self._need[1]
-        ws = self._scratch.get(stream)
-        if ws is None or ws[1] < need or ws[3] != self._index:   # (zeros, as every call finds and leaves the part that counts)
-            t = torch.zeros(need, dtype=torch.uint8, device=q.device)
-            ws = self._scratch[stream] = t.data_ptr(), need, t, self._index
+        mukv_stream_capture(stream, self._capture_at)
+        capture = self._capture.value   # (0: none)
+        place = stream, capture != 0
+        ws = self._scratch.get(place)
+        if ws is None or ws[1] < need or ws[3] != (self._index, capture):
+            t = torch.empty(need, dtype=torch.uint8, device=q.device)
+            t[:MUKV_PAGED_CLEAR].zero_()   # every call finds and leaves it so
+            ws = self._scratch[place] = t.data_ptr(), need, t, (self._index, capture)
         mukv_paged_attend(self._pages_at, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
                           None if w is None else C.addressof(w), ws[0], ws[1], stream)
         return out

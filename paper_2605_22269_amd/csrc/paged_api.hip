@@ -207,6 +207,16 @@ int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     return finished(mukv::launch_rope(a, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
 }
 
+int mukv_stream_capture(void *stream, uint64_t *id_out) {
+    if (!id_out) return MUKV_ERR_INVALID_ARG;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    const hipError_t e = hipStreamGetCaptureInfo(reinterpret_cast<hipStream_t>(stream), &status, &id);
+    *id_out = e == hipSuccess && status == hipStreamCaptureStatusActive ? id : 0;
+    return finished(e);
+}
+
+static_assert(MUKV_PAGED_CLEAR == 4 * mukv::kPlanRecords, "the counts");
 int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, int32_t with_weights, int64_t *bytes_out) {
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_pages(pages)) return rc;

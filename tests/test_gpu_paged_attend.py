@@ -365,3 +365,32 @@ def test_on_another_stream_and_in_a_graph():
         c.q.mul_(1.0 + 0.5 * (k % 2))
         want = c.attend()
         torch.cuda.synchronize()
+
+
+def test_graphs_whose_replays_come_in_any_order():
+    """Two graphs captured on one stream, nothing run on it before: the second's first replay comes before any of the first's, and
+    eager calls on that stream, larger than both, in between."""
+    c = Case([(1, 400), (2, 4000)], 128, 8, 2, 16, BF16, seed=12)
+    want = c.attend()
+    args = [torch.tensor(x, device="cuda") for x in (c.table, c.lengths, c.off)]
+    torch.cuda.synchronize()
+    side, graphs, outs = torch.cuda.Stream(), [], []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        outs.append(torch.zeros_like(want))
+        with torch.cuda.graph(graphs[-1], stream=side):
+            for _ in range(2):
+                c.cache.attend(1, args[0], args[1], c.q, offsets=args[2], out=outs[-1])
+    for k in (1, 0, 1, 1, 0):
+        outs[k].zero_()
+        torch.cuda.synchronize()
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[k], want)
+        got = torch.zeros_like(want)
+        w = torch.zeros(2, 2, 4000, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            c.cache.attend(1, args[0], args[1], c.q, offsets=args[2], out=got, weights_out=w)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)

@@ -161,3 +161,7 @@ def test_evict_refuses_weights(kw, status):
     ({"lengths": None}, BAD), ({"w": 0}, BAD), ({"budget": (1 << 30) + 1}, UNSUP)])
 def test_evict_refuses(kw, status):
     assert evict(**kw) == status
+
+
+def test_stream_capture_refuses_no_place():
+    assert mk.load().mukv_stream_capture(None, None) == BAD
