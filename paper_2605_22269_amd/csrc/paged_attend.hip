@@ -17,14 +17,43 @@ namespace {
 
 constexpr int kPQ = 16, kPWaves = 4; // queries and waves of a workgroup
 
+// Scores of 16 fp32 rows, k, and 16 queries, q(piece): sums of four terms each, joined pair by pair, which is nearer to 64 bits than
+// one sum of D terms.  Two pieces at a time: the compiler starts all 4 KK products at once otherwise, in as many registers, and puts
+// requested rows aside as they come (22 prompts of 700 to 1500 tokens, 16/4 heads of 128: 6140 us so, 1776 in pairs, 60 TFLOP/s).
+template <int KK, typename Q>
+__device__ __forceinline__ f32x4 scores_f32(const raw16 (&k)[KK], Q q) {
+    f32x4 part[4]; // of 1, 2, 4 and 8 pieces
+    f32x4 x;
+#pragma unroll
+    for (int k0 = 0; k0 < KK; k0 += 2) {
+        raw16 y[2] = {k[k0], k[k0 + 1 < KK ? k0 + 1 : k0]};
+        if (k0 > 0) asm volatile("" : "+v"(x), "+v"(y[0]), "+v"(y[1]));
+#pragma unroll
+        for (int kk = k0; kk < k0 + 2 && kk < KK; ++kk) {
+            f32x4 c[4];
+            const raw16 z = q(kk);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(y[kk - k0][e]), __uint_as_float(z[e]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            x = (c[0] + c[1]) + (c[2] + c[3]);
+            int level = 0;
+#pragma unroll
+            for (int n = kk; n & 1; n >>= 1) x = part[level++] + x;
+            part[level] = x;
+        }
+    }
+    return x;
+}
+
 // The rows of a tile, in blocks of 32 (bf16) or 16 (fp32), dealt to the waves in turn; nothing crosses the waves until the end.
 //   rows     a lane works out where one row lives, from a table entry that was requested a block earlier; the others fetch that by
 //            lane permutes.  Keys and values go straight to registers, the next block's requested as soon as this one's are used up.
 //   scores   S^T = K Q^T (16x16x32 bf16, 16x16x4 fp32): a lane holds ONE query (lane % 16) and the rows 4 (lane / 16) + r of every 16.
 //   values   O^T += V^T P^T: the weights are the B operand as they stand in the lane.  bf16: pairs hi + lo, nothing of the fp32
 //            weight is lost; the value rows pass through LDS the wave has to itself and the transpose read.  fp32: no transpose needed.
+// fp32 rows: three workgroups to a compute unit where the registers are there (1500 tokens, 16/4 heads of 64: 92 us, 103 with two).
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attend_kernel(PagedAttendArgs a) {
+__global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2, sizeof(T) == 4 && D <= 64 ? 3 : 2))) void paged_attend_kernel(PagedAttendArgs a) {
     constexpr int W = kPWaves;
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
@@ -77,7 +106,9 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int kBlocks = 4; // to one of the plan's
     const int n_blk = (n_rows + kRows - 1) / kRows;
     const int64_t lo = (int64_t)u.chunk * u.per * kBlocks, hi = lo + (int64_t)u.per * kBlocks;
-    const int b_lo = lo < n_blk ? (int)lo : n_blk, b_hi = hi < n_blk ? (int)hi : n_blk;
+    // (the same in all lanes: scalar registers, and branches that are)
+    const int b_lo = __builtin_amdgcn_readfirstlane(lo < n_blk ? (int)lo : n_blk);
+    const int b_hi = __builtin_amdgcn_readfirstlane(hi < n_blk ? (int)hi : n_blk);
     const unsigned char *const kb = v.k + g * v.stride_head, *const vb = v.v + g * v.stride_head;
 
     // Row lane % kRows of a block: the page it is on, requested early, where it lives, and the first token that sees it (INT_MAX: it
@@ -140,23 +171,8 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
                                                                     __builtin_bit_cast(bf16x8, qb[kk]), sc[t], 0, 0, 0);
                 }
             }
-        } else { // sums of four terms each, joined pair by pair: nearer to 64 bits than one sum of D terms
-            f32x4 part[KK];
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                f32x4 c[4];
-                const raw16 qk = kQueryLds ? s_q[kk][lane] : qb[kQueryLds ? 0 : kk];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[0][kk][e]), __uint_as_float(qk[e]),
-                                                                f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                part[kk] = (c[0] + c[1]) + (c[2] + c[3]);
-            }
-#pragma unroll
-            for (int n = KK; n > 1; n /= 2)
-#pragma unroll
-                for (int i = 0; i < n / 2; ++i) part[i] = part[2 * i] + part[2 * i + 1];
-            sc[0] = part[0];
+        } else {
+            sc[0] = scores_f32<KK>(kx[0], [&](int kk) { return kQueryLds ? s_q[kk][lane] : qb[kQueryLds ? 0 : kk]; });
         }
         int64_t off_next = 0;
         int ft_next = 0;
@@ -288,7 +304,11 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
                 for (int h = 0; h < kVH; ++h)
 #pragma unroll
-                    for (int e = 0; e < kVW; ++e) acc[kVW * h + e] += product(h, e, [](int) { return true; });
+                    for (int e = 0; e < kVW; ++e) {
+                        acc[kVW * h + e] += product(h, e, [](int) { return true; });
+                        if (e % 2) // (two at a time, for the registers' sake)
+                            asm volatile("" : "+v"(acc[kVW * h + e]), "+v"(p[0]), "+v"(p[1]), "+v"(p[2]), "+v"(p[3]));
+                    }
             } else {
 #pragma unroll 1
                 for (int tok = first_tok; tok <= last_tok; ++tok)
@@ -299,6 +319,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
                             const f32x4 d = product(h, e, [&](int i) { return tok >= first_to_see(i); });
 #pragma unroll
                             for (int r = 0; r < 4; ++r) acc[kVW * h + e][r] += tok == my_tok ? d[r] : 0.f;
+                            asm volatile("" : "+v"(acc[kVW * h + e]), "+v"(p[0]), "+v"(p[1]), "+v"(p[2]), "+v"(p[3]));
                         }
             }
             if constexpr (more.value) {
@@ -398,7 +419,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
 // stream past it, 16 at a time and requested one tile ahead, with what their weights subtract and the sum they are divided by: S^T
 // leaves a lane one query and four rows of every 16, so the sums over the queries run in the lane until the end, where 16 lanes join.
 template <typename T, int D, int kTiles>
-__global__ __launch_bounds__(256) void paged_weights_kernel(PagedAttendArgs a, int n_groups) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void paged_weights_kernel(PagedAttendArgs a, int n_groups) {
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
     constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16;
@@ -461,22 +482,8 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedAttendArgs a, i
 #pragma unroll
                     for (int kk = 0; kk < KK; ++kk)
                         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[t][kk]), __builtin_bit_cast(bf16x8, q[kk]), sc, 0, 0, 0);
-                } else { // (in the attention's own order: the same scores)
-                    f32x4 part[KK];
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        f32x4 c[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            c[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[t][kk][e]), __uint_as_float(q[kk][e]),
-                                                                        f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                        part[kk] = (c[0] + c[1]) + (c[2] + c[3]);
-                    }
-#pragma unroll
-                    for (int n = KK; n > 1; n /= 2)
-#pragma unroll
-                        for (int i = 0; i < n / 2; ++i) part[i] = part[2 * i] + part[2 * i + 1];
-                    sc = part[0];
+                } else {
+                    sc = scores_f32<KK>(kx[t], [&](int kk) { return q[kk]; });
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
