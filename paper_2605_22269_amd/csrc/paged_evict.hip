@@ -14,7 +14,8 @@ namespace {
 constexpr int kSelRows = 4;      // rows a thread takes at a time when the list is written
 constexpr int kSelCache = 32768; // keys that wait in LDS; those of further rows are worked out again on every pass
 constexpr int kSelCopies = 4;    // of the counts: lanes that count the same digit at once share an address less often
-constexpr int kSelCand = 512;    // rows that share the upper half of the key and are ranked by counting
+constexpr int kSelCand = 512;    // rows that share the upper half of the key and are ranked by counting, as one number each (56 lists
+                                 // of 1172 rows, 350 of them equal: 15 us, with key and row compared apart 46)
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
     if (w != w) return 1u;
@@ -27,11 +28,11 @@ template <int kSelThreads>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, int cache_keys) {
     constexpr int kSelWaves = kSelThreads / 64;
     extern __shared__ __align__(16) uint32_t s_key[]; // [cache_keys]
-    __shared__ int s_hist[kSelCopies][256];
+    __shared__ __align__(16) int s_hist[kSelCopies][256];
     __shared__ int s_found[3]; // the digit, how many keys are above it, how many share it
     __shared__ int s_sum[2][kSelWaves];
-    __shared__ uint32_t s_cand_key[kSelCand];
-    __shared__ int s_cand_row[kSelCand], s_n_cand, s_last_row;
+    __shared__ __align__(16) uint64_t s_cand[kSelCand]; // key, then ~row: larger ones come first
+    __shared__ int s_n_cand, s_last_row;
     const PagedView &v = a.view;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int g = blockIdx.x % v.Hkv, b = blockIdx.x / v.Hkv % v.n_seqs, layer = blockIdx.x / v.Hkv / v.n_seqs;
@@ -86,15 +87,10 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
             if (m == 0) break; // (the same in all threads)
         }
         if (wave == 0) { // lane: digits 255 - 4 lane .. 252 - 4 lane, the largest first
-            int h[4], sum = 0;
+            i32x4 all = {0, 0, 0, 0};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = 255 - 4 * lane - e;
-                h[e] = 0;
-#pragma unroll
-                for (int c = 0; c < kSelCopies; ++c) h[e] += s_hist[c][d];
-                sum += h[e];
-            }
+            for (int c = 0; c < kSelCopies; ++c) all += *reinterpret_cast<const i32x4 *>(&s_hist[c][252 - 4 * lane]);
+            const int h[4] = {all[3], all[2], all[1], all[0]}, sum = (h[0] + h[1]) + (h[2] + h[3]);
             const int upto = wave_prefix(sum);
             int before = upto - sum;
             if (before < need && need <= upto) {
@@ -123,20 +119,21 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
             for (int j = tid; j < n; j += kSelThreads) {
                 const uint32_t k = get(j);
                 if (k >> 16 != prefix) continue;
-                const int at = atomicAdd(&s_n_cand, 1);
-                s_cand_key[at] = k;
-                s_cand_row[at] = j;
+                s_cand[atomicAdd(&s_n_cand, 1)] = (uint64_t)k << 32 | ~(uint32_t)j;
             }
+            constexpr int kTogether = 8;
+            const int n_cand = s_found[2], n_read = (n_cand + kTogether - 1) & ~(kTogether - 1);
+            if (n_cand + tid < n_read) s_cand[n_cand + tid] = 0; // before nobody
             __syncthreads();
-            const int n_cand = s_n_cand;
             if (tid < n_cand) {
-                const uint32_t k = s_cand_key[tid];
-                const int j = s_cand_row[tid];
+                const uint64_t mine = s_cand[tid];
                 int ahead = 0;
-                for (int i = 0; i < n_cand; ++i) ahead += s_cand_key[i] > k || (s_cand_key[i] == k && s_cand_row[i] < j);
+                for (int i = 0; i < n_read; i += kTogether)
+#pragma unroll
+                    for (int e = 0; e < kTogether; ++e) ahead += s_cand[i + e] > mine;
                 if (ahead == need - 1) {
-                    s_found[0] = (int)k;
-                    s_last_row = j;
+                    s_last_row = (int)~(uint32_t)mine;
+                    s_found[0] = (int)(uint32_t)(mine >> 32);
                 }
             }
             __syncthreads();
@@ -199,17 +196,25 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a, 
     for (int i = m + tid; i < n_w; i += kSelThreads) w_out[i] = 0.f;
 }
 
-constexpr int kMoveRows = 64, kMoveThreads = 256;
+constexpr int kMoveThreads = 256, kMoveRows = kMoveThreads; // most rows of a workgroup
 
-// What stays of sequence b, the same in all its lists: the entries of one of them before the padding.
+// What stays of sequence b, the same in all its lists: the entries of one of them before the padding.  (12 lists of 31921 rows: read from
+// end to end the kernel took 62 us for it, 16 so.)
 __device__ __forceinline__ void write_length(const EvictArgs &a, const int32_t *kept, int b) {
-    for (int i = threadIdx.x; i < a.budget; i += kMoveThreads)
-        if (kept[i] >= 0 && (i + 1 == a.budget || kept[i + 1] < 0)) a.lengths_out[b] = i + 1;
-    if (threadIdx.x == 0 && kept[0] < 0) a.lengths_out[b] = 0;
+    int lo = 0, len = a.budget; // the first entry of the padding is in lo .. lo + len; every round leaves 1 / kMoveThreads of that
+    while (len > 0) {
+        const int step = (len + kMoveThreads - 1) / kMoveThreads, i = (int)threadIdx.x * step;
+        const int n = __syncthreads_count(i < len && kept[lo + i] >= 0);
+        if (n == 0) break;
+        const int at = (n - 1) * step + 1; // past the last one that is not padding
+        lo += at;
+        len = len - at < step - 1 ? len - at : step - 1;
+    }
+    if (threadIdx.x == 0) a.lengths_out[b] = lo;
 }
 
-// Onto other pages: every row on its own.  Grid (layer x sequence x KV head, 64 rows).
-__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, int row_bytes) {
+// Onto other pages: every row on its own.  Grid (layer x sequence x KV head, n_rows rows).
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, int row_bytes, int n_rows) {
     __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows]; // byte offsets in the layer's pages, -1: nothing to move
     const PagedView &v = a.view;
     const int tid = threadIdx.x, list = blockIdx.x;
@@ -218,8 +223,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
     if (blockIdx.y == 0 && layer == 0 && g == 0) write_length(a, kept, b);
     const int pieces = row_bytes / 16, rows_at_once = kMoveThreads / pieces, piece = tid % pieces, r0 = tid / pieces;
     unsigned char *const bases[2] = {v.k + layer * a.stride_layer + g * v.stride_head + 16 * piece, v.v + layer * a.stride_layer + g * v.stride_head + 16 * piece};
-    for (int64_t i0 = (int64_t)blockIdx.y * kMoveRows; i0 < a.budget; i0 += (int64_t)gridDim.y * kMoveRows) {
-        if (tid < kMoveRows) {
+    for (int64_t i0 = (int64_t)blockIdx.y * n_rows; i0 < a.budget; i0 += (int64_t)gridDim.y * n_rows) {
+        if (tid < n_rows) {
             const int i = (int)i0 + tid, row = i < a.budget ? kept[i] : -1;
             int64_t from = -1, to = -1;
             if (row >= 0 && i / v.page_rows < a.into_width) {
@@ -234,19 +239,19 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
         }
         __syncthreads();
         constexpr int kAhead = 4;
-        for (int r = r0; r < kMoveRows; r += kAhead * rows_at_once) {
+        for (int r = r0; r < n_rows; r += kAhead * rows_at_once) {
             raw16 x[kAhead][2];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int rr = r + u * rows_at_once;
-                if (rr >= kMoveRows || s_from[rr] < 0) continue;
+                if (rr >= n_rows || s_from[rr] < 0) continue;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) x[u][t] = *reinterpret_cast<const raw16 *>(bases[t] + s_from[rr]);
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int rr = r + u * rows_at_once;
-                if (rr >= kMoveRows || s_from[rr] < 0) continue;
+                if (rr >= n_rows || s_from[rr] < 0) continue;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) __builtin_nontemporal_store(x[u][t], reinterpret_cast<raw16 *>(bases[t] + s_to[rr]));
             }
@@ -323,9 +328,11 @@ hipError_t launch_paged_evict(const EvictArgs &a, int n_layers, int row_bytes, i
     // to 6000 rows 45 / 28.)
     hipError_t e = lists <= 256 ? launch_select<1024>(a, lists, keys, device, st) : launch_select<512>(a, lists, keys, device, st);
     if (e != hipSuccess) return e;
-    const int chunks = (a.budget + kMoveRows - 1) / kMoveRows;
     if (a.into) {
-        hipLaunchKernelGGL(evict_move_kernel, dim3(lists, chunks < 65535 ? chunks : 65535), dim3(kMoveThreads), 0, st, a, row_bytes);
+        // (a workgroup's threads ask for four pieces each, together)
+        const int rows = 1024 / (row_bytes / 16) < 64 ? 64 : 1024 / (row_bytes / 16) > kMoveRows ? kMoveRows : 1024 / (row_bytes / 16);
+        const int chunks = (a.budget + rows - 1) / rows;
+        hipLaunchKernelGGL(evict_move_kernel, dim3(lists, chunks < 65535 ? chunks : 65535), dim3(kMoveThreads), 0, st, a, row_bytes, rows);
     } else {
         hipLaunchKernelGGL(evict_pack_kernel, dim3(lists, row_bytes < 64 ? 1 : row_bytes / 64, 2), dim3(kMoveThreads), 0, st, a, row_bytes);
     }
