@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2,
     // the workgroup's blocks of rows, dealt to its waves
     constexpr int kBlocks = 4; // to one of the plan's
     const int n_blk = (n_rows + kRows - 1) / kRows;
-    const int64_t lo = (int64_t)u.chunk * u.per * kBlocks, hi = lo + (int64_t)u.per * kBlocks;
+    const int64_t lo = (int64_t)u.lo * kBlocks, hi = (int64_t)u.hi * kBlocks;
     // (the same in all lanes: scalar registers, and branches that are)
     const int b_lo = __builtin_amdgcn_readfirstlane(lo < n_blk ? (int)lo : n_blk);
     const int b_hi = __builtin_amdgcn_readfirstlane(hi < n_blk ? (int)hi : n_blk);

@@ -8,16 +8,122 @@ namespace mukv {
 
 struct Unit {
     SeqShape s;
-    int b, g, tile, chunk, chunks, per; // per: blocks of a chunk
-    int record;                         // of the tile's first chunk
+    int b, g, tile, chunk, chunks;
+    int lo, hi; // blocks of its rows
+    int record; // of the tile's first chunk
 };
 
-// Blocks of a chunk: the number of chunks that costs least, a lane a number.
-__device__ __forceinline__ int chunk_by_cost(const PlanShape &p, const PlanSums &x, bool one_sequence) {
+// Blocks of a chunk: the number of chunks that costs least, a lane a number, and what it costs.
+__device__ __forceinline__ int chunk_by_cost(const PlanShape &p, const PlanSums &x, bool one_sequence, float *least = nullptr) {
     const int chunks = (threadIdx.x & 63) + 1;
-    const float cost = chunks <= p.most ? cost_of(p, x, one_sequence, chunks) : 1e30f;
-    const int best = 1 + (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == -wave_max(-cost)));
+    const float cost = chunks <= p.most ? cost_of(p, x, one_sequence, chunks) : 1e30f, low = -wave_max(-cost);
+    const int best = 1 + (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(cost == low));
+    if (least) *least = low;
     return best == 1 ? kWhole : div_up32((int)x.longest, best);
+}
+
+// Unit `id` of those of u->s.
+__device__ __forceinline__ void place_unit(const PagedView &v, int id, Unit *u) {
+    // KV heads next to each other: workgroups go to the eight XCDs in turn, so an XCD meets few heads' rows
+    u->g = id % v.Hkv;
+    id /= v.Hkv;
+    u->chunk = id % u->chunks;
+    u->lo = u->chunk * u->hi; // (chunks are of hi blocks, all but the last)
+    u->hi += u->lo;
+    const int rank = id / u->chunks;
+    u->record += (rank * v.Hkv + u->g) * u->chunks;
+    u->tile = u->s.tiles - 1 - rank; // under the mask the last ones have the most to do: they start first
+}
+// The same of the only sequence; false: there is none.
+__device__ __forceinline__ bool only_unit(const PagedView &v, const PlanShape &p, int id, int per, Unit *u) {
+    u->b = 0;
+    u->chunks = chunks_of(p, u->s, per);
+    u->hi = chunk_of(p, u->s, per);
+    u->record = 0;
+    if (id >= u->s.tiles * v.Hkv * u->chunks) return false;
+    place_unit(v, id, u);
+    return true;
+}
+
+// In scalar registers (the compiler does not see that all lanes have the same).
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ void make_scalar(SeqShape &s) {
+    s = SeqShape{same(s.first), same(s.n_new), same(s.length), same(s.rows), same(s.tiles), same(s.blocks)};
+}
+__device__ __forceinline__ void make_scalar(Unit &u) {
+    make_scalar(u.s);
+    u.b = same(u.b), u.g = same(u.g), u.tile = same(u.tile), u.chunk = same(u.chunk), u.chunks = same(u.chunks);
+    u.lo = same(u.lo), u.hi = same(u.hi), u.record = same(u.record);
+}
+
+// The stretch of this workgroup where one sequence's tiles are shared out evenly.
+struct Share {
+    SeqShape s;
+    uint32_t at, end, head, line, workers; // the next step and the last one's; steps of a KV head, of all
+};
+// false: chunks of equal size cost no more, and *u is one if *there.
+__device__ __forceinline__ bool find_share(const PagedView &v, const PlanShape &p, uint32_t id, uint32_t groups, Share *x, Unit *u, bool *there) {
+    const int lane = threadIdx.x & 63;
+    x->s = shape_of(v, p, 0);
+    make_scalar(x->s);
+    const uint32_t workers = (uint32_t)p.places < groups ? (uint32_t)p.places : groups;
+    const int64_t tiles = (int64_t)x->s.tiles * v.Hkv;
+    const PlanSums sums = sums_of(v, p, x->s);
+    float least;
+    const int per = chunk_by_cost(p, sums, true, &least);
+    bool even = tiles >= 1 && tiles + workers <= p.records && tiles * x->s.blocks <= kMostSteps;
+    even = even && cost_of_shares(p, sums.tiles, sums.seen, (float)workers) < least;
+    if (even) {
+        int head = 0;
+        for (int t0 = 0; t0 < x->s.tiles; t0 += 64) {
+            const int t = t0 + lane;
+            head += t < x->s.tiles ? steps_of_tile(v, p, x->s, t) : 0;
+        }
+        x->head = (uint32_t)same(wave_sum(head));
+        x->line = x->head * (uint32_t)v.Hkv;
+        x->workers = workers;
+        even = x->line >= workers; // (a worker without a step would be missed where chunks are counted)
+    }
+    if (!even) {
+        u->s = x->s;
+        *there = only_unit(v, p, (int)id, per, u);
+        return false;
+    }
+    // workgroups go to the eight XCDs in turn: neighbouring stretches, which read the same rows, to one of them
+    const uint32_t worker = workers % 8 ? id : id % 8 * (workers / 8) + id / 8;
+    x->at = id < workers ? stretch_of(worker, workers, x->line) : 0;
+    x->end = id < workers ? stretch_of(worker + 1, workers, x->line) : 0;
+    return true;
+}
+// The stretch's next unit.
+__device__ __forceinline__ void next_unit(const PagedView &v, const PlanShape &p, Share *x, Unit *u) {
+    const int lane = threadIdx.x & 63;
+    u->s = x->s;
+    u->b = 0;
+    u->g = (int)(x->at / x->head);
+    const int step = (int)(x->at - (uint32_t)u->g * x->head);
+    int before = 0;
+    for (int t0 = 0;; t0 += 64) { // the tile that the step is in (it is in one: step < head)
+        const int steps = t0 + lane < x->s.tiles ? steps_of_tile(v, p, x->s, t0 + lane) : 0;
+        const int upto = before + wave_prefix(steps);
+        const uint64_t here = __builtin_amdgcn_ballot_w64(step < upto);
+        if (here || t0 + 64 >= x->s.tiles) {
+            const int at = here ? __builtin_ctzll(here) : 0;
+            const int n = __builtin_amdgcn_readlane(steps, at), first = __builtin_amdgcn_readlane(upto, at) - n;
+            u->tile = t0 + at;
+            u->lo = step - first;
+            const uint32_t left = x->end - x->at;
+            u->hi = (uint32_t)(n - u->lo) < left ? n : u->lo + (int)left;
+            const uint32_t start = (uint32_t)u->g * x->head + (uint32_t)first, me = worker_at(x->at, x->workers, x->line);
+            const uint32_t first_worker = worker_at(start, x->workers, x->line);
+            u->chunks = (int)(worker_at(start + (uint32_t)n - 1, x->workers, x->line) - first_worker) + 1;
+            u->chunk = (int)(me - first_worker);
+            u->record = record_of(first_worker, u->g * x->s.tiles + u->tile);
+            x->at += (uint32_t)(u->hi - u->lo);
+            return;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
 }
 
 // The unit of this workgroup, the same in all lanes; false: there is none.
@@ -25,13 +131,8 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
     const int lane = threadIdx.x & 63;
     if (v.n_seqs == 1) {
         u->s = shape_of(v, p, 0);
-        u->b = 0;
         const PlanSums x = sums_of(v, p, u->s);
-        const int per = p.start ? chunk_by_cost(p, x, true) : chunk_by_room(p, x);
-        u->chunks = chunks_of(p, u->s, per);
-        u->per = chunk_of(p, u->s, per);
-        u->record = 0;
-        if (id >= u->s.tiles * v.Hkv * u->chunks) return false;
+        return only_unit(v, p, id, p.start ? chunk_by_cost(p, x, true) : chunk_by_room(p, x), u);
     } else {
         const SeqShape none = {0, 0, 0, 0, 0, 1};
         SeqShape s = none;
@@ -66,7 +167,7 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
                 auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
                 u->s = SeqShape{of(s.first), of(s.n_new), of(s.length), of(s.rows), of(s.tiles), of(s.blocks)};
                 u->b = b0 + at;
-                u->per = chunk_of(p, u->s, per);
+                u->hi = chunk_of(p, u->s, per);
                 u->chunks = of(chunks);
                 u->record = of(records1 - records);
                 id -= of(units1 - units);
@@ -76,13 +177,7 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
             records0 = __builtin_amdgcn_readlane(records1, 63);
         }
     }
-    // KV heads next to each other: workgroups go to the eight XCDs in turn, so an XCD meets few heads' rows
-    u->g = id % v.Hkv;
-    id /= v.Hkv;
-    u->chunk = id % u->chunks;
-    const int rank = id / u->chunks;
-    u->record += (rank * v.Hkv + u->g) * u->chunks;
-    u->tile = u->s.tiles - 1 - rank; // under the mask the last ones have the most to do: they start first
+    place_unit(v, id, u);
     return true;
 }
 

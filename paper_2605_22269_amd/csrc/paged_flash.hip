@@ -18,9 +18,9 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), bf16x2{(__bf16)1.f, (__bf16)1.f}, x, false);
 }
 
-// One workgroup of four waves per unit; a wave owns 64 queries from the scores to the output.
+// One unit by a workgroup of four waves; a wave owns 64 queries from the scores to the output.
 template <int D, int kQB, bool PAIRS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_flash_kernel(PagedAttendArgs a) {
+__device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit &u) {
     using T = uint16_t;
     constexpr int kRowB = D * 2, kPieces = kRowB / 16, kRowsPerLoad = 64 / kPieces; // rows one load of a wave brings
     constexpr int kLoads = kFRows / 4 / kRowsPerLoad;                               // such loads per wave and step
@@ -35,11 +35,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     __shared__ unsigned s_inf[2][kFQ][D / 32]; // outputs that a value of +inf, of -inf reaches (both: NaN), where s_any says so
     __shared__ int s_last;
     const PagedView &v = a.view;
-    Unit u;
-    if (!find_unit(v, a.plan, blockIdx.x, &u)) return;
     if (threadIdx.x == 0) s_again = 0;
     const int g = u.g, b = u.b, G = v.G, n_new = u.s.n_new;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lq = lane & 31, half = lane >> 5;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid)); // (what follows from it is worked out for every unit, not kept in registers from one to the next)
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, lq = lane & 31, half = lane >> 5;
     const int n_queries = n_new * G;
     const int q0 = u.tile * kFQ + 32 * kQB * wave; // the wave's first
     const float scale = a.scale_log2e;
@@ -68,9 +68,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     // the unit's steps (a step is one of the plan's blocks)
     n_rows = __builtin_amdgcn_readfirstlane(n_rows); // (the same in all lanes: scalar registers, and branches that are)
     const int all_steps = (n_rows + kFRows - 1) / kFRows;
-    const int64_t lo = (int64_t)u.chunk * u.per, hi = lo + u.per;
-    const int t_lo = __builtin_amdgcn_readfirstlane(lo < all_steps ? (int)lo : all_steps);
-    const int n_steps = __builtin_amdgcn_readfirstlane((hi < all_steps ? (int)hi : all_steps) - t_lo);
+    const int t_lo = __builtin_amdgcn_readfirstlane(u.lo < all_steps ? u.lo : all_steps);
+    const int n_steps = __builtin_amdgcn_readfirstlane((u.hi < all_steps ? u.hi : all_steps) - t_lo);
     const int row0 = t_lo * kFRows;                                                     // the unit's first row
     const int n_halves = n_steps == 0 ? 0 : ((row0 + n_steps * kFRows < n_rows ? row0 + n_steps * kFRows : n_rows) - row0 + 31) / 32;
     const int all_halves = (n_halves + 1) & ~1;
@@ -568,15 +567,51 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     }
 }
 
+// A workgroup takes a unit; of one sequence's perhaps the units of its stretch, one after the other (us a launch, 28/4 heads of 128, chunks
+// alone / shares where they cost less: 1568 tokens over 6272 rows 239 / 177, 2000 over 10000 363 / 327; 1500 over 3000, 16/4 heads of 64, 63 / 55).
+template <int D, int kQB, bool PAIRS, bool SHARES>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_flash_kernel(PagedAttendArgs a) {
+    Unit u;
+    if constexpr (SHARES) {
+        Share share;
+        bool there = false;
+        const bool even = find_share(a.view, a.plan, blockIdx.x, gridDim.x, &share, &u, &there);
+        if (even ? share.at == share.end : !there) return;
+        for (;;) {
+            if (even) next_unit(a.view, a.plan, &share, &u);
+            make_scalar(u);
+            flash_unit<D, kQB, PAIRS>(a, u);
+            if (!even || share.at == share.end) return;
+            __syncthreads(); // the next unit takes this one's LDS
+        }
+    } else {
+        if (find_unit(a.view, a.plan, blockIdx.x, &u)) flash_unit<D, kQB, PAIRS>(a, u);
+    }
+}
+
 } // namespace
 
+// Whether one sequence's tiles may be shared out evenly: to look at that takes the kernel a microsecond, so not where it gains nothing:
+// few tiles, which come out even in chunks, more than twice the compute units, or few rows (us a launch without / with, 28/4 heads of 128:
+// 200 tokens over 20000 rows 89 / 93, 300 alone 14.5 / 15.5, 1000 30.1 / 30.9, 2000 55.4 / 57; the gains are at the kernel).
+static bool may_share(const PagedView &v, const PlanShape &p) {
+    const int64_t tiles = div_up((int64_t)v.n_tokens * v.G, p.queries) * v.Hkv, room = v.table ? room_of(v) : v.n_tokens;
+    return v.n_seqs == 1 && tiles > 64 && tiles <= p.records - p.places && room >= 4096;
+}
+template <int D, int kQB, bool PAIRS>
+static void start_flash(const PagedAttendArgs &a, unsigned grid, hipStream_t st) {
+    if (may_share(a.view, a.plan))
+        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, PAIRS, true>), dim3(grid), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, PAIRS, false>), dim3(grid), dim3(256), 0, st, a);
+}
 template <int D, int kQB>
 static hipError_t launch_flash(const PagedAttendArgs &a, hipStream_t st) {
     const unsigned grid = (unsigned)units_bound(a.view, a.plan);
     if (a.pairs)
-        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, true>), dim3(grid), dim3(256), 0, st, a);
+        start_flash<D, kQB, true>(a, grid, st);
     else
-        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, false>), dim3(grid), dim3(256), 0, st, a);
+        start_flash<D, kQB, false>(a, grid, st);
     return hipGetLastError();
 }
 

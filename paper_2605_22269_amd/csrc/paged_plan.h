@@ -143,6 +143,28 @@ MUKV_HD int chunks_of(const PlanShape &p, const SeqShape &s, int per) {
     if (per >= s.blocks) return 1;
     return div_up32(s.blocks, chunk_of(p, s, per));
 }
+// ---- even shares ----
+// One sequence whose tiles are about as many as there are compute units: chunks of a tile do not come out even (172 tiles in four chunks
+// each are three rounds of 256 with a third of the last one empty).  There all steps of all tiles (a step is one block of rows of a tile and
+// KV head, heads outermost) are one line, and `workers` workgroups take a stretch each, of one step more or less: the end of a
+// tile, whole ones, the beginning of another.  There are no more workers than steps; 32 bits hold a line of up to kMostSteps.
+constexpr uint32_t kMostSteps = 1u << 22;
+MUKV_HD int steps_of_tile(const PagedView &v, const PlanShape &p, const SeqShape &s, int tile) {
+    const int n_queries = s.n_new * v.G, end = (tile + 1) << p.log_queries, last_q = (end < n_queries ? end : n_queries) - 1;
+    int rows = s.rows;
+    if (p.causal) { // up to the last one that a query of the tile sees
+        const int seen = s.length - s.n_new + last_q / v.G + 1;
+        rows = seen < rows ? seen : rows;
+    }
+    return rows > 0 ? (int)(((unsigned)rows + p.rows - 1) >> p.log_rows) : 1;
+}
+MUKV_HD uint32_t stretch_of(uint32_t worker, uint32_t workers, uint32_t line) { return line * worker / workers; } // where its stretch begins
+MUKV_HD uint32_t worker_at(uint32_t step, uint32_t workers, uint32_t line) { return ((step + 1) * workers - 1) / line; }
+// The records of a tile start at this one: worker_at of its first step and its number (a tile's last worker is the next one's first at most).
+MUKV_HD int record_of(uint32_t first_worker, int tile) { return (int)first_worker + tile; }
+MUKV_HD float cost_of_shares(const PlanShape &p, float tiles, float line, float workers) {
+    return ceilf(line / workers) + (float)p.start * (1.f + tiles / workers) + p.join * (1.f + workers / tiles) + p.record * (workers + tiles);
+}
 // Workgroups that cover every unit.
 MUKV_HD int64_t units_bound(const PagedView &v, const PlanShape &p) {
     const int64_t with = v.n_seqs < v.n_tokens ? v.n_seqs : v.n_tokens;

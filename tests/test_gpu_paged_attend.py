@@ -394,3 +394,64 @@ def test_graphs_whose_replays_come_in_any_order():
             c.cache.attend(1, args[0], args[1], c.q, offsets=args[2], out=got, weights_out=w)
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def wanted_of_one(c, causal=True):
+    """Case.wanted of a single long sequence, in float64 on the device, a head at a time."""
+    n, new = int(c.lengths[0]), int(c.off[1])
+    at = torch.arange(n, device="cuda")
+    page = torch.tensor(c.table, device="cuda")[0].long()[at // c.R]
+    there = (page >= 0) & (page < c.kp.shape[1])
+    k, v = (x[c.layer][page.clamp(0, x.shape[1] - 1), :, at % c.R].double() for x in (c.kp, c.vp))
+    seen = there[None].expand(new, n)
+    if causal:
+        seen = seen & (at[None] <= n - new + torch.arange(new, device="cuda")[:, None])
+    outs, received = [], torch.zeros(c.hkv, n, dtype=torch.float64, device="cuda")
+    for h in range(c.hq):
+        g = h * c.hkv // c.hq
+        kk, vv, q = k[:, g].contiguous(), torch.where(there[:, None], v[:, g], 0.0).contiguous(), c.q[:, h].double()
+        w = torch.softmax((q @ kk.T / np.sqrt(c.D)).masked_fill(~seen, -np.inf), -1)
+        received[g] += w.sum(0)
+        reach = (q.abs() @ kk.abs().T).masked_fill(~seen, 0.0).amax(-1, keepdim=True)
+        outs.append([x.cpu().numpy() for x in (w @ vv, w @ vv.abs(), reach)])
+    out, amean, reach = (np.stack(x, 1) for x in zip(*outs))
+    return out, [received.cpu().numpy()], amean, reach
+
+
+def one_long(D, hq, hkv, new, past, seed):
+    c = Case([(new, new + past)], D, hq, hkv, 24, BF16, seed=seed)
+    c.wanted = lambda causal=True: wanted_of_one(c, causal)
+    return c
+
+
+@pytest.mark.parametrize("D,hq,hkv,new,past", [(128, 64, 8, 590, 4410), (128, 28, 4, 1568, 4000), (64, 28, 4, 1568, 6272), (128, 12, 12, 1500, 3001)])
+def test_one_long_prompt(D, hq, hkv, new, past):
+    """One sequence with somewhat fewer tiles than compute units, or somewhat more: its rows are shared out evenly, tile after tile."""
+    c = one_long(D, hq, hkv, new, past, new)
+    first = c.attend()
+    c.check(first)
+    assert torch.equal(c.attend(), first)
+    c.check(c.attend(causal=False), causal=False)
+    c.table[0, 5], c.table[0, 121] = -1, 2**31 - 1
+    rows = torch.zeros(1, hkv, new + past, device="cuda")
+    received = c.check(c.attend(weights_out=rows))
+    near(f64(rows)[0], received[0], (1 + received[0]) * weights_error(c, received), F32)
+
+
+def test_one_long_prompt_with_rows_that_decide_late():
+    c = one_long(128, 28, 4, 1568, 4000, 19)
+    n = 5568
+    for j in range(n):
+        c.kp[:, c.table[0][j // 24], :, j % 24] *= 0.02 if j < 4300 else 30.0
+    bad = slice(None), c.table[0][(n - 5) // 24], slice(None), (n - 5) % 24
+    c.vp[bad] = float("inf")   # seen by the last five tokens
+    c.q[:300] = 0.0
+    got = f64(c.attend())
+    assert np.isfinite(got[:-5]).all()
+    c.vp[bad] = 0.0
+    want, _, amean, reach = c.wanted()
+    err = attention_error(amean, reach, n, 128, BF16, True)
+    sure = (128 + 4) * 2.0**-24 * reach[..., 0] / np.sqrt(128) < 2.0**-4
+    sure[-5:] = False
+    assert sure.any()
+    near(got[sure], want[sure], err[sure], BF16)
