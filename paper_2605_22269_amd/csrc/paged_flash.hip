@@ -11,7 +11,8 @@ namespace {
 
 constexpr int kFRows = 64; // rows of a step
 constexpr int kRing = 8;                       // steps whose rows' places are held
-constexpr float kMostSum = 18446744073709551616.f; // 2^64: sums of weights past this are worked out again (see below)
+// 2^24: sums of weights past this are worked out again (see below).  Values of up to 2^100 or so stay in range.
+constexpr float kMostSum = 16777216.f;
 
 // sum of two bf16 and x, in fp32
 __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
@@ -381,7 +382,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     };
     // What exponents subtract is the largest score of the unit's first half, and stays: weights then are what they are, not at most
     // 1, and floating point holds them as well, so nothing in the loop waits for a maximum or brings sums to another one.  Sums that
-    // leave the range (a later score larger by 64 log2 units or so) are worked out again with the largest score of all rows.
+    // grow large (a later score larger by 24 log2 units or so) are worked out again with the largest score of all rows.
     if (n_halves > 0)
     for (bool again = false;; again = true) {
         if (__builtin_expect(again, 0)) {

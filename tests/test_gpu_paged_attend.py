@@ -455,3 +455,18 @@ def test_one_long_prompt_with_rows_that_decide_late():
     sure[-5:] = False
     assert sure.any()
     near(got[sure], want[sure], err[sure], BF16)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("high", [3.0, 8.0])
+def test_large_values_where_rows_decide_late(D, high):
+    """Weights are relative to the first rows' largest score at first: later ones far above it must not take large values out of range."""
+    c = Case([(150, 400), (60, 300)], D, 8, 2, 16, BF16, seed=D)
+    for b in range(2):
+        for j in range(40, int(c.lengths[b])):
+            c.kp[:, c.table[b][j // 16], :, j % 16] *= high
+    c.vp *= 1e30
+    got = c.attend()
+    assert np.isfinite(f64(got)).all()
+    want, _, amean, reach = c.wanted()
+    near(f64(got), want, attention_error(amean, reach, 400, D, BF16, True), BF16)
