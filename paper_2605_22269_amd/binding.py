@@ -690,6 +690,7 @@ class MuKV:
 _STRIDES = {}   # address of the C form of the strides met so far
 _STRIDES_KEPT = []
 _SEQS = struct.Struct("@QQQiiii")   # mukv_seqs
+_WEIGHTS = struct.Struct("@QQqqqif")   # mukv_row_weights
 _I32 = torch.int32
 MUKV_PAGED_CLEAR = 8192
 
@@ -754,7 +755,11 @@ class _Sequences:
         self._pages, self._seqs = mukv_paged(), mukv_seqs()
         self._pages_at, self._seqs_at = C.addressof(self._pages), C.addressof(self._seqs)
         self._seqs_memory = memoryview(self._seqs).cast("B")
+        self._weights = mukv_row_weights()
+        self._weights_at, self._weights_memory = C.addressof(self._weights), memoryview(self._weights).cast("B")
         self._scratch, self._need = {}, (None, 0)
+        lib = _lib or load()
+        self._c_append, self._c_attend, self._c_capture = lib.mukv_paged_append, lib.mukv_paged_attend, lib.mukv_stream_capture
         self._capture = C.c_uint64(0)
         self._capture_at = C.addressof(self._capture)
 
@@ -763,21 +768,25 @@ class _Sequences:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         else:
             assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous()
-        w = None
+        w, weights_in = None, 0
         if weights_out is not None:
             st = weights_out.stride()
             assert weights_out.dtype is torch.float32 and len(st) == 3 and st[2] == 1
             assert weights_out.shape[:2] == (self._seqs.n_seqs, self._pages.n_kv_heads)
             if weights is not None:
                 assert weights.dtype is torch.float32 and weights.shape == weights_out.shape and weights.stride() == st
-            w = mukv_row_weights(_ptr(weights), weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
+                weights_in = weights.data_ptr()
+            w = self._weights_at
+            _WEIGHTS.pack_into(self._weights_memory, 0, weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
         else:
             assert weights is None
         stream = _stream_of(self._index)
         if self._need[0] != key:
             self._need = key, mukv_paged_workspace_size(self._pages_at, s, int(w is not None))
         need = self._need[1]
-        mukv_stream_capture(stream, self._capture_at)
+        rc = self._c_capture(stream, self._capture_at)
+        if rc:
+            _check(rc, "mukv_stream_capture")
         capture = self._capture.value   # (0: none)
         place = stream, capture != 0
         ws = self._scratch.get(place)
@@ -785,8 +794,10 @@ class _Sequences:
             t = torch.empty(need, dtype=torch.uint8, device=q.device)
             t[:MUKV_PAGED_CLEAR].zero_()   # every call finds and leaves it so
             ws = self._scratch[place] = t.data_ptr(), need, t, (self._index, capture)
-        mukv_paged_attend(self._pages_at, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
-                          None if w is None else C.addressof(w), ws[0], ws[1], stream)
+        rc = self._c_attend(self._pages_at, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
+                            w, ws[0], ws[1], stream)
+        if rc:
+            _check(rc, "mukv_paged_attend")
         return out
 
 
@@ -803,17 +814,17 @@ class PagedKV(_Sequences):
         sl, sp, sh, sr, _ = k_pages.stride()
         self.dtype, self.device, self._index = k_pages.dtype, k_pages.device, k_pages.device.index or 0
         self._held = k_pages, v_pages
-        self._kv_row, self._q_row = (hkv, D), (n_q_heads, D)
+        self._heads, self._q_heads, self._dim = hkv, n_q_heads, D
         self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, _dtype(k_pages), self._index)
         self._pages_at = C.addressof(self._pages)
 
     def _sequences(self, table, lengths, offsets, n_tokens, max_new):
         n, width = table.shape
         assert table.dtype is _I32 and table.is_contiguous()
-        assert lengths.dtype is _I32 and lengths.shape == (n,) and lengths.is_contiguous()
+        assert lengths.dtype is _I32 and lengths.numel() == n and lengths.is_contiguous()
         off = 0
         if offsets is not None:
-            assert offsets.dtype is _I32 and offsets.shape == (n + 1,) and offsets.is_contiguous()
+            assert offsets.dtype is _I32 and offsets.numel() == n + 1 and offsets.is_contiguous()
             off = offsets.data_ptr()
         _SEQS.pack_into(self._seqs_memory, 0, table.data_ptr(), lengths.data_ptr(), off, n, width, n_tokens, max_new)
         return self._seqs_at
@@ -821,15 +832,14 @@ class PagedKV(_Sequences):
     def append(self, layer, table, lengths, k, v, *, q=None, offsets=None, rope=None, positions=None, q_out=None):
         """New tokens' keys and values [n_tokens][n_kv_heads][head_dim] become the last rows of their sequences (lengths count
         them already); with `rope` the keys, and q [n_tokens][n_q_heads][head_dim], are rotated on the way.  Returns q_out."""
-        shape, dt = k.shape, self.dtype
-        T = shape[0]
-        assert shape[1:] == self._kv_row and v.shape == shape and k.dtype is dt and v.dtype is dt
+        shape, dt, known = k.shape, self.dtype, _STRIDES.get
+        T, heads, dim = shape
+        assert dim == self._dim and heads == self._heads and v.shape == shape and k.dtype is dt and v.dtype is dt
         s = self._sequences(table, lengths, offsets, T, 0)
         qp = op = qs = os_ = turn = pos = None
-        known = _STRIDES.get
         if q is not None:
-            shape = q.shape
-            assert shape[0] == T and shape[1:] == self._q_row and q.dtype is dt
+            shape = T, self._q_heads, dim
+            assert q.shape == shape and q.dtype is dt
             if q_out is None:
                 q_out = torch.empty(shape, dtype=dt, device=q.device)
             else:
@@ -839,9 +849,12 @@ class PagedKV(_Sequences):
         if rope is not None:
             assert positions.dtype is _I32 and positions.shape == (rope.n_axes, T) and positions.is_contiguous()
             turn, pos = rope.table, positions.data_ptr()
-        mukv_paged_append(self._pages_at, layer, s, k.data_ptr(), known(k.stride()) or _rows(k), v.data_ptr(),
-                          known(v.stride()) or _rows(v), qp, qs, op, os_, turn, pos,
-                          _stream_of(self._index))
+        st = k.stride()
+        ks = known(st) or _rows(k)
+        rc = self._c_append(self._pages_at, layer, s, k.data_ptr(), ks, v.data_ptr(), ks if v.stride() == st else _rows(v), qp, qs, op, os_,
+                            turn, pos, _stream_of(self._index))
+        if rc:
+            _check(rc, "mukv_paged_append")
         return q_out
 
     def attend(self, layer, table, lengths, q, *, offsets=None, max_new=0, causal=True, out=None, weights=None, weights_out=None,
@@ -849,9 +862,8 @@ class PagedKV(_Sequences):
         """q [n_tokens][n_q_heads][head_dim]: every sequence's new tokens (lengths count them) attend to its rows.  With
         weights_out, float32 [sequence][KV head][row], it becomes decay * weights + what every row received (weights None: zeros;
         weights_out may be weights).  max_new: most new tokens of a sequence, as a hint.  Returns out."""
-        shape = q.shape
-        T = shape[0]
-        assert shape[1:] == self._q_row and q.dtype is self.dtype
+        T, heads, dim = q.shape
+        assert heads == self._q_heads and dim == self._dim and q.dtype is self.dtype
         s = self._sequences(table, lengths, offsets, T, max_new)
         key = T, self._seqs.n_seqs, self._seqs.table_width, max_new, weights_out is None   # (what else scratch depends on is the cache's)
         return self._attend(s, key, layer, q, causal, out, weights, weights_out, decay)
@@ -879,9 +891,9 @@ class PagedKV(_Sequences):
             lengths_out = torch.empty_like(lengths)
         assert kept.dtype is _I32 and lengths_out.dtype is _I32 and kept.shape == shape and lengths_out.shape == lengths.shape
         assert kept.is_contiguous() and lengths_out.is_contiguous()
-        w = mukv_row_weights(weights.data_ptr(), weights_out.data_ptr(), st[0], st[1], st[2], weights.shape[3], 0.0)
-        mukv_paged_evict(self._pages_at, s, C.addressof(w), budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1], kept.data_ptr(),
-                         lengths_out.data_ptr(), _stream_of(self._index))
+        _WEIGHTS.pack_into(self._weights_memory, 0, weights.data_ptr(), weights_out.data_ptr(), *st[:3], weights.shape[3], 0.0)
+        mukv_paged_evict(self._pages_at, s, self._weights_at, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1],
+                         kept.data_ptr(), lengths_out.data_ptr(), _stream_of(self._index))
         return kept, lengths_out
 
 
