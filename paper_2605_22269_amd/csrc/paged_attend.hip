@@ -51,9 +51,11 @@ __device__ __forceinline__ f32x4 scores_f32(const raw16 (&k)[KK], Q q) {
 //   scores   S^T = K Q^T (16x16x32 bf16, 16x16x4 fp32): a lane holds ONE query (lane % 16) and the rows 4 (lane / 16) + r of every 16.
 //   values   O^T += V^T P^T: the weights are the B operand as they stand in the lane.  bf16: pairs hi + lo, nothing of the fp32
 //            weight is lost; the value rows pass through LDS the wave has to itself and the transpose read.  fp32: no transpose needed.
-// fp32 rows: three workgroups to a compute unit where the registers are there (1500 tokens, 16/4 heads of 64: 92 us, 103 with two).
+// As many workgroups to a compute unit as the registers allow (us a launch, two / as now: 100 users of 3 rows, 12 heads of 64 bf16, 13.7 / 10.2;
+// 12 users, 5 tokens over 1000 to 9000 rows, 28/4 heads of 64 bf16, 26.5 / 22.3; 6 prompts of 700 to 1500 tokens, 28/4 heads of 32 bf16, 148 / 94;
+// of fp32 252 / 218; 1500 tokens, 16/4 heads of 64 fp32, 103 / 92).
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(2, sizeof(T) == 4 && D <= 64 ? 3 : 2))) void paged_attend_kernel(PagedAttendArgs a) {
+__global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D <= 32 ? 4 : D == 64 ? 3 : 2, D <= 32 ? 5 : D == 64 ? 3 : 2))) void paged_attend_kernel(PagedAttendArgs a) {
     constexpr int W = kPWaves;
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
