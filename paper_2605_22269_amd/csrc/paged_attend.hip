@@ -489,8 +489,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    // (bf16 payloads: rounded at the size of the difference, 2^-21 of a weight that matters)
-                    const float w = large ? weight_of_any(sc[e], scale, ref) : kBf16 ? __builtin_amdgcn_exp2f(fmaf(sc[e], scale, -ref)) : weight_of(sc[e], scale, ref);
+                    // (bf16 payloads: rounded at the size of the difference, 2^-21 of a weight that matters.  The prompt kernel's references
+                    // are no whole numbers, so weight_of is not for them, whatever the neighbours' are)
+                    float w;
+                    if constexpr (kBf16)
+                        w = __builtin_amdgcn_exp2f(large && fabsf(ref) > kLargeRef ? scaled_apart(sc[e], scale, ref) : fmaf(sc[e], scale, -ref));
+                    else
+                        w = large ? weight_of_any(sc[e], scale, ref) : weight_of(sc[e], scale, ref);
                     sum[t][e] += tok[at] >= from[t][e] && tok[at] >= 0 ? w * inv : 0.f;
                 }
             }

@@ -1,0 +1,53 @@
+"""Calls of the paged cache where something unusual of one query, value or argument must stay with it, against the formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paged_testlib import f64, near
+from paper_2605_22269_amd import binding as mk
+from test_gpu_paged_attend import BF16, F32, Case, weights_error
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- weights of rows beside a query whose scores are out of the ordinary ----
+def window(D, dtype, causal_rows=300):
+    """Two users' prompts whose bf16 form goes to the prompt kernel, and what a row's weight may be off."""
+    c = Case([(32, causal_rows), (40, 200)], D, 28, 4, 16, dtype, seed=D)
+    received = c.wanted()[1]
+    return c, weights_error(c, received)
+
+
+def weights_of(c):
+    rows = torch.zeros(2, 4, int(c.lengths.max()), device="cuda")
+    c.attend(weights_out=rows)
+    return f64(rows)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_query_of_large_scores_leaves_its_neighbours_weights_alone(D, dtype):
+    c, tol = window(D, dtype)
+    c.q[2, 0] *= 2.0**30      # scores of 2^30 and more: one row has all of its weight
+    received, got = c.wanted()[1], weights_of(c)
+    for b, n in enumerate(c.lengths):
+        near(got[b][:, :n], received[b], (1 + received[b]) * tol, F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_an_infinite_score_stays_with_the_rows_that_its_query_sees(D, dtype):
+    c, tol = window(D, dtype)
+    past, token, row = 300 - 32, 3, 100
+    at = (1, c.table[0][row // 16], slice(None), row % 16, 3)
+    c.q[..., 3] = -1.0
+    c.kp[at] = 30000.0        # a weight of nothing for everybody
+    received = c.wanted()[1]
+    c.kp[at] = float("inf")   # the same: -inf, but for one query
+    c.q[token, 0, 3] = 1.0
+    got = weights_of(c)
+    unseen = slice(past + token + 1, 300)
+    assert np.isnan(got[0][0, : past + token + 1]).all()
+    near(got[0][:, unseen], received[0][:, unseen], (1 + received[0][:, unseen]) * tol, F32)
+    near(got[0][1:, :300], received[0][1:], (1 + received[0][1:]) * tol, F32)
+    near(got[1][:, :200], received[1], (1 + received[1]) * tol, F32)
