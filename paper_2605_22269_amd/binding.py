@@ -687,8 +687,8 @@ class MuKV:
 # ---- the conversation's cache ----------------------------------------------------------------
 # A generated token is two of these calls a layer, of a few microseconds each on the device, so what Python does for one is kept short: every
 # attribute of a tensor is asked for once, a structure is filled by one pack, strides keep their C form.
-_STRIDES = {}   # address of the C form of the strides met so far
-_STRIDES_KEPT = []
+_STRIDES = {}   # C form of strides met lately, as bytes: nobody changes them, and a call's own reference keeps them
+_STRIDES_MOST = 256   # (strides may depend on the number of tokens)
 _SEQS = struct.Struct("@QQQiiii")   # mukv_seqs
 _WEIGHTS = struct.Struct("@QQqqqif")   # mukv_row_weights
 _I32 = torch.int32
@@ -696,17 +696,16 @@ MUKV_PAGED_CLEAR = 8192
 
 
 def _rows(t):
-    """Strides of [token][head][feature] as the C ABI takes them: the address of a structure that stays."""
+    """Strides of [token][head][feature] as the C ABI takes them."""
     key = t.stride()
     at = _STRIDES.get(key)
     if at is None:
         if t.numel() == 0:   # (its strides are anything, and not read)
             key = (0, 0, 1)
-            if key in _STRIDES:
-                return _STRIDES[key]
         assert len(key) == 3 and key[2] == 1
-        _STRIDES_KEPT.append(mukv_strides(0, key[1], key[0]))
-        at = _STRIDES[key] = C.addressof(_STRIDES_KEPT[-1])
+        if len(_STRIDES) >= _STRIDES_MOST:
+            _STRIDES.clear()
+        at = _STRIDES[key] = bytes(mukv_strides(0, key[1], key[0]))
     return at
 
 
