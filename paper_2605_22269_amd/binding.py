@@ -686,9 +686,10 @@ class MuKV:
 
 # ---- the conversation's cache ----------------------------------------------------------------
 # A generated token is two of these calls a layer, of a few microseconds each on the device, so what Python does for one is kept short: every
-# attribute of a tensor is asked for once, a structure is filled by one pack, strides keep their C form.
+# attribute of a tensor is asked for once, a structure is one pack, strides keep their C form.
 _STRIDES = {}   # C form of strides met lately, as bytes: nobody changes them, and a call's own reference keeps them
 _STRIDES_MOST = 256   # (strides may depend on the number of tokens)
+_PAGED = struct.Struct("@QQqqqqiiiiiiii")   # mukv_paged
 _SEQS = struct.Struct("@QQQiiii")   # mukv_seqs
 _WEIGHTS = struct.Struct("@QQqqqif")   # mukv_row_weights
 _I32 = torch.int32
@@ -746,54 +747,50 @@ class Rope:
 
 
 class _Sequences:
-    """What the caches share: the C structures, and scratch of the attention calls, a piece for every stream that calls (calls on
-    different streams may overlap).  A graph that is being captured has a piece of its own, in the graph's memory, and clears what has
-    to be clear itself: its replays may come before, after or beside anything else."""
+    """What the caches share: scratch of the attention calls, a piece for every stream that calls (calls on different streams may
+    overlap).  A graph that is being captured has a piece of its own, in the graph's memory, and clears what has to be clear
+    itself: its replays may come before, after or beside anything else.  A call's structures are bytes of its own, so threads may use a
+    cache together."""
 
     def __init__(self):
-        self._pages, self._seqs = mukv_paged(), mukv_seqs()
-        self._pages_at, self._seqs_at = C.addressof(self._pages), C.addressof(self._seqs)
-        self._seqs_memory = memoryview(self._seqs).cast("B")
-        self._weights = mukv_row_weights()
-        self._weights_at, self._weights_memory = C.addressof(self._weights), memoryview(self._weights).cast("B")
         self._scratch, self._need = {}, (None, 0)
         lib = _lib or load()
         self._c_append, self._c_attend, self._c_capture = lib.mukv_paged_append, lib.mukv_paged_attend, lib.mukv_stream_capture
-        self._capture = C.c_uint64(0)
-        self._capture_at = C.addressof(self._capture)
 
-    def _attend(self, s, key, layer, q, causal, out, weights, weights_out, decay):
+    def _attend(self, pages, s, index, heads, key, layer, q, causal, out, weights, weights_out, decay):
+        """heads: sequences and KV heads; key: all that the scratch's size follows from."""
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         else:
             assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous()
-        w, weights_in = None, 0
+        w = None
         if weights_out is not None:
-            st = weights_out.stride()
+            st, weights_in = weights_out.stride(), 0
             assert weights_out.dtype is torch.float32 and len(st) == 3 and st[2] == 1
-            assert weights_out.shape[:2] == (self._seqs.n_seqs, self._pages.n_kv_heads)
+            assert weights_out.shape[:2] == heads
             if weights is not None:
                 assert weights.dtype is torch.float32 and weights.shape == weights_out.shape and weights.stride() == st
                 weights_in = weights.data_ptr()
-            w = self._weights_at
-            _WEIGHTS.pack_into(self._weights_memory, 0, weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
+            w = _WEIGHTS.pack(weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
         else:
             assert weights is None
-        stream = _stream_of(self._index)
-        if self._need[0] != key:
-            self._need = key, mukv_paged_workspace_size(self._pages_at, s, int(w is not None))
-        need = self._need[1]
-        rc = self._c_capture(stream, self._capture_at)
+        stream = _stream_of(index)
+        need = self._need
+        if need[0] != key:
+            need = self._need = key, mukv_paged_workspace_size(pages, s, int(w is not None))
+        need = need[1]
+        capture = C.c_uint64()
+        rc = self._c_capture(stream, C.byref(capture))
         if rc:
             _check(rc, "mukv_stream_capture")
-        capture = self._capture.value   # (0: none)
-        place = stream, capture != 0
+        capture = capture.value   # (0: none)
+        place = index, stream, capture != 0
         ws = self._scratch.get(place)
-        if ws is None or ws[1] < need or ws[3] != (self._index, capture):
+        if ws is None or ws[1] < need or ws[3] != capture:
             t = torch.empty(need, dtype=torch.uint8, device=q.device)
             t[:MUKV_PAGED_CLEAR].zero_()   # every call finds and leaves it so
-            ws = self._scratch[place] = t.data_ptr(), need, t, (self._index, capture)
-        rc = self._c_attend(self._pages_at, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
+            ws = self._scratch[place] = t.data_ptr(), need, t, capture
+        rc = self._c_attend(pages, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
                             w, ws[0], ws[1], stream)
         if rc:
             _check(rc, "mukv_paged_attend")
@@ -825,8 +822,7 @@ class PagedKV(_Sequences):
         if offsets is not None:
             assert offsets.dtype is _I32 and offsets.numel() == n + 1 and offsets.is_contiguous()
             off = offsets.data_ptr()
-        _SEQS.pack_into(self._seqs_memory, 0, table.data_ptr(), lengths.data_ptr(), off, n, width, n_tokens, max_new)
-        return self._seqs_at
+        return _SEQS.pack(table.data_ptr(), lengths.data_ptr(), off, n, width, n_tokens, max_new)
 
     def append(self, layer, table, lengths, k, v, *, q=None, offsets=None, rope=None, positions=None, q_out=None):
         """New tokens' keys and values [n_tokens][n_kv_heads][head_dim] become the last rows of their sequences (lengths count
@@ -864,8 +860,9 @@ class PagedKV(_Sequences):
         T, heads, dim = q.shape
         assert heads == self._q_heads and dim == self._dim and q.dtype is self.dtype
         s = self._sequences(table, lengths, offsets, T, max_new)
-        key = T, self._seqs.n_seqs, self._seqs.table_width, max_new, weights_out is None   # (what else scratch depends on is the cache's)
-        return self._attend(s, key, layer, q, causal, out, weights, weights_out, decay)
+        n, width = table.shape
+        key = T, n, width, max_new, weights_out is None   # (what else scratch depends on is the cache's)
+        return self._attend(self._pages_at, s, self._index, (n, self._heads), key, layer, q, causal, out, weights, weights_out, decay)
 
     def evict(self, table, lengths, weights, budget, *, sink=0, recent=0, into=None, weights_out=None, kept=None, lengths_out=None):
         """Brings every sequence down to `budget` rows per layer and KV head: the first `sink`, the last `recent`, and the others
@@ -890,8 +887,8 @@ class PagedKV(_Sequences):
             lengths_out = torch.empty_like(lengths)
         assert kept.dtype is _I32 and lengths_out.dtype is _I32 and kept.shape == shape and lengths_out.shape == lengths.shape
         assert kept.is_contiguous() and lengths_out.is_contiguous()
-        _WEIGHTS.pack_into(self._weights_memory, 0, weights.data_ptr(), weights_out.data_ptr(), *st[:3], weights.shape[3], 0.0)
-        mukv_paged_evict(self._pages_at, s, self._weights_at, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1],
+        w = _WEIGHTS.pack(weights.data_ptr(), weights_out.data_ptr(), *st[:3], weights.shape[3], 0.0)
+        mukv_paged_evict(self._pages_at, s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1],
                          kept.data_ptr(), lengths_out.data_ptr(), _stream_of(self._index))
         return kept, lengths_out
 
@@ -902,23 +899,18 @@ class PackedKV(_Sequences):
 
     def __init__(self, *, n_q_heads):
         super().__init__()
-        self._pages.n_q_heads = n_q_heads
-        self._kind = None
+        self._q_heads = n_q_heads
 
     def attend(self, q, k, v, offsets, *, max_new=0, causal=True, out=None, weights=None, weights_out=None, decay=1.0):
         """As PagedKV.attend; weights are [sequence][KV head][token of the sequence]."""
-        p, (T, hkv, D), st = self._pages, k.shape, k.stride()
+        (T, hkv, D), st = k.shape, k.stride()
         assert v.shape == k.shape and v.stride() == st and (st[2] == 1 or T == 0)
-        assert q.shape == (T, p.n_q_heads, D) and q.dtype is k.dtype and k.dtype is v.dtype
+        assert q.shape == (T, self._q_heads, D) and q.dtype is k.dtype and k.dtype is v.dtype
         assert offsets.dtype is _I32 and offsets.is_contiguous()
-        p.k_pages, p.v_pages, p.stride_row, p.stride_head = k.data_ptr(), v.data_ptr(), st[0], st[1]
-        kind = k.dtype, hkv, D, k.device
-        if self._kind != kind:
-            self._kind, self._need, self._index = kind, (None, 0), k.device.index or 0
-            p.n_layers, p.n_pages, p.n_kv_heads, p.head_dim, p.dtype, p.device_id = 1, 1, hkv, D, _dtype(k), self._index
-        p.page_rows = T if T > 0 else 1
-        n = offsets.numel() - 1
-        _SEQS.pack_into(self._seqs_memory, 0, 0, 0, offsets.data_ptr(), n, 0, T, max_new)
+        index, dtype, n = k.device.index or 0, _dtype(k), offsets.numel() - 1
         if T == 0 and weights_out is None:
             return q if out is None else out
-        return self._attend(self._seqs_at, (T, n, max_new, weights_out is None), 0, q, causal, out, weights, weights_out, decay)
+        pages = _PAGED.pack(k.data_ptr(), v.data_ptr(), 0, 0, st[1], st[0], 1, 1, T if T > 0 else 1, self._q_heads, hkv, D, dtype, index)
+        s = _SEQS.pack(0, 0, offsets.data_ptr(), n, 0, T, max_new)
+        return self._attend(pages, s, index, (n, hkv), (T, n, max_new, weights_out is None, hkv, D, dtype), 0, q, causal, out, weights,
+                            weights_out, decay)

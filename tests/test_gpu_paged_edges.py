@@ -51,3 +51,43 @@ def test_an_infinite_score_stays_with_the_rows_that_its_query_sees(D, dtype):
     near(got[0][:, unseen], received[0][:, unseen], (1 + received[0][:, unseen]) * tol, F32)
     near(got[0][1:, :300], received[0][1:], (1 + received[0][1:]) * tol, F32)
     near(got[1][:, :200], received[1], (1 + received[1]) * tol, F32)
+
+
+# ---- threads ----
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_threads_on_streams_of_their_own_share_a_cache(dtype):
+    """Each has its own sequences of the cache's pages, tables of its own width, and weights; the answers are those of one at a time."""
+    import threading
+
+    c = Case([(1, 300), (2, 77), (3, 1000), (40, 90), (1, 5), (6, 6)], 64, 8, 2, 16, dtype, seed=21)
+    jobs = []
+    for i in range(6):
+        n, width = int(c.lengths[i]), -(-int(c.lengths[i]) // 16) + i
+        table = np.full((1, width), -1, np.int32)
+        table[0, : -(-n // 16)] = c.table[i, : -(-n // 16)]
+        q = c.q[int(c.off[i]):int(c.off[i + 1])].contiguous()
+        k, v = (torch.tensor(c.rng.standard_normal((q.shape[0], 2, 64)), dtype=torch.float32).to(dtype).cuda() for _ in "kv")
+        jobs.append([torch.tensor(table, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda"), q, k, v])
+
+    def once(j):
+        table, lengths, q, k, v = j
+        w = torch.zeros(1, 2, int(c.lengths.max()), device="cuda")
+        c.cache.append(1, table, lengths, k, v)
+        return c.cache.attend(1, table, lengths, q, weights_out=w), w
+
+    want = [once(j) for j in jobs]
+    torch.cuda.synchronize()
+    wrong, streams = [], [torch.cuda.Stream() for _ in jobs]
+
+    def work(i):
+        with torch.cuda.stream(streams[i]):
+            for _ in range(30):
+                out, w = once(jobs[i])
+                streams[i].synchronize()
+                if not (torch.equal(out, want[i][0]) and torch.equal(w, want[i][1])):
+                    wrong.append(i)
+
+    all_of_them = [threading.Thread(target=work, args=(i,)) for i in range(6)]
+    [t.start() for t in all_of_them]
+    [t.join() for t in all_of_them]
+    assert not wrong

@@ -44,11 +44,12 @@ class Stand:
 
 def threads(n, work):
     """n threads that change as often as they can; what they raised."""
-    raised, was = [], sys.getswitchinterval()
+    raised, was, together = [], sys.getswitchinterval(), threading.Barrier(n)
     sys.setswitchinterval(1e-6)
 
     def guarded(i):
         try:
+            together.wait(60)   # (all of them are there: no number of a thread is given twice)
             work(i)
         except BaseException as e:  # noqa: BLE001
             raised.append(repr(e))
@@ -88,3 +89,106 @@ def test_strides_of_other_kinds_are_refused():
         with pytest.raises(AssertionError):
             mk._rows(Stand(*[2] * len(strides), strides=strides))
     assert C.string_at(mk._rows(Stand(0, 2, 8, strides=(5, 5, 5))), 24) == bytes(24)
+
+
+# ---- threads that use one cache ----
+SLOW = 2e-5   # a call that takes its time before it reads what it was given
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """What the C functions were given, read a while after the call: (thread, pages, seqs, weights, q or k)."""
+    import time
+
+    real, made = torch.empty, []
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: real(*a, **kw))   # (scratch, where there is no device)
+    monkeypatch.setattr(mk, "_stream_of", lambda index: threading.get_ident())
+    lib, held = mk.load(), []
+
+    def stand_in(name, work):
+        f = C.CFUNCTYPE(C.c_int, *getattr(lib, name).argtypes)(work)
+        held.append(f)
+        return f
+
+    def read(kind, at):
+        return kind.from_buffer_copy(C.string_at(at, C.sizeof(kind))) if at else None
+
+    def append(pages, layer, s, k, *rest):
+        time.sleep(SLOW)
+        made.append((threading.get_ident(), read(mk.mukv_paged, pages), read(mk.mukv_seqs, s), None, k))
+        return 0
+
+    def attend(pages, layer, s, q, q_strides, causal, out, w, ws, ws_bytes, stream):
+        time.sleep(SLOW)
+        made.append((threading.get_ident(), read(mk.mukv_paged, pages), read(mk.mukv_seqs, s), read(mk.mukv_row_weights, w), q))
+        assert stream == threading.get_ident()
+        return 0
+
+    def capture(stream, at):
+        C.c_uint64.from_address(at).value = 0
+        return 0
+
+    def cache(c):
+        c._c_append, c._c_attend = stand_in("mukv_paged_append", append), stand_in("mukv_paged_attend", attend)
+        c._c_capture = stand_in("mukv_stream_capture", capture)
+        return c
+
+    yield cache, made
+
+
+def i32(*shape):
+    return Stand(*shape, dtype=torch.int32)
+
+
+def test_threads_that_share_a_paged_cache_call_with_their_own_arguments(calls):
+    cache, made = calls
+    c = cache(mk.PagedKV(Stand(1, 9, 2, 16, 64), Stand(1, 9, 2, 16, 64), n_q_heads=4))
+    given = {}
+
+    def work(i):
+        n, T = 2 + i, 5 * (2 + i)
+        table, lengths, off = i32(n, 7 + i), i32(n), i32(n + 1)
+        q, out, k, v = Stand(T, 4, 64), Stand(T, 4, 64), Stand(T, 2, 64), Stand(T, 2, 64)
+        w, was = (Stand(n, 2, 50 + i, dtype=torch.float32) for _ in "ab")
+        given[threading.get_ident()] = table, lengths, off, q, k, w, was, n, T
+        for _ in range(100):
+            c.append(0, table, lengths, k, v, offsets=off)
+            c.attend(0, table, lengths, q, offsets=off, out=out, weights=was, weights_out=w, max_new=i)
+
+    threads(6, work)
+    assert len(made) == 1200
+    for who, _, s, w_got, x in made:
+        table, lengths, off, q, k, w, was, n, T = given[who]
+        assert (s.table, s.lengths, s.offsets, s.n_seqs, s.table_width, s.n_tokens) == (
+            table.data_ptr(), lengths.data_ptr(), off.data_ptr(), n, table.shape[1], T)
+        assert x == (q if w_got else k).data_ptr()
+        if w_got:
+            assert (w_got.in_, w_got.out, w_got.rows) == (was.data_ptr(), w.data_ptr(), w.shape[2])
+
+
+def test_threads_that_share_a_packed_cache_call_with_their_own_arguments(calls):
+    cache, made = calls
+    c = cache(mk.PackedKV(n_q_heads=4))
+    given = {}
+
+    def work(i):
+        T, D, dt = 10 + i, (64, 128)[i % 2], (torch.bfloat16, torch.float32)[i // 2 % 2]
+        q, out, k, v, off = Stand(T, 4, D, dtype=dt), Stand(T, 4, D, dtype=dt), Stand(T, 2, D, dtype=dt), Stand(T, 2, D, dtype=dt), i32(3 + i)
+        given[threading.get_ident()] = q, k, v, off, T, D, mk.MUKV_BF16 if dt == torch.bfloat16 else mk.MUKV_F32
+        for _ in range(200):
+            c.attend(q, k, v, off, out=out)
+
+    threads(6, work)
+    assert len(made) == 1200
+    for who, p, s, _, x in made:
+        q, k, v, off, T, D, dt = given[who]
+        assert (p.k_pages, p.v_pages, p.page_rows, p.head_dim, p.dtype, p.stride_row) == (k.data_ptr(), v.data_ptr(), T, D, dt, 2 * D)
+        assert (s.offsets, s.n_seqs, s.n_tokens) == (off.data_ptr(), off.shape[0] - 1, T) and x == q.data_ptr()
+
+
+def test_structures_are_packed_as_they_are_declared():
+    for layout, kind in ((mk._SEQS, mk.mukv_seqs), (mk._WEIGHTS, mk.mukv_row_weights), (mk._PAGED, mk.mukv_paged)):
+        assert layout.size == C.sizeof(kind)
+        numbers = list(range(1, len(kind._fields_) + 1))
+        got = kind.from_buffer_copy(layout.pack(*numbers))
+        assert [getattr(got, name) for name, _ in kind._fields_] == numbers
