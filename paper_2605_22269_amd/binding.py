@@ -725,9 +725,10 @@ class Rope:
     int32 [n_rot/2] (None: one axis) on the device."""
 
     def __init__(self, inv_freq, axis=None, *, n_axes=1, pairing="halves"):
-        assert inv_freq.dtype == torch.float64 and inv_freq.is_contiguous()
-        assert axis is None or (axis.dtype == _I32 and axis.is_contiguous() and axis.numel() == inv_freq.numel())
+        assert inv_freq.dtype == torch.float64 and inv_freq.is_contiguous() and inv_freq.is_cuda
+        assert axis is None or (axis.dtype == _I32 and axis.is_contiguous() and axis.numel() == inv_freq.numel() and axis.device == inv_freq.device)
         self._held = inv_freq, axis
+        self.index = inv_freq.get_device()
         self.n_axes = n_axes
         kind = {"halves": MUKV_ROPE_HALVES, "neighbours": MUKV_ROPE_NEIGHBOURS}[pairing]
         self._tables = [mukv_rope_table(_ptr(inv_freq), _ptr(axis), 2 * inv_freq.numel(), n_axes, kind, back) for back in (0, 1)]
@@ -740,7 +741,8 @@ class Rope:
         T, H, D = x.shape
         assert out.shape == x.shape and out.dtype == x.dtype
         assert positions.dtype is _I32 and positions.shape == (self.n_axes, T) and positions.is_contiguous()
-        dev = x.device.index or 0
+        dev = self.index
+        assert x.get_device() == out.get_device() == positions.get_device() == dev
         mukv_rope(self.back if inverse else self.table, x.data_ptr(), _rows(x), positions.data_ptr(), T, H, D, _dtype(x), out.data_ptr(),
                   _rows(out), dev, _stream_of(dev))
         return out
@@ -762,14 +764,16 @@ class _Sequences:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         else:
-            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous()
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
+        assert q.get_device() == index
         w = None
         if weights_out is not None:
             st, weights_in = weights_out.stride(), 0
             assert weights_out.dtype is torch.float32 and len(st) == 3 and st[2] == 1
-            assert weights_out.shape[:2] == heads
+            assert weights_out.shape[:2] == heads and weights_out.get_device() == index
             if weights is not None:
                 assert weights.dtype is torch.float32 and weights.shape == weights_out.shape and weights.stride() == st
+                assert weights.get_device() == index
                 weights_in = weights.data_ptr()
             w = _WEIGHTS.pack(weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
         else:
@@ -805,10 +809,10 @@ class PagedKV(_Sequences):
     def __init__(self, k_pages, v_pages, *, n_q_heads):
         super().__init__()
         assert k_pages.dim() == 5 and v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
-        assert v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device and k_pages.stride(4) == 1
+        assert v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device and k_pages.is_cuda and k_pages.stride(4) == 1
         L, n, hkv, R, D = k_pages.shape
         sl, sp, sh, sr, _ = k_pages.stride()
-        self.dtype, self.device, self._index = k_pages.dtype, k_pages.device, k_pages.device.index or 0
+        self.dtype, self.device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
         self._held = k_pages, v_pages
         self._heads, self._q_heads, self._dim = hkv, n_q_heads, D
         self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, _dtype(k_pages), self._index)
@@ -818,36 +822,40 @@ class PagedKV(_Sequences):
         n, width = table.shape
         assert table.dtype is _I32 and table.is_contiguous()
         assert lengths.dtype is _I32 and lengths.numel() == n and lengths.is_contiguous()
+        index = self._index   # (what lies elsewhere, host memory above all, must not reach a kernel)
+        assert table.get_device() == index and lengths.get_device() == index
         off = 0
         if offsets is not None:
-            assert offsets.dtype is _I32 and offsets.numel() == n + 1 and offsets.is_contiguous()
+            assert offsets.dtype is _I32 and offsets.numel() == n + 1 and offsets.is_contiguous() and offsets.get_device() == index
             off = offsets.data_ptr()
         return _SEQS.pack(table.data_ptr(), lengths.data_ptr(), off, n, width, n_tokens, max_new)
 
     def append(self, layer, table, lengths, k, v, *, q=None, offsets=None, rope=None, positions=None, q_out=None):
         """New tokens' keys and values [n_tokens][n_kv_heads][head_dim] become the last rows of their sequences (lengths count
         them already); with `rope` the keys, and q [n_tokens][n_q_heads][head_dim], are rotated on the way.  Returns q_out."""
-        shape, dt, known = k.shape, self.dtype, _STRIDES.get
+        shape, dt, known, index = k.shape, self.dtype, _STRIDES.get, self._index
         T, heads, dim = shape
         assert dim == self._dim and heads == self._heads and v.shape == shape and k.dtype is dt and v.dtype is dt
+        assert k.get_device() == index and v.get_device() == index
         s = self._sequences(table, lengths, offsets, T, 0)
         qp = op = qs = os_ = turn = pos = None
         if q is not None:
             shape = T, self._q_heads, dim
-            assert q.shape == shape and q.dtype is dt
+            assert q.shape == shape and q.dtype is dt and q.get_device() == index
             if q_out is None:
                 q_out = torch.empty(shape, dtype=dt, device=q.device)
             else:
-                assert q_out.shape == shape and q_out.dtype is dt
+                assert q_out.shape == shape and q_out.dtype is dt and q_out.get_device() == index
             qp, qs = q.data_ptr(), known(q.stride()) or _rows(q)
             op, os_ = q_out.data_ptr(), known(q_out.stride()) or _rows(q_out)
         if rope is not None:
             assert positions.dtype is _I32 and positions.shape == (rope.n_axes, T) and positions.is_contiguous()
+            assert positions.get_device() == index and rope.index == index
             turn, pos = rope.table, positions.data_ptr()
         st = k.stride()
         ks = known(st) or _rows(k)
         rc = self._c_append(self._pages_at, layer, s, k.data_ptr(), ks, v.data_ptr(), ks if v.stride() == st else _rows(v), qp, qs, op, os_,
-                            turn, pos, _stream_of(self._index))
+                            turn, pos, _stream_of(index))
         if rc:
             _check(rc, "mukv_paged_append")
         return q_out
@@ -869,7 +877,7 @@ class PagedKV(_Sequences):
         by weights, float32 [layer][sequence][KV head][row].  The rows that stay are packed in their order, in place or into the
         pages of the table `into`, and so are their weights (weights_out None: in place).  Returns the rows kept, int32
         [layer][sequence][KV head][budget] padded with -1, and the new lengths (lengths_out may be lengths)."""
-        p = self._pages
+        p, index = self._pages, self._index
         s = self._sequences(table, lengths, None, 0, 0)
         n = table.shape[0]
         if weights_out is None:
@@ -878,18 +886,19 @@ class PagedKV(_Sequences):
         assert weights.dtype is torch.float32 and weights_out.dtype is torch.float32 and len(st) == 4 and st[3] == 1
         assert weights.shape[:3] == (p.n_layers, n, p.n_kv_heads)
         assert weights_out.shape == weights.shape and weights_out.stride() == st
+        assert weights.get_device() == index and weights_out.get_device() == index
         if into is not None:
-            assert into.dtype is _I32 and into.is_contiguous() and into.dim() == 2 and into.shape[0] == n
+            assert into.dtype is _I32 and into.is_contiguous() and into.dim() == 2 and into.shape[0] == n and into.get_device() == index
         shape = (p.n_layers, n, p.n_kv_heads, budget)
         if kept is None:
             kept = torch.empty(shape, dtype=_I32, device=self.device)
         if lengths_out is None:
             lengths_out = torch.empty_like(lengths)
         assert kept.dtype is _I32 and lengths_out.dtype is _I32 and kept.shape == shape and lengths_out.shape == lengths.shape
-        assert kept.is_contiguous() and lengths_out.is_contiguous()
+        assert kept.is_contiguous() and lengths_out.is_contiguous() and kept.get_device() == index and lengths_out.get_device() == index
         w = _WEIGHTS.pack(weights.data_ptr(), weights_out.data_ptr(), *st[:3], weights.shape[3], 0.0)
         mukv_paged_evict(self._pages_at, s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1],
-                         kept.data_ptr(), lengths_out.data_ptr(), _stream_of(self._index))
+                         kept.data_ptr(), lengths_out.data_ptr(), _stream_of(index))
         return kept, lengths_out
 
 
@@ -907,7 +916,8 @@ class PackedKV(_Sequences):
         assert v.shape == k.shape and v.stride() == st and (st[2] == 1 or T == 0)
         assert q.shape == (T, self._q_heads, D) and q.dtype is k.dtype and k.dtype is v.dtype
         assert offsets.dtype is _I32 and offsets.is_contiguous()
-        index, dtype, n = k.device.index or 0, _dtype(k), offsets.numel() - 1
+        index, dtype, n = k.get_device(), _dtype(k), offsets.numel() - 1
+        assert index >= 0 and v.get_device() == index and q.get_device() == index and offsets.get_device() == index
         if T == 0 and weights_out is None:
             return q if out is None else out
         pages = _PAGED.pack(k.data_ptr(), v.data_ptr(), 0, 0, st[1], st[0], 1, 1, T if T > 0 else 1, self._q_heads, hkv, D, dtype, index)

@@ -192,3 +192,90 @@ def test_structures_are_packed_as_they_are_declared():
         numbers = list(range(1, len(kind._fields_) + 1))
         got = kind.from_buffer_copy(layout.pack(*numbers))
         assert [getattr(got, name) for name, _ in kind._fields_] == numbers
+
+
+# ---- tensors that lie elsewhere ----
+PLACES = [-1, 1]   # host memory, another device
+
+
+@pytest.fixture
+def refuses(monkeypatch):
+    """Nothing may be launched; a call with one of its tensors elsewhere raises."""
+    reached = []
+    for name in ("mukv_rope", "mukv_paged_append", "mukv_paged_attend", "mukv_paged_evict"):
+        monkeypatch.setattr(mk, name, lambda *a: reached.append(a))
+    real = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: real(*a, **kw))
+    monkeypatch.setattr(mk, "_stream_of", lambda index: 0)
+
+    def check(call, names, place, cache=None):
+        if cache is not None:
+            cache._c_append = cache._c_attend = lambda *a: reached.append(a) or 0
+            cache._c_capture = lambda stream, at: 0
+        call({})
+        assert reached, "the call itself goes through"
+        reached.clear()
+        for name in names:
+            with pytest.raises(AssertionError):
+                call({name: place})
+            assert not reached, name
+
+    return check
+
+
+def tensors(where, **shapes):
+    kinds = {"i": torch.int32, "f": torch.float32, "d": torch.float64, "b": torch.bfloat16}
+    return {name: Stand(*shape, dtype=kinds[kind], device=where.get(name, 0)) for name, (kind, *shape) in shapes.items()}
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_rotations_refuse_tensors_that_lie_elsewhere(refuses, place):
+    def call(where):
+        t = tensors(where, inv_freq=("d", 16), axis=("i", 16), x=("b", 3, 2, 32), positions=("i", 2, 3), out=("b", 3, 2, 32))
+        mk.Rope(t["inv_freq"], t["axis"], n_axes=2).rotate(t["x"], t["positions"], out=t["out"])
+
+    refuses(call, ["inv_freq", "axis", "x", "positions", "out"], place)
+
+
+SEQUENCES = dict(table=("i", 2, 5), lengths=("i", 2), offsets=("i", 3))
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_append_refuses_tensors_that_lie_elsewhere(refuses, place):
+    c = mk.PagedKV(Stand(1, 9, 2, 16, 64), Stand(1, 9, 2, 16, 64), n_q_heads=4)
+
+    def call(where):
+        t = tensors(where, **SEQUENCES, k=("b", 3, 2, 64), v=("b", 3, 2, 64), q=("b", 3, 4, 64), q_out=("b", 3, 4, 64), positions=("i", 1, 3))
+        rope = mk.Rope(Stand(16, dtype=torch.float64, device=max(where.get("rope", 0), 0)))
+        c.append(0, **t, rope=rope)
+
+    names = [*SEQUENCES, "k", "v", "q", "q_out", "positions"]
+    refuses(call, names if place < 0 else [*names, "rope"], place, c)
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_attention_refuses_tensors_that_lie_elsewhere(refuses, place):
+    c = mk.PagedKV(Stand(1, 9, 2, 16, 64), Stand(1, 9, 2, 16, 64), n_q_heads=4)
+    rows = dict(q=("b", 3, 4, 64), out=("b", 3, 4, 64), weights=("f", 2, 2, 80), weights_out=("f", 2, 2, 80))
+    refuses(lambda where: c.attend(0, **tensors(where, **SEQUENCES, **rows)), [*SEQUENCES, *rows], place, c)
+    packed = mk.PackedKV(n_q_heads=4)
+    rows = dict(rows, k=("b", 3, 2, 64), v=("b", 3, 2, 64), offsets=("i", 3))
+    refuses(lambda where: packed.attend(**tensors(where, **rows)), rows, place, packed)
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_eviction_refuses_tensors_that_lie_elsewhere(refuses, place):
+    c = mk.PagedKV(Stand(1, 9, 2, 16, 64), Stand(1, 9, 2, 16, 64), n_q_heads=4)
+    rest = dict(table=("i", 2, 5), lengths=("i", 2), weights=("f", 1, 2, 2, 80), weights_out=("f", 1, 2, 2, 80), into=("i", 2, 5),
+                kept=("i", 1, 2, 2, 40), lengths_out=("i", 2))
+    refuses(lambda where: c.evict(budget=40, **tensors(where, **rest)), rest, place, c)
+
+
+def test_pages_in_host_memory_are_refused():
+    for where in ((-1, -1), (0, -1), (0, 1)):
+        with pytest.raises(AssertionError):
+            mk.PagedKV(*(Stand(1, 9, 2, 16, 64, device=d) for d in where), n_q_heads=4)
+    with pytest.raises(AssertionError):   # real ones
+        mk.PagedKV(torch.zeros(1, 2, 2, 4, 64), torch.zeros(1, 2, 2, 4, 64), n_q_heads=4)
+    with pytest.raises(AssertionError):
+        mk.Rope(torch.ones(16, dtype=torch.float64))
