@@ -679,7 +679,8 @@ typedef struct mukv_row_weights {
  *
  * Arithmetic in fp32, sums in an order that does not depend on timing; `out` is rounded to
  * the payload dtype.
- * n_tokens = 0 does nothing, except that weights are brought from in to out.
+ * n_tokens = 0 does nothing, except that weights are brought from in to out; packed, where
+ * there are no rows either, nothing at all, and pages need no address.
  * Errors: INVALID_ARG, SHAPE, CAPACITY (workspace too small), UNSUPPORTED.
  */
 enum { MUKV_PAGED_CLEAR = 8192 };

@@ -918,8 +918,8 @@ class PackedKV(_Sequences):
         assert offsets.dtype is _I32 and offsets.is_contiguous()
         index, dtype, n = k.get_device(), _dtype(k), offsets.numel() - 1
         assert index >= 0 and v.get_device() == index and q.get_device() == index and offsets.get_device() == index
-        if T == 0 and weights_out is None:
-            return q if out is None else out
+        if T == 0:   # (no sequence has a row, so none has a weight either)
+            return torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         pages = _PAGED.pack(k.data_ptr(), v.data_ptr(), 0, 0, st[1], st[0], 1, 1, T if T > 0 else 1, self._q_heads, hkv, D, dtype, index)
         s = _SEQS.pack(0, 0, offsets.data_ptr(), n, 0, T, max_new)
         return self._attend(pages, s, index, (n, hkv), (T, n, max_new, weights_out is None, hkv, D, dtype), 0, q, causal, out, weights,

@@ -25,9 +25,10 @@ int check_stride(int64_t stride, int64_t count, int esz) {
 
 int64_t in_bytes(int64_t stride, int64_t count, int esz) { return count > 1 ? stride * esz : 0; }
 
-int check_pages(const mukv_paged *p) {
-    if (!p || !p->k_pages || !p->v_pages) return MUKV_ERR_INVALID_ARG;
-    if (p->n_layers < 1 || p->n_pages < 1 || p->page_rows < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->device_id < 0)
+// empty: no row is ever looked at, and empty tensors need not have an address
+int check_pages(const mukv_paged *p, bool empty = false) {
+    if (!p || (!empty && (!p->k_pages || !p->v_pages))) return MUKV_ERR_INVALID_ARG;
+    if (p->n_layers < 1 || p->n_pages < 1 || p->page_rows < (empty ? 0 : 1) || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->device_id < 0)
         return MUKV_ERR_INVALID_ARG;
     if (p->dtype != MUKV_BF16 && p->dtype != MUKV_F32) return MUKV_ERR_INVALID_ARG;
     if (p->n_q_heads % p->n_kv_heads) return MUKV_ERR_SHAPE;
@@ -41,6 +42,8 @@ int check_pages(const mukv_paged *p) {
     if (!aligned(p->k_pages) || !aligned(p->v_pages)) return MUKV_ERR_UNSUPPORTED;
     return MUKV_OK;
 }
+
+bool packed_nothing(const mukv_seqs *s) { return s && !s->table && s->n_tokens == 0; }
 
 int check_seqs(const mukv_paged *p, const mukv_seqs *s, bool may_be_packed, bool has_tokens) {
     if (!s) return MUKV_ERR_INVALID_ARG;
@@ -219,7 +222,7 @@ int mukv_stream_capture(void *stream, uint64_t *id_out) {
 static_assert(MUKV_PAGED_CLEAR == 4 * mukv::kPlanRecords, "the counts");
 int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, int32_t with_weights, int64_t *bytes_out) {
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
-    if (const int rc = check_pages(pages)) return rc;
+    if (const int rc = check_pages(pages, packed_nothing(seqs))) return rc;
     if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
     *bytes_out = space_of(*pages, *seqs, true, with_weights != 0).bytes;
     return MUKV_OK;
@@ -228,13 +231,13 @@ int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, in
 int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *seqs, const void *q,
                       const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
                       void *workspace, int64_t workspace_bytes, void *stream) {
-    if (const int rc = check_pages(pages)) return rc;
+    if (const int rc = check_pages(pages, packed_nothing(seqs))) return rc;
     if (layer < 0 || layer >= pages->n_layers || (causal != 0 && causal != 1)) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
     if (weights)
         if (const int rc = check_weights(weights)) return rc;
     const int T = seqs->n_tokens, D = pages->head_dim, esz = elem_size(pages->dtype);
-    if (T == 0 && !weights) return MUKV_OK;
+    if (T == 0 && (!weights || !seqs->table)) return MUKV_OK; // (packed, no sequence has a row that could have a weight)
     const mukv_strides dense = {0, D, (int64_t)D * pages->n_q_heads};
     const mukv_strides *qs = q_strides ? q_strides : &dense;
     if (T > 0) { // (empty tensors need not have an address)

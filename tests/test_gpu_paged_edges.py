@@ -91,3 +91,11 @@ def test_threads_on_streams_of_their_own_share_a_cache(dtype):
     [t.start() for t in all_of_them]
     [t.join() for t in all_of_them]
     assert not wrong
+
+
+def test_packed_sequences_of_no_tokens():
+    q, k = (torch.empty(0, h, 64, dtype=BF16, device="cuda") for h in (4, 2))
+    off, w = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.full((2, 2, 7), 5.0, device="cuda")
+    for kw in ({}, dict(weights_out=w), dict(weights=w, weights_out=w, decay=0.5)):
+        assert mk.PackedKV(n_q_heads=4).attend(q, k, k, off, **kw).shape == (0, 4, 64)
+    assert (w == 5.0).all()   # rows past a sequence's length are left as they are

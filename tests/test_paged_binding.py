@@ -279,3 +279,34 @@ def test_pages_in_host_memory_are_refused():
         mk.PagedKV(torch.zeros(1, 2, 2, 4, 64), torch.zeros(1, 2, 2, 4, 64), n_q_heads=4)
     with pytest.raises(AssertionError):
         mk.Rope(torch.ones(16, dtype=torch.float64))
+
+
+def test_packed_sequences_of_no_tokens_are_no_error(monkeypatch):
+    """Empty tensors have no address; with weights or without, there is nothing to do."""
+    real = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: real(*a, **kw))
+    monkeypatch.setattr(mk, "_stream_of", lambda index: 0)
+    packed = mk.PackedKV(n_q_heads=4)
+    packed._c_capture = lambda stream, at: 0
+    t = dict(q=Stand(0, 4, 64), k=Stand(0, 2, 64), v=Stand(0, 2, 64), offsets=i32(3))
+    for name in "qkv":
+        t[name]._at = 0
+    out, w = Stand(0, 4, 64), Stand(2, 2, 7, dtype=torch.float32)
+    assert packed.attend(**t, out=out) is out and packed.attend(**t, out=out, weights_out=w) is out
+    got = packed.attend(**t, weights=w, weights_out=w)
+    assert got.shape == (0, 4, 64) and got is not t["q"] and packed.attend(**t) is not t["q"]
+
+
+def test_packed_nothing_is_no_error_at_the_c_entry():
+    pages = mk.mukv_paged(None, None, 0, 0, 64, 128, 1, 1, 0, 4, 2, 64, mk.MUKV_BF16, 0)
+    seqs = mk.mukv_seqs(None, None, 1 << 20, 2, 0, 0, 0)
+    rows = mk.mukv_row_weights(1 << 20, 1 << 20, 0, 14, 7, 7, 1.0)
+    size = C.c_int64()
+    lib, at = mk.load(), C.addressof
+    assert lib.mukv_paged_workspace_size(at(pages), at(seqs), 1, C.byref(size)) == mk.MUKV_OK and size.value >= mk.MUKV_PAGED_CLEAR
+    for w in (None, at(rows)):
+        assert lib.mukv_paged_attend(at(pages), 0, at(seqs), None, None, 1, None, w, None, 0, None) == mk.MUKV_OK
+    seqs.n_tokens = 3   # but of some tokens it is
+    assert lib.mukv_paged_attend(at(pages), 0, at(seqs), 1 << 20, None, 1, 1 << 20, None, 1 << 20, 1 << 40, None) == mk.MUKV_ERR_INVALID_ARG
+    seqs.n_tokens, seqs.table, seqs.lengths, seqs.table_width = 0, 1 << 20, 1 << 20, 4   # and of pages
+    assert lib.mukv_paged_attend(at(pages), 0, at(seqs), None, None, 1, None, None, None, 0, None) == mk.MUKV_ERR_INVALID_ARG
