@@ -582,7 +582,9 @@ typedef struct mukv_seqs {
     const int32_t *lengths; /* device [n_seqs]                                                  */
     const int32_t *offsets; /* device [n_seqs+1]: sequence b owns the new tokens offsets[b] ..
                                offsets[b+1]-1, ascending from 0 to n_tokens; NULL: n_tokens / n_seqs
-                               tokens each                                                      */
+                               tokens each.  What is outside 0 .. n_tokens is brought inside; where those
+                               of several sequences do not ascend, mukv_paged_attend leaves out as it
+                               is, and what weights receive is undefined                        */
     int32_t n_seqs;         /* 1 .. 65536                                                       */
     int32_t table_width;    /* pages a sequence can have                                        */
     int32_t n_tokens;       /* new tokens of all sequences                                      */

@@ -126,7 +126,7 @@ __device__ __forceinline__ void next_unit(const PagedView &v, const PlanShape &p
     }
 }
 
-// The unit of this workgroup, the same in all lanes; false: there is none.
+// The unit of this workgroup, the same in all lanes; false: there is none (nobody has one where offsets do not ascend).
 __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p, int id, Unit *u) {
     const int lane = threadIdx.x & 63;
     if (v.n_seqs == 1) {
@@ -137,14 +137,17 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
         const SeqShape none = {0, 0, 0, 0, 0, 1};
         SeqShape s = none;
         PlanSums all = {0.f, 0.f, 0.f, 0.f};
+        bool fit = true;
         for (int b0 = 0; b0 < v.n_seqs; b0 += 64) {
             s = b0 + lane < v.n_seqs ? shape_of(v, p, b0 + lane) : none;
+            fit = fit && (b0 + lane >= v.n_seqs || offsets_fit(v, b0 + lane));
             const PlanSums x = sums_of(v, p, s);
             all.tiles += x.tiles;
             all.blocks += x.blocks;
             all.seen += x.seen;
             all.longest = fmaxf(all.longest, x.longest);
         }
+        if (__builtin_amdgcn_ballot_w64(!fit) != 0) return false;
         all.blocks = wave_sum(all.blocks);
         all.tiles = wave_sum(all.tiles);
         all.longest = wave_max(all.longest);

@@ -34,6 +34,11 @@ MUKV_HD void tokens_of(const PagedView &v, int b, int *first, int *count) {
     *count = hi - lo;
 }
 
+// Whether sequence b's offsets ascend.  Where all of a call's do, no token is two sequences' (brought inside 0 .. n_tokens they still ascend), which
+// units_bound reckons with: otherwise a tile's chunks could be more than there are workgroups, and those that ran would wait in the counts
+// for the next call.
+MUKV_HD bool offsets_fit(const PagedView &v, int b) { return !v.offsets || v.offsets[b] <= v.offsets[b + 1]; }
+
 // Rows the table has room for.
 MUKV_HD int64_t room_of(const PagedView &v) { return (int64_t)v.table_width * v.page_rows; }
 

@@ -99,3 +99,30 @@ def test_packed_sequences_of_no_tokens():
     for kw in ({}, dict(weights_out=w), dict(weights=w, weights_out=w, decay=0.5)):
         assert mk.PackedKV(n_q_heads=4).attend(q, k, k, off, **kw).shape == (0, 4, 64)
     assert (w == 5.0).all()   # rows past a sequence's length are left as they are
+
+
+# ---- offsets that do not ascend ----
+def test_offsets_that_overlap_leave_nothing_behind():
+    """Tokens that are two sequences': more units than workgroups, of a tile some chunks and not others (tests/test_paged_offsets.py walks through
+    it).  The next call on the same scratch is what it is on fresh scratch."""
+    c = Case([(32, 128), (0, 50), (0, 384)], 64, 8, 1, 16, BF16, seed=30)
+    table, lengths = torch.tensor(c.table, device="cuda"), torch.tensor(c.lengths, device="cuda")
+    off = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    good, bad = off(0, 0, 0, 32), off(0, 32, 0, 32)
+    fresh = mk.PagedKV(c.kp, c.vp, n_q_heads=8)
+    want = fresh.attend(1, table, lengths, c.q, offsets=good)
+    for _ in range(3):
+        out = torch.full_like(c.q, 7.0)
+        c.cache.attend(1, table, lengths, c.q, offsets=bad, out=out)
+        assert (out == 7.0).all()
+        assert torch.equal(c.cache.attend(1, table, lengths, c.q, offsets=good), want)
+    c.news, c.off, c.lengths = np.array([0, 0, 32], np.int32), np.array([0, 0, 0, 32], np.int32), c.lengths
+    c.check(want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_past_the_tokens_are_brought_inside(dtype):
+    c = Case([(3, 40), (40, 300), (5, 64)], 64, 8, 1, 16, dtype, seed=31)
+    want = c.attend()
+    c.off[0], c.off[3] = -9, 2**31 - 1
+    assert torch.equal(c.attend(), want)
