@@ -681,6 +681,8 @@ typedef struct mukv_row_weights {
  *
  * Arithmetic in fp32, sums in an order that does not depend on timing; `out` is rounded to
  * the payload dtype.
+ * Values are added up, by weights of at most 1, before they are divided: an output is finite
+ * where the largest value times the sum of those weights is finite in fp32.
  * n_tokens = 0 does nothing, except that weights are brought from in to out; packed, where
  * there are no rows either, nothing at all, and pages need no address.
  * Errors: INVALID_ARG, SHAPE, CAPACITY (workspace too small), UNSUPPORTED.

@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kFRows = 64; // rows of a step
 constexpr int kRing = 8;                       // steps whose rows' places are held
-// 2^24: sums of weights past this are worked out again (see below).  Values of up to 2^100 or so stay in range.
+// 2^24: sums of weights past this are worked out again (see below).
 constexpr float kMostSum = 16777216.f;
 
 // sum of two bf16 and x, in fp32
@@ -48,19 +48,25 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     bf16x8 qb[kQB][KK];
     int my_tok[kQB];
 #pragma unroll
-    for (int i = 0; i < kQB; ++i) {
+    for (int i = 0; i < kQB; ++i) { // nothing is visible to a query that does not exist
         const int qq = q0 + 32 * i + lq;
-        const bool ok = qq < n_queries;
-        const int tok = ok ? qq / G : 0;
-        my_tok[i] = ok ? tok : INT_MIN; // nothing is visible to a query that does not exist
-        const unsigned char *qp = a.q + (int64_t)(u.s.first + tok) * a.q_token + (int64_t)(g * G + (ok ? qq - tok * G : 0)) * a.q_head + 16 * half;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            raw16 x = *reinterpret_cast<const raw16 *>(qp + 32 * kk);
-            if (!ok) x = raw16{0u, 0u, 0u, 0u};
-            qb[i][kk] = __builtin_bit_cast(bf16x8, x);
-        }
+        my_tok[i] = qq < n_queries ? qq / G : INT_MIN;
     }
+    auto load_queries = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            const bool ok = my_tok[i] >= 0;
+            const int tok = ok ? my_tok[i] : 0;
+            const unsigned char *qp =
+                a.q + (int64_t)(u.s.first + tok) * a.q_token + (int64_t)(g * G + (ok ? q0 + 32 * i + lq - tok * G : 0)) * a.q_head + 16 * half;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                raw16 x = *reinterpret_cast<const raw16 *>(qp + 32 * kk);
+                if (!ok) x = raw16{0u, 0u, 0u, 0u};
+                qb[i][kk] = __builtin_bit_cast(bf16x8, x);
+            }
+        }
+    };
     const int first_tok = u.tile * kFQ / G;
     const int last_q = u.tile * kFQ + kFQ - 1 < n_queries ? u.tile * kFQ + kFQ - 1 : n_queries - 1, last_tok = last_q / G;
     const int past = u.s.length - n_new;
@@ -380,113 +386,142 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             page = page_at((h >> 1) + 9 + wave);
         }
     };
+    T *const out = static_cast<T *>(a.out);
+    float l_sum[kQB], at[kQB]; // sum of the weights, and what they are relative to
+    // o over the sums of weights to `out`.  past: becomes a NaN where an output is none, or past what fp32 holds
+    auto put_results = [&](float(*past)[kQB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            const int qq = q0 + 32 * i + lq;
+            const bool ok = qq < n_queries, seen = l_sum[i] != 0.f; // a query that saw nothing gets zeros; NaN stays NaN
+            const float inv = 1.f / l_sum[i];
+            const int tok = ok ? my_tok[i] : 0;
+            const int64_t row = (int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0);
+            T *const op = out + row * D + 8 * half;
+            if (PAIRS && ok && half == 0) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = seen ? f32x2{at[i], inv} : f32x2{0.f, 0.f};
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int jj = 0; jj < 4; jj += 2) { // a lane holds features 8 jj + 4 half .. + 3: the halves swap, and it stores 16 bytes
+                    raw16 w;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t pk[2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float y0 = o[i][f][4 * (jj + x) + 2 * e], y1 = o[i][f][4 * (jj + x) + 2 * e + 1];
+                            pk[x] = bf16_pair(y0 * inv, y1 * inv);
+                            if (past) (*past)[i] = fmaf(y1, 0.f, fmaf(y0, 0.f, (*past)[i]));
+                        }
+                        auto sw = __builtin_amdgcn_permlane32_swap(pk[0], pk[1], false, false);
+                        w[e] = sw[0];
+                        w[2 + e] = sw[1];
+                    }
+                    if (!seen) w = raw16{0u, 0u, 0u, 0u};
+                    if (ok) *reinterpret_cast<raw16 *>(op + 32 * f + 8 * jj) = w;
+                }
+        }
+    };
+    // The chunk's record: values as they stand in the lanes, so that every access is a kilobyte in a row (query by query they were
+    // 16-byte pieces of lines: a call of 220 tiles in two chunks 122 us, unsplit 70).  The last workgroup of the tile to get here
+    // joins them, in their order.
+    auto piece = [&](int i, int f, int jj) { return (((wave * kQB + i) * NF + f) * 4 + jj) * 256 + 4 * lane; };
     // What exponents subtract is the largest score of the unit's first half, and stays: weights then are what they are, not at most
     // 1, and floating point holds them as well, so nothing in the loop waits for a maximum or brings sums to another one.  Sums that
-    // grow large (a later score larger by 24 log2 units or so) are worked out again with the largest score of all rows.
-    if (n_halves > 0)
+    // grow large (a later score larger by 24 log2 units or so), or take an output past what fp32 holds, are worked out again with the
+    // largest score of all rows.  Outputs are looked at on their way out, where they are in reach of vector instructions anyway.
     for (bool again = false;; again = true) {
-        if (__builtin_expect(again, 0)) {
-            stage();
+        load_queries();
+        if (n_halves > 0) {
+            if (__builtin_expect(again, 0)) {
+                stage();
 #pragma unroll
-            for (int i = 0; i < kQB; ++i) ref[i] = -INFINITY;
-            auto max_of = [&](auto par, int h) __attribute__((always_inline)) {
-                scores_of(par, sc[0]);
-                if (is_masked(h)) hide(h, sc[0]);
+                for (int i = 0; i < kQB; ++i) ref[i] = -INFINITY;
+                auto max_of = [&](auto par, int h) __attribute__((always_inline)) {
+                    scores_of(par, sc[0]);
+                    if (is_masked(h)) hide(h, sc[0]);
 #pragma unroll
-                for (int i = 0; i < kQB; ++i) ref[i] = fmaxf(ref[i], largest(sc[0][i]));
-            };
+                    for (int i = 0; i < kQB; ++i) ref[i] = fmaxf(ref[i], largest(sc[0][i]));
+                };
 #pragma unroll 1
-            for (int h = 0; h < n_halves; h += 2) {
-                max_of(std::integral_constant<int, 0>{}, h);
-                max_of(std::integral_constant<int, 1>{}, h + 1);
-                rows_landed(); // of the next step; this one's keys are done with
-                __syncthreads();
-                request((h >> 1) + 2);
-                next_keys();
-                next_places(h + 1);
-            }
-        }
-        stage();
-        if (tid < 2) s_bad[tid] = 0;
-        if (tid == 0) s_any = 0;
-        for (int i = tid; i < 2 * kFQ * (D / 32); i += 256) (&s_inf[0][0][0])[i] = 0u;
-        scores_of(std::integral_constant<int, 0>{}, sc[0]);
-        if (!again) {
-            f32x16 s[kQB];
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) s[i] = sc[0][i];
-            if (is_masked(0)) hide(0, s);
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) ref[i] = largest(s[i]);
-        }
-        set_ref();
-#pragma unroll
-        for (int i = 0; i < kQB; ++i) {
-            l_run[i] = 0.f;
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
-        }
-        __syncthreads(); // the flags are cleared
-        load_ahead(std::integral_constant<int, 0>{});
-#pragma unroll
-        for (int i = 0; i < kQB; ++i) asm volatile("" : "+v"(sc[0][i]));
-        look(std::integral_constant<int, 0>{}, 0, s_masked[0][0]);
-#pragma unroll 1
-        for (int h = 0; h < n_halves; h += 2) { // (an odd half out is joined by one whose rows nobody sees)
-            const int odd = step(std::integral_constant<int, 0>{}, h);
-            look(std::integral_constant<int, 1>{}, h + 1, odd);
-            const int even = step(std::integral_constant<int, 1>{}, h + 1);
-            next_places(h + 1);
-            look(std::integral_constant<int, 0>{}, h + 2, even);
-        }
-        if (again) break;
-        bool out_of_range = false;
-#pragma unroll
-        for (int i = 0; i < kQB; ++i) // (no row of the first half seen, but perhaps others: not with all pages there)
-            out_of_range |= l_run[i] > kMostSum || (ref[i] == -INFINITY && n_halves > 1 && my_tok[i] >= (a.causal ? row0 + 32 - past : 0));
-        if (__builtin_amdgcn_ballot_w64(out_of_range) != 0 && lane == 0) s_again = 1;
-        __syncthreads();
-        if (__builtin_expect(s_again == 0, 1)) break;
-    }
-    if (n_halves == 0) {
-#pragma unroll
-        for (int i = 0; i < kQB; ++i) {
-            ref[i] = l_run[i] = 0.f;
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
-        }
-    }
-    // ---- results ----
-    if (n_halves > 0 && __builtin_expect(s_any != 0, 0)) {
-#pragma unroll
-        for (int i = 0; i < kQB; ++i)
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                const unsigned up = s_inf[0][32 * (kQB * wave + i) + lq][f], down = s_inf[1][32 * (kQB * wave + i) + lq][f];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int d = 8 * (j / 4) + 4 * half + j % 4;
-                    if (up >> d & 1) o[i][f][j] += INFINITY;
-                    if (down >> d & 1) o[i][f][j] -= INFINITY;
+                for (int h = 0; h < n_halves; h += 2) {
+                    max_of(std::integral_constant<int, 0>{}, h);
+                    max_of(std::integral_constant<int, 1>{}, h + 1);
+                    rows_landed(); // of the next step; this one's keys are done with
+                    __syncthreads();
+                    request((h >> 1) + 2);
+                    next_keys();
+                    next_places(h + 1);
                 }
             }
-    }
-    float l_sum[kQB], at[kQB]; // sum of the weights, and what they are relative to
+            stage();
+            if (tid < 2) s_bad[tid] = 0;
+            if (tid == 0) s_any = 0;
+            for (int i = tid; i < 2 * kFQ * (D / 32); i += 256) (&s_inf[0][0][0])[i] = 0u;
+            scores_of(std::integral_constant<int, 0>{}, sc[0]);
+            if (!again) {
+                f32x16 s[kQB];
 #pragma unroll
-    for (int i = 0; i < kQB; ++i) {
-        l_sum[i] = half_sum(l_run[i]);
-        at[i] = base_of(i);
-    }
-    if (u.chunks > 1) {
-        // The chunk's record: values as they stand in the lanes, so that every access is a kilobyte in a row (query by query they were
-        // 16-byte pieces of lines: a call of 220 tiles in two chunks 122 us, unsplit 70).  The last workgroup of the tile to get here
-        // joins them, in their order.
-        auto piece = [&](int i, int f, int jj) { return (((wave * kQB + i) * NF + f) * 4 + jj) * 256 + 4 * lane; };
-        {
+                for (int i = 0; i < kQB; ++i) s[i] = sc[0][i];
+                if (is_masked(0)) hide(0, s);
+#pragma unroll
+                for (int i = 0; i < kQB; ++i) ref[i] = largest(s[i]);
+            }
+            set_ref();
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) {
+                l_run[i] = 0.f;
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
+            }
+            __syncthreads(); // the flags are cleared
+            load_ahead(std::integral_constant<int, 0>{});
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) asm volatile("" : "+v"(sc[0][i]));
+            look(std::integral_constant<int, 0>{}, 0, s_masked[0][0]);
+#pragma unroll 1
+            for (int h = 0; h < n_halves; h += 2) { // (an odd half out is joined by one whose rows nobody sees)
+                const int odd = step(std::integral_constant<int, 0>{}, h);
+                look(std::integral_constant<int, 1>{}, h + 1, odd);
+                const int even = step(std::integral_constant<int, 1>{}, h + 1);
+                next_places(h + 1);
+                look(std::integral_constant<int, 0>{}, h + 2, even);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) {
+                ref[i] = l_run[i] = 0.f;
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
+            }
+        }
+        // ---- results ----
+        if (n_halves > 0 && __builtin_expect(s_any != 0, 0)) {
+#pragma unroll
+            for (int i = 0; i < kQB; ++i)
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    const unsigned up = s_inf[0][32 * (kQB * wave + i) + lq][f], down = s_inf[1][32 * (kQB * wave + i) + lq][f];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int d = 8 * (j / 4) + 4 * half + j % 4;
+                        if (up >> d & 1) o[i][f][j] += INFINITY;
+                        if (down >> d & 1) o[i][f][j] -= INFINITY;
+                    }
+                }
+        }
+        float past_it[kQB];
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            l_sum[i] = half_sum(l_run[i]);
+            at[i] = base_of(i);
+            past_it[i] = 0.f;
+        }
+        if (u.chunks > 1) {
             const auto values = chunk_values<kFQ, D>(a.records, u.record + u.chunk);
             float *const stats = a.records.stats + (int64_t)(u.record + u.chunk) * kFQ * 2;
 #pragma unroll
@@ -495,77 +530,66 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
-                    for (int jj = 0; jj < 4; ++jj)
-                        store_far4(values, piece(i, f, jj), f32x4{o[i][f][4 * jj], o[i][f][4 * jj + 1], o[i][f][4 * jj + 2], o[i][f][4 * jj + 3]});
+                    for (int jj = 0; jj < 4; ++jj) {
+                        const f32x4 y = {o[i][f][4 * jj], o[i][f][4 * jj + 1], o[i][f][4 * jj + 2], o[i][f][4 * jj + 3]};
+                        store_far4(values, piece(i, f, jj), y);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) past_it[i] = fmaf(y[e], 0.f, past_it[i]);
+                    }
             }
+        } else {
+            put_results(&past_it);
         }
-        if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
-        const float *const stats = a.records.stats + ((int64_t)u.record * kFQ + 32 * kQB * wave + lq) * 2;
+        if (again || n_halves == 0) break;
+        bool out_of_range = false;
 #pragma unroll
-        for (int i = 0; i < kQB; ++i) {
-            at[i] = -INFINITY;
-            l_sum[i] = 0.f;
-#pragma unroll 8
-            for (int c = 0; c < u.chunks; ++c) {
-                const f32x2 st = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
-                at[i] = st[1] != 0.f ? fmaxf(at[i], st[0]) : at[i]; // (else none of the chunk's rows is seen; a NaN is)
-            }
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
+        for (int i = 0; i < kQB; ++i) { // (no row of the first half seen, but perhaps others: not with all pages there)
+            out_of_range |= l_run[i] > kMostSum || (ref[i] == -INFINITY && n_halves > 1 && my_tok[i] >= (a.causal ? row0 + 32 - past : 0));
+            out_of_range |= past_it[i] != past_it[i] && l_sum[i] == l_sum[i];
         }
-#pragma unroll 1
-        for (int c = 0; c < u.chunks; ++c) {
-            const auto values = chunk_values<kFQ, D>(a.records, u.record + c);
-            f32x2 st[kQB];
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) st[i] = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) {
-                f32x4 x[NF][4];
-#pragma unroll
-                for (int f = 0; f < NF; ++f)
-#pragma unroll
-                    for (int jj = 0; jj < 4; ++jj) x[f][jj] = load_far4(values, piece(i, f, jj));
-                const bool some = st[i][1] != 0.f;
-                const float by = some ? __builtin_amdgcn_exp2f(st[i][0] - at[i]) : 0.f;
-                if (some) l_sum[i] = fmaf(st[i][1], by, l_sum[i]);
-#pragma unroll
-                for (int f = 0; f < NF; ++f)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[i][f][j] = some ? fmaf(x[f][j / 4][j % 4], by, o[i][f][j]) : o[i][f][j];
-            }
-        }
+        if (__builtin_amdgcn_ballot_w64(out_of_range) != 0 && lane == 0) s_again = 1;
+        __syncthreads();
+        if (__builtin_expect(s_again == 0, 1)) break;
     }
-    T *const out = static_cast<T *>(a.out);
+    if (u.chunks == 1 || !last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
+    const float *const stats = a.records.stats + ((int64_t)u.record * kFQ + 32 * kQB * wave + lq) * 2;
 #pragma unroll
     for (int i = 0; i < kQB; ++i) {
-        const int qq = q0 + 32 * i + lq;
-        const bool ok = qq < n_queries, seen = l_sum[i] != 0.f; // a query that saw nothing gets zeros; NaN stays NaN
-        const float inv = 1.f / l_sum[i];
-        const int tok = ok ? my_tok[i] : 0;
-        const int64_t row = (int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0);
-        T *const op = out + row * D + 8 * half;
-        if (PAIRS && ok && half == 0) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = seen ? f32x2{at[i], inv} : f32x2{0.f, 0.f};
+        at[i] = -INFINITY;
+        l_sum[i] = 0.f;
+#pragma unroll 8
+        for (int c = 0; c < u.chunks; ++c) {
+            const f32x2 st = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
+            at[i] = st[1] != 0.f ? fmaxf(at[i], st[0]) : at[i]; // (else none of the chunk's rows is seen; a NaN is)
+        }
 #pragma unroll
         for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int jj = 0; jj < 4; jj += 2) { // a lane holds features 8 jj + 4 half .. + 3: the halves swap, and it stores 16 bytes
-                raw16 w;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint32_t pk[2];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) pk[x] = bf16_pair(o[i][f][4 * (jj + x) + 2 * e] * inv, o[i][f][4 * (jj + x) + 2 * e + 1] * inv);
-                    auto sw = __builtin_amdgcn_permlane32_swap(pk[0], pk[1], false, false);
-                    w[e] = sw[0];
-                    w[2 + e] = sw[1];
-                }
-                if (!seen) w = raw16{0u, 0u, 0u, 0u};
-                if (ok) *reinterpret_cast<raw16 *>(op + 32 * f + 8 * jj) = w;
-            }
+            for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
     }
+#pragma unroll 1
+    for (int c = 0; c < u.chunks; ++c) {
+        const auto values = chunk_values<kFQ, D>(a.records, u.record + c);
+        f32x2 st[kQB];
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) st[i] = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
+#pragma unroll
+        for (int i = 0; i < kQB; ++i) {
+            f32x4 x[NF][4];
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int jj = 0; jj < 4; ++jj) x[f][jj] = load_far4(values, piece(i, f, jj));
+            const bool some = st[i][1] != 0.f;
+            const float by = some ? __builtin_amdgcn_exp2f(st[i][0] - at[i]) : 0.f;
+            if (some) l_sum[i] = fmaf(st[i][1], by, l_sum[i]);
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][f][j] = some ? fmaf(x[f][j / 4][j % 4], by, o[i][f][j]) : o[i][f][j];
+        }
+    }
+    put_results(nullptr);
 }
 
 // A workgroup takes a unit; of one sequence's perhaps the units of its stretch, one after the other (us a launch, 28/4 heads of 128, chunks

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from paged_testlib import f64, near
+from paged_testlib import attention_error, f64, near
 from paper_2605_22269_amd import binding as mk
 from test_gpu_paged_attend import BF16, F32, Case, weights_error
 
@@ -126,3 +126,27 @@ def test_offsets_past_the_tokens_are_brought_inside(dtype):
     want = c.attend()
     c.off[0], c.off[3] = -9, 2**31 - 1
     assert torch.equal(c.attend(), want)
+
+
+# ---- values near the end of the range ----
+@pytest.mark.parametrize("seqs,room", [([(150, 400), (60, 300)], 0), ([(150, 400), (60, 300)], 9000), ([(120, 5000)], 0), ([(3, 400), (1, 300)], 0)],
+                         ids=["128", "256", "chunks", "few"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("high", [3.0, 8.0])
+def test_the_largest_values_where_rows_decide_late(D, high, seqs, room):
+    """Later rows' weights are far above 1 relative to the first rows' largest score, and the values so large that their products are past
+    fp32, though no output is."""
+    c = Case(seqs, D, 8, 2, 16, BF16, seed=D, width=-(-room // 16) if room else None)
+    for b in range(len(seqs)):
+        for j in range(40, int(c.lengths[b])):
+            c.kp[:, c.table[b][j // 16], :, j % 16] *= high
+    c.vp *= 1e35
+    got, most = c.attend(), max(int(c.lengths.max()), 1)
+    assert np.isfinite(f64(got)).all()
+    want, _, amean, reach = c.wanted()
+    near(f64(got), want, attention_error(amean, reach, most, D, BF16, True), BF16)
+    rows = torch.zeros(len(seqs), 2, most, device="cuda")
+    got, received = c.attend(weights_out=rows), c.wanted()[1]
+    near(f64(got), want, attention_error(amean, reach, most, D, BF16, True), BF16)
+    for b, n in enumerate(c.lengths):
+        near(f64(rows)[b][:, :n], received[b], (1 + received[b]) * weights_error(c, received), F32)
