@@ -668,7 +668,8 @@ typedef struct mukv_row_weights {
  * what rows hold that it does not see never reaches it.
  *
  *   q          device, [n_tokens][n_q_heads][head_dim] with strides (NULL: contiguous)
- *   out        device, [n_tokens][n_q_heads][head_dim] contiguous
+ *   out        device, [n_tokens][n_q_heads][head_dim] contiguous; must not overlap q, which may be
+ *              read again
  *   weights    NULL, or where the rows' weights go: `out` receives, for every row of
  *              every sequence, decay * in + the sum of its softmax weights over the
  *              sequence's new tokens and the heads of its KV head's group (rows on pages

@@ -130,19 +130,21 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
     a.inverse = r->inverse != 0;
 }
 
-// Which kernel takes an attention call, and its workspace: counts, records, then (with weights) a pair per query.
+// Which kernel takes an attention call, and its workspace: counts, records, then (with weights) the prompt kernel's sums and a pair per query.
 struct Space {
     mukv::PlanShape plan;
-    int64_t stats, values, pairs, bytes; // offsets; the counts are at 0
+    int64_t stats, values, sums, pairs, bytes; // offsets; the counts are at 0
 };
 Space space_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool with_weights) {
     const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
     Space x;
-    x.plan = mukv::paged_plan(p.dtype, mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint), causal);
+    const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint);
+    x.plan = mukv::paged_plan(p.dtype, tile, causal);
     const int64_t rows = (int64_t)x.plan.records * x.plan.queries;
     x.stats = 4 * mukv::kPlanRecords;
     x.values = x.stats + 8 * rows;
-    x.pairs = x.values + 4 * rows * p.head_dim;
+    x.sums = x.values + 4 * rows * p.head_dim;
+    x.pairs = x.sums + (with_weights && tile ? 4 * rows : 0);
     x.bytes = x.pairs + (with_weights ? 8 * (int64_t)s.n_tokens * p.n_q_heads : 0);
     return x;
 }
@@ -260,6 +262,7 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
     a.counts = reinterpret_cast<int *>(ws);
     a.records.stats = reinterpret_cast<float *>(ws + x.stats);
     a.records.values = reinterpret_cast<float *>(ws + x.values);
+    a.records.sums = reinterpret_cast<float *>(ws + x.sums);
     a.pairs = weights ? reinterpret_cast<float *>(ws + x.pairs) : nullptr;
     a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
     a.causal = causal;

@@ -196,6 +196,12 @@ __device__ __forceinline__ f32x4 load_far4(__amdgpu_buffer_rsrc_t r, int floats)
 __device__ __forceinline__ void store_far4(__amdgpu_buffer_rsrc_t r, int floats, f32x4 x) {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw16, x), r, 4 * floats, 0, kFar);
 }
+__device__ __forceinline__ void store_far1(float *p, float x) {
+    __hip_atomic_store(reinterpret_cast<uint32_t *>(p), __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float load_far1(const float *p) {
+    return __uint_as_float(__hip_atomic_load(reinterpret_cast<const uint32_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
 // the values of one chunk of a tile
 template <int kQueries, int D>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_values(const ChunkRecords &r, int record) {

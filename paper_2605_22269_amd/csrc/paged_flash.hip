@@ -120,7 +120,8 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     };
 
     // ---- state ----
-    float ref[kQB], l_run[kQB]; // what exponents subtract; sum of the weights over the rows this lane holds
+    // what exponents subtract; sums of the weights over the rows this lane holds, as they enter the product, and with PAIRS as they were
+    float ref[kQB], l_run[kQB], l_whole[kQB];
     f32x16 o[kQB][NF];          // features 32 f + 8 (j / 4) + 4 half + j % 4 of query lq
     f32x16 sc[2][kQB];          // scores of two halves of a step: rows 8 (j / 4) + 4 half + j % 4
     float s_scale = scale, s_ref[kQB]; // a weight is 2^(score * s_scale - s_ref)
@@ -159,16 +160,17 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     };
     auto values_of = [&](int h) { return s_kv + (2 + (h >> 1) % 3) * kBuf + (h & 1) * 32 * kRowB; };
     // weights of query block i and 16 rows as a matrix operand
-    auto weights_of = [&](const f32x16 &s, int i, int grp, float *sum) __attribute__((always_inline)) {
+    auto weights_of = [&](const f32x16 &s, int i, int grp) __attribute__((always_inline)) {
         raw16 w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e], s_scale, -s_ref[i]));
             const float y = __builtin_amdgcn_exp2f(fmaf(s[8 * grp + 2 * e + 1], s_scale, -s_ref[i]));
             w[e] = bf16_pair(x, y);
-            // (the weights as they enter the product: a row that has nearly all of it keeps its value; where the weights of rows are
-            // asked for, the sum is theirs, before the rounding)
-            *sum = PAIRS ? *sum + (x + y) : add_pair(w[e], *sum);
+            // (outputs are divided by the sum of the weights as they enter the product, so that a row that has nearly all of it keeps its
+            // value; what rows receive, in 32 bits, by that before the rounding)
+            l_run[i] = add_pair(w[e], l_run[i]);
+            if (PAIRS) l_whole[i] += x + y;
         }
         return __builtin_bit_cast(bf16x8, w);
     };
@@ -320,7 +322,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
             for (int i = 0; i < kQB; ++i) nxt[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[kk], qb[i][kk], nxt[i], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < kQB; ++i) pw[0][i] = weights_of(sc[P][i], i, 0, &l_run[i]);
+        for (int i = 0; i < kQB; ++i) pw[0][i] = weights_of(sc[P][i], i, 0);
 #pragma unroll
         for (int n = 0; n < K1 * kQB; ++n) {
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0); // reads of LDS
@@ -338,7 +340,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
             for (int i = 0; i < kQB; ++i) o[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[0][f], pw[0][i], o[i][f], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < kQB; ++i) pw[1][i] = weights_of(sc[P][i], i, 1, &l_run[i]);
+        for (int i = 0; i < kQB; ++i) pw[1][i] = weights_of(sc[P][i], i, 1);
 #pragma unroll
         for (int n = 0; n < (KK - K1 + NF) * kQB; ++n) {
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
@@ -387,7 +389,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         }
     };
     T *const out = static_cast<T *>(a.out);
-    float l_sum[kQB], at[kQB]; // sum of the weights, and what they are relative to
+    float l_sum[kQB], l_all[kQB], at[kQB]; // the sums of weights, and what they are relative to
     // o over the sums of weights to `out`.  past: becomes a NaN where an output is none, or past what fp32 holds
     auto put_results = [&](float(*past)[kQB]) __attribute__((always_inline)) {
 #pragma unroll
@@ -398,7 +400,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             const int tok = ok ? my_tok[i] : 0;
             const int64_t row = (int64_t)(u.s.first + tok) * v.Hq + g * G + (ok ? qq - tok * G : 0);
             T *const op = out + row * D + 8 * half;
-            if (PAIRS && ok && half == 0) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = seen ? f32x2{at[i], inv} : f32x2{0.f, 0.f};
+            if (PAIRS && ok && half == 0) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = seen ? f32x2{at[i], 1.f / l_all[i]} : f32x2{0.f, 0.f};
 #pragma unroll
             for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -470,7 +472,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             set_ref();
 #pragma unroll
             for (int i = 0; i < kQB; ++i) {
-                l_run[i] = 0.f;
+                l_run[i] = l_whole[i] = 0.f;
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -492,7 +494,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         } else {
 #pragma unroll
             for (int i = 0; i < kQB; ++i) {
-                ref[i] = l_run[i] = 0.f;
+                ref[i] = l_run[i] = l_whole[i] = 0.f;
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -518,6 +520,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
         for (int i = 0; i < kQB; ++i) {
             l_sum[i] = half_sum(l_run[i]);
+            l_all[i] = PAIRS ? half_sum(l_whole[i]) : 0.f;
             at[i] = base_of(i);
             past_it[i] = 0.f;
         }
@@ -526,7 +529,9 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             float *const stats = a.records.stats + (int64_t)(u.record + u.chunk) * kFQ * 2;
 #pragma unroll
             for (int i = 0; i < kQB; ++i) {
-                if (half == 0) store_far(stats + 2 * (32 * (kQB * wave + i) + lq), at[i], l_sum[i]);
+                const int n = 32 * (kQB * wave + i) + lq;
+                if (half == 0) store_far(stats + 2 * n, at[i], l_sum[i]);
+                if (PAIRS && half == 0) store_far1(a.records.sums + (int64_t)(u.record + u.chunk) * kFQ + n, l_all[i]);
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -556,7 +561,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
     for (int i = 0; i < kQB; ++i) {
         at[i] = -INFINITY;
-        l_sum[i] = 0.f;
+        l_sum[i] = l_all[i] = 0.f;
 #pragma unroll 8
         for (int c = 0; c < u.chunks; ++c) {
             const f32x2 st = load_far(stats + ((int64_t)c * kFQ + 32 * i) * 2);
@@ -583,6 +588,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             const bool some = st[i][1] != 0.f;
             const float by = some ? __builtin_amdgcn_exp2f(st[i][0] - at[i]) : 0.f;
             if (some) l_sum[i] = fmaf(st[i][1], by, l_sum[i]);
+            if (PAIRS && some) l_all[i] = fmaf(load_far1(a.records.sums + (int64_t)(u.record + c) * kFQ + 32 * (kQB * wave + i) + lq), by, l_all[i]);
 #pragma unroll
             for (int f = 0; f < NF; ++f)
 #pragma unroll

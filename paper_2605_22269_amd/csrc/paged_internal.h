@@ -34,6 +34,8 @@ constexpr int kPlanRecords = 2048;  // most that any plan has: the counts at a w
 struct ChunkRecords {
     float *stats;  // [record][queries][2]
     float *values; // [record][queries][D]
+    float *sums;   // [record][queries]: of weights that the values were not multiplied by as they are, before their rounding (paged_flash.hip,
+                   // where the weights of rows are asked for)
 };
 
 struct PagedAttendArgs {

@@ -150,3 +150,18 @@ def test_the_largest_values_where_rows_decide_late(D, high, seqs, room):
     near(f64(got), want, attention_error(amean, reach, most, D, BF16, True), BF16)
     for b, n in enumerate(c.lengths):
         near(f64(rows)[b][:, :n], received[b], (1 + received[b]) * weights_error(c, received), F32)
+
+
+# ---- outputs beside the weights of rows ----
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D,hq,hkv", [(128, 28, 4), (64, 8, 1)])
+@pytest.mark.parametrize("seqs,room", [([(16, 900), (40, 200), (0, 7)], 0), ([(300, 300), (200, 1000)], 9000), ([(120, 6000)], 0), ([(700, 5000)], 0),
+                                       ([(1, 40), (2, 700)], 0)], ids=["window", "256", "chunks", "shares", "few"])
+def test_asking_for_the_weights_changes_no_output(D, hq, hkv, seqs, room, dtype):
+    c = Case(seqs, D, hq, hkv, 16, dtype, seed=40 + D, width=-(-room // 16) if room else None)
+    rows = torch.zeros(len(seqs), hkv, int(c.lengths.max()), device="cuda")
+    assert torch.equal(c.attend(weights_out=rows), c.attend())
+    assert torch.isfinite(rows).all()
+    for b, (new, n) in enumerate(seqs):   # what a query gives adds up to 1
+        total, tokens = f64(rows)[b].sum(-1), new * hq // hkv
+        assert (np.abs(total - tokens) <= (n + 64) * 2.0**-20 * max(tokens, 1)).all(), (total, tokens)
