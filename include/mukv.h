@@ -585,11 +585,13 @@ typedef struct mukv_seqs {
                                tokens each.  What is outside 0 .. n_tokens is brought inside; where those
                                of several sequences do not ascend, mukv_paged_attend leaves out as it
                                is, and what weights receive is undefined                        */
-    int32_t n_seqs;         /* 1 .. 65536                                                       */
+    int32_t n_seqs;         /* 1 .. 65536 (an attention call's workgroups each go through all of
+                               them: thousands cost more than their rows do)                    */
     int32_t table_width;    /* pages a sequence can have                                        */
     int32_t n_tokens;       /* new tokens of all sequences                                      */
     int32_t max_new;        /* most new tokens of a sequence (0: not known).  A hint: it chooses
-                               between kernels, nothing is left out if it is wrong              */
+                               between kernels, nothing is left out if it is wrong; the kernels
+                               round differently (below)                                        */
 } mukv_seqs;
 
 /* Rotary positions with several axes.  Pair i of a head's first n_rot features is
@@ -680,8 +682,12 @@ typedef struct mukv_row_weights {
  *              before its first use; every call leaves it fit for the next one, of any shape.
  *              Calls that share a workspace must not overlap on the device.
  *
- * Arithmetic in fp32, sums in an order that does not depend on timing; `out` is rounded to
- * the payload dtype.
+ * Scores, softmax statistics and all sums are fp32, in an order that does not depend on timing;
+ * `out` is rounded to the payload dtype.  With bf16 payloads values are multiplied by weights
+ * of 16 bits, or, for calls with many new tokens a sequence and heads of 64 or 128, by weights
+ * rounded to bf16, and divided by the sum of those.  Which of the two a call takes follows
+ * from n_tokens, n_seqs, max_new, the heads and the table's room: a sequence's outputs can
+ * differ by such roundings with what else is in the call.  Rows receive weights of 32 bits.
  * Values are added up, by weights of at most 1, before they are divided: an output is finite
  * where the largest value times the sum of those weights is finite in fp32.
  * n_tokens = 0 does nothing, except that weights are brought from in to out; packed, where

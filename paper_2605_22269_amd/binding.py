@@ -864,7 +864,8 @@ class PagedKV(_Sequences):
                decay=1.0):
         """q [n_tokens][n_q_heads][head_dim]: every sequence's new tokens (lengths count them) attend to its rows.  With
         weights_out, float32 [sequence][KV head][row], it becomes decay * weights + what every row received (weights None: zeros;
-        weights_out may be weights).  max_new: most new tokens of a sequence, as a hint.  Returns out."""
+        weights_out may be weights).  max_new: most new tokens of a sequence, as a hint (kernels round
+        differently).  Returns out, which must not overlap q."""
         T, heads, dim = q.shape
         assert heads == self._q_heads and dim == self._dim and q.dtype is self.dtype
         s = self._sequences(table, lengths, offsets, T, max_new)

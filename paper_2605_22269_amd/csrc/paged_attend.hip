@@ -49,8 +49,8 @@ __device__ __forceinline__ f32x4 scores_f32(const raw16 (&k)[KK], Q q) {
 //   rows     a lane works out where one row lives, from a table entry that was requested a block earlier; the others fetch that by
 //            lane permutes.  Keys and values go straight to registers, the next block's requested as soon as this one's are used up.
 //   scores   S^T = K Q^T (16x16x32 bf16, 16x16x4 fp32): a lane holds ONE query (lane % 16) and the rows 4 (lane / 16) + r of every 16.
-//   values   O^T += V^T P^T: the weights are the B operand as they stand in the lane.  bf16: pairs hi + lo, nothing of the fp32
-//            weight is lost; the value rows pass through LDS the wave has to itself and the transpose read.  fp32: no transpose needed.
+//   values   O^T += V^T P^T: the weights are the B operand as they stand in the lane.  bf16: pairs hi + lo, 16 of the fp32
+//            weight's 24 bits; the value rows pass through LDS the wave has to itself and the transpose read.  fp32: no transpose needed.
 // As many workgroups to a compute unit as the registers allow (us a launch, two / as now: 100 users of 3 rows, 12 heads of 64 bf16, 13.7 / 10.2;
 // 12 users, 5 tokens over 1000 to 9000 rows, 28/4 heads of 64 bf16, 26.5 / 22.3; 6 prompts of 700 to 1500 tokens, 28/4 heads of 32 bf16, 148 / 94;
 // of fp32 252 / 218; 1500 tokens, 16/4 heads of 64 fp32, 103 / 92).
@@ -550,7 +550,7 @@ hipError_t launch_typed(const PagedAttendArgs &a, hipStream_t st) {
     }
     if (!a.weights_out) return hipSuccess;
     // Queries that stream past are shared by the rows a wave holds; where there are few of them it is more waves that count (us a
-    // call, 16 / 64 rows a wave: 64 users, one token, 2000 rows, 64/8 heads 62 / 85; 6 users, 16 tokens, 36000 rows in all, 28/4 heads 35 / 20).
+    // launch, 16 / 64 rows a wave: 64 users, one token, 2000 rows, 64/8 heads 61 / 70; 6 users, 16 tokens, 36000 rows in all, 28/4 heads 38 / 29).
     if ((int64_t)a.view.n_tokens * a.view.G <= 32 * (int64_t)a.view.n_seqs) return launch_weights<T, D, 1>(a, st);
     return launch_weights<T, D, sizeof(T) == 2 ? 4 : 2>(a, st);
 }
@@ -567,15 +567,16 @@ hipError_t launch_by_dim(const PagedAttendArgs &a, int D, hipStream_t st) {
 
 } // namespace
 
-// Which kernel takes a call, by what is known on the host; us a launch, 28/4 heads of 128.
+// Which kernel takes a call, by what is known on the host; us a call, 28/4 heads of 128, what the rule takes marked.
 // The kernel for any shape reads a sequence's rows once for every 16 queries of a KV head, the one for prompts once for 128 or 256, but its
-// units are large and start slowly: it takes calls with more queries than that (any / prompts: one user, 16 tokens over 8000 rows
-// 24* / 35, over 32000 51* / 60, 32 tokens over 8000 30* / 36, 64 tokens 58 / 37*, over 1000 15.8* / 19.9; 8 users over 8000 rows, 4 tokens
-// 34* / 46, 8 tokens 53 / 46*, 16 tokens 94 / 48*).
+// units are large and start slowly: it takes calls with more queries than that (any / prompts in tiles of 128 / of 256: one user, 16 tokens
+// over 8000 rows 19.5* / 34 / 50, over 32000 59* / 58 / 87, 32 tokens over 8000 28.6* / 35 / 51, 64 tokens over 8000 52 / 36 / 52*, over 1000
+// 14.0 / 19.5* / 28.8; 8 users over 8000 rows, 4 tokens 31.5* / 42 / 61, 8 tokens 55 / 42* / 61, 16 tokens 89 / 43* / 62).
 // Tiles of 128 or of 256 queries: the wide ones read operands for twice the products, so they are faster where there is enough to
 // do for every compute unit, and slower where a tile is half empty or the last tiles' rows are what the call waits for (128 / 256: 6
-// users, 16 tokens over 3000 to 9000 rows 41* / 60; 300 tokens 15* / 20; 2000 tokens 58* / 71; 8192 tokens 712 / 560*; 1568 over 6272 rows
-// 312 / 263*; 8 users, 64 tokens over 8000 rows 148 / 109*).
+// users, 16 tokens over 3000 to 9000 rows 39* / 56; 300 tokens 14.6* / 20.2; 2000 tokens 55* / 71; 8192 tokens 650 / 493*; 1568 over 6272 rows
+// 277 / 238*; 8 users, 64 tokens over 8000 rows 135 / 101*).  What a table has room for stands in for the rows that are there, which the
+// host does not know: one user's 64 tokens over 8000 rows are the case above where that takes the slower tile.
 int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint) {
     if (dtype != MUKV_BF16 || D < 64) return 0;
     const int64_t queries = new_hint * v.G; // of a sequence and KV head

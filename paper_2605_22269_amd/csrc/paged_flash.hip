@@ -1,5 +1,8 @@
 // Attention of many new tokens a sequence over a paged cache, or over packed sequences, on the matrix cores: bf16 rows of 64 or 128
-// features.  The mathematics, and how rows are shared out and joined, are those of paged_attend.hip.
+// features.  How rows are shared out and joined is as in paged_attend.hip.  The softmax differs in two things: what exponents subtract (the
+// largest score of a unit's first rows, see below), and the weights, which enter the product rounded to bf16, as the matrix cores take
+// them: as the pairs that paged_attend.hip multiplies by they would be twice the products.  Each weight is off by 2^-9 of itself at
+// most, no more than an output is by its own rounding: outputs are 0.0019-0.0023 off (2-norm, normal numbers), 0.0017 with that rounding alone.
 #include <climits>
 #include <type_traits>
 
@@ -19,7 +22,7 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), bf16x2{(__bf16)1.f, (__bf16)1.f}, x, false);
 }
 
-// One unit by a workgroup of four waves; a wave owns 64 queries from the scores to the output.
+// One unit by a workgroup of four waves; a wave owns 32 kQB queries from the scores to the output.
 template <int D, int kQB, bool PAIRS>
 __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit &u) {
     using T = uint16_t;
@@ -599,7 +602,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 }
 
 // A workgroup takes a unit; of one sequence's perhaps the units of its stretch, one after the other (us a launch, 28/4 heads of 128, chunks
-// alone / shares where they cost less: 1568 tokens over 6272 rows 239 / 177, 2000 over 10000 363 / 327; 1500 over 3000, 16/4 heads of 64, 63 / 55).
+// alone / shares where they cost less: 1568 tokens over 6272 rows 239 / 177, 2000 over 10000 361 / 327; 1500 over 3000, 16/4 heads of 64, 63 / 55).
 template <int D, int kQB, bool PAIRS, bool SHARES>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_flash_kernel(PagedAttendArgs a) {
     Unit u;
@@ -624,7 +627,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 
 // Whether one sequence's tiles may be shared out evenly: to look at that takes the kernel a microsecond, so not where it gains nothing:
 // few tiles, which come out even in chunks, more than twice the compute units, or few rows (us a launch without / with, 28/4 heads of 128:
-// 200 tokens over 20000 rows 89 / 93, 300 alone 14.5 / 15.5, 1000 30.1 / 30.9, 2000 55.4 / 57; the gains are at the kernel).
+// 200 tokens over 20000 rows 89 / 93, 300 alone 14.5 / 15.6, 1000 29.8 / 31.0, 2000 55.0 / 57.3; the gains are at the kernel).
 static bool may_share(const PagedView &v, const PlanShape &p) {
     const int64_t tiles = div_up((int64_t)v.n_tokens * v.G, p.queries) * v.Hkv, room = v.table ? room_of(v) : v.n_tokens;
     return v.n_seqs == 1 && tiles > 64 && tiles <= p.records - p.places && room >= 4096;
