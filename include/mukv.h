@@ -725,6 +725,56 @@ int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_
                      int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
                      int32_t *kept_out, int32_t *lengths_out, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The same cache in 8 bits: twice the rows in the same memory, and half the bytes to
+ * read for each.  A row (the key or value of one token and KV head) is held as e4m3
+ * numbers (OCP: four exponent bits, no infinities, largest 448) and one power of two:
+ *
+ *   2^e, the smallest with max |x| <= 448 * 2^e over the row's finite features, e in -117 .. 119
+ *   code = x / 2^e to nearest even (past 448, which takes |x| > 2.9e38: 448); NaN where x is not finite
+ *
+ * so a feature is off by 2^-4 of itself at most, or by 2^(e-10) where it is below 2^(e-6).  What a
+ * code stands for is a bf16 and an fp32 number as it is: reading rounds nothing.
+ *
+ * mukv_paged describes the pages, whose elements are bytes (k_pages, v_pages, strides);
+ * its dtype is that of queries, new rows and outputs.  The powers of two are bytes
+ * e + 127 (E8M0): that of row j of sequence b, KV head g, layer l at
+ *   l * stride_layer + p * stride_page + g * stride_head + (j % page_rows) * stride_row
+ * of k and of v.  What other bytes and rows never written stand for is undefined.
+ * ------------------------------------------------------------------------ */
+typedef struct mukv_row_scales {
+    void *k;                /* device, a byte a row                                            */
+    void *v;
+    int64_t stride_layer;   /* in bytes, not negative (that of a dimension of one is not read)   */
+    int64_t stride_page;
+    int64_t stride_head;
+    int64_t stride_row;
+} mukv_row_scales;
+
+/*
+ * mukv_paged_append to a cache in 8 bits.  Keys are rotated in fp32 and held as they
+ * come out of that, with no rounding to the payload dtype between.
+ * Errors: as mukv_paged_append; INVALID_ARG, UNSUPPORTED for scales.
+ */
+int mukv_paged_append8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                       const void *k, const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides,
+                       const void *q, const mukv_strides *q_strides, void *q_out, const mukv_strides *q_out_strides,
+                       const mukv_rope_table *rope, const int32_t *positions, void *stream);
+
+/*
+ * Rows of a cache in 8 bits as the payload dtype: token i of the n_b "new" ones of
+ * sequence b gets row lengths[b] - n_b + i, the row that mukv_paged_append8 would
+ * write for it (all rows of b: n_b = lengths[b]).  Rows that do not exist are zeros.
+ *
+ *   k_out, v_out  device, [n_tokens][n_kv_heads][head_dim] with strides
+ *
+ * Tokens that are no sequence's are zeros too.  n_tokens = 0 does nothing.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (alignment, strides).
+ */
+int mukv_paged_read8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                     void *k_out, const mukv_strides *k_strides, void *v_out, const mukv_strides *v_strides,
+                     void *stream);
+
 /*
  * The graph capture that `stream` is in: a number that no other capture of the
  * process has, 0 if there is none.  Scratch that a capture clears is fit for the

@@ -81,6 +81,11 @@ class mukv_row_weights(C.Structure):
                 ("stride_head", C.c_int64), ("rows", C.c_int32), ("decay", C.c_float)]
 
 
+class mukv_row_scales(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_layer", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_row", C.c_int64)]
+
+
 class mukv_rope_table(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("n_rot", C.c_int32), ("n_axes", C.c_int32),
                 ("pairing", C.c_int32), ("inverse", C.c_int32)]
@@ -98,7 +103,7 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_attend", "mukv_prefill_workspace_size", "mukv_prefill_attend", "mukv_prefill_attend_static",
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
            "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append",
-           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_stream_capture", "mukv_strerror")
+           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_paged_append8", "mukv_paged_read8", "mukv_stream_capture", "mukv_strerror")
 
 _lib = None
 
@@ -146,6 +151,8 @@ def load():
     lib.mukv_paged_workspace_size.argtypes = [paged, seqs, i32, C.POINTER(C.c_int64)]
     lib.mukv_paged_attend.argtypes = [paged, i32, seqs, vp, strides, i32, vp, vp, vp, C.c_int64, vp]
     lib.mukv_paged_evict.argtypes = [paged, seqs, vp, i32, i32, i32, vp, i32, vp, vp, vp]
+    lib.mukv_paged_append8.argtypes = [paged, vp, i32, seqs, vp, strides, vp, strides, vp, strides, vp, strides, vp, vp, vp]
+    lib.mukv_paged_read8.argtypes = [paged, vp, i32, seqs, vp, strides, vp, strides, vp]
     lib.mukv_stream_capture.argtypes = [vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
@@ -341,6 +348,10 @@ def mukv_paged_attend(pages, layer, seqs, q_ptr, q_strides, causal, out_ptr, wei
 def mukv_paged_evict(pages, seqs, weights, budget, n_sink, n_recent, into_ptr, into_width, kept_ptr, lengths_ptr, stream):
     _check((_lib or load()).mukv_paged_evict(pages, seqs, weights, budget, n_sink, n_recent, into_ptr, into_width, kept_ptr, lengths_ptr,
                                              stream), "mukv_paged_evict")
+
+
+def mukv_paged_read8(pages, scales, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, stream):
+    _check((_lib or load()).mukv_paged_read8(pages, scales, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, stream), "mukv_paged_read8")
 
 
 # ---- convenience object ----------------------------------------------------------------------
@@ -901,6 +912,52 @@ class PagedKV(_Sequences):
         mukv_paged_evict(self._pages_at, s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1],
                          kept.data_ptr(), lengths_out.data_ptr(), _stream_of(index))
         return kept, lengths_out
+
+
+class PagedKV8(PagedKV):
+    """The conversation's cache in 8 bits: k_pages, v_pages float8_e4m3fn [layer][page][KV head][row][feature], k_scales, v_scales
+    float8_e8m0fnu (or their bytes, uint8) [layer][page][KV head][row], any strides but the pages' last.  dtype: that of queries, new rows and
+    outputs."""
+
+    attend = evict = None   # (those of PagedKV take the rows for numbers of its dtype)
+
+    def __init__(self, k_pages, v_pages, k_scales, v_scales, *, n_q_heads, dtype=torch.bfloat16):
+        _Sequences.__init__(self)
+        assert k_pages.dim() == 5 and v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
+        assert k_pages.dtype is torch.float8_e4m3fn and v_pages.dtype is torch.float8_e4m3fn
+        assert v_pages.device == k_pages.device and k_pages.is_cuda and k_pages.stride(4) == 1
+        assert k_scales.shape == k_pages.shape[:4] and v_scales.shape == k_scales.shape and v_scales.stride() == k_scales.stride()
+        assert k_scales.dtype in (torch.float8_e8m0fnu, torch.uint8) and v_scales.dtype is k_scales.dtype
+        assert k_scales.device == k_pages.device and v_scales.device == k_pages.device
+        assert dtype in (torch.bfloat16, torch.float32)
+        L, n, hkv, R, D = k_pages.shape
+        sl, sp, sh, sr, _ = k_pages.stride()
+        self.dtype, self.device, self._index = dtype, k_pages.device, k_pages.get_device()
+        self._held = k_pages, v_pages, k_scales, v_scales
+        self._heads, self._q_heads, self._dim = hkv, n_q_heads, D
+        kind = MUKV_BF16 if dtype is torch.bfloat16 else MUKV_F32
+        self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, kind, self._index)
+        self._scales = mukv_row_scales(_ptr(k_scales), _ptr(v_scales), *k_scales.stride())
+        self._pages_at, self._scales_at = C.addressof(self._pages), C.addressof(self._scales)
+        call, at = (_lib or load()).mukv_paged_append8, self._scales_at
+        self._c_append = lambda pages, *rest: call(pages, at, *rest)
+
+    def read(self, layer, table, lengths, offsets, *, n_tokens=None, k_out=None, v_out=None):
+        """Rows as they were written, as the cache's dtype: [n_tokens][n_kv_heads][head_dim], those of sequence b at offsets[b] ..
+        offsets[b+1]-1, its last ones (all of them where that is lengths[b] many).  n_tokens: where no outputs are given.
+        Returns k_out, v_out."""
+        index = self._index
+        if k_out is None:
+            k_out = torch.empty(n_tokens, self._heads, self._dim, dtype=self.dtype, device=self.device)
+        if v_out is None:
+            v_out = torch.empty(k_out.shape, dtype=self.dtype, device=self.device)
+        T = k_out.shape[0]
+        assert k_out.shape == v_out.shape == (T, self._heads, self._dim) and n_tokens in (None, T)
+        assert k_out.dtype is self.dtype and v_out.dtype is self.dtype and k_out.get_device() == index and v_out.get_device() == index
+        s = self._sequences(table, lengths, offsets, T, 0)
+        mukv_paged_read8(self._pages_at, self._scales_at, layer, s, k_out.data_ptr(), _rows(k_out), v_out.data_ptr(), _rows(v_out),
+                         _stream_of(index))
+        return k_out, v_out
 
 
 class PackedKV(_Sequences):

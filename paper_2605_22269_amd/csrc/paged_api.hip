@@ -25,8 +25,8 @@ int check_stride(int64_t stride, int64_t count, int esz) {
 
 int64_t in_bytes(int64_t stride, int64_t count, int esz) { return count > 1 ? stride * esz : 0; }
 
-// empty: no row is ever looked at, and empty tensors need not have an address
-int check_pages(const mukv_paged *p, bool empty = false) {
+// empty: no row is ever looked at, and empty tensors need not have an address.  eight: elements of the pages are bytes
+int check_pages(const mukv_paged *p, bool empty = false, bool eight = false) {
     if (!p || (!empty && (!p->k_pages || !p->v_pages))) return MUKV_ERR_INVALID_ARG;
     if (p->n_layers < 1 || p->n_pages < 1 || p->page_rows < (empty ? 0 : 1) || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->device_id < 0)
         return MUKV_ERR_INVALID_ARG;
@@ -34,13 +34,30 @@ int check_pages(const mukv_paged *p, bool empty = false) {
     if (p->n_q_heads % p->n_kv_heads) return MUKV_ERR_SHAPE;
     if (p->head_dim < 16 || p->head_dim > 128 || (p->head_dim & (p->head_dim - 1))) return MUKV_ERR_UNSUPPORTED;
     if (p->n_q_heads / p->n_kv_heads > 1024 || p->n_q_heads > 65535) return MUKV_ERR_UNSUPPORTED;
-    const int esz = elem_size(p->dtype);
+    const int esz = eight ? 1 : elem_size(p->dtype);
     const int64_t strides[4] = {p->stride_layer, p->stride_page, p->stride_head, p->stride_row};
     const int64_t counts[4] = {p->n_layers, p->n_pages, p->n_kv_heads, p->page_rows};
     for (int i = 0; i < 4; ++i)
         if (const int rc = check_stride(strides[i], counts[i], esz)) return rc;
     if (!aligned(p->k_pages) || !aligned(p->v_pages)) return MUKV_ERR_UNSUPPORTED;
     return MUKV_OK;
+}
+
+// Scales of rows in 8 bits; NULL where the cache is not in 8 bits.
+int check_scales(const mukv_paged *p, const mukv_row_scales *s) {
+    if (!s || !s->k || !s->v) return MUKV_ERR_INVALID_ARG;
+    const int64_t strides[4] = {s->stride_layer, s->stride_page, s->stride_head, s->stride_row};
+    const int64_t counts[4] = {p->n_layers, p->n_pages, p->n_kv_heads, p->page_rows};
+    for (int i = 0; i < 4; ++i) {
+        if (counts[i] <= 1) continue;
+        if (strides[i] < 0) return MUKV_ERR_INVALID_ARG;
+        if (strides[i] > (INT64_MAX >> 4) / counts[i]) return MUKV_ERR_UNSUPPORTED;
+    }
+    return MUKV_OK;
+}
+int check_pages8(const mukv_paged *p, const mukv_row_scales *s) {
+    if (const int rc = check_pages(p, false, true)) return rc;
+    return check_scales(p, s);
 }
 
 bool packed_nothing(const mukv_seqs *s) { return s && !s->table && s->n_tokens == 0; }
@@ -64,9 +81,17 @@ int check_seqs(const mukv_paged *p, const mukv_seqs *s, bool may_be_packed, bool
     return MUKV_OK;
 }
 
-PagedView view_of(const mukv_paged &p, int layer, const mukv_seqs &s) {
-    const int esz = elem_size(p.dtype);
-    PagedView v;
+// scales: of rows in 8 bits, else NULL
+PagedView view_of(const mukv_paged &p, int layer, const mukv_seqs &s, const mukv_row_scales *scales = nullptr) {
+    const int esz = scales ? 1 : elem_size(p.dtype);
+    PagedView v = {};
+    if (scales) {
+        v.scales.k = static_cast<unsigned char *>(scales->k) + layer * in_bytes(scales->stride_layer, p.n_layers, 1);
+        v.scales.v = static_cast<unsigned char *>(scales->v) + layer * in_bytes(scales->stride_layer, p.n_layers, 1);
+        v.scales.stride_page = in_bytes(scales->stride_page, p.n_pages, 1);
+        v.scales.stride_head = in_bytes(scales->stride_head, p.n_kv_heads, 1);
+        v.scales.stride_row = in_bytes(scales->stride_row, p.page_rows, 1);
+    }
     v.k = static_cast<unsigned char *>(p.k_pages) + layer * in_bytes(p.stride_layer, p.n_layers, esz);
     v.v = static_cast<unsigned char *>(p.v_pages) + layer * in_bytes(p.stride_layer, p.n_layers, esz);
     v.stride_page = in_bytes(p.stride_page, p.n_pages, esz);
@@ -156,6 +181,38 @@ int check_weights(const mukv_row_weights *w) {
     return MUKV_OK;
 }
 
+// New rows to the pages: as they are, or (scales) in 8 bits.
+int append(const mukv_paged *pages, const mukv_row_scales *scales, bool eight, int32_t layer, const mukv_seqs *seqs, const void *k,
+           const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides, const void *q, const mukv_strides *q_strides,
+           void *q_out, const mukv_strides *q_out_strides, const mukv_rope_table *rope, const int32_t *positions, void *stream) {
+    if (const int rc = eight ? check_pages8(pages, scales) : check_pages(pages)) return rc;
+    if (layer < 0 || layer >= pages->n_layers) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
+    const int esz = elem_size(pages->dtype), T = seqs->n_tokens;
+    if (rope)
+        if (const int rc = check_rope(rope, T == 0 || positions, pages->head_dim)) return rc;
+    if (T == 0) return MUKV_OK; // (empty tensors need not have an address)
+    if ((q != nullptr) != (q_out != nullptr)) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_rows(k, k_strides, T, pages->n_kv_heads, esz)) return rc;
+    if (const int rc = check_rows(v, v_strides, T, pages->n_kv_heads, esz)) return rc;
+    if (q) {
+        if (const int rc = check_rows(q, q_strides, T, pages->n_q_heads, esz)) return rc;
+        if (const int rc = check_rows(q_out, q_out_strides, T, pages->n_q_heads, esz)) return rc;
+    }
+    RopeArgs a = {};
+    a.q = rows_in(q, q_strides, q_out, q_out_strides, T, pages->n_q_heads, esz);
+    a.k = rows_in(k, k_strides, nullptr, nullptr, T, pages->n_kv_heads, esz);
+    a.v = rows_in(v, v_strides, nullptr, nullptr, T, pages->n_kv_heads, esz);
+    a.view = view_of(*pages, layer, *seqs, scales);
+    a.n_tokens = T;
+    a.D = pages->head_dim;
+    set_rope(a, rope, positions);
+    DeviceScope dev(pages->device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    return finished(eight ? mukv::launch_rows8(a, pages->dtype, false, st) : mukv::launch_rope(a, pages->dtype, st));
+}
+
 } // namespace
 
 extern "C" {
@@ -185,31 +242,34 @@ int mukv_paged_append(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
                       const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides, const void *q,
                       const mukv_strides *q_strides, void *q_out, const mukv_strides *q_out_strides,
                       const mukv_rope_table *rope, const int32_t *positions, void *stream) {
-    if (const int rc = check_pages(pages)) return rc;
+    return append(pages, nullptr, false, layer, seqs, k, k_strides, v, v_strides, q, q_strides, q_out, q_out_strides, rope, positions, stream);
+}
+
+int mukv_paged_append8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                       const void *k, const mukv_strides *k_strides, const void *v, const mukv_strides *v_strides,
+                       const void *q, const mukv_strides *q_strides, void *q_out, const mukv_strides *q_out_strides,
+                       const mukv_rope_table *rope, const int32_t *positions, void *stream) {
+    return append(pages, scales, true, layer, seqs, k, k_strides, v, v_strides, q, q_strides, q_out, q_out_strides, rope, positions, stream);
+}
+
+int mukv_paged_read8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                     void *k_out, const mukv_strides *k_strides, void *v_out, const mukv_strides *v_strides, void *stream) {
+    if (const int rc = check_pages8(pages, scales)) return rc;
     if (layer < 0 || layer >= pages->n_layers) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
     const int esz = elem_size(pages->dtype), T = seqs->n_tokens;
-    if (rope)
-        if (const int rc = check_rope(rope, T == 0 || positions, pages->head_dim)) return rc;
     if (T == 0) return MUKV_OK; // (empty tensors need not have an address)
-    if ((q != nullptr) != (q_out != nullptr)) return MUKV_ERR_INVALID_ARG;
-    if (const int rc = check_rows(k, k_strides, T, pages->n_kv_heads, esz)) return rc;
-    if (const int rc = check_rows(v, v_strides, T, pages->n_kv_heads, esz)) return rc;
-    if (q) {
-        if (const int rc = check_rows(q, q_strides, T, pages->n_q_heads, esz)) return rc;
-        if (const int rc = check_rows(q_out, q_out_strides, T, pages->n_q_heads, esz)) return rc;
-    }
+    if (const int rc = check_rows(k_out, k_strides, T, pages->n_kv_heads, esz)) return rc;
+    if (const int rc = check_rows(v_out, v_strides, T, pages->n_kv_heads, esz)) return rc;
     RopeArgs a = {};
-    a.q = rows_in(q, q_strides, q_out, q_out_strides, T, pages->n_q_heads, esz);
-    a.k = rows_in(k, k_strides, nullptr, nullptr, T, pages->n_kv_heads, esz);
-    a.v = rows_in(v, v_strides, nullptr, nullptr, T, pages->n_kv_heads, esz);
-    a.view = view_of(*pages, layer, *seqs);
+    a.k = rows_in(k_out, k_strides, k_out, k_strides, T, pages->n_kv_heads, esz);
+    a.v = rows_in(v_out, v_strides, v_out, v_strides, T, pages->n_kv_heads, esz);
+    a.view = view_of(*pages, layer, *seqs, scales);
     a.n_tokens = T;
     a.D = pages->head_dim;
-    set_rope(a, rope, positions);
     DeviceScope dev(pages->device_id);
     if (!dev.ok) return MUKV_ERR_HIP;
-    return finished(mukv::launch_rope(a, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
+    return finished(mukv::launch_rows8(a, pages->dtype, true, reinterpret_cast<hipStream_t>(stream)));
 }
 
 int mukv_stream_capture(void *stream, uint64_t *id_out) {

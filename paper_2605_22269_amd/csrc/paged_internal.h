@@ -21,6 +21,8 @@ struct RopeArgs {
     bool rotate, neighbours, inverse;
 };
 hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
+// k and v to pages of 8 bits; read: from them to k.out and v.out
+hipError_t launch_rows8(const RopeArgs &a, int dtype, bool read, hipStream_t st);
 
 // Which kernel takes an attention call follows from types and sizes that the host knows (paged_attend.hip): 0 that for any shape, otherwise
 // the one for prompts, with tiles of so many queries.  new_hint: new tokens of a sequence, as far as that is known.

@@ -12,6 +12,12 @@
 
 namespace mukv {
 
+// Of a cache in 8 bits: where the powers of two of one layer's rows are, a byte each.
+struct ScaleView {
+    unsigned char *k, *v;
+    int64_t stride_page, stride_head, stride_row;
+};
+
 // One layer of a paged cache and the sequences that lie in it.  Strides in bytes.
 struct PagedView {
     unsigned char *k, *v; // the layer's
@@ -19,6 +25,7 @@ struct PagedView {
     const int32_t *table, *lengths, *offsets;
     int n_pages, page_rows, n_seqs, table_width, n_tokens, per_seq; // per_seq: new tokens each, where there are no offsets
     int Hq, Hkv, G;
+    ScaleView scales; // rows in 8 bits
 };
 
 // The new tokens of sequence b: first and number, both inside 0 .. n_tokens whatever the offsets say.
@@ -59,6 +66,9 @@ MUKV_HD int64_t entry_of(const PagedView &v, int b, int j) { return (int64_t)b *
 // Byte offset of row j (KV head 0) on page `page`, which the caller has found to be one of the pages.
 MUKV_HD int64_t offset_of(const PagedView &v, int page, int j) {
     return (int64_t)page * v.stride_page + (int64_t)((unsigned)j % (unsigned)v.page_rows) * v.stride_row;
+}
+MUKV_HD int64_t scale_offset_of(const PagedView &v, int page, int j) { // of its scales
+    return (int64_t)page * v.scales.stride_page + (int64_t)((unsigned)j % (unsigned)v.page_rows) * v.scales.stride_row;
 }
 MUKV_HD bool is_page(const PagedView &v, int page) { return (unsigned)page < (unsigned)v.n_pages; }
 

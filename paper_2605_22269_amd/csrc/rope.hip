@@ -4,8 +4,7 @@
 // sine of its pairs, the row of the cache it becomes -- is worked out once a workgroup, in LDS; the rows themselves go from memory to
 // memory in 16-byte pieces, both pieces of a pair in one thread.
 // The angle in turns, position * inv_freq / 2 pi, is formed and reduced in 64 bits: at position 10^6 fp32 would be off by 0.06 rad.
-#include "attend_dev.h"
-#include "paged_internal.h"
+#include "rope_dev.h"
 
 namespace mukv {
 
@@ -15,27 +14,6 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 4;   // most tokens of a workgroup
 constexpr int kRopePairs = 256;  // most pairs of a head
 constexpr int kRopeAhead = 4;    // rows a thread requests at a time
-
-template <typename T>
-__device__ __forceinline__ float piece_get(const raw16 &x, int e) {
-    if constexpr (sizeof(T) == 4)
-        return __uint_as_float(x[e]);
-    else
-        return __uint_as_float(e & 1 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16);
-}
-template <typename T>
-__device__ __forceinline__ void piece_put(raw16 &x, int e, float y0, float y1) { // elements e, e + 1
-    if constexpr (sizeof(T) == 4) {
-        x[e] = __float_as_uint(y0);
-        x[e + 1] = __float_as_uint(y1);
-    } else {
-        x[e / 2] = bf16_pair(y0, y1);
-    }
-}
-
-// Past the caches: what is written here is read by other launches, on other XCDs (1568 tokens, 28/4 heads of 128: 7.6 us a launch, 8.8
-// without; 24 prompts of 64/8 heads, 0.45 GB: 90, 95).
-__device__ __forceinline__ void put_piece(unsigned char *p, raw16 x) { __builtin_nontemporal_store(x, reinterpret_cast<raw16 *>(p)); }
 
 template <typename T, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_wg) {
@@ -55,21 +33,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int per_
     auto worked_out = [&]() {
         for (int i = tid; i < nt * n_pairs; i += kRopeThreads) {
             const int t = i / n_pairs, p = i - t * n_pairs;
-            // (up to three axes: all positions of the token, so that nothing waits for which one it is)
-            const int ax = a.axis ? a.axis[p] : 0;
-            const int32_t *at = a.positions + t0 + t;
-            int pos = at[0];
-            if (a.n_axes <= 3) {
-                const int second = a.n_axes > 1 ? at[a.n_tokens] : 0, third = a.n_axes > 2 ? at[2 * (int64_t)a.n_tokens] : 0;
-                pos = ax == 0 ? pos : ax == 1 ? second : ax == 2 ? third : 0;
-            } else {
-                pos = (unsigned)ax < (unsigned)a.n_axes ? at[(int64_t)ax * a.n_tokens] : 0;
-            }
-            double turns = (double)pos * a.inv_freq[p] * 0.15915494309189533577; // 1 / 2 pi
-            turns -= rint(turns);
-            float s, c;
-            sincospif((float)(2.0 * turns), &s, &c);
-            s_turn[t][p] = float2{c, a.inverse ? -s : s};
+            s_turn[t][p] = turn_of(a, t0 + t, p);
         }
     };
     // by the last wave, beside the first one's cosines

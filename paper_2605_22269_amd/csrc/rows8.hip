@@ -1,0 +1,240 @@
+// The way of new rows into a paged cache of 8 bits, and back (eight_dev.h says what a row is held as).
+//
+// Both kernels only move rows: what bounds them is memory, and a launch where there are few rows.  A lane has 8 neighbouring features of a
+// row, D / 8 neighbouring lanes the row, so a row's largest feature takes log2(D / 8) exchanges between lanes and its codes leave
+// as one line of 8 bytes a lane.  A pair's other feature, where halves are rotated, is in the lane n_rot / 16 further on.
+#include <climits>
+
+#include "eight_dev.h"
+#include "rope_dev.h"
+
+namespace mukv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWriteTokens = 4;  // most tokens of a workgroup that writes
+constexpr int kReadTokens = 64;  // of one that reads
+constexpr int kAhead = 4;        // pieces a thread requests at a time
+
+// The rows of tokens t0 .. t0 + nt - 1 (at most 64), by one wave, lane t token t0 + t: byte offset of the row in the pages and of its
+// scale in theirs, -1 if it has none.
+__device__ __forceinline__ void places_of(const PagedView &v, int t0, int nt, int64_t *place, int64_t *scale_place) {
+    const int lane = threadIdx.x & 63, tok = t0 + lane;
+    int b = 0;
+    if (v.offsets) { // the last sequence that starts at or before the token: as many start there, or before, but the first
+        for (int b0 = 1; b0 < v.n_seqs; b0 += 64) {
+            const int starts = b0 + lane < v.n_seqs ? v.offsets[b0 + lane] : INT_MAX;
+            for (int t = 0; t < nt; ++t) {
+                const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(starts <= t0 + t));
+                if (lane == t) b += n;
+            }
+            if (__builtin_amdgcn_readlane(starts, 63) >= t0 + nt) break; // (where offsets ascend, none of the others counts)
+        }
+    } else if (v.per_seq > 0) {
+        b = tok / v.per_seq;
+    }
+    *place = *scale_place = -1;
+    if (lane >= nt || b >= v.n_seqs) return;
+    int first, count;
+    tokens_of(v, b, &first, &count);
+    const int i = tok - first, length = length_of(v, b, count), row = length - count + i;
+    if (i < 0 || i >= count || row < 0 || row >= rows_of(v, first, length)) return;
+    const int page = v.table[entry_of(v, b, row)];
+    if (!is_page(v, page)) return;
+    *place = offset_of(v, page, row);
+    *scale_place = scale_offset_of(v, page, row);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void write8_kernel(RopeArgs a, int per_wg) {
+    constexpr int L = D / 8, N = (int)sizeof(T) / 2; // lanes of a row, 16-byte pieces of a lane's features
+    constexpr int kAtOnce = kThreads / L;            // rows
+    __shared__ float2 s_turn[kWriteTokens][D / 2];
+    __shared__ int64_t s_place[kWriteTokens], s_scale[kWriteTokens];
+    const int tid = threadIdx.x, piece = tid % L;
+    const int t0 = blockIdx.x * per_wg, nt = a.n_tokens - t0 < per_wg ? a.n_tokens - t0 : per_wg;
+    const int n_pairs = a.rotate ? a.n_rot / 2 : 0;
+    const int heads = a.q.heads + a.k.heads, rows_per = heads + a.v.heads, n_rows = nt * rows_per;
+    for (int r0 = 0; r0 < n_rows; r0 += kAhead * kAtOnce) { // (the same rounds in all threads: lanes exchange what they have)
+        raw16 x[kAhead][N];
+        int tok[kAhead], head[kAhead]; // head: -1 if there is no such row
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + u * kAtOnce + tid / L;
+            tok[u] = r / rows_per;
+            head[u] = r < n_rows ? r - tok[u] * rows_per : -1;
+            if (head[u] < 0) continue;
+            const int h = head[u];
+            const RopeArgs::Rows &m = h < a.q.heads ? a.q : h < heads ? a.k : a.v;
+            const int in = h < a.q.heads ? h : h < heads ? h - a.q.heads : h - heads;
+            const unsigned char *p = m.x + (int64_t)(t0 + tok[u]) * m.token + in * m.head + piece * 16 * N;
+#pragma unroll
+            for (int n = 0; n < N; ++n) x[u][n] = *reinterpret_cast<const raw16 *>(p + 16 * n);
+        }
+        if (r0 == 0) {
+            if (tid >= kThreads - 64) { // the last wave, beside the first one's cosines
+                int64_t place, scale;
+                places_of(a.view, t0, nt, &place, &scale);
+                const int lane = tid & 63;
+                if (lane < nt) {
+                    s_place[lane] = place;
+                    s_scale[lane] = scale;
+                }
+            }
+            for (int i = tid; i < nt * n_pairs; i += kThreads) {
+                const int t = i / n_pairs, p = i - t * n_pairs;
+                s_turn[t][p] = turn_of(a, t0 + t, p);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const bool turned = head[u] >= 0 && head[u] < heads && 8 * piece < 2 * n_pairs;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = piece_get<T>(x[u][e / (8 / N)], e % (8 / N));
+            if (a.neighbours) {
+                if (turned)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float2 c = s_turn[tok[u]][4 * piece + e / 2];
+                        const float y0 = f[e] * c.x - f[e + 1] * c.y, y1 = f[e + 1] * c.x + f[e] * c.y;
+                        f[e] = y0;
+                        f[e + 1] = y1;
+                    }
+            } else if (n_pairs > 0) {
+                const bool upper = 8 * piece >= n_pairs; // of the rotated half
+                const int away = n_pairs / 8;            // lanes
+                const int other = (tid & 63) + (turned ? upper ? -away : away : 0);
+                float g[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = 0.f;
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    raw16 y;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) y[w] = (unsigned)__shfl((int)x[u][n][w], other);
+#pragma unroll
+                    for (int e = 0; e < 8 / N; ++e) g[n * (8 / N) + e] = piece_get<T>(y, e);
+                }
+                if (turned)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 c = s_turn[tok[u]][8 * piece + e - (upper ? n_pairs : 0)];
+                        f[e] = upper ? f[e] * c.x + g[e] * c.y : f[e] * c.x - g[e] * c.y;
+                    }
+            }
+            // the row's largest finite feature
+            float most = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fabsf(f[e]) < INFINITY ? fmaxf(most, fabsf(f[e])) : most;
+#pragma unroll
+            for (int m = 1; m < L; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+            if (head[u] < 0) continue;
+            if (head[u] < a.q.heads) {
+                unsigned char *p = a.q.out + (int64_t)(t0 + tok[u]) * a.q.out_token + head[u] * a.q.out_head + piece * 16 * N;
+                raw16 y[N];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) piece_put<T>(y[e / (8 / N)], e % (8 / N), f[e], f[e + 1]);
+#pragma unroll
+                for (int n = 0; n < N; ++n) put_piece(p + 16 * n, y[n]);
+                continue;
+            }
+            if (s_place[tok[u]] < 0) continue;
+            const bool is_k = head[u] < heads;
+            const int g = head[u] - (is_k ? a.q.heads : heads);
+            const int byte = scale_byte(most);
+            const float by = inverse_scale((uint32_t)byte);
+            const u32x2 w = {codes_of(f[0] * by, f[1] * by, f[2] * by, f[3] * by), codes_of(f[4] * by, f[5] * by, f[6] * by, f[7] * by)};
+            unsigned char *p = (is_k ? a.view.k : a.view.v) + s_place[tok[u]] + g * a.view.stride_head + 8 * piece;
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x2 *>(p));
+            if (piece == 0) ((is_k ? a.view.scales.k : a.view.scales.v) + s_scale[tok[u]] + g * a.view.scales.stride_head)[0] = (unsigned char)byte;
+        }
+    }
+}
+
+// Rows of the sequences' last tokens as they were written: k.out and v.out [token][head][D].  A row that does not exist is zeros.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void read8_kernel(RopeArgs a, int per_wg) {
+    constexpr int L = D / 8, N = (int)sizeof(T) / 2, kAtOnce = kThreads / L;
+    __shared__ int64_t s_place[kReadTokens], s_scale[kReadTokens];
+    const int tid = threadIdx.x, piece = tid % L;
+    const int t0 = blockIdx.x * per_wg, nt = a.n_tokens - t0 < per_wg ? a.n_tokens - t0 : per_wg;
+    if (tid < 64) {
+        int64_t place, scale;
+        places_of(a.view, t0, nt, &place, &scale);
+        if (tid < nt) {
+            s_place[tid] = place;
+            s_scale[tid] = scale;
+        }
+    }
+    __syncthreads();
+    const int heads = a.k.heads, rows_per = 2 * heads, n_rows = nt * rows_per;
+    for (int r0 = tid / L; r0 < n_rows; r0 += kAhead * kAtOnce) {
+        u32x2 x[kAhead];
+        uint32_t byte[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + u * kAtOnce;
+            x[u] = u32x2{0u, 0u};
+            byte[u] = 127u;
+            if (r >= n_rows) continue;
+            const int t = r / rows_per, h = r - t * rows_per, g = h < heads ? h : h - heads;
+            if (s_place[t] < 0) continue;
+            x[u] = *reinterpret_cast<const u32x2 *>((h < heads ? a.view.k : a.view.v) + s_place[t] + g * a.view.stride_head + 8 * piece);
+            byte[u] = ((h < heads ? a.view.scales.k : a.view.scales.v) + s_scale[t] + g * a.view.scales.stride_head)[0];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + u * kAtOnce;
+            if (r >= n_rows) continue;
+            const int t = r / rows_per, h = r - t * rows_per, g = h < heads ? h : h - heads;
+            const RopeArgs::Rows &m = h < heads ? a.k : a.v;
+            unsigned char *p = m.out + (int64_t)(t0 + t) * m.out_token + g * m.out_head + piece * 16 * N;
+            const float scale = scale_of(byte[u]);
+            if constexpr (N == 1) {
+                put_piece(p, bf16_piece(x[u][0], x[u][1], scale));
+            } else {
+                put_piece(p, f32_piece(x[u][0], scale));
+                put_piece(p + 16, f32_piece(x[u][1], scale));
+            }
+        }
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_typed(const RopeArgs &a, bool read, hipStream_t st) {
+    int per_wg;
+    if (read) {
+        per_wg = a.n_tokens / 2048;
+        per_wg = per_wg < 1 ? 1 : per_wg > kReadTokens ? kReadTokens : per_wg;
+    } else {
+        per_wg = a.n_tokens / 768;
+        per_wg = per_wg < 1 ? 1 : per_wg > kWriteTokens ? kWriteTokens : per_wg;
+    }
+    const unsigned grid = (unsigned)((a.n_tokens + per_wg - 1) / per_wg);
+    if (read)
+        hipLaunchKernelGGL((read8_kernel<T, D>), dim3(grid), dim3(kThreads), 0, st, a, per_wg);
+    else
+        hipLaunchKernelGGL((write8_kernel<T, D>), dim3(grid), dim3(kThreads), 0, st, a, per_wg);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_by_dim(const RopeArgs &a, bool read, hipStream_t st) {
+    switch (a.D) {
+    case 16: return launch_typed<T, 16>(a, read, st);
+    case 32: return launch_typed<T, 32>(a, read, st);
+    case 64: return launch_typed<T, 64>(a, read, st);
+    default: return launch_typed<T, 128>(a, read, st);
+    }
+}
+
+} // namespace
+
+hipError_t launch_rows8(const RopeArgs &a, int dtype, bool read, hipStream_t st) {
+    return dtype == MUKV_BF16 ? launch_by_dim<uint16_t>(a, read, st) : launch_by_dim<float>(a, read, st);
+}
+
+} // namespace mukv

@@ -1,0 +1,131 @@
+"""What the calls on a cache in 8 bits refuse, on the host, before anything is launched (no GPU here: pointers are never followed)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2605_22269_amd import binding as mk
+from test_paged_binding import PLACES, SEQUENCES, Stand, refuses, tensors  # noqa: F401
+from test_paged_refusals import BAD, P, SEQS, SHAPE, ST, UNSUP, pages, rope, seqs
+
+ref = lambda x: None if x is None else C.byref(x)  # noqa: E731
+
+
+def scales(**kw):
+    return mk.mukv_row_scales(**{**dict(k=P + 1, v=P + 3, stride_layer=6400, stride_page=64, stride_head=16, stride_row=1), **kw})
+
+
+# strides of pages are bytes
+PAGES8 = [({"k_pages": None}, BAD), ({"v_pages": None}, BAD), ({"n_layers": 0}, BAD), ({"n_pages": 0}, BAD), ({"page_rows": 0}, BAD),
+          ({"n_kv_heads": 0}, BAD), ({"device_id": -1}, BAD), ({"dtype": 2}, BAD), ({"n_q_heads": 6}, SHAPE), ({"head_dim": 48}, UNSUP),
+          ({"head_dim": 256}, UNSUP), ({"stride_row": -64}, BAD), ({"stride_row": 72}, UNSUP), ({"stride_head": 8}, UNSUP),
+          ({"stride_page": 1 << 60}, UNSUP), ({"k_pages": P + 8}, UNSUP), ({"page_rows": (1 << 24) + 1}, UNSUP)]
+SCALES = [(None, BAD), ({"k": None}, BAD), ({"v": None}, BAD), ({"stride_layer": -1}, BAD), ({"stride_page": -64}, BAD), ({"stride_head": -1}, BAD),
+          ({"stride_row": -1}, BAD), ({"stride_page": 1 << 60}, UNSUP)]
+
+
+def of(kw):
+    return None if kw is None else scales(**kw)
+
+
+def append(p=None, sc=scales(), layer=0, s=None, k=P, ks=ST, v=P, vs=ST, q=P, qs=ST, qo=P, qos=ST, r=None, pos=P):
+    return mk.load().mukv_paged_append8(ref(p or pages()), ref(sc), layer, ref(s or seqs()), k, ref(ks), v, ref(vs), q, ref(qs), qo, ref(qos),
+                                        ref(r), pos, None)
+
+
+def read(p=None, sc=scales(), layer=0, s=None, k=P, ks=ST, v=P, vs=ST):
+    return mk.load().mukv_paged_read8(ref(p or pages()), ref(sc), layer, ref(s or seqs()), k, ref(ks), v, ref(vs), None)
+
+
+@pytest.mark.parametrize("call", [append, read])
+def test_pages_scales_and_sequences_are_refused(call):
+    for kw, status in PAGES8:
+        assert call(p=pages(**kw)) == status, kw
+    for kw, status in SCALES:
+        assert call(sc=of(kw)) == status, kw
+    for kw, status in SEQS:
+        assert call(s=seqs(**kw)) == status, kw
+    assert call(layer=-1) == call(layer=2) == BAD
+    assert call(s=seqs(n_tokens=0)) == mk.MUKV_OK
+    # a dimension of one is never walked
+    one = dict(n_layers=1, stride_layer=-5)
+    assert call(p=pages(**one), sc=scales(stride_layer=-5), s=seqs(n_tokens=0)) == mk.MUKV_OK
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({"k": None}, BAD), ({"v": None}, BAD), ({"ks": None}, BAD), ({"q": None}, BAD), ({"qo": None}, BAD), ({"qs": None}, BAD),
+    ({"k": P + 2}, UNSUP), ({"ks": mk.mukv_strides(0, 65, 1024)}, UNSUP), ({"vs": mk.mukv_strides(0, 64, -1024)}, BAD),
+    ({"r": rope(), "pos": None}, BAD), ({"r": rope(n_rot=24)}, UNSUP), ({"r": rope(n_rot=80)}, SHAPE)])
+def test_append_refuses_tensors(kw, status):
+    assert append(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [({"k": None}, BAD), ({"v": None}, BAD), ({"ks": None}, BAD), ({"vs": None}, BAD), ({"v": P + 2}, UNSUP),
+                                       ({"ks": mk.mukv_strides(0, 65, 1024)}, UNSUP), ({"vs": mk.mukv_strides(0, 64, -1024)}, BAD)])
+def test_read_refuses_tensors(kw, status):
+    assert read(**kw) == status
+
+
+# ---- the Python side ----
+def cache8(where={}, dtype=torch.bfloat16, **kw):
+    e, s = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    at = lambda name, *shape, dtype: Stand(*shape, dtype=dtype, device=where.get(name, 0), **kw.get(name, {}))  # noqa: E731
+    return mk.PagedKV8(at("k_pages", 1, 9, 2, 16, 64, dtype=e), at("v_pages", 1, 9, 2, 16, 64, dtype=e), at("k_scales", 1, 9, 2, 16, dtype=s),
+                       at("v_scales", 1, 9, 2, 16, dtype=s), n_q_heads=4, dtype=dtype)
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_caches_whose_parts_lie_apart_are_refused(place):
+    cache8()
+    for name in ("k_pages", "v_pages", "k_scales", "v_scales"):
+        with pytest.raises(AssertionError):
+            cache8({name: place})
+
+
+def test_caches_of_other_types_and_shapes_are_refused():
+    e, s = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    good = dict(k_pages=Stand(1, 9, 2, 16, 64, dtype=e), v_pages=Stand(1, 9, 2, 16, 64, dtype=e), k_scales=Stand(1, 9, 2, 16, dtype=s),
+                v_scales=Stand(1, 9, 2, 16, dtype=s))
+    mk.PagedKV8(**good, n_q_heads=4)
+    for name, other in (("k_pages", Stand(1, 9, 2, 16, 64)), ("v_pages", Stand(1, 9, 2, 16, 64, dtype=torch.float8_e5m2)),
+                        ("k_scales", Stand(1, 9, 2, 16, dtype=torch.float32)), ("v_scales", Stand(1, 9, 2, 16, dtype=torch.uint8)),
+                        ("v_scales", Stand(1, 9, 2, 15, dtype=s)), ("v_scales", Stand(1, 9, 2, 16, dtype=s, strides=(0, 16, 144, 1))),
+                        ("v_pages", Stand(1, 9, 2, 16, 32, dtype=e))):
+        with pytest.raises(AssertionError):
+            mk.PagedKV8(**{**good, name: other}, n_q_heads=4)
+    with pytest.raises(AssertionError):
+        mk.PagedKV8(**good, n_q_heads=4, dtype=torch.float16)
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_tensors_that_lie_elsewhere_are_refused(refuses, place, monkeypatch):  # noqa: F811
+    c = cache8()
+    kv = dict(k=("b", 3, 2, 64), v=("b", 3, 2, 64))
+
+    def put(where):
+        t = tensors(where, **SEQUENCES, **kv, q=("b", 3, 4, 64), q_out=("b", 3, 4, 64), positions=("i", 1, 3))
+        c.append(0, **t, rope=mk.Rope(Stand(16, dtype=torch.float64)))
+
+    refuses(put, [*SEQUENCES, *kv, "q", "q_out", "positions"], place, c)
+    reached = []
+    monkeypatch.setattr(mk, "mukv_paged_read8", lambda *a: reached.append(a))
+
+    def back(where):
+        c.read(0, **tensors(where, **SEQUENCES, k_out=("b", 3, 2, 64), v_out=("b", 3, 2, 64)))
+
+    back({})
+    assert reached
+    for name in (*SEQUENCES, "k_out", "v_out"):
+        with pytest.raises(AssertionError):
+            back({name: place})
+    assert len(reached) == 1
+    for kw in (dict(n_tokens=4, k_out=Stand(3, 2, 64)), dict(k_out=Stand(3, 2, 64), v_out=Stand(3, 2, 32)), dict(k_out=Stand(3, 2, 64, dtype=torch.float32))):
+        with pytest.raises(AssertionError):
+            c.read(0, **tensors({}, **SEQUENCES), **kw)
+
+
+def test_structures_are_declared_as_they_are():
+    assert C.sizeof(mk.mukv_row_scales) == 48
+    c = cache8()
+    assert (c._scales.k, c._scales.stride_page, c._scales.stride_head, c._scales.stride_row) == (c._held[2].data_ptr(), 32, 16, 1)
+    assert (c._pages.stride_row, c._pages.dtype) == (64, mk.MUKV_BF16) and cache8(dtype=torch.float32)._pages.dtype == mk.MUKV_F32
