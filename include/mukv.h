@@ -776,6 +776,44 @@ int mukv_paged_read8(const mukv_paged *pages, const mukv_row_scales *scales, int
                      void *stream);
 
 /*
+ * mukv_paged_attend over a cache in 8 bits (seqs->table is not NULL), with the same
+ * workspace: rows count for what mukv_paged_read8 gives, and everything that is said
+ * there holds.
+ */
+int mukv_paged_attend8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                       const void *q, const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
+                       void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Attention where groups of sequences share rows (a video that several users ask
+ * about, instructions before every conversation): the shared rows lie in the pages once
+ * and are read once for all of a group's tokens.  A token sees all rows that its group
+ * shares and, as in mukv_paged_attend, those of its sequence (causal: up to its own); one
+ * softmax goes over both.
+ *
+ *   scales          NULL, or those of a cache in 8 bits
+ *   seqs            the sequences' own rows; table is not NULL.  lengths count no shared rows
+ *   shared          the groups: tables and lengths of the rows they share; offsets say
+ *                   which of the new tokens are a group's (offsets[g] .. offsets[g+1]-1,
+ *                   ascending; NULL: n_tokens / n_seqs each), so sequences of a group are next to
+ *                   each other.  Tokens before the first and behind the last see no
+ *                   shared rows.  n_tokens as in seqs, max_new: most new tokens of a group
+ *                   (0: not known).  Where offsets do not ascend, out is left as it is
+ *   weights, shared_weights   NULL, or where the weights of the sequences' own rows, of the
+ *                   shared rows of every group go: the sum over all that see them
+ *   workspace       at least mukv_paged_shared_workspace_size() bytes, otherwise as there
+ *
+ * What is shared is added up apart and joined to the rest in fp32 before the one rounding.
+ * Errors: as mukv_paged_attend; SHAPE (n_tokens differ).
+ */
+int mukv_paged_shared_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_seqs *shared, int32_t with_weights,
+                                     int64_t *bytes_out);
+int mukv_paged_attend_shared(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                             const mukv_seqs *shared, const void *q, const mukv_strides *q_strides, int32_t causal, void *out,
+                             const mukv_row_weights *weights, const mukv_row_weights *shared_weights, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+
+/*
  * The graph capture that `stream` is in: a number that no other capture of the
  * process has, 0 if there is none.  Scratch that a capture clears is fit for the
  * calls of that capture alone: nothing has run when the capture ends.

@@ -103,7 +103,8 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_attend", "mukv_prefill_workspace_size", "mukv_prefill_attend", "mukv_prefill_attend_static",
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
            "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append",
-           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_paged_append8", "mukv_paged_read8", "mukv_stream_capture", "mukv_strerror")
+           "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_paged_append8", "mukv_paged_read8",
+           "mukv_paged_attend8", "mukv_paged_shared_workspace_size", "mukv_paged_attend_shared", "mukv_stream_capture", "mukv_strerror")
 
 _lib = None
 
@@ -153,6 +154,9 @@ def load():
     lib.mukv_paged_evict.argtypes = [paged, seqs, vp, i32, i32, i32, vp, i32, vp, vp, vp]
     lib.mukv_paged_append8.argtypes = [paged, vp, i32, seqs, vp, strides, vp, strides, vp, strides, vp, strides, vp, vp, vp]
     lib.mukv_paged_read8.argtypes = [paged, vp, i32, seqs, vp, strides, vp, strides, vp]
+    lib.mukv_paged_attend8.argtypes = [paged, vp, i32, seqs, vp, strides, i32, vp, vp, vp, C.c_int64, vp]
+    lib.mukv_paged_shared_workspace_size.argtypes = [paged, seqs, seqs, i32, C.POINTER(C.c_int64)]
+    lib.mukv_paged_attend_shared.argtypes = [paged, vp, i32, seqs, seqs, vp, strides, i32, vp, vp, vp, vp, C.c_int64, vp]
     lib.mukv_stream_capture.argtypes = [vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
@@ -352,6 +356,12 @@ def mukv_paged_evict(pages, seqs, weights, budget, n_sink, n_recent, into_ptr, i
 
 def mukv_paged_read8(pages, scales, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, stream):
     _check((_lib or load()).mukv_paged_read8(pages, scales, layer, seqs, k_ptr, k_strides, v_ptr, v_strides, stream), "mukv_paged_read8")
+
+
+def mukv_paged_shared_workspace_size(pages, seqs, shared, with_weights):
+    n = C.c_int64(0)
+    _check((_lib or load()).mukv_paged_shared_workspace_size(pages, seqs, shared, with_weights, C.byref(n)), "mukv_paged_shared_workspace_size")
+    return n.value
 
 
 # ---- convenience object ----------------------------------------------------------------------
@@ -766,34 +776,27 @@ class _Sequences:
     cache together."""
 
     def __init__(self):
-        self._scratch, self._need = {}, (None, 0)
+        self._scratch, self._need, self._shared_need, self._scales_at = {}, (None, 0), (None, 0), None
         lib = _lib or load()
         self._c_append, self._c_attend, self._c_capture = lib.mukv_paged_append, lib.mukv_paged_attend, lib.mukv_stream_capture
+        self._c_shared = lib.mukv_paged_attend_shared
 
-    def _attend(self, pages, s, index, heads, key, layer, q, causal, out, weights, weights_out, decay):
-        """heads: sequences and KV heads; key: all that the scratch's size follows from."""
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        else:
-            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
-        assert q.get_device() == index
-        w = None
-        if weights_out is not None:
-            st, weights_in = weights_out.stride(), 0
-            assert weights_out.dtype is torch.float32 and len(st) == 3 and st[2] == 1
-            assert weights_out.shape[:2] == heads and weights_out.get_device() == index
-            if weights is not None:
-                assert weights.dtype is torch.float32 and weights.shape == weights_out.shape and weights.stride() == st
-                assert weights.get_device() == index
-                weights_in = weights.data_ptr()
-            w = _WEIGHTS.pack(weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
-        else:
+    def _weights(self, weights, weights_out, heads, index, decay):
+        """C form of where weights go, float32 [*heads][row]; None: nowhere."""
+        if weights_out is None:
             assert weights is None
-        stream = _stream_of(index)
-        need = self._need
-        if need[0] != key:
-            need = self._need = key, mukv_paged_workspace_size(pages, s, int(w is not None))
-        need = need[1]
+            return None
+        st, weights_in = weights_out.stride(), 0
+        assert weights_out.dtype is torch.float32 and len(st) == 3 and st[2] == 1
+        assert weights_out.shape[:2] == heads and weights_out.get_device() == index
+        if weights is not None:
+            assert weights.dtype is torch.float32 and weights.shape == weights_out.shape and weights.stride() == st
+            assert weights.get_device() == index
+            weights_in = weights.data_ptr()
+        return _WEIGHTS.pack(weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
+
+    def _space(self, need, index, stream, device):
+        """Address and size of scratch for a call on this stream."""
         capture = C.c_uint64()
         rc = self._c_capture(stream, C.byref(capture))
         if rc:
@@ -802,14 +805,50 @@ class _Sequences:
         place = index, stream, capture != 0
         ws = self._scratch.get(place)
         if ws is None or ws[1] < need or ws[3] != capture:
-            t = torch.empty(need, dtype=torch.uint8, device=q.device)
+            t = torch.empty(need, dtype=torch.uint8, device=device)
             t[:MUKV_PAGED_CLEAR].zero_()   # every call finds and leaves it so
             ws = self._scratch[place] = t.data_ptr(), need, t, capture
+        return ws
+
+    def _attend(self, pages, s, index, heads, key, layer, q, causal, out, weights, weights_out, decay):
+        """heads: sequences and KV heads; key: all that the scratch's size follows from."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
+        assert q.get_device() == index
+        w = self._weights(weights, weights_out, heads, index, decay)
+        stream = _stream_of(index)
+        need = self._need
+        if need[0] != key:
+            need = self._need = key, mukv_paged_workspace_size(pages, s, int(w is not None))
+        ws = self._space(need[1], index, stream, q.device)
         rc = self._c_attend(pages, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
                             w, ws[0], ws[1], stream)
         if rc:
             _check(rc, "mukv_paged_attend")
         return out
+
+
+class Shared:
+    """Rows that groups of sequences share: table int32 [group][page], lengths int32 [group], offsets int32 [group+1] -- group g's new
+    tokens are offsets[g] .. offsets[g+1]-1 of a call's (None: as many each).  max_tokens: most of a group, as a hint."""
+
+    def __init__(self, table, lengths, offsets=None, *, max_tokens=0):
+        n, width = table.shape
+        index = self.index = table.get_device()
+        assert index >= 0 and table.dtype is _I32 and table.is_contiguous()
+        assert lengths.dtype is _I32 and lengths.shape == (n,) and lengths.is_contiguous() and lengths.get_device() == index
+        off = 0
+        if offsets is not None:
+            assert offsets.dtype is _I32 and offsets.shape == (n + 1,) and offsets.is_contiguous() and offsets.get_device() == index
+            off = offsets.data_ptr()
+        self._held = table, lengths, offsets
+        self.n, self.width, self.max_tokens = n, width, max_tokens
+        self._at = table.data_ptr(), lengths.data_ptr(), off, n, width
+
+    def pack(self, n_tokens):
+        return _SEQS.pack(*self._at, n_tokens, self.max_tokens)
 
 
 class PagedKV(_Sequences):
@@ -872,17 +911,39 @@ class PagedKV(_Sequences):
         return q_out
 
     def attend(self, layer, table, lengths, q, *, offsets=None, max_new=0, causal=True, out=None, weights=None, weights_out=None,
-               decay=1.0):
+               decay=1.0, shared=None, shared_weights=None, shared_weights_out=None):
         """q [n_tokens][n_q_heads][head_dim]: every sequence's new tokens (lengths count them) attend to its rows.  With
         weights_out, float32 [sequence][KV head][row], it becomes decay * weights + what every row received (weights None: zeros;
         weights_out may be weights).  max_new: most new tokens of a sequence, as a hint (kernels round
-        differently).  Returns out, which must not overlap q."""
+        differently).  shared (a Shared): the tokens of each group attend to the rows it shares as well, whose weights go to
+        shared_weights_out, float32 [group][KV head][row].  Returns out, which must not overlap q."""
         T, heads, dim = q.shape
         assert heads == self._q_heads and dim == self._dim and q.dtype is self.dtype
         s = self._sequences(table, lengths, offsets, T, max_new)
         n, width = table.shape
         key = T, n, width, max_new, weights_out is None   # (what else scratch depends on is the cache's)
-        return self._attend(self._pages_at, s, self._index, (n, self._heads), key, layer, q, causal, out, weights, weights_out, decay)
+        if shared is None:
+            assert shared_weights is None and shared_weights_out is None
+            return self._attend(self._pages_at, s, self._index, (n, self._heads), key, layer, q, causal, out, weights, weights_out, decay)
+        index = self._index
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
+        assert q.get_device() == index and shared.index == index
+        w = self._weights(weights, weights_out, (n, self._heads), index, decay)
+        sw = self._weights(shared_weights, shared_weights_out, (shared.n, self._heads), index, decay)
+        groups = shared.pack(T)
+        stream, need = _stream_of(index), self._shared_need
+        key = *key, sw is None, shared.n, shared.width, shared.max_tokens
+        if need[0] != key:
+            need = self._shared_need = key, mukv_paged_shared_workspace_size(self._pages_at, s, groups, int(w is not None or sw is not None))
+        ws = self._space(need[1], index, stream, q.device)
+        rc = self._c_shared(self._pages_at, self._scales_at, layer, s, groups, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q),
+                            1 if causal else 0, out.data_ptr(), w, sw, ws[0], ws[1], stream)
+        if rc:
+            _check(rc, "mukv_paged_attend_shared")
+        return out
 
     def evict(self, table, lengths, weights, budget, *, sink=0, recent=0, into=None, weights_out=None, kept=None, lengths_out=None):
         """Brings every sequence down to `budget` rows per layer and KV head: the first `sink`, the last `recent`, and the others
@@ -917,9 +978,9 @@ class PagedKV(_Sequences):
 class PagedKV8(PagedKV):
     """The conversation's cache in 8 bits: k_pages, v_pages float8_e4m3fn [layer][page][KV head][row][feature], k_scales, v_scales
     float8_e8m0fnu (or their bytes, uint8) [layer][page][KV head][row], any strides but the pages' last.  dtype: that of queries, new rows and
-    outputs."""
+    outputs.  Calls are those of PagedKV, and read()."""
 
-    attend = evict = None   # (those of PagedKV take the rows for numbers of its dtype)
+    evict = None   # (that of PagedKV takes the rows for numbers of its dtype)
 
     def __init__(self, k_pages, v_pages, k_scales, v_scales, *, n_q_heads, dtype=torch.bfloat16):
         _Sequences.__init__(self)
@@ -939,8 +1000,10 @@ class PagedKV8(PagedKV):
         self._pages = mukv_paged(_ptr(k_pages), _ptr(v_pages), sl, sp, sh, sr, L, n, R, n_q_heads, hkv, D, kind, self._index)
         self._scales = mukv_row_scales(_ptr(k_scales), _ptr(v_scales), *k_scales.stride())
         self._pages_at, self._scales_at = C.addressof(self._pages), C.addressof(self._scales)
-        call, at = (_lib or load()).mukv_paged_append8, self._scales_at
-        self._c_append = lambda pages, *rest: call(pages, at, *rest)
+        lib, at = _lib or load(), self._scales_at
+        append, attend = lib.mukv_paged_append8, lib.mukv_paged_attend8
+        self._c_append = lambda pages, *rest: append(pages, at, *rest)
+        self._c_attend = lambda pages, *rest: attend(pages, at, *rest)
 
     def read(self, layer, table, lengths, offsets, *, n_tokens=None, k_out=None, v_out=None):
         """Rows as they were written, as the cache's dtype: [n_tokens][n_kv_heads][head_dim], those of sequence b at offsets[b] ..

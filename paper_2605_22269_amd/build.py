@@ -10,7 +10,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmukv.so")
 SOURCES = ["api.hip", "compress.hip", "att_mfma.hip", "retrieve.hip", "attend.hip", "paged_api.hip", "rope.hip", "paged_attend.hip",
-           "paged_flash.hip", "paged_evict.hip", "rows8.hip"]
+           "paged_flash.hip", "paged_evict.hip", "rows8.hip", "paged_attend8.hip", "paged_flash8.hip",
+           "paged_shared.hip", "paged_shared_flash.hip", "paged_shared_flash8.hip"]
 OBJ = os.path.join(PKG, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -155,22 +155,43 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
     a.inverse = r->inverse != 0;
 }
 
-// Which kernel takes an attention call, and its workspace: counts, records, then (with weights) the prompt kernel's sums and a pair per query.
+// Which kernel takes an attention call, and its workspace: counts, records, then (with weights) the prompt kernel's sums and a pair per query,
+// and what attention over shared rows leaves.
 struct Space {
-    mukv::PlanShape plan;
-    int64_t stats, values, sums, pairs, bytes; // offsets; the counts are at 0
+    mukv::PlanShape plan, shared_plan;
+    int64_t stats, values, sums, pairs, fit, left_stats, left_values, bytes; // offsets; the counts are at 0
 };
-Space space_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool with_weights) {
+int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
+mukv::PlanShape plan_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool *prompts) {
     const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
-    Space x;
     const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint);
-    x.plan = mukv::paged_plan(p.dtype, tile, causal);
-    const int64_t rows = (int64_t)x.plan.records * x.plan.queries;
+    *prompts = tile != 0;
+    return mukv::paged_plan(p.dtype, tile, causal);
+}
+Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
+    Space x;
+    bool prompts, shared_prompts = false;
+    x.plan = plan_of(p, s, causal, &prompts);
+    int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
+    if (shared) { // one launch after the other: they have the counts and the records in common
+        x.shared_plan = plan_of(p, *shared, false, &shared_prompts);
+        const int64_t n = (int64_t)x.shared_plan.records * x.shared_plan.queries;
+        if (shared_prompts && n > sums) sums = n;
+        if (n > rows) rows = n;
+    }
     x.stats = 4 * mukv::kPlanRecords;
     x.values = x.stats + 8 * rows;
     x.sums = x.values + 4 * rows * p.head_dim;
-    x.pairs = x.sums + (with_weights && tile ? 4 * rows : 0);
-    x.bytes = x.pairs + (with_weights ? 8 * (int64_t)s.n_tokens * p.n_q_heads : 0);
+    x.pairs = x.sums + (with_weights ? 4 * sums : 0);
+    const int64_t queries = (int64_t)s.n_tokens * p.n_q_heads;
+    x.bytes = x.pairs + (with_weights ? 8 * queries : 0);
+    x.fit = x.left_stats = x.left_values = 0;
+    if (shared) {
+        x.fit = up_to_16(x.bytes);
+        x.left_stats = x.fit + 16;
+        x.left_values = x.left_stats + 16 * queries;
+        x.bytes = x.left_values + 4 * queries * p.head_dim;
+    }
     return x;
 }
 
@@ -211,6 +232,89 @@ int append(const mukv_paged *pages, const mukv_row_scales *scales, bool eight, i
     if (!dev.ok) return MUKV_ERR_HIP;
     const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     return finished(eight ? mukv::launch_rows8(a, pages->dtype, false, st) : mukv::launch_rope(a, pages->dtype, st));
+}
+
+void set_weights(mukv::PagedAttendArgs &a, const mukv_row_weights &w) {
+    a.weights_in = w.in;
+    a.weights_out = w.out;
+    a.weights_seq = w.stride_seq;
+    a.weights_head = w.stride_head;
+    a.weights_rows = w.rows;
+    a.decay = w.decay;
+}
+
+// Attention over rows as they are or (scales) in 8 bits, perhaps over shared ones too; the pages have been checked.
+int attend(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs, const mukv_seqs *shared,
+           const void *q, const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
+           const mukv_row_weights *shared_weights, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (layer < 0 || layer >= pages->n_layers || (causal != 0 && causal != 1)) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
+    if (shared) {
+        if (const int rc = check_seqs(pages, shared, false, true)) return rc;
+        if (shared->n_tokens != seqs->n_tokens) return MUKV_ERR_SHAPE;
+    }
+    if (weights)
+        if (const int rc = check_weights(weights)) return rc;
+    if (shared_weights)
+        if (const int rc = check_weights(shared_weights)) return rc;
+    const int T = seqs->n_tokens, D = pages->head_dim, esz = elem_size(pages->dtype);
+    const bool any_weights = weights || shared_weights;
+    if (T == 0 && (!any_weights || !seqs->table)) return MUKV_OK; // (packed, no sequence has a row that could have a weight)
+    const mukv_strides dense = {0, D, (int64_t)D * pages->n_q_heads};
+    const mukv_strides *qs = q_strides ? q_strides : &dense;
+    if (T > 0) { // (empty tensors need not have an address)
+        if (const int rc = check_rows(q, qs, T, pages->n_q_heads, esz)) return rc;
+        if (!out) return MUKV_ERR_INVALID_ARG;
+        if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
+    }
+    if (!workspace) return MUKV_ERR_INVALID_ARG;
+    const Space x = space_of(*pages, *seqs, shared, causal != 0, any_weights);
+    if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
+    if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
+    mukv::PagedAttendArgs a = {};
+    a.view = view_of(*pages, layer, *seqs, scales);
+    a.plan = x.plan;
+    a.q = static_cast<const unsigned char *>(q);
+    a.q_token = in_bytes(qs->token, T, esz);
+    a.q_head = in_bytes(qs->head, pages->n_q_heads, esz);
+    a.out = out;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    a.counts = reinterpret_cast<int *>(ws);
+    a.records.stats = reinterpret_cast<float *>(ws + x.stats);
+    a.records.values = reinterpret_cast<float *>(ws + x.values);
+    a.records.sums = reinterpret_cast<float *>(ws + x.sums);
+    a.pairs = any_weights ? reinterpret_cast<float *>(ws + x.pairs) : nullptr;
+    a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
+    a.causal = causal;
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    DeviceScope dev(pages->device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    auto launch = [&](const mukv::PagedAttendArgs &b) {
+        if (shared) return mukv::launch_shared_attend(b, D, pages->dtype, scales != nullptr, st);
+        return scales ? mukv::launch_paged_attend8(b, D, pages->dtype, st) : mukv::launch_paged_attend(b, D, pages->dtype, st);
+    };
+    mukv::PagedAttendArgs of_groups = a;
+    if (shared) {
+        a.shared.mode = mukv::SharedResults::kTake;
+        a.shared.n_groups = shared->n_seqs;
+        a.shared.offsets = shared->offsets;
+        a.shared.fit = reinterpret_cast<int *>(ws + x.fit);
+        a.shared.stats = reinterpret_cast<float *>(ws + x.left_stats);
+        a.shared.values = reinterpret_cast<float *>(ws + x.left_values);
+        of_groups.view = view_of(*pages, layer, *shared, scales);
+        of_groups.plan = x.shared_plan;
+        of_groups.causal = 0;
+        of_groups.shared = a.shared;
+        of_groups.shared.mode = mukv::SharedResults::kLeave;
+        if (T > 0)
+            if (const hipError_t e = launch(of_groups); e != hipSuccess) return MUKV_ERR_HIP;
+    }
+    if (weights) set_weights(a, *weights);
+    if (const hipError_t e = launch(a); e != hipSuccess) return MUKV_ERR_HIP;
+    if (!shared_weights) return MUKV_OK;
+    set_weights(of_groups, *shared_weights);
+    const bool bf16 = pages->dtype == MUKV_BF16;
+    return finished(scales ? mukv::launch_paged_weights8(of_groups, D, bf16, st) : mukv::launch_paged_weights(of_groups, D, bf16, st));
 }
 
 } // namespace
@@ -286,7 +390,7 @@ int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, in
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_pages(pages, packed_nothing(seqs))) return rc;
     if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
-    *bytes_out = space_of(*pages, *seqs, true, with_weights != 0).bytes;
+    *bytes_out = space_of(*pages, *seqs, nullptr, true, with_weights != 0).bytes;
     return MUKV_OK;
 }
 
@@ -294,49 +398,35 @@ int mukv_paged_attend(const mukv_paged *pages, int32_t layer, const mukv_seqs *s
                       const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
                       void *workspace, int64_t workspace_bytes, void *stream) {
     if (const int rc = check_pages(pages, packed_nothing(seqs))) return rc;
-    if (layer < 0 || layer >= pages->n_layers || (causal != 0 && causal != 1)) return MUKV_ERR_INVALID_ARG;
-    if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
-    if (weights)
-        if (const int rc = check_weights(weights)) return rc;
-    const int T = seqs->n_tokens, D = pages->head_dim, esz = elem_size(pages->dtype);
-    if (T == 0 && (!weights || !seqs->table)) return MUKV_OK; // (packed, no sequence has a row that could have a weight)
-    const mukv_strides dense = {0, D, (int64_t)D * pages->n_q_heads};
-    const mukv_strides *qs = q_strides ? q_strides : &dense;
-    if (T > 0) { // (empty tensors need not have an address)
-        if (const int rc = check_rows(q, qs, T, pages->n_q_heads, esz)) return rc;
-        if (!out) return MUKV_ERR_INVALID_ARG;
-        if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
-    }
-    if (!workspace) return MUKV_ERR_INVALID_ARG;
-    const Space x = space_of(*pages, *seqs, causal != 0, weights != nullptr);
-    if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
-    if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
-    mukv::PagedAttendArgs a = {};
-    a.view = view_of(*pages, layer, *seqs);
-    a.plan = x.plan;
-    a.q = static_cast<const unsigned char *>(q);
-    a.q_token = in_bytes(qs->token, T, esz);
-    a.q_head = in_bytes(qs->head, pages->n_q_heads, esz);
-    a.out = out;
-    unsigned char *ws = static_cast<unsigned char *>(workspace);
-    a.counts = reinterpret_cast<int *>(ws);
-    a.records.stats = reinterpret_cast<float *>(ws + x.stats);
-    a.records.values = reinterpret_cast<float *>(ws + x.values);
-    a.records.sums = reinterpret_cast<float *>(ws + x.sums);
-    a.pairs = weights ? reinterpret_cast<float *>(ws + x.pairs) : nullptr;
-    a.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
-    a.causal = causal;
-    if (weights) {
-        a.weights_in = weights->in;
-        a.weights_out = weights->out;
-        a.weights_seq = weights->stride_seq;
-        a.weights_head = weights->stride_head;
-        a.weights_rows = weights->rows;
-        a.decay = weights->decay;
-    }
-    DeviceScope dev(pages->device_id);
-    if (!dev.ok) return MUKV_ERR_HIP;
-    return finished(mukv::launch_paged_attend(a, D, pages->dtype, reinterpret_cast<hipStream_t>(stream)));
+    return attend(pages, nullptr, layer, seqs, nullptr, q, q_strides, causal, out, weights, nullptr, workspace, workspace_bytes, stream);
+}
+
+int mukv_paged_attend8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                       const void *q, const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
+                       void *workspace, int64_t workspace_bytes, void *stream) {
+    if (const int rc = check_pages8(pages, scales)) return rc;
+    if (seqs && !seqs->table) return MUKV_ERR_INVALID_ARG; // (packed rows have no scales)
+    return attend(pages, scales, layer, seqs, nullptr, q, q_strides, causal, out, weights, nullptr, workspace, workspace_bytes, stream);
+}
+
+int mukv_paged_shared_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_seqs *shared, int32_t with_weights,
+                                     int64_t *bytes_out) {
+    if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
+    if (const int rc = check_pages(pages, false, true)) return rc; // (either kind of pages: only counts are read)
+    if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
+    if (const int rc = check_seqs(pages, shared, false, true)) return rc;
+    if (shared->n_tokens != seqs->n_tokens) return MUKV_ERR_SHAPE;
+    *bytes_out = space_of(*pages, *seqs, shared, true, with_weights != 0).bytes;
+    return MUKV_OK;
+}
+
+int mukv_paged_attend_shared(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
+                             const mukv_seqs *shared, const void *q, const mukv_strides *q_strides, int32_t causal, void *out,
+                             const mukv_row_weights *weights, const mukv_row_weights *shared_weights, void *workspace,
+                             int64_t workspace_bytes, void *stream) {
+    if (const int rc = scales ? check_pages8(pages, scales) : check_pages(pages)) return rc;
+    if (!shared || (seqs && !seqs->table)) return MUKV_ERR_INVALID_ARG; // (packed rows are not in the pages that shared ones are in)
+    return attend(pages, scales, layer, seqs, shared, q, q_strides, causal, out, weights, shared_weights, workspace, workspace_bytes, stream);
 }
 
 int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,

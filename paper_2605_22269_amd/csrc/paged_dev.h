@@ -184,6 +184,35 @@ __device__ __forceinline__ bool find_unit(const PagedView &v, const PlanShape &p
     return true;
 }
 
+// ---- results of shared rows ----
+// Whether the groups' offsets ascend, for the other launch: by the first wave of workgroup 0.
+__device__ __forceinline__ void tell_fit(const PagedView &v, const SharedResults &r) {
+    if (blockIdx.x != 0 || threadIdx.x >= 64) return;
+    bool fit = true;
+    for (int b = threadIdx.x; b < v.n_seqs; b += 64) fit = fit && offsets_fit(v, b);
+    if (__builtin_amdgcn_ballot_w64(!fit) == 0) {
+        if (threadIdx.x == 0) *r.fit = 1;
+    } else if (threadIdx.x == 0) {
+        *r.fit = 0;
+    }
+}
+__device__ __forceinline__ bool in_a_group(const SharedResults &r, int token) {
+    return !r.offsets || (token >= r.offsets[0] && token < r.offsets[r.n_groups]);
+}
+// How two parts of a row's softmax become one: what each is multiplied by, and what weights are relative to then.  A part without
+// weights (their sum is zero; a NaN is not) counts for nothing.
+struct JoinBy {
+    float at, own, other;
+};
+__device__ __forceinline__ JoinBy join_by(float at, float sum, float other_at, float other_sum) {
+    const bool some = sum != 0.f, others = other_sum != 0.f;
+    JoinBy j;
+    j.at = some && others ? fmaxf(at, other_at) : others ? other_at : at;
+    j.own = some ? (others ? __builtin_amdgcn_exp2f(at - j.at) : 1.f) : 0.f;
+    j.other = others ? (some ? __builtin_amdgcn_exp2f(other_at - j.at) : 1.f) : 0.f;
+    return j;
+}
+
 // ---- joining a tile's chunks ----
 // Records are written through to, and read from, the memory that all XCDs share.
 constexpr int kFar = 16; // cache policy of a buffer access: the scope of the whole GPU (sc1)

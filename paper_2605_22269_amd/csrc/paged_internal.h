@@ -40,6 +40,18 @@ struct ChunkRecords {
                    // where the weights of rows are asked for)
 };
 
+// What attention over shared rows leaves for the call's other launch, over the sequences' own: per (token, head) its unnormalised output
+// and, of its weights, what their exponents subtract, their sum as the output was multiplied by them and their sum as they were.
+struct SharedResults {
+    enum { kNone, kLeave, kTake };
+    int mode;
+    int n_groups;
+    const int32_t *offsets; // of the groups' tokens; tokens before the first and behind the last are no group's.  Null: all are some group's
+    float *values;          // [n_tokens * Hq][D]
+    float *stats;           // [n_tokens * Hq][4]
+    int *fit;               // whether the groups' offsets ascend: otherwise nothing is left, and nothing may be taken
+};
+
 struct PagedAttendArgs {
     PagedView view;
     PlanShape plan;
@@ -57,9 +69,20 @@ struct PagedAttendArgs {
     int64_t weights_seq, weights_head; // strides in elements
     int weights_rows;                  // rows a head has room for
     float decay;
+    SharedResults shared;
 };
 hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st);
 hipError_t launch_paged_flash(const PagedAttendArgs &a, int D, hipStream_t st);
+// the same over rows in 8 bits
+hipError_t launch_paged_attend8(const PagedAttendArgs &a, int D, int dtype, hipStream_t st);
+hipError_t launch_paged_flash8(const PagedAttendArgs &a, int D, hipStream_t st);
+// what rows receive, by a.pairs
+hipError_t launch_paged_weights(const PagedAttendArgs &a, int D, bool bf16, hipStream_t st);
+hipError_t launch_paged_weights8(const PagedAttendArgs &a, int D, bool bf16, hipStream_t st);
+// the same with results left or taken
+hipError_t launch_shared_attend(const PagedAttendArgs &a, int D, int dtype, bool eight, hipStream_t st);
+hipError_t launch_shared_flash(const PagedAttendArgs &a, int D, hipStream_t st);
+hipError_t launch_shared_flash8(const PagedAttendArgs &a, int D, hipStream_t st);
 
 struct EvictArgs {
     PagedView view; // of layer 0

@@ -6,7 +6,7 @@ import torch
 
 from paper_2605_22269_amd import binding as mk
 from test_paged_binding import PLACES, SEQUENCES, Stand, refuses, tensors  # noqa: F401
-from test_paged_refusals import BAD, P, SEQS, SHAPE, ST, UNSUP, pages, rope, seqs
+from test_paged_refusals import BAD, P, SEQS, SHAPE, ST, UNSUP, WEIGHTS, pages, rope, seqs, weights
 
 ref = lambda x: None if x is None else C.byref(x)  # noqa: E731
 
@@ -129,3 +129,110 @@ def test_structures_are_declared_as_they_are():
     c = cache8()
     assert (c._scales.k, c._scales.stride_page, c._scales.stride_head, c._scales.stride_row) == (c._held[2].data_ptr(), 32, 16, 1)
     assert (c._pages.stride_row, c._pages.dtype) == (64, mk.MUKV_BF16) and cache8(dtype=torch.float32)._pages.dtype == mk.MUKV_F32
+
+
+# ---- attention ----
+def attend(p=None, sc=scales(), layer=0, s=None, q=P, qs=ST, causal=1, out=P, w=None, ws=P, n=1 << 40):
+    return mk.load().mukv_paged_attend8(ref(p or pages()), ref(sc), layer, ref(s or seqs()), q, ref(qs), causal, out, ref(w), ws, n, None)
+
+
+GROUPS = dict(n_seqs=2, n_tokens=5)
+
+
+def shared(p=None, sc=scales(), layer=0, s=None, g=seqs(**GROUPS), q=P, qs=ST, causal=1, out=P, w=None, sw=None, ws=P, n=1 << 40):
+    return mk.load().mukv_paged_attend_shared(ref(p or pages()), ref(sc), layer, ref(s or seqs()), ref(g), q, ref(qs), causal, out, ref(w), ref(sw),
+                                              ws, n, None)
+
+
+@pytest.mark.parametrize("call", [attend, shared])
+def test_attention_refuses_pages_scales_and_sequences(call):
+    for kw, status in PAGES8:
+        assert call(p=pages(**kw)) == status, kw
+    for kw, status in SCALES:
+        if call is attend or kw is not None:      # (without scales the rows are of the payload dtype)
+            assert call(sc=of(kw)) == status, kw
+    for kw, status in SEQS:
+        if "offsets" not in kw:
+            assert call(s=seqs(**kw)) == status, kw
+    assert call(s=seqs(offsets=None)) == SHAPE and call(s=seqs(table=None, lengths=None)) == BAD
+    assert call(layer=-1) == call(layer=2) == call(causal=2) == BAD
+
+
+@pytest.mark.parametrize("call", [attend, shared])
+@pytest.mark.parametrize("kw,status", [
+    ({"q": None}, BAD), ({"out": None}, BAD), ({"ws": None}, BAD), ({"n": 1000}, mk.MUKV_ERR_CAPACITY), ({"q": P + 8}, UNSUP), ({"out": P + 8}, UNSUP),
+    ({"ws": P + 8}, UNSUP), ({"qs": mk.mukv_strides(0, 60, 1024)}, UNSUP), ({"qs": mk.mukv_strides(0, -64, 1024)}, BAD)])
+def test_attention_refuses_tensors(call, kw, status):
+    assert call(**kw) == status
+
+
+def test_attention_refuses_weights_and_groups():
+    for kw, status in WEIGHTS:
+        assert attend(w=weights(**kw)) == shared(w=weights(**kw)) == shared(sw=weights(**kw)) == status, kw
+    assert shared(g=None) == BAD
+    for kw, status in SEQS:
+        if "offsets" not in kw:
+            assert shared(g=seqs(**{**GROUPS, **kw})) == status, kw
+    assert shared(g=seqs(n_seqs=2, offsets=None)) == SHAPE        # 5 tokens are not 2 groups of as many
+    assert shared(g=seqs(n_tokens=4)) == SHAPE                    # not the call's tokens
+    assert attend(s=seqs(n_tokens=0)) == shared(s=seqs(n_tokens=0), g=seqs(n_tokens=0)) == mk.MUKV_OK
+    # pages of the payload dtype: strides are its elements
+    assert shared(sc=None, p=pages(stride_row=68)) == UNSUP and shared(sc=None, s=seqs(n_tokens=0), g=seqs(n_tokens=0)) == mk.MUKV_OK
+
+
+def test_shared_workspace_size():
+    call = lambda p, s, g, w, out: mk.load().mukv_paged_shared_workspace_size(ref(p), ref(s), ref(g), w, out)  # noqa: E731
+    plain, n, m = C.c_int64(), C.c_int64(), C.c_int64()
+    assert mk.load().mukv_paged_workspace_size(ref(pages()), ref(seqs()), 0, C.byref(plain)) == mk.MUKV_OK
+    assert call(pages(), seqs(), seqs(**GROUPS), 0, C.byref(n)) == call(pages(), seqs(), seqs(**GROUPS), 1, C.byref(m)) == mk.MUKV_OK
+    assert n.value >= plain.value + 5 * 8 * (4 * 64 + 16) and m.value >= n.value + 8 * 5 * 8
+    assert call(pages(), seqs(), None, 0, C.byref(n)) == call(pages(), None, seqs(), 0, C.byref(n)) == call(None, seqs(), seqs(), 0, C.byref(n)) == BAD
+    assert call(pages(), seqs(), seqs(), 2, C.byref(n)) == call(pages(), seqs(), seqs(), 0, None) == BAD
+    assert call(pages(), seqs(), seqs(n_tokens=3), 0, C.byref(n)) == SHAPE
+    # a long prompt over shared rows, single tokens over their own: room for the records of either kernel
+    one = dict(n_seqs=64, n_tokens=64, offsets=None, max_new=1)
+    assert call(pages(head_dim=128, n_q_heads=32), seqs(**one), seqs(n_seqs=1, n_tokens=64, max_new=64), 0, C.byref(n)) == mk.MUKV_OK
+    assert mk.load().mukv_paged_workspace_size(ref(pages(head_dim=128, n_q_heads=32)), ref(seqs(n_seqs=1, n_tokens=64, max_new=64)), 0, C.byref(plain)) == mk.MUKV_OK
+    assert n.value > plain.value
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_attention_refuses_tensors_that_lie_elsewhere(refuses, place):  # noqa: F811
+    c = cache8()
+    rows = dict(q=("b", 3, 4, 64), out=("b", 3, 4, 64), weights=("f", 2, 2, 80), weights_out=("f", 2, 2, 80))
+    refuses(lambda where: c.attend(0, **tensors(where, **SEQUENCES, **rows)), [*SEQUENCES, *rows], place, c)
+    for c in (cache8(), mk.PagedKV(Stand(1, 9, 2, 16, 64), Stand(1, 9, 2, 16, 64), n_q_heads=4)):
+        reached = []
+        c._c_shared, c._c_capture = (lambda *a: reached.append(a) or 0), lambda stream, at: 0
+        more = dict(rows, shared_weights=("f", 1, 2, 90), shared_weights_out=("f", 1, 2, 90))
+        group = {f"of_{k}": v for k, v in dict(table=("i", 1, 6), lengths=("i", 1), offsets=("i", 2)).items()}
+
+        def call(where):
+            t = tensors(where, **SEQUENCES, **more, **group)
+            s = mk.Shared(*(t.pop(k) for k in group))
+            c.attend(0, **t, shared=s)
+
+        call({})
+        assert len(reached) == 1 and (reached[0][1] is None) == (not isinstance(c, mk.PagedKV8))
+        for name in (*SEQUENCES, *more, *group):
+            with pytest.raises(AssertionError):
+                call({name: place})
+        assert len(reached) == 1
+        with pytest.raises(AssertionError):      # nothing is shared
+            t = tensors({}, **SEQUENCES, **more)
+            c.attend(0, **t)
+        with pytest.raises(AssertionError):      # all of it elsewhere
+            mk_shared = mk.Shared(*tensors({f"of_{k}": 1 for k in ("table", "lengths", "offsets")}, **group).values())
+            c.attend(0, **tensors({}, **SEQUENCES, **rows), shared=mk_shared)
+
+
+def test_groups_are_packed_as_they_are_declared():
+    t = tensors({}, table=("i", 3, 7), lengths=("i", 3), offsets=("i", 4))
+    s = mk.mukv_seqs.from_buffer_copy(mk.Shared(*t.values(), max_tokens=9).pack(11))
+    assert (s.table, s.lengths, s.offsets) == tuple(x.data_ptr() for x in t.values())
+    assert (s.n_seqs, s.table_width, s.n_tokens, s.max_new) == (3, 7, 11, 9)
+    assert mk.mukv_seqs.from_buffer_copy(mk.Shared(t["table"], t["lengths"]).pack(6)).offsets is None
+    for bad in (dict(lengths=Stand(2, dtype=torch.int32)), dict(offsets=Stand(3, dtype=torch.int32)), dict(table=Stand(3, 7, dtype=torch.int64)),
+                dict(table=Stand(3, 7, dtype=torch.int32, strides=(8, 1)))):
+        with pytest.raises(AssertionError):
+            mk.Shared(*{**t, **bad}.values())

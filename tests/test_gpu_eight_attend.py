@@ -1,0 +1,149 @@
+"""Attention over a paged cache in 8 bits against the formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from batch_testlib import BF16, F32, Batch, i32
+from paged_testlib import f64, near
+from paper_2605_22269_amd import binding as mk
+
+pytestmark = pytest.mark.gpu
+SHAPES = [  # D, query heads, KV heads, page rows
+    (128, 28, 4, 16), (64, 14, 2, 7), (32, 8, 8, 24), (16, 6, 1, 1), (128, 5, 5, 64), (64, 64, 2, 128)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D,hq,hkv,R", SHAPES)
+@pytest.mark.parametrize("seqs", [
+    [(1, 1)], [(1, 500)], [(1, 31), (1, 32), (1, 33), (1, 0), (1, 129)], [(16, 16), (5, 900), (0, 40), (1, 2)],
+    [(3, 2), (2, 0), (4, 3001)]], ids=["one", "some", "edges", "mixed", "short_and_long"])
+def test_attention_over_pages(D, hq, hkv, R, dtype, seqs):
+    c = Batch(seqs, None, D, hq, hkv, R, dtype, True, seed=D + R + len(seqs))
+    first = c.attend()
+    c.check(first)
+    assert torch.equal(c.attend(), first)
+    c.check(c.attend(causal=False), causal=False)
+
+
+@pytest.mark.parametrize("D,hq,hkv,R", [(128, 28, 4, 16), (64, 14, 2, 7), (128, 4, 4, 64), (64, 8, 1, 1), (128, 12, 1, 24)])
+@pytest.mark.parametrize("seqs", [[(300, 300)], [(37, 1000), (256, 257), (0, 10), (60, 31), (129, 129)], [(100, 6001)], [(70, 64), (64, 2000), (500, 500)]],
+                         ids=["whole", "mixed", "past", "edges"])
+@pytest.mark.parametrize("room", [0, 9000])
+def test_prompts(D, hq, hkv, R, seqs, room):
+    c = Batch(seqs, None, D, hq, hkv, R, BF16, True, seed=D + R + len(seqs), width=-(-room // R) if room else None)
+    first = c.attend()
+    c.check(first)
+    assert torch.equal(c.attend(), first)
+    c.check(c.attend(causal=False), causal=False)
+
+
+@pytest.mark.parametrize("seqs", [[(300, 900)], [(1600, 6400)], [(64, 64), (200, 500)]])
+def test_prompts_are_bit_for_bit_those_over_what_the_rows_stand_for(seqs):
+    c = Batch(seqs, None, 128, 8, 2, 16, BF16, True, seed=5)
+    k, v = (torch.tensor(x).to(BF16).cuda() for x in c.values())
+    plain = mk.PagedKV(k, v, n_q_heads=8).attend(c.layer, i32(c.table), i32(c.lengths), c.q, offsets=i32(c.off))
+    assert torch.equal(c.attend(), plain)
+
+
+@pytest.mark.parametrize("order", ["page_row_head", "head_page_row"])
+def test_orders_of_the_pages_and_strided_queries(order):
+    c = Batch([(3, 77), (1, 300)], None, 64, 8, 2, 16, BF16, True, seed=5, order=order)
+    wide = torch.full((4, 20, 64), 9.0, dtype=BF16, device="cuda")
+    wide[:, 6:14] = c.q
+    c.q = wide[:, 6:14]
+    c.check(c.attend())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D,news,rows,room", [(64, 6, 50, 0), (128, 16, 40, 0), (16, 3, 3, 0), (32, 5, 90, 0), (64, 200, 230, 0), (128, 130, 140, 0),
+                                              (64, 400, 401, 5000), (128, 230, 260, 5000)])
+def test_hidden_rows_and_scales_never_reach_a_token(D, news, rows, room, dtype):
+    """What only the last token sees is no number; past the last row nothing was ever written, scales are any bytes, and so is the first
+    page of the layer, where rows that live nowhere are read."""
+    c = Batch([(news, rows), (news, rows)], None, D, 4, 2, 16, dtype, True, seed=D + news, width=-(-room // 16) if room else None)
+    c.lengths[1] = rows - 1
+    c.table[1, 0] = -1
+    clean = c.attend()
+    page, r = c.table[0][(rows - 1) // 16], (rows - 1) % 16
+    for t, s in ((c.kp.view(torch.uint8), c.ks.view(torch.uint8)), (c.vp.view(torch.uint8), c.vs.view(torch.uint8))):
+        t[1, page, :, r, ::3] = 0x7F
+        t[1, page, :, r + 1:] = 0xFF
+        s[1, page, :, r + 1:] = 255
+        s[1, c.table[1][(rows - 1) // 16], :, r:] = 255
+        free = [p for p in range(c.n_pages) if p not in c.table]
+        t[1, free], s[1, free] = 0x7E, 255
+    got = c.attend()
+    last = c.off[1] - 1
+    assert torch.equal(got[:last], clean[:last]) and torch.equal(got[c.off[1]:], clean[c.off[1]:])
+    assert not torch.isfinite(got[last]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_pages_that_are_none_and_rows_past_the_table(dtype):
+    c = Batch([(2, 96), (1, 64), (3, 50), (1, 10), (80, 90)], None, 64, 4, 2, 8, dtype, True, seed=8, width=12)
+    c.lengths[0] = 110
+    c.table[1, 3] = -1
+    c.table[1, 0] = c.n_pages
+    c.table[2, :] = 2**31 - 1
+    c.table[3, 1] = -(2**31)
+    c.table[4, 5] = -3
+    for hint in (0, 80):
+        c.check(c.attend(max_new=hint))
+    assert not f64(c.attend())[c.off[2]:c.off[3]].any()
+    c.check(c.attend(causal=False), causal=False)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_long_rows_are_shared_out_and_joined(dtype):
+    c = Batch([(1, 20011)], None, 128, 8, 1, 16, dtype, True, seed=1)
+    first = c.attend()
+    c.check(first)
+    for _ in range(3):
+        assert torch.equal(c.attend(), first)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D,hq,hkv,R", [(128, 28, 4, 32), (64, 4, 1, 5), (32, 6, 6, 16), (16, 32, 2, 16)])
+@pytest.mark.parametrize("seqs", [[(1, 700)], [(16, 333), (3, 2), (0, 12), (1, 0), (2, 1500)], [(60, 300), (90, 90)]], ids=["one", "mixed", "prompts"])
+def test_weights_that_rows_receive(D, hq, hkv, R, seqs, dtype):
+    c = Batch(seqs, None, D, hq, hkv, R, dtype, True, seed=R + D)
+    c.table[0, 2] = -1
+    N = int(c.lengths.max()) + 5
+    before = torch.tensor(c.rng.random((len(seqs), hkv, N)), dtype=torch.float32, device="cuda")
+    after = torch.full_like(before, -3.0)
+    out = c.attend(weights=before, weights_out=after, decay=0.5)
+    assert torch.equal(out, c.attend())
+    received, _, reach = c.check(out)
+    tol = c.weights_error(reach, int(c.news.max()))
+    for b, n in enumerate(c.lengths):
+        was, got = f64(before)[b], f64(after)[b]
+        near(got[:, :n], 0.5 * was[:, :n] + received[b], (1 + received[b]) * tol, F32)
+        assert (got[:, n:] == -3.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_of_very_different_sizes(dtype):
+    """Scales from the smallest to large ones, keys of 2^20 and of 2^-60 side by side."""
+    c = Batch([(4, 200), (70, 300)], None, 64, 8, 2, 16, dtype, True, seed=3)
+    for s, lo, hi in ((c.ks, 60, 122), (c.vs, 10, 150)):
+        s.view(torch.uint8)[:] = torch.tensor(c.rng.integers(lo, hi, s.shape), dtype=torch.uint8, device="cuda")
+    for hint in (1, 70):
+        c.check(c.attend(max_new=hint))
+
+
+def test_captured_and_replayed_beside_eager_calls():
+    c = Batch([(1, 300), (1, 2000), (1, 17)], None, 128, 8, 2, 16, BF16, True, seed=30)
+    table, lengths = i32(c.table), i32(c.lengths)
+    out, eager = torch.empty_like(c.q), torch.empty_like(c.q)
+    call = lambda o: c.cache.attend(1, table, lengths, c.q, out=o)  # noqa: E731
+    call(out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for i in range(5):
+        c.q.normal_()
+        lengths -= 1
+        graph.replay()
+        call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), i
