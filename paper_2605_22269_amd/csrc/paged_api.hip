@@ -162,19 +162,20 @@ struct Space {
     int64_t stats, values, sums, pairs, fit, left_stats, left_values, bytes; // offsets; the counts are at 0
 };
 int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
-mukv::PlanShape plan_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool *prompts) {
+mukv::PlanShape plan_of(const mukv_paged &p, bool eight, const mukv_seqs &s, bool causal, bool *prompts) {
     const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
     const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint);
     *prompts = tile != 0;
-    return mukv::paged_plan(p.dtype, tile, causal);
+    return mukv::paged_plan(p.dtype, eight, tile, causal);
 }
-Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
+// (how large it is does not depend on `eight`)
+Space space_of(const mukv_paged &p, bool eight, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
     Space x;
     bool prompts, shared_prompts = false;
-    x.plan = plan_of(p, s, causal, &prompts);
+    x.plan = plan_of(p, eight, s, causal, &prompts);
     int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
     if (shared) { // one launch after the other: they have the counts and the records in common
-        x.shared_plan = plan_of(p, *shared, false, &shared_prompts);
+        x.shared_plan = plan_of(p, eight, *shared, false, &shared_prompts);
         const int64_t n = (int64_t)x.shared_plan.records * x.shared_plan.queries;
         if (shared_prompts && n > sums) sums = n;
         if (n > rows) rows = n;
@@ -268,7 +269,7 @@ int attend(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer
         if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
     }
     if (!workspace) return MUKV_ERR_INVALID_ARG;
-    const Space x = space_of(*pages, *seqs, shared, causal != 0, any_weights);
+    const Space x = space_of(*pages, scales != nullptr, *seqs, shared, causal != 0, any_weights);
     if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
     if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
     mukv::PagedAttendArgs a = {};
@@ -390,7 +391,7 @@ int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, in
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_pages(pages, packed_nothing(seqs))) return rc;
     if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
-    *bytes_out = space_of(*pages, *seqs, nullptr, true, with_weights != 0).bytes;
+    *bytes_out = space_of(*pages, false, *seqs, nullptr, true, with_weights != 0).bytes;
     return MUKV_OK;
 }
 
@@ -416,7 +417,7 @@ int mukv_paged_shared_workspace_size(const mukv_paged *pages, const mukv_seqs *s
     if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
     if (const int rc = check_seqs(pages, shared, false, true)) return rc;
     if (shared->n_tokens != seqs->n_tokens) return MUKV_ERR_SHAPE;
-    *bytes_out = space_of(*pages, *seqs, shared, true, with_weights != 0).bytes;
+    *bytes_out = space_of(*pages, false, *seqs, shared, true, with_weights != 0).bytes;
     return MUKV_OK;
 }
 

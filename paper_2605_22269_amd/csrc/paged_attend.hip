@@ -21,7 +21,7 @@ int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint) {
     return queries <= 128 || (tiles <= 256 && room <= 4096) ? 128 : 256;
 }
 
-PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
+PlanShape paged_plan(int dtype, bool eight, int prompt_tile, bool causal) {
     PlanShape p;
     p.causal = causal;
     p.most = kPlanChunks;
@@ -35,14 +35,15 @@ PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
         p.record = 0.06f;
     } else {
         p.queries = kPQ;
-        p.rows = dtype == MUKV_BF16 ? 128 : 64; // a block of every wave
+        // a block of every wave
+        p.rows = kPWaves * (dtype != MUKV_BF16 ? attend_rows<float, false>() : eight ? attend_rows<uint16_t, true>() : attend_rows<uint16_t, false>());
         p.records = 2048;
         p.places = 512;
         p.start = 0;
         p.join = p.record = 0.f;
     }
     p.log_queries = p.queries == 256 ? 8 : p.queries == 128 ? 7 : 4;
-    p.log_rows = p.rows == 128 ? 7 : 6;
+    p.log_rows = p.rows == 256 ? 8 : p.rows == 128 ? 7 : 6;
     return p;
 }
 

@@ -19,6 +19,12 @@ namespace {
 
 constexpr int kPQ = 16, kPWaves = 4; // queries and waves of a workgroup
 
+// Rows of a wave's block.
+template <typename T, bool EIGHT>
+constexpr int attend_rows() {
+    return sizeof(T) == 4 ? 16 : EIGHT ? 64 : 32;
+}
+
 // Keys of 8 bits as the rows of a score: a lane of four has D / 4 neighbouring codes (or two such runs of 16), which are one operand after
 // the other.
 template <typename T, int D>
@@ -97,7 +103,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     constexpr int W = kPWaves;
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
-    constexpr int kRows = kBf16 ? 32 : 16;             // rows of a block
+    constexpr int kRows = attend_rows<T, EIGHT>();     // rows of a block
     constexpr int kTiles = kRows / 16;                 // 16-row tiles of the scores
     constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16; // 16-byte pieces of a key row (and of a query) per lane
     constexpr int NF = D / 16;                         // 16-feature tiles of the output
@@ -105,6 +111,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     // load is two pieces, where a row has more than two)
     constexpr int kVH = kBf16 ? (EIGHT && D > 16 ? 2 : 1) : (D == 128 ? 2 : 1); // pieces, or loads, per row
     constexpr int kRowsPerLoad = 64 * (kBf16 ? kVH : 1) / kPieces, NV = kBf16 ? kRows / kRowsPerLoad : 4;
+    constexpr int kParts = kBf16 ? kRows / 32 : 1, kPartLoads = NV / kParts; // the values of 32 rows at a time are in LDS
     constexpr int kVW = kBf16 ? 4 : (D >= 64 ? 4 : D / 16); // dwords of a piece
     constexpr int kValueLanes = kBf16 ? kPieces / kVH : 16; // of a row
     typedef __attribute__((ext_vector_type(kVW))) unsigned int raw_v;
@@ -237,13 +244,14 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         // ---- scores S^T = K Q^T: query lr, rows 16 t + 4 lg + r ----
         f32x4 sc[kTiles];
         if constexpr (kQueryLds) asm volatile("" ::: "memory"); // (the queries are read again, not held)
-        if constexpr (EIGHT)
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) kc[t].spread(scale_of((uint32_t)__shfl((int)k_scale, 16 * t + lr)), kx[t]);
         if constexpr (kBf16) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if constexpr (EIGHT) {
+                    if (t > 0) asm volatile("" : "+v"(sc[t - 1])); // (one tile's rows at a time, for the registers' sake)
+                    kc[t].spread(scale_of((uint32_t)__shfl((int)k_scale, 16 * t + lr)), kx[t]);
+                }
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) {
                     if (!has_piece) kx[t][kk] = raw16{0u, 0u, 0u, 0u};
@@ -252,6 +260,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                 }
             }
         } else {
+            if constexpr (EIGHT) kc[0].spread(scale_of((uint32_t)__shfl((int)k_scale, lr)), kx[0]);
             sc[0] = scores_f32<KK>(kx[0], [&](int kk) { return kQueryLds ? s_q[kk][lane] : qb[kQueryLds ? 0 : kk]; });
         }
         int64_t off_next = 0;
@@ -274,7 +283,8 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         // ---- statistics and weights, all of query lr (a NaN score is in no maximum and makes the sum one).  What the
         // exponents subtract is a whole number, so that bringing sums from one to another multiplies by a power of two ----
         float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
-        if constexpr (kTiles == 2) mx = fmaxf(mx, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+#pragma unroll
+        for (int t = 1; t < kTiles; ++t) mx = fmaxf(mx, fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3])));
         mx = ceilf(xrow_max(mx) * scale);
         if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) { // a maximum moved: bring what was summed to it
             const float m_new = fmaxf(m_run, mx);
@@ -303,23 +313,39 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                     p[4 * t + r] = kBf16 ? __builtin_amdgcn_exp2f(fmaf(sc[t][r], scale, -ref)) : weight_of(sc[t][r], scale, ref);
         }
         float sum = (p[0] + p[1]) + (p[2] + p[3]);
-        if constexpr (kTiles == 2) sum += (p[4] + p[5]) + (p[6] + p[7]);
+#pragma unroll
+        for (int t = 1; t < kTiles; ++t) sum += (p[4 * t] + p[4 * t + 1]) + (p[4 * t + 2] + p[4 * t + 3]);
         l_run += sum;
         // A value that is no number, in a row that a token of the tile does not see, must not reach that token: its weight is zero,
         // the product is not.  Such blocks (rare) are multiplied token by token, hidden rows as zeros.
         bool apart = false;
-        if constexpr (EIGHT)
+        auto spread_values = [&](int i) __attribute__((always_inline)) { // EIGHT
+            const float s = scale_of((uint32_t)__shfl((int)v_scale, value_row(i)));
+#pragma unroll
+            for (int h = 0; h < kVH; ++h) {
+                const raw16 x = kBf16 ? bf16_piece(vc[i][kBf16 ? 2 * h : 0], vc[i][kBf16 ? 2 * h + 1 : 0], s) : f32_piece(vc[i][kBf16 ? 0 : h], s);
+#pragma unroll
+                for (int e = 0; e < kVW; ++e) vx[i][h][e] = x[e];
+            }
+        };
+        if (EIGHT && late) { // (the one thing that a code can be and no number is 7F; a scale that is none, FF)
+            bool none = false;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const float s = scale_of((uint32_t)__shfl((int)v_scale, value_row(i)));
+                const bool nowhere = __shfl(ft, value_row(i)) == INT_MAX;
+                const int scale = __shfl((int)v_scale, value_row(i));
+                none |= !nowhere && scale == 255;
 #pragma unroll
-                for (int h = 0; h < kVH; ++h) {
-                    const raw16 x = kBf16 ? bf16_piece(vc[i][kBf16 ? 2 * h : 0], vc[i][kBf16 ? 2 * h + 1 : 0], s) : f32_piece(vc[i][kBf16 ? 0 : h], s);
-#pragma unroll
-                    for (int e = 0; e < kVW; ++e) vx[i][h][e] = x[e];
+                for (int w = 0; w < kVC; ++w) {
+                    const uint32_t x = nowhere ? 0u : vc[i][w];
+                    vc[i][w] = x;
+                    none |= (((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0u;
                 }
             }
-        if (late) {
+            // (zero times a scale that is none is one as well: rows that live nowhere get another)
+            if (ft == INT_MAX) v_scale = 127;
+            apart = first_tok != last_tok && __builtin_amdgcn_ballot_w64(none) != 0;
+        } else if (late) {
             unsigned worst = 0; // (only whether it reaches the exponent of infinities)
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -339,52 +365,61 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         }
         // ---- O^T += V^T P^T: the weights are the B operand as they stand in the lane ----
         if constexpr (kBf16) {
-            raw16 hi, lo;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                hi[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
-                lo[e] = bf16_pair(p[2 * e] - __uint_as_float(hi[e] << 16), p[2 * e + 1] - __uint_as_float(hi[e] & 0xFFFF0000u));
-            }
+            for (int part = 0; part < kParts; ++part) {
+                raw16 hi, lo;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int row = value_row(i);
-#pragma unroll
-                for (int h = 0; h < kVH; ++h)
-                    *reinterpret_cast<raw_v *>(buf + row * kRowB + 16 * ((kVH * (lane % kValueLanes) + h) ^ row_swizzle<D>(row))) = vx[i][h];
-            }
-            if constexpr (more.value) request_values(off_next);
-            asm volatile("" ::: "memory"); // a wave's LDS accesses keep their order; no other wave reads these rows
-            const int q4 = lr >> 2, piece = (lane & 3) >> 1, sub = 8 * (lane & 1);
-            auto values_of = [&](int f) __attribute__((always_inline)) { // rows 4 lg + t and 16 + 4 lg + t of feature 16 f + lr
-                const int r0 = 4 * lg + q4, r1 = r0 + 16;
-                const i16x4 v0 = lds_read_tr16(buf + r0 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r0)) + sub);
-                const i16x4 v1 = lds_read_tr16(buf + r1 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r1)) + sub);
-                return i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-            };
-            if (__builtin_expect(!apart, 1)) {
-#pragma unroll
-                for (int f = 0; f < NF; ++f) {
-                    const bf16x8 av = __builtin_bit_cast(bf16x8, values_of(f));
-                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi), acc[f], 0, 0, 0);
-                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo), acc[f], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) {
+                    const float x = p[8 * part + 2 * e], y = p[8 * part + 2 * e + 1];
+                    hi[e] = bf16_pair(x, y);
+                    lo[e] = bf16_pair(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xFFFF0000u));
                 }
-            } else {
-#pragma unroll 1
-                for (int tok = first_tok; tok <= last_tok; ++tok)
+#pragma unroll
+                for (int i = part * kPartLoads; i < (part + 1) * kPartLoads; ++i) {
+                    const int row = value_row(i) - 32 * part;
+                    if constexpr (EIGHT) spread_values(i);
+#pragma unroll
+                    for (int h = 0; h < kVH; ++h)
+                        *reinterpret_cast<raw_v *>(buf + row * kRowB + 16 * ((kVH * (lane % kValueLanes) + h) ^ row_swizzle<D>(row))) = vx[i][h];
+                }
+                if constexpr (more.value)
+                    if (part == kParts - 1) request_values(off_next);
+                asm volatile("" ::: "memory"); // a wave's LDS accesses keep their order; no other wave reads these rows
+                const int q4 = lr >> 2, piece = (lane & 3) >> 1, sub = 8 * (lane & 1);
+                auto values_of = [&](int f) __attribute__((always_inline)) { // rows 4 lg + t and 16 + 4 lg + t of feature 16 f + lr
+                    const int r0 = 4 * lg + q4, r1 = r0 + 16;
+                    const i16x4 v0 = lds_read_tr16(buf + r0 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r0)) + sub);
+                    const i16x4 v1 = lds_read_tr16(buf + r1 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r1)) + sub);
+                    return i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+                };
+                if (__builtin_expect(!apart, 1)) {
 #pragma unroll
                     for (int f = 0; f < NF; ++f) {
-                        i16x8 x = values_of(f);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = tok >= first_to_see(e) ? x[e] : (short)0;
-                        f32x4 c = acc[f];
-                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
-                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[f][r] = tok == my_tok ? c[r] : acc[f][r];
+                        const bf16x8 av = __builtin_bit_cast(bf16x8, values_of(f));
+                        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi), acc[f], 0, 0, 0);
+                        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo), acc[f], 0, 0, 0);
                     }
+                } else {
+#pragma unroll 1
+                    for (int tok = first_tok; tok <= last_tok; ++tok)
+#pragma unroll
+                        for (int f = 0; f < NF; ++f) {
+                            i16x8 x = values_of(f);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = tok >= first_to_see(8 * part + e) ? x[e] : (short)0;
+                            f32x4 c = acc[f];
+                            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
+                            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[f][r] = tok == my_tok ? c[r] : acc[f][r];
+                        }
+                }
+                asm volatile("" ::: "memory"); // the next rows take their place
             }
-            asm volatile("" ::: "memory"); // the next block's rows take their place
         } else {
+            if constexpr (EIGHT)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) spread_values(i);
             __builtin_amdgcn_sched_barrier(0);
             auto product = [&](int h, int e, auto seen) __attribute__((always_inline)) { // four rows at a time, joined pair by pair
                 f32x4 d[4];
@@ -548,6 +583,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
     constexpr int kRows = 16 * kTiles; // of a wave
     for (int r0 = kRows * ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)); r0 < n_w; r0 += 4 * kRows * n_groups) {
         raw16 kx[kTiles][KK];
+        typename Keys::Codes kc[EIGHT ? kTiles : 1];
+        uint32_t k_scale[EIGHT ? kTiles : 1];
         int from[kTiles][4]; // first token that sees row 16 t + 4 lg + e
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
@@ -556,20 +593,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
             const bool there = is_page(v, page);
             const int64_t off = !there ? 0 : v.table ? offset_of(v, page, r) : (int64_t)(s.first + r) * v.stride_row;
             if constexpr (EIGHT) {
-                typename Keys::Codes kc;
-                kc.load(v.k + g * v.stride_head + off, my_piece);
-                kc.spread(scale_of((v.scales.k + g * v.scales.stride_head + (there ? scale_offset_of(v, page, r) : 0))[0]), kx[t]);
+                kc[t].load(v.k + g * v.stride_head + off, my_piece);
+                k_scale[t] = (v.scales.k + g * v.scales.stride_head + (there ? scale_offset_of(v, page, r) : 0))[0];
             }
             const unsigned char *kp = v.k + g * v.stride_head + off + 16 * my_piece;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                if constexpr (!EIGHT) kx[t][kk] = *reinterpret_cast<const raw16 *>(kp + 64 * kk);
+                if constexpr (EIGHT) break;
+                kx[t][kk] = *reinterpret_cast<const raw16 *>(kp + 64 * kk);
                 if (!has_piece) kx[t][kk] = raw16{0u, 0u, 0u, 0u};
             }
             const int ft = there ? (a.causal ? r - past : 0) : INT_MAX;
 #pragma unroll
             for (int e = 0; e < 4; ++e) from[t][e] = __shfl(ft, 4 * lg + e);
         }
+        if constexpr (EIGHT)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) { // (requested together before)
+                kc[t].spread(scale_of(k_scale[t]), kx[t]);
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    if (!has_piece) kx[t][kk] = raw16{0u, 0u, 0u, 0u};
+            }
         float sum[kTiles][4];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)

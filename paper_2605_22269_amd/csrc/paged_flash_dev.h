@@ -27,7 +27,7 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
 
 // One unit by a workgroup of four waves; a wave owns 32 kQB queries from the scores to the output.
 // EIGHT: rows of 8 bits (eight_dev.h) come through registers, where they become bf16, and lie in LDS as the others do: a step's codes are
-// requested where its rows would be, and put down a step later, before the barrier that lets them be read.
+// requested where its rows would be, and put down half a step later, between the products of the step before.
 // SHARED: one of two launches, as in paged_attend_dev.h.
 template <int D, int kQB, bool PAIRS, bool EIGHT, bool SHARED>
 __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit &u) {
@@ -390,15 +390,13 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (P == 0) { // the rows of the next step are there; the next but one's take the place of this one's keys
-            if constexpr (EIGHT)
-                put_down((h >> 1) + 1);
-            else
-                rows_landed();
+            if constexpr (!EIGHT) rows_landed();
             __syncthreads();
             request((h >> 1) + 2);
             next_keys();
         } else {
             next_values(h >> 1);
+            put_down((h >> 1) + 2);
         }
         // ---- values of the other 16 rows; the scores go to where vector instructions reach them ----
         load_ahead(There{});
@@ -424,7 +422,10 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         if constexpr (EIGHT) put_down(0);
         request(1);
         first_operands();
-        if constexpr (!EIGHT) rows_landed();
+        if constexpr (EIGHT)
+            put_down(1);
+        else
+            rows_landed();
         __syncthreads();
     };
     auto next_places = [&](int h) __attribute__((always_inline)) {
@@ -536,12 +537,10 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                 for (int h = 0; h < n_halves; h += 2) {
                     max_of(std::integral_constant<int, 0>{}, h);
                     max_of(std::integral_constant<int, 1>{}, h + 1);
-                    if constexpr (EIGHT) // of the next step; this one's keys are done with
-                        put_down((h >> 1) + 1);
-                    else
-                        rows_landed();
+                    if constexpr (!EIGHT) rows_landed(); // of the next step; this one's keys are done with
                     __syncthreads();
                     request((h >> 1) + 2);
+                    put_down((h >> 1) + 2);
                     next_keys();
                     next_places(h + 1);
                 }

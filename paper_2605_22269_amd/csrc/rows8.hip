@@ -46,59 +46,81 @@ __device__ __forceinline__ void places_of(const PagedView &v, int t0, int nt, in
     *scale_place = scale_offset_of(v, page, row);
 }
 
+// Keys and values come first and are requested before anything is worked out; queries, of which there are more, go on as they would to a
+// cache of 16 bits, both features of a pair in one lane (1568 tokens, 28/4 heads of 128: XX us a launch; all rows alike YY).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void write8_kernel(RopeArgs a, int per_wg) {
     constexpr int L = D / 8, N = (int)sizeof(T) / 2; // lanes of a row, 16-byte pieces of a lane's features
     constexpr int kAtOnce = kThreads / L;            // rows
+    constexpr int E = 16 / (int)sizeof(T);           // features of a piece
     __shared__ float2 s_turn[kWriteTokens][D / 2];
     __shared__ int64_t s_place[kWriteTokens], s_scale[kWriteTokens];
     const int tid = threadIdx.x, piece = tid % L;
     const int t0 = blockIdx.x * per_wg, nt = a.n_tokens - t0 < per_wg ? a.n_tokens - t0 : per_wg;
     const int n_pairs = a.rotate ? a.n_rot / 2 : 0;
-    const int heads = a.q.heads + a.k.heads, rows_per = heads + a.v.heads, n_rows = nt * rows_per;
-    for (int r0 = 0; r0 < n_rows; r0 += kAhead * kAtOnce) { // (the same rounds in all threads: lanes exchange what they have)
-        raw16 x[kAhead][N];
-        int tok[kAhead], head[kAhead]; // head: -1 if there is no such row
+    const int heads = a.k.heads, rows_per = 2 * heads, n_rows = nt * rows_per;
+    constexpr int kRounds = 2; // of keys and values, requested together
+    raw16 x[kRounds][N];
+    auto request = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kRounds; ++u) {
             const int r = r0 + u * kAtOnce + tid / L;
-            tok[u] = r / rows_per;
-            head[u] = r < n_rows ? r - tok[u] * rows_per : -1;
-            if (head[u] < 0) continue;
-            const int h = head[u];
-            const RopeArgs::Rows &m = h < a.q.heads ? a.q : h < heads ? a.k : a.v;
-            const int in = h < a.q.heads ? h : h < heads ? h - a.q.heads : h - heads;
-            const unsigned char *p = m.x + (int64_t)(t0 + tok[u]) * m.token + in * m.head + piece * 16 * N;
+            if (r >= n_rows) continue;
+            const int t = r / rows_per, h = r - t * rows_per;
+            const RopeArgs::Rows &m = h < heads ? a.k : a.v;
+            const unsigned char *p = m.x + (int64_t)(t0 + t) * m.token + (h < heads ? h : h - heads) * m.head + piece * 16 * N;
 #pragma unroll
             for (int n = 0; n < N; ++n) x[u][n] = *reinterpret_cast<const raw16 *>(p + 16 * n);
         }
-        if (r0 == 0) {
-            if (tid >= kThreads - 64) { // the last wave, beside the first one's cosines
-                int64_t place, scale;
-                places_of(a.view, t0, nt, &place, &scale);
-                const int lane = tid & 63;
-                if (lane < nt) {
-                    s_place[lane] = place;
-                    s_scale[lane] = scale;
-                }
-            }
-            for (int i = tid; i < nt * n_pairs; i += kThreads) {
-                const int t = i / n_pairs, p = i - t * n_pairs;
-                s_turn[t][p] = turn_of(a, t0 + t, p);
-            }
-            __syncthreads();
-        }
+    };
+    request(0);
+    // queries: the first `joint` items of a row are two pieces half a rotated part apart, the others one piece
+    const int joint = a.neighbours ? 0 : n_pairs / E, items = D / E - joint;
+    const int q_rows = nt * a.q.heads, q_at_once = kThreads / items, my_item = tid % items, my_first = tid < q_at_once * items ? tid / items : q_rows;
+    const bool both = my_item < joint;
+    raw16 qx[kAhead], qy[kAhead];
+    auto request_queries = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const bool turned = head[u] >= 0 && head[u] < heads && 8 * piece < 2 * n_pairs;
+            const int r = r0 + my_first + u * q_at_once;
+            if (r >= q_rows) break;
+            const int t = r / a.q.heads, h = r - t * a.q.heads;
+            const unsigned char *p = a.q.x + (int64_t)(t0 + t) * a.q.token + h * a.q.head;
+            qx[u] = *reinterpret_cast<const raw16 *>(p + 16 * (both ? my_item : my_item + joint));
+            if (both) qy[u] = *reinterpret_cast<const raw16 *>(p + 16 * (my_item + joint));
+        }
+    };
+    request_queries(0);
+    if (tid >= kThreads - 64) { // the last wave, beside the first one's cosines
+        int64_t place, scale;
+        places_of(a.view, t0, nt, &place, &scale);
+        const int lane = tid & 63;
+        if (lane < nt) {
+            s_place[lane] = place;
+            s_scale[lane] = scale;
+        }
+    }
+    for (int i = tid; i < nt * n_pairs; i += kThreads) {
+        const int t = i / n_pairs, p = i - t * n_pairs;
+        s_turn[t][p] = turn_of(a, t0 + t, p);
+    }
+    __syncthreads();
+    for (int r0 = 0; r0 < n_rows; r0 += kRounds * kAtOnce) { // (the same rounds in all threads: lanes exchange what they have)
+        if (r0 > 0) request(r0);
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) {
+            if (r0 + u * kAtOnce >= n_rows) break;
+            const int r = r0 + u * kAtOnce + tid / L;
+            const int t = r < n_rows ? r / rows_per : 0, h = r < n_rows ? r - t * rows_per : heads;
+            const bool is_k = h < heads, turned = is_k && 8 * piece < 2 * n_pairs;
             float f[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = piece_get<T>(x[u][e / (8 / N)], e % (8 / N));
+            for (int e = 0; e < 8; ++e) f[e] = piece_get<T>(x[u][e / E], e % E);
             if (a.neighbours) {
                 if (turned)
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
-                        const float2 c = s_turn[tok[u]][4 * piece + e / 2];
+                        const float2 c = s_turn[t][4 * piece + e / 2];
                         const float y0 = f[e] * c.x - f[e + 1] * c.y, y1 = f[e + 1] * c.x + f[e] * c.y;
                         f[e] = y0;
                         f[e + 1] = y1;
@@ -107,22 +129,17 @@ __global__ __launch_bounds__(kThreads) void write8_kernel(RopeArgs a, int per_wg
                 const bool upper = 8 * piece >= n_pairs; // of the rotated half
                 const int away = n_pairs / 8;            // lanes
                 const int other = (tid & 63) + (turned ? upper ? -away : away : 0);
-                float g[8];
+                raw16 y[N];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = 0.f;
+                for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    raw16 y;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) y[w] = (unsigned)__shfl((int)x[u][n][w], other);
-#pragma unroll
-                    for (int e = 0; e < 8 / N; ++e) g[n * (8 / N) + e] = piece_get<T>(y, e);
-                }
+                    for (int w = 0; w < 4; ++w) y[n][w] = (unsigned)__shfl((int)x[u][n][w], other);
                 if (turned)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float2 c = s_turn[tok[u]][8 * piece + e - (upper ? n_pairs : 0)];
-                        f[e] = upper ? f[e] * c.x + g[e] * c.y : f[e] * c.x - g[e] * c.y;
+                        const float2 c = s_turn[t][8 * piece + e - (upper ? n_pairs : 0)];
+                        const float g = piece_get<T>(y[e / E], e % E);
+                        f[e] = upper ? f[e] * c.x + g * c.y : f[e] * c.x - g * c.y;
                     }
             }
             // the row's largest finite feature
@@ -131,25 +148,45 @@ __global__ __launch_bounds__(kThreads) void write8_kernel(RopeArgs a, int per_wg
             for (int e = 0; e < 8; ++e) most = fabsf(f[e]) < INFINITY ? fmaxf(most, fabsf(f[e])) : most;
 #pragma unroll
             for (int m = 1; m < L; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-            if (head[u] < 0) continue;
-            if (head[u] < a.q.heads) {
-                unsigned char *p = a.q.out + (int64_t)(t0 + tok[u]) * a.q.out_token + head[u] * a.q.out_head + piece * 16 * N;
-                raw16 y[N];
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) piece_put<T>(y[e / (8 / N)], e % (8 / N), f[e], f[e + 1]);
-#pragma unroll
-                for (int n = 0; n < N; ++n) put_piece(p + 16 * n, y[n]);
-                continue;
-            }
-            if (s_place[tok[u]] < 0) continue;
-            const bool is_k = head[u] < heads;
-            const int g = head[u] - (is_k ? a.q.heads : heads);
+            if (r >= n_rows || s_place[t] < 0) continue;
+            const int g = is_k ? h : h - heads;
             const int byte = scale_byte(most);
             const float by = inverse_scale((uint32_t)byte);
             const u32x2 w = {codes_of(f[0] * by, f[1] * by, f[2] * by, f[3] * by), codes_of(f[4] * by, f[5] * by, f[6] * by, f[7] * by)};
-            unsigned char *p = (is_k ? a.view.k : a.view.v) + s_place[tok[u]] + g * a.view.stride_head + 8 * piece;
+            unsigned char *p = (is_k ? a.view.k : a.view.v) + s_place[t] + g * a.view.stride_head + 8 * piece;
             __builtin_nontemporal_store(w, reinterpret_cast<u32x2 *>(p));
-            if (piece == 0) ((is_k ? a.view.scales.k : a.view.scales.v) + s_scale[tok[u]] + g * a.view.scales.stride_head)[0] = (unsigned char)byte;
+            if (piece == 0) ((is_k ? a.view.scales.k : a.view.scales.v) + s_scale[t] + g * a.view.scales.stride_head)[0] = (unsigned char)byte;
+        }
+    }
+    for (int r0 = 0; r0 < q_rows; r0 += kAhead * q_at_once) {
+        if (r0 > 0) request_queries(r0);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + my_first + u * q_at_once;
+            if (r >= q_rows) break;
+            const int t = r / a.q.heads, h = r - t * a.q.heads;
+            unsigned char *p = a.q.out + (int64_t)(t0 + t) * a.q.out_token + h * a.q.out_head;
+            if (both) {
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const float2 c0 = s_turn[t][E * my_item + e], c1 = s_turn[t][E * my_item + e + 1];
+                    const float x0 = piece_get<T>(qx[u], e), y0 = piece_get<T>(qy[u], e), x1 = piece_get<T>(qx[u], e + 1), y1 = piece_get<T>(qy[u], e + 1);
+                    piece_put<T>(qx[u], e, x0 * c0.x - y0 * c0.y, x1 * c1.x - y1 * c1.y);
+                    piece_put<T>(qy[u], e, y0 * c0.x + x0 * c0.y, y1 * c1.x + x1 * c1.y);
+                }
+                put_piece(p + 16 * my_item, qx[u]);
+                put_piece(p + 16 * (my_item + joint), qy[u]);
+                continue;
+            }
+            if (a.neighbours && E * my_item < 2 * n_pairs) {
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const float2 c = s_turn[t][(E * my_item + e) / 2];
+                    const float x0 = piece_get<T>(qx[u], e), y0 = piece_get<T>(qx[u], e + 1);
+                    piece_put<T>(qx[u], e, x0 * c.x - y0 * c.y, y0 * c.x + x0 * c.y);
+                }
+            }
+            put_piece(p + 16 * (my_item + joint), qx[u]);
         }
     }
 }
