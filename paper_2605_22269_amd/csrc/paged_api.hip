@@ -159,7 +159,8 @@ void set_rope(RopeArgs &a, const mukv_rope_table *r, const int32_t *positions) {
 // and what attention over shared rows leaves.
 struct Space {
     mukv::PlanShape plan, shared_plan;
-    int64_t stats, values, sums, pairs, fit, left_stats, left_values, bytes; // offsets; the counts are at 0
+    int64_t stats, values, sums, pairs, fit, left_heads, left_stats, left_values, bytes; // offsets; the counts are at 0
+    int single;                                                                          // SharedResults
 };
 int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 mukv::PlanShape plan_of(const mukv_paged &p, bool eight, const mukv_seqs &s, bool causal, bool *prompts) {
@@ -170,28 +171,25 @@ mukv::PlanShape plan_of(const mukv_paged &p, bool eight, const mukv_seqs &s, boo
 }
 // (how large it is does not depend on `eight`)
 Space space_of(const mukv_paged &p, bool eight, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
-    Space x;
+    Space x = {};
     bool prompts, shared_prompts = false;
     x.plan = plan_of(p, eight, s, causal, &prompts);
-    int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
-    if (shared) { // one launch after the other: they have the counts and the records in common
-        x.shared_plan = plan_of(p, eight, *shared, false, &shared_prompts);
-        const int64_t n = (int64_t)x.shared_plan.records * x.shared_plan.queries;
-        if (shared_prompts && n > sums) sums = n;
-        if (n > rows) rows = n;
-    }
+    const int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
     x.stats = 4 * mukv::kPlanRecords;
     x.values = x.stats + 8 * rows;
     x.sums = x.values + 4 * rows * p.head_dim;
     x.pairs = x.sums + (with_weights ? 4 * sums : 0);
     const int64_t queries = (int64_t)s.n_tokens * p.n_q_heads;
     x.bytes = x.pairs + (with_weights ? 8 * queries : 0);
-    x.fit = x.left_stats = x.left_values = 0;
-    if (shared) {
+    if (shared) { // places for the queries of as many chunks as there can be, then for those of tiles with one
+        x.shared_plan = plan_of(p, eight, *shared, false, &shared_prompts);
+        const int64_t units = mukv::units_bound(view_of(p, 0, *shared), x.shared_plan);
+        x.single = (int)((units < x.shared_plan.records ? units : x.shared_plan.records) * x.shared_plan.queries);
         x.fit = up_to_16(x.bytes);
-        x.left_stats = x.fit + 16;
-        x.left_values = x.left_stats + 16 * queries;
-        x.bytes = x.left_values + 4 * queries * p.head_dim;
+        x.left_heads = x.fit + 16;
+        x.left_stats = x.left_heads + 16 * queries;
+        x.left_values = x.left_stats + 16 * (x.single + queries);
+        x.bytes = x.left_values + 4 * (x.single + queries) * p.head_dim;
     }
     return x;
 }
@@ -300,6 +298,8 @@ int attend(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer
         a.shared.n_groups = shared->n_seqs;
         a.shared.offsets = shared->offsets;
         a.shared.fit = reinterpret_cast<int *>(ws + x.fit);
+        a.shared.heads = reinterpret_cast<int32_t *>(ws + x.left_heads);
+        a.shared.single = x.single;
         a.shared.stats = reinterpret_cast<float *>(ws + x.left_stats);
         a.shared.values = reinterpret_cast<float *>(ws + x.left_values);
         of_groups.view = view_of(*pages, layer, *shared, scales);

@@ -504,20 +504,19 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         const int64_t row = row_of(n);
         float l_all = l; // (the other launch's weights may have been rounded)
         if constexpr (SHARED) {
-            if (a.shared.mode == SharedResults::kLeave) {
-                *reinterpret_cast<f32x4 *>(a.shared.values + row * D + 4 * c) = o;
-                if (c == 0) *reinterpret_cast<f32x4 *>(a.shared.stats + 4 * row) = f32x4{m, l, l, 0.f};
-                return;
-            }
             if (*a.shared.fit == 0) return;
             if (in_a_group(a.shared, u.s.first + (u.tile * kPQ + n) / G)) {
-                const f32x4 st = *reinterpret_cast<const f32x4 *>(a.shared.stats + 4 * row);
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(a.shared.values + row * D + 4 * c);
-                const JoinBy by = join_by(m, l, st[0], st[1]);
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                const Taken t = take_left(a.shared, row, [&](int64_t place, bool some, float by) {
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(a.shared.values + place * D + 4 * c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = some ? fmaf(y[e], by, x[e]) : x[e];
+                });
+                const JoinBy by = join_by(m, l, t.at, t.sum);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = by.other == 0.f ? o[e] : fmaf(x[e], by.other, by.own == 0.f ? 0.f : o[e] * by.own);
-                l_all = (by.own == 0.f ? 0.f : l * by.own) + (by.other == 0.f ? 0.f : st[2] * by.other);
-                l = (by.own == 0.f ? 0.f : l * by.own) + (by.other == 0.f ? 0.f : st[1] * by.other);
+                l_all = (by.own == 0.f ? 0.f : l * by.own) + (by.other == 0.f ? 0.f : t.sum_all * by.other);
+                l = (by.own == 0.f ? 0.f : l * by.own) + (by.other == 0.f ? 0.f : t.sum * by.other);
                 m = by.at;
             }
         }
@@ -547,14 +546,21 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(ow[e], x, o[e]);
             }
         }
-        if (u.chunks > 1) {
+        if (SHARED && a.shared.mode == SharedResults::kLeave) {
+            const int64_t row = row_of(n), place = place_left(a.shared, u, kPQ, n, row);
+            *reinterpret_cast<f32x4 *>(a.shared.values + place * D + 4 * c) = o;
+            if (c == 0) {
+                *reinterpret_cast<f32x4 *>(a.shared.stats + 4 * place) = f32x4{m, l, l, 0.f};
+                leave_head(a.shared, u, kPQ, n, row);
+            }
+        } else if (u.chunks > 1) {
             if (c == 0) store_far(a.records.stats + ((int64_t)(u.record + u.chunk) * kPQ + n) * 2, m, l);
             store_far4(chunk_values<kPQ, D>(a.records, u.record + u.chunk), n * D + 4 * c, o);
         } else {
             finish(n, c, m, l, o);
         }
     }
-    if (u.chunks == 1) return;
+    if (u.chunks == 1 || (SHARED && a.shared.mode == SharedResults::kLeave)) return;
     __shared__ int s_last;
     if (!last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
     __shared__ float s_join[join_scratch(kPlanChunks, kPQ)];

@@ -213,6 +213,39 @@ __device__ __forceinline__ JoinBy join_by(float at, float sum, float other_at, f
     return j;
 }
 
+// What a lane leaves of a unit's query n (query `row` among the outputs): where.
+__device__ __forceinline__ int place_left(const SharedResults &r, const Unit &u, int queries, int n, int64_t row) {
+    return u.chunks == 1 ? r.single + (int)row : (u.record + u.chunk) * queries + n;
+}
+__device__ __forceinline__ void leave_head(const SharedResults &r, const Unit &u, int queries, int n, int64_t row) {
+    if (u.chunk == 0) *reinterpret_cast<i32x4 *>(r.heads + 4 * row) = i32x4{u.chunks, place_left(r, u, queries, n, row), queries, 0};
+}
+// What was left of query `row`, joined in the chunks' order: f(place, by) for each of them that counts, and at, sum and sum_all.
+struct Taken {
+    float at, sum, sum_all;
+};
+template <typename F>
+__device__ __forceinline__ Taken take_left(const SharedResults &r, int64_t row, F f) {
+    const i32x4 head = *reinterpret_cast<const i32x4 *>(r.heads + 4 * row);
+    Taken t = {-INFINITY, 0.f, 0.f};
+    const float *const stats = r.stats + 4 * (int64_t)head[1];
+#pragma unroll 4
+    for (int c = 0; c < head[0]; ++c) {
+        const f32x2 st = *reinterpret_cast<const f32x2 *>(stats + 4 * (int64_t)c * head[2]);
+        t.at = st[1] != 0.f ? fmaxf(t.at, st[0]) : t.at; // (else none of the chunk's rows is seen; a NaN is)
+    }
+#pragma unroll 4
+    for (int c = 0; c < head[0]; ++c) {
+        const f32x4 st = *reinterpret_cast<const f32x4 *>(stats + 4 * (int64_t)c * head[2]);
+        const bool some = st[1] != 0.f;
+        const float by = some ? __builtin_amdgcn_exp2f(st[0] - t.at) : 0.f;
+        t.sum = some ? fmaf(st[1], by, t.sum) : t.sum;
+        t.sum_all = some ? fmaf(st[2], by, t.sum_all) : t.sum_all;
+        f((int64_t)head[1] + (int64_t)c * head[2], some, by);
+    }
+    return t;
+}
+
 // ---- joining a tile's chunks ----
 // Records are written through to, and read from, the memory that all XCDs share.
 constexpr int kFar = 16; // cache policy of a buffer access: the scope of the whole GPU (sc1)

@@ -440,45 +440,39 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     // o over the sums of weights to `out`.  past: becomes a NaN where an output is none, or past what fp32 holds
     auto put_results = [&](float(*past)[kQB]) __attribute__((always_inline)) {
         if constexpr (SHARED) {
-            const bool leave = a.shared.mode == SharedResults::kLeave;
-            if (!leave && *a.shared.fit == 0) return;
+            if (*a.shared.fit == 0) return;
 #pragma unroll
             for (int i = 0; i < kQB; ++i) {
                 const int qq = q0 + 32 * i + lq, tok = u.s.first + (qq < n_queries ? my_tok[i] : 0);
                 const int64_t row = (int64_t)tok * v.Hq + g * G + (qq < n_queries ? qq - my_tok[i] * G : 0);
-                if (qq >= n_queries || (!leave && !in_a_group(a.shared, tok))) continue;
-                float *const vp = a.shared.values + row * D + 4 * half;
-                if (leave) {
+                if (qq >= n_queries || !in_a_group(a.shared, tok)) continue;
+                f32x4 x[NF][4];
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int jj = 0; jj < 4; ++jj) x[f][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const Taken t = take_left(a.shared, row, [&](int64_t place, bool some, float by) __attribute__((always_inline)) {
+                    const float *const vp = a.shared.values + place * D + 4 * half;
 #pragma unroll
                     for (int f = 0; f < NF; ++f)
 #pragma unroll
                         for (int jj = 0; jj < 4; ++jj) {
-                            const f32x4 y = {o[i][f][4 * jj], o[i][f][4 * jj + 1], o[i][f][4 * jj + 2], o[i][f][4 * jj + 3]};
-                            *reinterpret_cast<f32x4 *>(vp + 32 * f + 8 * jj) = y;
-                            if (past)
+                            const f32x4 y = *reinterpret_cast<const f32x4 *>(vp + 32 * f + 8 * jj);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) (*past)[i] = fmaf(y[e], 0.f, (*past)[i]);
+                            for (int e = 0; e < 4; ++e) x[f][jj][e] = some ? fmaf(y[e], by, x[f][jj][e]) : x[f][jj][e];
                         }
-                    if (half == 0) *reinterpret_cast<f32x4 *>(a.shared.stats + 4 * row) = f32x4{at[i], l_sum[i], PAIRS ? l_all[i] : l_sum[i], 0.f};
-                    continue;
-                }
-                const f32x4 st = *reinterpret_cast<const f32x4 *>(a.shared.stats + 4 * row);
-                const JoinBy by = join_by(at[i], l_sum[i], st[0], st[1]);
+                });
+                const JoinBy by = join_by(at[i], l_sum[i], t.at, t.sum);
                 if (by.other == 0.f) continue;
                 const bool some = by.own != 0.f;
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
-                    for (int jj = 0; jj < 4; ++jj) {
-                        const f32x4 x = *reinterpret_cast<const f32x4 *>(vp + 32 * f + 8 * jj);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[i][f][4 * jj + e] = fmaf(x[e], by.other, some ? o[i][f][4 * jj + e] * by.own : 0.f);
-                    }
-                l_sum[i] = fmaf(st[1], by.other, some ? l_sum[i] * by.own : 0.f);
-                if (PAIRS) l_all[i] = fmaf(st[2], by.other, some ? l_all[i] * by.own : 0.f);
+                    for (int j = 0; j < 16; ++j) o[i][f][j] = fmaf(x[f][j / 4][j % 4], by.other, some ? o[i][f][j] * by.own : 0.f);
+                l_sum[i] = fmaf(t.sum, by.other, some ? l_sum[i] * by.own : 0.f);
+                if (PAIRS) l_all[i] = fmaf(t.sum_all, by.other, some ? l_all[i] * by.own : 0.f);
                 at[i] = by.at;
             }
-            if (leave) return;
         }
 #pragma unroll
         for (int i = 0; i < kQB; ++i) {
@@ -613,7 +607,29 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             at[i] = base_of(i);
             past_it[i] = 0.f;
         }
-        if (u.chunks > 1) {
+        if (SHARED && a.shared.mode == SharedResults::kLeave) {
+#pragma unroll
+            for (int i = 0; i < kQB; ++i) {
+                const int qq = q0 + 32 * i + lq;
+                if (qq >= n_queries) continue;
+                const int64_t row = (int64_t)(u.s.first + my_tok[i]) * v.Hq + g * G + (qq - my_tok[i] * G);
+                const int64_t place = place_left(a.shared, u, kFQ, qq - u.tile * kFQ, row);
+                float *const vp = a.shared.values + place * D + 4 * half;
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int jj = 0; jj < 4; ++jj) {
+                        const f32x4 y = {o[i][f][4 * jj], o[i][f][4 * jj + 1], o[i][f][4 * jj + 2], o[i][f][4 * jj + 3]};
+                        *reinterpret_cast<f32x4 *>(vp + 32 * f + 8 * jj) = y;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) past_it[i] = fmaf(y[e], 0.f, past_it[i]);
+                    }
+                if (half == 0) {
+                    *reinterpret_cast<f32x4 *>(a.shared.stats + 4 * place) = f32x4{at[i], l_sum[i], PAIRS ? l_all[i] : l_sum[i], 0.f};
+                    leave_head(a.shared, u, kFQ, qq - u.tile * kFQ, row);
+                }
+            }
+        } else if (u.chunks > 1) {
             const auto values = chunk_values<kFQ, D>(a.records, u.record + u.chunk);
             float *const stats = a.records.stats + (int64_t)(u.record + u.chunk) * kFQ * 2;
 #pragma unroll
@@ -645,6 +661,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         __syncthreads();
         if (__builtin_expect(s_again == 0, 1)) break;
     }
+    if (SHARED && a.shared.mode == SharedResults::kLeave) return;
     if (u.chunks == 1 || !last_to_arrive(a.counts + u.record, u.chunks, &s_last)) return;
     const float *const stats = a.records.stats + ((int64_t)u.record * kFQ + 32 * kQB * wave + lq) * 2;
 #pragma unroll

@@ -40,15 +40,19 @@ struct ChunkRecords {
                    // where the weights of rows are asked for)
 };
 
-// What attention over shared rows leaves for the call's other launch, over the sequences' own: per (token, head) its unnormalised output
-// and, of its weights, what their exponents subtract, their sum as the output was multiplied by them and their sum as they were.
+// What attention over shared rows leaves for the call's other launch, over the sequences' own.  Chunks of a tile are not joined there but
+// left as they are, for the other launch has more workgroups to read them than the shared rows have tiles: a place per chunk and query
+// (of tiles with one chunk: per query) with the unnormalised output and, of its weights, what their exponents subtract, their sum as the
+// output was multiplied by them and their sum as they were.
 struct SharedResults {
     enum { kNone, kLeave, kTake };
     int mode;
     int n_groups;
     const int32_t *offsets; // of the groups' tokens; tokens before the first and behind the last are no group's.  Null: all are some group's
-    float *values;          // [n_tokens * Hq][D]
-    float *stats;           // [n_tokens * Hq][4]
+    int32_t *heads;         // [n_tokens * Hq][4]: chunks, the first one's place, places from one to the next
+    float *values;          // [place][D]
+    float *stats;           // [place][4]
+    int single;             // place of query 0 of tiles with one chunk
     int *fit;               // whether the groups' offsets ascend: otherwise nothing is left, and nothing may be taken
 };
 

@@ -189,11 +189,12 @@ def test_shared_workspace_size():
     assert call(pages(), seqs(), None, 0, C.byref(n)) == call(pages(), None, seqs(), 0, C.byref(n)) == call(None, seqs(), seqs(), 0, C.byref(n)) == BAD
     assert call(pages(), seqs(), seqs(), 2, C.byref(n)) == call(pages(), seqs(), seqs(), 0, None) == BAD
     assert call(pages(), seqs(), seqs(n_tokens=3), 0, C.byref(n)) == SHAPE
-    # a long prompt over shared rows, single tokens over their own: room for the records of either kernel
-    one = dict(n_seqs=64, n_tokens=64, offsets=None, max_new=1)
-    assert call(pages(head_dim=128, n_q_heads=32), seqs(**one), seqs(n_seqs=1, n_tokens=64, max_new=64), 0, C.byref(n)) == mk.MUKV_OK
-    assert mk.load().mukv_paged_workspace_size(ref(pages(head_dim=128, n_q_heads=32)), ref(seqs(n_seqs=1, n_tokens=64, max_new=64)), 0, C.byref(plain)) == mk.MUKV_OK
-    assert n.value > plain.value
+    # rows that may be many chunks: a place for the queries of each
+    wide = pages(head_dim=128, n_q_heads=32)
+    one = seqs(n_seqs=64, n_tokens=64, offsets=None, max_new=1)
+    assert call(wide, one, seqs(n_seqs=1, n_tokens=64, max_new=64, table_width=1), 0, C.byref(n)) == mk.MUKV_OK
+    assert call(wide, one, seqs(n_seqs=1, n_tokens=64, max_new=64, table_width=4000), 0, C.byref(m)) == mk.MUKV_OK
+    assert m.value > n.value + 500 * 128 * (4 * 128 + 16)
 
 
 @pytest.mark.parametrize("place", PLACES)
