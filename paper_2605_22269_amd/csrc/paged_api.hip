@@ -162,17 +162,17 @@ struct Space {
     int64_t stats, values, sums, pairs, fit, left_heads, left_stats, left_values, bytes; // offsets; the counts are at 0
     int single;                                                                          // SharedResults
 };
+int64_t hint_of(const mukv_seqs &s) { return s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs); } // new tokens of a sequence
 int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 mukv::PlanShape plan_of(const mukv_paged &p, bool eight, const mukv_seqs &s, bool causal, bool *prompts) {
-    const int64_t hint = s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs);
-    const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint);
+    const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint_of(s));
     *prompts = tile != 0;
     return mukv::paged_plan(p.dtype, eight, tile, causal);
 }
 // (how large it is does not depend on `eight`)
 Space space_of(const mukv_paged &p, bool eight, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
     Space x = {};
-    bool prompts, shared_prompts = false;
+    bool prompts;
     x.plan = plan_of(p, eight, s, causal, &prompts);
     const int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
     x.stats = 4 * mukv::kPlanRecords;
@@ -182,9 +182,8 @@ Space space_of(const mukv_paged &p, bool eight, const mukv_seqs &s, const mukv_s
     const int64_t queries = (int64_t)s.n_tokens * p.n_q_heads;
     x.bytes = x.pairs + (with_weights ? 8 * queries : 0);
     if (shared) { // places for the queries of as many chunks as there can be, then for those of tiles with one
-        x.shared_plan = plan_of(p, eight, *shared, false, &shared_prompts);
-        const int64_t units = mukv::units_bound(view_of(p, 0, *shared), x.shared_plan);
-        x.single = (int)((units < x.shared_plan.records ? units : x.shared_plan.records) * x.shared_plan.queries);
+        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype, eight, p.head_dim, hint_of(*shared));
+        x.single = x.shared_plan.records * x.shared_plan.queries;
         x.fit = up_to_16(x.bytes);
         x.left_heads = x.fit + 16;
         x.left_stats = x.left_heads + 16 * queries;

@@ -47,6 +47,28 @@ PlanShape paged_plan(int dtype, bool eight, int prompt_tile, bool causal) {
     return p;
 }
 
+// Which kernel takes rows that groups share, and its plan: chunks are left, not joined, so that tiles are better small and many units cheap.
+// us a call, what the rule takes marked (any / prompts in tiles of 128 / of 256): 8 users over 6272 rows, 28/4 heads of 128, 27.3* / 31.8 / 41.6; 16 over
+// 500 18.1* / 20.9 / 27.1; 48 users in three rooms of 2113 to 6272 45.7 / 40.5* / 55.2; 64 in eight rooms 57.3 / 42.7* / 60.5; 64 users, 64/8 heads,
+// over 10000 rows in 8 bits 111 / 57* / 65, over 40000 408 / 175 / 171*; 718 tokens over 6272, 28/4 heads, 303 / 127 / 118*.
+// Workgroups without a unit still have to start, after all that have one.  Few tiles: no more units than places, or one group's tiles
+// shared out step by step, which leaves no place without work either (the last two cases above: 171.6 and 121.8 with 704 units).
+PlanShape shared_plan(const PagedView &groups, int dtype, bool eight, int D, int64_t new_hint) {
+    const int64_t queries = new_hint * groups.G, tiles256 = div_up(queries, 256) * groups.n_seqs * groups.Hkv;
+    int tile = 0;
+    if (dtype == MUKV_BF16 && D >= 64 && queries >= 48 && (int64_t)groups.n_tokens * groups.Hq >= 1000)
+        tile = queries > 128 && tiles256 * div_up(room_of(groups), 64) > 24 * 256 ? 256 : 128;
+    PlanShape p = paged_plan(dtype, eight, tile, false);
+    if (!tile) return p;
+    p.join = 0.2f; // (the other launch's, shared by more workgroups)
+    p.record = 0.02f;
+    const int64_t tiles = tiles_bound(groups, p);
+    if (tiles > p.places / 2) return p;
+    p.units = p.places + 8;
+    p.records = p.places + 8 + (int)tiles;
+    return p;
+}
+
 hipError_t launch_paged_attend(const PagedAttendArgs &a, int D, int dtype, hipStream_t st) {
     return dtype == MUKV_BF16 ? launch_by_dim<uint16_t, false, false>(a, D, st) : launch_by_dim<float, false, false>(a, D, st);
 }

@@ -468,6 +468,17 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         for (; blk + W < b_hi; blk += W) step(std::true_type{}, blk + W);
         step(std::false_type{}, 0);
     }
+    // What the other launch left, but for the values: to LDS, by the wave that has the fewest rows.  (Before its rows the wave waits for three loads
+    // one after the other: 48 users' tokens in three rooms 44.9 us, so 43.x.)
+    __shared__ Taken s_taken[SHARED ? kPQ : 1];
+    __shared__ float s_by[SHARED ? kPlanChunks : 1][kPQ];
+    __shared__ int s_fit;
+    if (SHARED && a.shared.mode == SharedResults::kTake && wave == W - 1 && lane < kPQ) {
+        const int qq = u.tile * kPQ + lane, tok = u.s.first + qq / G;
+        if (qq < n_queries)
+            s_taken[lane] = take_left(a.shared, tok, (int64_t)tok * v.Hq + g * G + (qq - (qq / G) * G), [&](int c, float x) { s_by[c][lane] = x; });
+        if (lane == 0) s_fit = *a.shared.fit;
+    }
     // ---- the waves' results join in LDS ----
     const float l_sum = xrow_sum(l_run);
     if (lg == 0) {
@@ -504,14 +515,18 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         const int64_t row = row_of(n);
         float l_all = l; // (the other launch's weights may have been rounded)
         if constexpr (SHARED) {
-            if (*a.shared.fit == 0) return;
-            if (in_a_group(a.shared, u.s.first + (u.tile * kPQ + n) / G)) {
+            if (!s_fit) return;
+            const Taken t = s_taken[n];
+            if (t.chunks > 0) {
                 f32x4 x = {0.f, 0.f, 0.f, 0.f};
-                const Taken t = take_left(a.shared, row, [&](int64_t place, bool some, float by) {
-                    const f32x4 y = *reinterpret_cast<const f32x4 *>(a.shared.values + place * D + 4 * c);
+                const float *const values = a.shared.values + (int64_t)t.place * D + 4 * c;
+#pragma unroll 8
+                for (int k = 0; k < t.chunks; ++k) {
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(values + (int64_t)k * t.stride * D);
+                    const float by = s_by[k][n];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = some ? fmaf(y[e], by, x[e]) : x[e];
-                });
+                    for (int e = 0; e < 4; ++e) x[e] = by < 0.f ? x[e] : fmaf(y[e], by, x[e]);
+                }
                 const JoinBy by = join_by(m, l, t.at, t.sum);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = by.other == 0.f ? o[e] : fmaf(x[e], by.other, by.own == 0.f ? 0.f : o[e] * by.own);

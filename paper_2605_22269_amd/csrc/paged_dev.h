@@ -220,28 +220,33 @@ __device__ __forceinline__ int place_left(const SharedResults &r, const Unit &u,
 __device__ __forceinline__ void leave_head(const SharedResults &r, const Unit &u, int queries, int n, int64_t row) {
     if (u.chunk == 0) *reinterpret_cast<i32x4 *>(r.heads + 4 * row) = i32x4{u.chunks, place_left(r, u, queries, n, row), queries, 0};
 }
-// What was left of query `row`, joined in the chunks' order: f(place, by) for each of them that counts, and at, sum and sum_all.
+// What was left of query `row`: chunks, where, and in the chunks' order what each is multiplied by (by(c, x), -1: it counts for nothing).
 struct Taken {
+    int chunks, place, stride; // of the chunks' values
     float at, sum, sum_all;
 };
 template <typename F>
-__device__ __forceinline__ Taken take_left(const SharedResults &r, int64_t row, F f) {
-    const i32x4 head = *reinterpret_cast<const i32x4 *>(r.heads + 4 * row);
-    Taken t = {-INFINITY, 0.f, 0.f};
+__device__ __forceinline__ Taken take_left(const SharedResults &r, int token, int64_t row, F by) {
+    Taken t = {0, 0, 0, -INFINITY, 0.f, 0.f};
+    const i32x4 head = *reinterpret_cast<const i32x4 *>(r.heads + 4 * row); // (read whether or not it has been written)
+    if (*r.fit == 0 || !in_a_group(r, token)) return t;
+    t.chunks = head[0];
+    t.place = head[1];
+    t.stride = head[2];
     const float *const stats = r.stats + 4 * (int64_t)head[1];
-#pragma unroll 4
+#pragma unroll 8
     for (int c = 0; c < head[0]; ++c) {
         const f32x2 st = *reinterpret_cast<const f32x2 *>(stats + 4 * (int64_t)c * head[2]);
         t.at = st[1] != 0.f ? fmaxf(t.at, st[0]) : t.at; // (else none of the chunk's rows is seen; a NaN is)
     }
-#pragma unroll 4
+#pragma unroll 8
     for (int c = 0; c < head[0]; ++c) {
         const f32x4 st = *reinterpret_cast<const f32x4 *>(stats + 4 * (int64_t)c * head[2]);
         const bool some = st[1] != 0.f;
-        const float by = some ? __builtin_amdgcn_exp2f(st[0] - t.at) : 0.f;
-        t.sum = some ? fmaf(st[1], by, t.sum) : t.sum;
-        t.sum_all = some ? fmaf(st[2], by, t.sum_all) : t.sum_all;
-        f((int64_t)head[1] + (int64_t)c * head[2], some, by);
+        const float x = some ? __builtin_amdgcn_exp2f(st[0] - t.at) : -1.f;
+        t.sum = some ? fmaf(st[1], x, t.sum) : t.sum;
+        t.sum_all = some ? fmaf(st[2], x, t.sum_all) : t.sum_all;
+        by(c, x);
     }
     return t;
 }

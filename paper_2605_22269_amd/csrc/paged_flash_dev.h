@@ -72,7 +72,8 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
                 raw16 x = *reinterpret_cast<const raw16 *>(qp + 32 * kk);
-                if (!ok) x = raw16{0u, 0u, 0u, 0u};
+                // (EIGHT, SHARED: another query's in the place of none will do, and nothing waits for it here)
+                if (!EIGHT && !SHARED && !ok) x = raw16{0u, 0u, 0u, 0u};
                 qb[i][kk] = __builtin_bit_cast(bf16x8, x);
             }
         }
@@ -120,35 +121,42 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     }
     // EIGHT: a lane has 16 codes, two pieces of a row, of each load
     constexpr int kCodeLanes = D / 16, kCodeRows = 64 / kCodeLanes, kCodeLoads = EIGHT ? kFRows / 4 / kCodeRows : 1;
-    raw16 kc[kCodeLoads], vc[kCodeLoads];
-    uint32_t k_scale[kCodeLoads], v_scale[kCodeLoads];
+    struct Codes {
+        raw16 k[kCodeLoads], v[kCodeLoads];
+        uint32_t k_scale[kCodeLoads], v_scale[kCodeLoads];
+    };
+    Codes next; // requested
     const unsigned char *const ksb = EIGHT ? v.scales.k + g * v.scales.stride_head : nullptr, *const vsb = EIGHT ? v.scales.v + g * v.scales.stride_head : nullptr;
     const int c_row = 16 * wave + lane / kCodeLanes, c_piece = lane % kCodeLanes;
-    auto put_down = [&](int t) __attribute__((always_inline)) { // the rows of step t, requested before
+    auto put_down = [&](int t, const Codes &x) __attribute__((always_inline)) { // the rows of step t, requested before
         if (!EIGHT || t >= n_steps) return;
         unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % 3) * kBuf;
 #pragma unroll
         for (int i = 0; i < kCodeLoads; ++i) {
             const int row = c_row + i * kCodeRows;
-            const float ks = scale_of(k_scale[i]), vs = scale_of(v_scale[i]);
+            const float ks = scale_of(x.k_scale[i]), vs = scale_of(x.v_scale[i]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                *reinterpret_cast<raw16 *>(dk + row * kRowB + 16 * key_slot<D>(2 * c_piece + h, row)) = bf16_piece(kc[i][2 * h], kc[i][2 * h + 1], ks);
-                *reinterpret_cast<raw16 *>(dv + row * kRowB + 16 * val_slot<D>(2 * c_piece + h, row)) = bf16_piece(vc[i][2 * h], vc[i][2 * h + 1], vs);
+                *reinterpret_cast<raw16 *>(dk + row * kRowB + 16 * key_slot<D>(2 * c_piece + h, row)) = bf16_piece(x.k[i][2 * h], x.k[i][2 * h + 1], ks);
+                *reinterpret_cast<raw16 *>(dv + row * kRowB + 16 * val_slot<D>(2 * c_piece + h, row)) = bf16_piece(x.v[i][2 * h], x.v[i][2 * h + 1], vs);
             }
+        }
+    };
+    auto request_codes = [&](int t, Codes &x) __attribute__((always_inline)) {
+        if (!EIGHT || t >= n_steps) return;
+#pragma unroll
+        for (int i = 0; i < kCodeLoads; ++i) {
+            const int64_t off = s_off[t & (kRing - 1)][c_row + i * kCodeRows], scale = s_scale_off[t & (kRing - 1)][c_row + i * kCodeRows];
+            x.k[i] = *reinterpret_cast<const raw16 *>(kb + off + 16 * c_piece);
+            x.v[i] = *reinterpret_cast<const raw16 *>(vb + off + 16 * c_piece);
+            x.k_scale[i] = ksb[scale];
+            x.v_scale[i] = vsb[scale];
         }
     };
     auto request = [&](int t) __attribute__((always_inline)) { // the rows of step t
         if (t >= n_steps) return;
         if constexpr (EIGHT) {
-#pragma unroll
-            for (int i = 0; i < kCodeLoads; ++i) {
-                const int64_t off = s_off[t & (kRing - 1)][c_row + i * kCodeRows], scale = s_scale_off[t & (kRing - 1)][c_row + i * kCodeRows];
-                kc[i] = *reinterpret_cast<const raw16 *>(kb + off + 16 * c_piece);
-                vc[i] = *reinterpret_cast<const raw16 *>(vb + off + 16 * c_piece);
-                k_scale[i] = ksb[scale];
-                v_scale[i] = vsb[scale];
-            }
+            request_codes(t, next);
             return;
         }
         unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % 3) * kBuf;
@@ -396,7 +404,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             next_keys();
         } else {
             next_values(h >> 1);
-            put_down((h >> 1) + 2);
+            put_down((h >> 1) + 2, next);
         }
         // ---- values of the other 16 rows; the scores go to where vector instructions reach them ----
         load_ahead(There{});
@@ -418,14 +426,19 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         tabulate(wave, p0);
         tabulate(wave + 4, p1);
         __syncthreads();
-        request(0);
-        if constexpr (EIGHT) put_down(0);
-        request(1);
-        first_operands();
-        if constexpr (EIGHT)
-            put_down(1);
-        else
+        if constexpr (EIGHT) {
+            Codes first;
+            request_codes(0, first);
+            request_codes(1, next);
+            first_operands();
+            put_down(0, first);
+            put_down(1, next);
+        } else {
+            request(0);
+            request(1);
+            first_operands();
             rows_landed();
+        }
         __syncthreads();
     };
     auto next_places = [&](int h) __attribute__((always_inline)) {
@@ -440,28 +453,32 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     // o over the sums of weights to `out`.  past: becomes a NaN where an output is none, or past what fp32 holds
     auto put_results = [&](float(*past)[kQB]) __attribute__((always_inline)) {
         if constexpr (SHARED) {
-            if (*a.shared.fit == 0) return;
+            if (*a.shared.fit == 0) return; // (leaving does not come here)
 #pragma unroll
             for (int i = 0; i < kQB; ++i) {
                 const int qq = q0 + 32 * i + lq, tok = u.s.first + (qq < n_queries ? my_tok[i] : 0);
                 const int64_t row = (int64_t)tok * v.Hq + g * G + (qq < n_queries ? qq - my_tok[i] * G : 0);
-                if (qq >= n_queries || !in_a_group(a.shared, tok)) continue;
+                if (qq >= n_queries) continue;
+                const Taken t = take_left(a.shared, tok, row, [](int, float) {});
                 f32x4 x[NF][4];
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
                     for (int jj = 0; jj < 4; ++jj) x[f][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
-                const Taken t = take_left(a.shared, row, [&](int64_t place, bool some, float by) __attribute__((always_inline)) {
-                    const float *const vp = a.shared.values + place * D + 4 * half;
+#pragma unroll 1
+                for (int c = 0; c < t.chunks; ++c) {
+                    const float *const vp = a.shared.values + ((int64_t)t.place + (int64_t)c * t.stride) * D + 4 * half;
+                    const f32x2 st = *reinterpret_cast<const f32x2 *>(a.shared.stats + 4 * ((int64_t)t.place + (int64_t)c * t.stride));
+                    const float by = st[1] != 0.f ? __builtin_amdgcn_exp2f(st[0] - t.at) : -1.f;
 #pragma unroll
                     for (int f = 0; f < NF; ++f)
 #pragma unroll
                         for (int jj = 0; jj < 4; ++jj) {
                             const f32x4 y = *reinterpret_cast<const f32x4 *>(vp + 32 * f + 8 * jj);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[f][jj][e] = some ? fmaf(y[e], by, x[f][jj][e]) : x[f][jj][e];
+                            for (int e = 0; e < 4; ++e) x[f][jj][e] = by < 0.f ? x[f][jj][e] : fmaf(y[e], by, x[f][jj][e]);
                         }
-                });
+                }
                 const JoinBy by = join_by(at[i], l_sum[i], t.at, t.sum);
                 if (by.other == 0.f) continue;
                 const bool some = by.own != 0.f;
@@ -534,7 +551,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                     if constexpr (!EIGHT) rows_landed(); // of the next step; this one's keys are done with
                     __syncthreads();
                     request((h >> 1) + 2);
-                    put_down((h >> 1) + 2);
+                    put_down((h >> 1) + 2, next);
                     next_keys();
                     next_places(h + 1);
                 }
@@ -733,6 +750,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 // few tiles, which come out even in chunks, more than twice the compute units, or few rows (us a launch without / with, 28/4 heads of 128:
 // 200 tokens over 20000 rows 89 / 93, 300 alone 14.5 / 15.6, 1000 29.8 / 31.0, 2000 55.0 / 57.3; the gains are at the kernel).
 static bool may_share(const PagedView &v, const PlanShape &p) {
+    if (p.units) return v.n_seqs == 1; // shared rows of one group
     const int64_t tiles = div_up((int64_t)v.n_tokens * v.G, p.queries) * v.Hkv, room = v.table ? room_of(v) : v.n_tokens;
     return v.n_seqs == 1 && tiles > 64 && tiles <= p.records - p.places && room >= 4096;
 }

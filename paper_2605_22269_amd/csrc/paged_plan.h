@@ -85,7 +85,9 @@ struct PlanShape {
     int start;         // what a unit costs before its first block, in blocks; 0: rows are all that has to move (chunk_by_room)
     float join, record; // what joining a chunk of a tile costs, and a chunk of any tile, in blocks
     int causal;
+    int units = 0; // units there are workgroups for, where a tile has two chunks or more (0: as many as records)
 };
+MUKV_HD int most_units(const PlanShape &p) { return p.units ? p.units : p.records; }
 MUKV_HD int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // (Numbers here stay so far below 2^31 that 32 bits hold the sums; a division of 64 bits is a quarter of a microsecond of instructions.)
 MUKV_HD int div_up32(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
@@ -124,7 +126,7 @@ MUKV_HD float cost_of(const PlanShape &p, const PlanSums &x, bool one_sequence, 
     float units = x.tiles;
     if (chunks > 1) {
         units = one_sequence ? x.tiles * (float)chunks : x.blocks / per + x.tiles;
-        if (units * 1.001f > (float)p.records || (float)chunks > x.longest) return 1e30f;
+        if (units * 1.001f > (float)most_units(p) || (float)chunks > x.longest) return 1e30f;
     }
     const float rounds = ceilf(units / (float)p.places) * (x.seen / units + (float)p.start), last = per + (float)p.start;
     return (rounds > last ? rounds : last) + (chunks > 1 ? p.join * (float)chunks + p.record * units : 0.f);
@@ -181,14 +183,17 @@ MUKV_HD float cost_of_shares(const PlanShape &p, float tiles, float line, float 
     return ceilf(line / workers) + (float)p.start * (1.f + tiles / workers) + p.join * (1.f + workers / tiles) + p.record * (workers + tiles);
 }
 // Workgroups that cover every unit.
-MUKV_HD int64_t units_bound(const PagedView &v, const PlanShape &p) {
+MUKV_HD int64_t tiles_bound(const PagedView &v, const PlanShape &p) {
     const int64_t with = v.n_seqs < v.n_tokens ? v.n_seqs : v.n_tokens;
-    const int64_t tiles = ((int64_t)v.n_tokens * v.G / p.queries + with) * v.Hkv;
+    return ((int64_t)v.n_tokens * v.G / p.queries + with) * v.Hkv;
+}
+MUKV_HD int64_t units_bound(const PagedView &v, const PlanShape &p) {
+    const int64_t tiles = tiles_bound(v, p);
     const int64_t room = v.table ? room_of(v) : v.n_tokens; // (packed: a sequence has no more rows than there are tokens)
     int64_t chunks = div_up(room, p.rows);
     chunks = chunks > p.most ? p.most : chunks < 1 ? 1 : chunks;
     // with start: all units are within the records if any tile has two chunks; without: tiles of one chunk come on top
-    const int64_t split = p.start ? (tiles > p.records ? tiles : p.records) : tiles + p.records;
+    const int64_t split = p.start ? (tiles > most_units(p) ? tiles : most_units(p)) : tiles + p.records;
     return tiles * chunks < split ? tiles * chunks : split;
 }
 
