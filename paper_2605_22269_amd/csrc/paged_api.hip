@@ -164,16 +164,15 @@ struct Space {
 };
 int64_t hint_of(const mukv_seqs &s) { return s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs); } // new tokens of a sequence
 int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
-mukv::PlanShape plan_of(const mukv_paged &p, bool eight, const mukv_seqs &s, bool causal, bool *prompts) {
+mukv::PlanShape plan_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool *prompts) {
     const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint_of(s));
     *prompts = tile != 0;
-    return mukv::paged_plan(p.dtype, eight, tile, causal);
+    return mukv::paged_plan(p.dtype, tile, causal);
 }
-// (how large it is does not depend on `eight`)
-Space space_of(const mukv_paged &p, bool eight, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
+Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
     Space x = {};
     bool prompts;
-    x.plan = plan_of(p, eight, s, causal, &prompts);
+    x.plan = plan_of(p, s, causal, &prompts);
     const int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
     x.stats = 4 * mukv::kPlanRecords;
     x.values = x.stats + 8 * rows;
@@ -182,7 +181,7 @@ Space space_of(const mukv_paged &p, bool eight, const mukv_seqs &s, const mukv_s
     const int64_t queries = (int64_t)s.n_tokens * p.n_q_heads;
     x.bytes = x.pairs + (with_weights ? 8 * queries : 0);
     if (shared) { // places for the queries of as many chunks as there can be, then for those of tiles with one
-        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype, eight, p.head_dim, hint_of(*shared));
+        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype, p.head_dim, hint_of(*shared));
         x.single = x.shared_plan.records * x.shared_plan.queries;
         x.fit = up_to_16(x.bytes);
         x.left_heads = x.fit + 16;
@@ -266,7 +265,7 @@ int attend(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer
         if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
     }
     if (!workspace) return MUKV_ERR_INVALID_ARG;
-    const Space x = space_of(*pages, scales != nullptr, *seqs, shared, causal != 0, any_weights);
+    const Space x = space_of(*pages, *seqs, shared, causal != 0, any_weights);
     if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
     if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
     mukv::PagedAttendArgs a = {};
@@ -390,7 +389,7 @@ int mukv_paged_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, in
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
     if (const int rc = check_pages(pages, packed_nothing(seqs))) return rc;
     if (const int rc = check_seqs(pages, seqs, true, true)) return rc;
-    *bytes_out = space_of(*pages, false, *seqs, nullptr, true, with_weights != 0).bytes;
+    *bytes_out = space_of(*pages, *seqs, nullptr, true, with_weights != 0).bytes;
     return MUKV_OK;
 }
 
@@ -416,7 +415,7 @@ int mukv_paged_shared_workspace_size(const mukv_paged *pages, const mukv_seqs *s
     if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
     if (const int rc = check_seqs(pages, shared, false, true)) return rc;
     if (shared->n_tokens != seqs->n_tokens) return MUKV_ERR_SHAPE;
-    *bytes_out = space_of(*pages, false, *seqs, shared, true, with_weights != 0).bytes;
+    *bytes_out = space_of(*pages, *seqs, shared, true, with_weights != 0).bytes;
     return MUKV_OK;
 }
 

@@ -19,12 +19,6 @@ namespace {
 
 constexpr int kPQ = 16, kPWaves = 4; // queries and waves of a workgroup
 
-// Rows of a wave's block.
-template <typename T, bool EIGHT>
-constexpr int attend_rows() {
-    return sizeof(T) == 4 ? 16 : EIGHT ? 64 : 32;
-}
-
 // Keys of 8 bits as the rows of a score: a lane of four has D / 4 neighbouring codes (or two such runs of 16), which are one operand after
 // the other.
 template <typename T, int D>
@@ -103,7 +97,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     constexpr int W = kPWaves;
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
-    constexpr int kRows = attend_rows<T, EIGHT>();     // rows of a block
+    constexpr int kRows = kBf16 ? 32 : 16;             // rows of a block
     constexpr int kTiles = kRows / 16;                 // 16-row tiles of the scores
     constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16; // 16-byte pieces of a key row (and of a query) per lane
     constexpr int NF = D / 16;                         // 16-feature tiles of the output
@@ -111,7 +105,6 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     // load is two pieces, where a row has more than two)
     constexpr int kVH = kBf16 ? (EIGHT && D > 16 ? 2 : 1) : (D == 128 ? 2 : 1); // pieces, or loads, per row
     constexpr int kRowsPerLoad = 64 * (kBf16 ? kVH : 1) / kPieces, NV = kBf16 ? kRows / kRowsPerLoad : 4;
-    constexpr int kParts = kBf16 ? kRows / 32 : 1, kPartLoads = NV / kParts; // the values of 32 rows at a time are in LDS
     constexpr int kVW = kBf16 ? 4 : (D >= 64 ? 4 : D / 16); // dwords of a piece
     constexpr int kValueLanes = kBf16 ? kPieces / kVH : 16; // of a row
     typedef __attribute__((ext_vector_type(kVW))) unsigned int raw_v;
@@ -283,8 +276,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         // ---- statistics and weights, all of query lr (a NaN score is in no maximum and makes the sum one).  What the
         // exponents subtract is a whole number, so that bringing sums from one to another multiplies by a power of two ----
         float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
-#pragma unroll
-        for (int t = 1; t < kTiles; ++t) mx = fmaxf(mx, fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3])));
+        if constexpr (kTiles == 2) mx = fmaxf(mx, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
         mx = ceilf(xrow_max(mx) * scale);
         if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) { // a maximum moved: bring what was summed to it
             const float m_new = fmaxf(m_run, mx);
@@ -313,8 +305,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                     p[4 * t + r] = kBf16 ? __builtin_amdgcn_exp2f(fmaf(sc[t][r], scale, -ref)) : weight_of(sc[t][r], scale, ref);
         }
         float sum = (p[0] + p[1]) + (p[2] + p[3]);
-#pragma unroll
-        for (int t = 1; t < kTiles; ++t) sum += (p[4 * t] + p[4 * t + 1]) + (p[4 * t + 2] + p[4 * t + 3]);
+        if constexpr (kTiles == 2) sum += (p[4] + p[5]) + (p[6] + p[7]);
         l_run += sum;
         // A value that is no number, in a row that a token of the tile does not see, must not reach that token: its weight is zero,
         // the product is not.  Such blocks (rare) are multiplied token by token, hidden rows as zeros.
@@ -365,57 +356,52 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         }
         // ---- O^T += V^T P^T: the weights are the B operand as they stand in the lane ----
         if constexpr (kBf16) {
+            raw16 hi, lo;
 #pragma unroll
-            for (int part = 0; part < kParts; ++part) {
-                raw16 hi, lo;
+            for (int e = 0; e < 4; ++e) {
+                hi[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
+                lo[e] = bf16_pair(p[2 * e] - __uint_as_float(hi[e] << 16), p[2 * e + 1] - __uint_as_float(hi[e] & 0xFFFF0000u));
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = p[8 * part + 2 * e], y = p[8 * part + 2 * e + 1];
-                    hi[e] = bf16_pair(x, y);
-                    lo[e] = bf16_pair(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xFFFF0000u));
+            for (int i = 0; i < NV; ++i) {
+                const int row = value_row(i);
+                if constexpr (EIGHT) spread_values(i);
+#pragma unroll
+                for (int h = 0; h < kVH; ++h)
+                    *reinterpret_cast<raw_v *>(buf + row * kRowB + 16 * ((kVH * (lane % kValueLanes) + h) ^ row_swizzle<D>(row))) = vx[i][h];
+            }
+            if constexpr (more.value) request_values(off_next);
+            asm volatile("" ::: "memory"); // a wave's LDS accesses keep their order; no other wave reads these rows
+            const int q4 = lr >> 2, piece = (lane & 3) >> 1, sub = 8 * (lane & 1);
+            auto values_of = [&](int f) __attribute__((always_inline)) { // rows 4 lg + t and 16 + 4 lg + t of feature 16 f + lr
+                const int r0 = 4 * lg + q4, r1 = r0 + 16;
+                const i16x4 v0 = lds_read_tr16(buf + r0 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r0)) + sub);
+                const i16x4 v1 = lds_read_tr16(buf + r1 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r1)) + sub);
+                return i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            };
+            if (__builtin_expect(!apart, 1)) {
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    const bf16x8 av = __builtin_bit_cast(bf16x8, values_of(f));
+                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi), acc[f], 0, 0, 0);
+                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo), acc[f], 0, 0, 0);
                 }
-#pragma unroll
-                for (int i = part * kPartLoads; i < (part + 1) * kPartLoads; ++i) {
-                    const int row = value_row(i) - 32 * part;
-                    if constexpr (EIGHT) spread_values(i);
-#pragma unroll
-                    for (int h = 0; h < kVH; ++h)
-                        *reinterpret_cast<raw_v *>(buf + row * kRowB + 16 * ((kVH * (lane % kValueLanes) + h) ^ row_swizzle<D>(row))) = vx[i][h];
-                }
-                if constexpr (more.value)
-                    if (part == kParts - 1) request_values(off_next);
-                asm volatile("" ::: "memory"); // a wave's LDS accesses keep their order; no other wave reads these rows
-                const int q4 = lr >> 2, piece = (lane & 3) >> 1, sub = 8 * (lane & 1);
-                auto values_of = [&](int f) __attribute__((always_inline)) { // rows 4 lg + t and 16 + 4 lg + t of feature 16 f + lr
-                    const int r0 = 4 * lg + q4, r1 = r0 + 16;
-                    const i16x4 v0 = lds_read_tr16(buf + r0 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r0)) + sub);
-                    const i16x4 v1 = lds_read_tr16(buf + r1 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r1)) + sub);
-                    return i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                };
-                if (__builtin_expect(!apart, 1)) {
+            } else {
+#pragma unroll 1
+                for (int tok = first_tok; tok <= last_tok; ++tok)
 #pragma unroll
                     for (int f = 0; f < NF; ++f) {
-                        const bf16x8 av = __builtin_bit_cast(bf16x8, values_of(f));
-                        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi), acc[f], 0, 0, 0);
-                        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo), acc[f], 0, 0, 0);
+                        i16x8 x = values_of(f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = tok >= first_to_see(e) ? x[e] : (short)0;
+                        f32x4 c = acc[f];
+                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
+                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[f][r] = tok == my_tok ? c[r] : acc[f][r];
                     }
-                } else {
-#pragma unroll 1
-                    for (int tok = first_tok; tok <= last_tok; ++tok)
-#pragma unroll
-                        for (int f = 0; f < NF; ++f) {
-                            i16x8 x = values_of(f);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = tok >= first_to_see(8 * part + e) ? x[e] : (short)0;
-                            f32x4 c = acc[f];
-                            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
-                            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) acc[f][r] = tok == my_tok ? c[r] : acc[f][r];
-                        }
-                }
-                asm volatile("" ::: "memory"); // the next rows take their place
             }
+            asm volatile("" ::: "memory"); // the next block's rows take their place
         } else {
             if constexpr (EIGHT)
 #pragma unroll
