@@ -29,14 +29,15 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
 // EIGHT: rows of 8 bits (eight_dev.h) come through registers, where they become bf16, and lie in LDS as the others do: a step's codes are
 // requested where its rows would be, and put down half a step later, between the products of the step before.
 // SHARED: one of two launches, as in paged_attend_dev.h.
-template <int D, int kQB, bool PAIRS, bool EIGHT, bool SHARED>
+template <int D, int kQB, int W, bool PAIRS, bool EIGHT, bool SHARED>
 __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit &u) {
     using T = uint16_t;
     constexpr int kRowB = D * 2, kPieces = kRowB / 16, kRowsPerLoad = 64 / kPieces; // rows one load of a wave brings
-    constexpr int kLoads = kFRows / 4 / kRowsPerLoad;                               // such loads per wave and step
+    constexpr int kWaveRows = kFRows / W, kLoads = kWaveRows / kRowsPerLoad;        // rows of a step a wave brings, in such loads
     constexpr int KK = D / 16, NF = D / 32; // 16-feature steps of the scores, 32-feature blocks of the output
     constexpr int kBuf = kFRows * kRowB;
-    constexpr int kFQ = 128 * kQB; // queries of the workgroup, kQB blocks of 32 a wave
+    constexpr bool kPlain = W == 8;
+    constexpr int kFQ = 32 * kQB * W; // queries of the workgroup, kQB blocks of 32 a wave
     __shared__ __align__(1024) unsigned char s_kv[5 * kBuf]; // keys of two steps, values of three
     __shared__ int64_t s_off[kRing][kFRows];                 // byte offset of a row
     __shared__ int64_t s_scale_off[EIGHT ? kRing : 1][EIGHT ? kFRows : 1]; // and of its scales
@@ -112,7 +113,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     };
     // A wave brings rows 16 wave .. 16 wave + 15 of a step, kRowsPerLoad at a time.  A row's 16-byte pieces are stored permuted, so
     // that neither the reads of key operands nor the transpose reads of values meet in a bank.
-    const int ld_row = 16 * wave + lane / kPieces, ld_piece = lane % kPieces;
+    const int ld_row = kWaveRows * wave + lane / kPieces, ld_piece = lane % kPieces;
     unsigned k_piece = 0, v_piece = 0; // where in its row the lane's piece of load i comes from, a byte each
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -120,14 +121,14 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         v_piece |= 16u * val_slot<D>(ld_piece, ld_row + i * kRowsPerLoad) << (8 * i);
     }
     // EIGHT: a lane has 16 codes, two pieces of a row, of each load
-    constexpr int kCodeLanes = D / 16, kCodeRows = 64 / kCodeLanes, kCodeLoads = EIGHT ? kFRows / 4 / kCodeRows : 1;
+    constexpr int kCodeLanes = D / 16, kCodeRows = 64 / kCodeLanes, kCodeLoads = EIGHT ? kWaveRows / kCodeRows : 1;
     struct Codes {
         raw16 k[kCodeLoads], v[kCodeLoads];
         uint32_t k_scale[kCodeLoads], v_scale[kCodeLoads];
     };
     Codes next; // requested
     const unsigned char *const ksb = EIGHT ? v.scales.k + g * v.scales.stride_head : nullptr, *const vsb = EIGHT ? v.scales.v + g * v.scales.stride_head : nullptr;
-    const int c_row = 16 * wave + lane / kCodeLanes, c_piece = lane % kCodeLanes;
+    const int c_row = kWaveRows * wave + lane / kCodeLanes, c_piece = lane % kCodeLanes;
     auto put_down = [&](int t, const Codes &x) __attribute__((always_inline)) { // the rows of step t, requested before
         if (!EIGHT || t >= n_steps) return;
         unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % 3) * kBuf;
@@ -163,7 +164,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int64_t off = s_off[t & (kRing - 1)][ld_row + i * kRowsPerLoad];
-            const int lds = (16 * wave + i * kRowsPerLoad) * kRowB; // the wave's 1024 bytes, lane order
+            const int lds = (kWaveRows * wave + i * kRowsPerLoad) * kRowB; // the wave's 1024 bytes, lane order
             load_to_lds(kb + (off + (k_piece >> (8 * i) & 255u)), dk + lds);
             load_to_lds(vb + (off + (v_piece >> (8 * i) & 255u)), dv + lds);
         }
@@ -275,7 +276,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     };
     // The scores of half h, before their weights are taken.
     auto look = [&](auto par, int h, int flag) __attribute__((always_inline)) { // flag: s_masked of the half
-        constexpr int P = par.value;
+        constexpr int P = kPlain ? 0 : par.value;
         const int slot = (h >> 1) & (kRing - 1);
         const bool masked = h < all_halves && __builtin_amdgcn_readfirstlane(flag) != 0;
         if (masked) hide(h, sc[P]);
@@ -288,10 +289,10 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         // A value that is no number must not reach a token that does not see its row: the weight is zero, the product is not.
         if (masked) {
             unsigned char *const vs = values_of(h);
-            const raw16 *own = reinterpret_cast<const raw16 *>(vs + wave * 8 * kRowB);
+            const raw16 *own = reinterpret_cast<const raw16 *>(vs + wave * (32 / W) * kRowB);
             unsigned worst = 0;
 #pragma unroll
-            for (int i = 0; i < 8 * kPieces / 64; ++i) {
+            for (int i = 0; i < 32 / W * kPieces / 64; ++i) {
                 const raw16 x = own[lane + 64 * i];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -300,7 +301,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                     worst = worst > lower ? worst : lower;
                 }
             }
-            if (8 * kPieces < 64 && lane >= 8 * kPieces) worst = 0;
+            static_assert(32 / W * kPieces >= 64, "whole waves");
             if (__builtin_amdgcn_ballot_w64(worst == 0x7F800000u) != 0 && lane == 0) s_bad[h & 1] = 1;
             __syncthreads();
             if (__builtin_expect(s_bad[h & 1] != 0, 0)) {
@@ -335,7 +336,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                     }
                 }
                 __syncthreads(); // every wave has looked at the values
-                for (int i = tid; i < 32 * D; i += 256) {
+                for (int i = tid; i < 32 * D; i += 64 * W) {
                     uint16_t *const x = reinterpret_cast<uint16_t *>(vs) + i;
                     if ((*x & 0x7F80u) == 0x7F80u) *x = 0;
                 }
@@ -344,11 +345,24 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                     s_any = 1;
                 }
                 __syncthreads();
-                load_ahead(par); // (they were there already)
+                if constexpr (!kPlain) load_ahead(par); // (they were there already)
             }
         }
     };
 
+    // Eight waves: half h, its scores, weights and values one after the other; the other wave of the SIMD does its weights meanwhile.
+    auto plain_step = [&](auto par, int h) __attribute__((always_inline)) {
+        const int flag = s_masked[(h >> 1) & (kRing - 1)][par.value];
+        scores_of(par, sc[0]);
+        look(par, h, flag);
+        bf16x8 pw[2];
+#pragma unroll
+        for (int grp = 0; grp < 2; ++grp) pw[grp] = weights_of(sc[0][0], 0, grp);
+#pragma unroll
+        for (int grp = 0; grp < 2; ++grp)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) o[0][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load_v(par, grp, f), pw[grp], o[0][f], 0, 0, 0);
+    };
     // Half h: its weights and values, and the scores of half h + 1 between them.  Operands are in registers a section before their products.
     constexpr int K1 = KK * 3 / 4; // products of the scores in the first section
     auto step = [&](auto par, int h) __attribute__((always_inline)) {
@@ -420,11 +434,11 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 
     int page;
     auto stage = [&]() __attribute__((always_inline)) { // the first two steps' rows
-        const int p0 = page_at(wave), p1 = page_at(wave + 4);
+        const int p0 = page_at(wave), p1 = W == 4 ? page_at(wave + 4) : 0;
         page = page_at(wave + 8);
         __syncthreads(); // everybody is done with what was there
         tabulate(wave, p0);
-        tabulate(wave + 4, p1);
+        if (W == 4) tabulate(wave + 4, p1);
         __syncthreads();
         if constexpr (EIGHT) {
             Codes first;
@@ -443,7 +457,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     };
     auto next_places = [&](int h) __attribute__((always_inline)) {
         // places of the steps up to this one are free: four new ones every four steps (which are read from two steps on)
-        if ((h & 7) == 7) {
+        if ((h & 7) == 7 && (W == 4 || wave < 4)) {
             tabulate((h >> 1) + 5 + wave, page);
             page = page_at((h >> 1) + 9 + wave);
         }
@@ -559,7 +573,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             stage();
             if (tid < 2) s_bad[tid] = 0;
             if (tid == 0) s_any = 0;
-            for (int i = tid; i < 2 * kFQ * (D / 32); i += 256) (&s_inf[0][0][0])[i] = 0u;
+            for (int i = tid; i < 2 * kFQ * (D / 32); i += 64 * W) (&s_inf[0][0][0])[i] = 0u;
             scores_of(std::integral_constant<int, 0>{}, sc[0]);
             if (!again) {
                 f32x16 s[kQB];
@@ -579,12 +593,28 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                     for (int j = 0; j < 16; ++j) o[i][f][j] = 0.f;
             }
             __syncthreads(); // the flags are cleared
-            load_ahead(std::integral_constant<int, 0>{});
-#pragma unroll
-            for (int i = 0; i < kQB; ++i) asm volatile("" : "+v"(sc[0][i]));
-            look(std::integral_constant<int, 0>{}, 0, s_masked[0][0]);
+            if constexpr (kPlain) {
 #pragma unroll 1
-            for (int h = 0; h < n_halves; h += 2) { // (an odd half out is joined by one whose rows nobody sees)
+                for (int h = 0; h < n_halves; h += 2) { // (an odd half out is joined by one whose rows nobody sees)
+                    plain_step(std::integral_constant<int, 0>{}, h);
+                    if (h > 0) put_down((h >> 1) + 1, next);
+                    plain_step(std::integral_constant<int, 1>{}, h + 1);
+                    if constexpr (!EIGHT) rows_landed();
+                    __syncthreads(); // the next step's rows are there; the next but one's take the place of this one's
+                    request((h >> 1) + 2);
+                    next_keys();
+                    next_values(h >> 1);
+                    next_places(h + 1);
+                }
+            }
+            if constexpr (!kPlain) {
+                load_ahead(std::integral_constant<int, 0>{});
+#pragma unroll
+                for (int i = 0; i < kQB; ++i) asm volatile("" : "+v"(sc[0][i]));
+                look(std::integral_constant<int, 0>{}, 0, s_masked[0][0]);
+            }
+#pragma unroll 1
+            for (int h = 0; !kPlain && h < n_halves; h += 2) { // (an odd half out is joined by one whose rows nobody sees)
                 const int odd = step(std::integral_constant<int, 0>{}, h);
                 look(std::integral_constant<int, 1>{}, h + 1, odd);
                 const int even = step(std::integral_constant<int, 1>{}, h + 1);
@@ -723,8 +753,8 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
 
 // A workgroup takes a unit; of one sequence's perhaps the units of its stretch, one after the other (us a launch, 28/4 heads of 128, chunks
 // alone / shares where they cost less: 1568 tokens over 6272 rows 239 / 177, 2000 over 10000 361 / 327; 1500 over 3000, 16/4 heads of 64, 63 / 55).
-template <int D, int kQB, bool PAIRS, bool SHARES, bool EIGHT, bool SHARED>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void paged_flash_kernel(PagedAttendArgs a) {
+template <int D, int kQB, int W, bool PAIRS, bool SHARES, bool EIGHT, bool SHARED>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W / 4))) void paged_flash_kernel(PagedAttendArgs a) {
     if (SHARED && a.shared.mode == SharedResults::kLeave) tell_fit(a.view, a.shared);
     Unit u;
     if constexpr (SHARES) {
@@ -735,12 +765,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         for (;;) {
             if (even) next_unit(a.view, a.plan, &share, &u);
             make_scalar(u);
-            flash_unit<D, kQB, PAIRS, EIGHT, SHARED>(a, u);
+            flash_unit<D, kQB, W, PAIRS, EIGHT, SHARED>(a, u);
             if (!even || share.at == share.end) return;
             __syncthreads(); // the next unit takes this one's LDS
         }
     } else {
-        if (find_unit(a.view, a.plan, blockIdx.x, &u)) flash_unit<D, kQB, PAIRS, EIGHT, SHARED>(a, u);
+        if (find_unit(a.view, a.plan, blockIdx.x, &u)) flash_unit<D, kQB, W, PAIRS, EIGHT, SHARED>(a, u);
     }
 }
 
@@ -754,28 +784,35 @@ static bool may_share(const PagedView &v, const PlanShape &p) {
     const int64_t tiles = div_up((int64_t)v.n_tokens * v.G, p.queries) * v.Hkv, room = v.table ? room_of(v) : v.n_tokens;
     return v.n_seqs == 1 && tiles > 64 && tiles <= p.records - p.places && room >= 4096;
 }
-template <int D, int kQB, bool PAIRS, bool EIGHT, bool SHARED>
+template <int D, int kQB, int W, bool PAIRS, bool EIGHT, bool SHARED>
 static void start_flash(const PagedAttendArgs &a, unsigned grid, hipStream_t st) {
     if (may_share(a.view, a.plan))
-        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, PAIRS, true, EIGHT, SHARED>), dim3(grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, W, PAIRS, true, EIGHT, SHARED>), dim3(grid), dim3(64 * W), 0, st, a);
     else
-        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, PAIRS, false, EIGHT, SHARED>), dim3(grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((paged_flash_kernel<D, kQB, W, PAIRS, false, EIGHT, SHARED>), dim3(grid), dim3(64 * W), 0, st, a);
 }
-template <int D, int kQB, bool EIGHT, bool SHARED>
+template <int D, int kQB, int W, bool EIGHT, bool SHARED>
 static hipError_t launch_flash(const PagedAttendArgs &a, hipStream_t st) {
     const unsigned grid = (unsigned)units_bound(a.view, a.plan);
     if (a.pairs)
-        start_flash<D, kQB, true, EIGHT, SHARED>(a, grid, st);
+        start_flash<D, kQB, W, true, EIGHT, SHARED>(a, grid, st);
     else
-        start_flash<D, kQB, false, EIGHT, SHARED>(a, grid, st);
+        start_flash<D, kQB, W, false, EIGHT, SHARED>(a, grid, st);
     return hipGetLastError();
 }
 
 template <bool EIGHT, bool SHARED>
 static hipError_t launch_flash_by_dim(const PagedAttendArgs &a, int D, hipStream_t st) {
     const bool wide = a.plan.queries == 256;
-    if (D == 128) return wide ? launch_flash<128, 2, EIGHT, SHARED>(a, st) : launch_flash<128, 1, EIGHT, SHARED>(a, st);
-    return wide ? launch_flash<64, 2, EIGHT, SHARED>(a, st) : launch_flash<64, 1, EIGHT, SHARED>(a, st);
+    // tiles of 256: in eight waves, where those of 128 features have the registers
+    if (D == 128 && wide) {
+        if constexpr (EIGHT || SHARED)
+            return launch_flash<128, 1, 8, EIGHT, SHARED>(a, st);
+        else
+            return launch_flash<128, 2, 4, EIGHT, SHARED>(a, st);
+    }
+    if (D == 128) return launch_flash<128, 1, 4, EIGHT, SHARED>(a, st);
+    return wide ? launch_flash<64, 2, 4, EIGHT, SHARED>(a, st) : launch_flash<64, 1, 4, EIGHT, SHARED>(a, st);
 }
 
 } // namespace mukv
