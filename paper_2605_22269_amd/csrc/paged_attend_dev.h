@@ -639,12 +639,34 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
             for (int kk = 0; kk < KK; ++kk) qx[at][kk] = *reinterpret_cast<const raw16 *>(qp + 16 * (EIGHT ? Keys::piece_of(my_piece, kk) : my_piece + 4 * kk));
             if (q0 + lr >= n_queries) tok[at] = -1; // sees nothing
         };
-        auto add = [&](int at) __attribute__((always_inline)) {
+        // EIGHT: most rows are seen by all tokens, where nothing has to be looked at
+        bool late = false;
+        if constexpr (EIGHT) {
+            int last = INT_MIN;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) last = last > from[t][e] ? last : from[t][e];
+            late = __builtin_amdgcn_ballot_w64(last > 0) != 0;
+        }
+        auto add = [&](int at, int q0) __attribute__((always_inline)) {
             raw16 q[KK];
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) q[kk] = has_piece ? brought_down<T, D>(qx[at][kk]) : raw16{0u, 0u, 0u, 0u};
             const float ref = pair[at][0], inv = pair[at][1];
             const bool large = __builtin_amdgcn_ballot_w64(fabsf(ref) > kLargeRef) != 0; // (its rounding shows)
+            if (EIGHT && kBf16 && !late && !large && q0 + 16 <= n_queries) {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk)
+                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[t][kk]), __builtin_bit_cast(bf16x8, q[kk]), sc, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[t][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[e], scale, -ref)), inv, sum[t][e]);
+                }
+                return;
+            }
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -673,9 +695,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
         if (q0 < n_queries) request(q0, 0);
         for (; q0 < n_queries; q0 += 32) {
             if (q0 + 16 < n_queries) request(q0 + 16, 1);
-            add(0);
+            add(0, q0);
             if (q0 + 32 < n_queries) request(q0 + 32, 0);
-            if (q0 + 16 < n_queries) add(1);
+            if (q0 + 16 < n_queries) add(1, q0 + 16);
         }
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
