@@ -785,6 +785,13 @@ int mukv_paged_attend8(const mukv_paged *pages, const mukv_row_scales *scales, i
                        void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * mukv_paged_evict from a cache in 8 bits: rows and their scales move as they are.
+ */
+int mukv_paged_evict8(const mukv_paged *pages, const mukv_row_scales *scales, const mukv_seqs *seqs, const mukv_row_weights *weights,
+                      int32_t budget, int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
+                      int32_t *kept_out, int32_t *lengths_out, void *stream);
+
+/*
  * Attention where groups of sequences share rows (a video that several users ask
  * about, instructions before every conversation): the shared rows lie in the pages once
  * and are read once for all of a group's tokens.  A token sees all rows that its group

@@ -104,7 +104,7 @@ EXPORTS = ("mukv_create", "mukv_destroy", "mukv_reset", "mukv_flush", "mukv_comp
            "mukv_snapshot_size", "mukv_snapshot_save", "mukv_snapshot_load", "mukv_profile_begin", "mukv_profile_end",
            "mukv_plain_copy", "mukv_get_state", "mukv_rope", "mukv_paged_append",
            "mukv_paged_workspace_size", "mukv_paged_attend", "mukv_paged_evict", "mukv_paged_append8", "mukv_paged_read8",
-           "mukv_paged_attend8", "mukv_paged_shared_workspace_size", "mukv_paged_attend_shared", "mukv_stream_capture", "mukv_strerror")
+           "mukv_paged_attend8", "mukv_paged_shared_workspace_size", "mukv_paged_attend_shared", "mukv_paged_evict8", "mukv_stream_capture", "mukv_strerror")
 
 _lib = None
 
@@ -157,6 +157,7 @@ def load():
     lib.mukv_paged_attend8.argtypes = [paged, vp, i32, seqs, vp, strides, i32, vp, vp, vp, C.c_int64, vp]
     lib.mukv_paged_shared_workspace_size.argtypes = [paged, seqs, seqs, i32, C.POINTER(C.c_int64)]
     lib.mukv_paged_attend_shared.argtypes = [paged, vp, i32, seqs, seqs, vp, strides, i32, vp, vp, vp, vp, C.c_int64, vp]
+    lib.mukv_paged_evict8.argtypes = [paged, vp, seqs, vp, i32, i32, i32, vp, i32, vp, vp, vp]
     lib.mukv_stream_capture.argtypes = [vp, vp]
     lib.mukv_strerror.argtypes = [i32]
     lib.mukv_strerror.restype = C.c_char_p
@@ -362,6 +363,11 @@ def mukv_paged_shared_workspace_size(pages, seqs, shared, with_weights):
     n = C.c_int64(0)
     _check((_lib or load()).mukv_paged_shared_workspace_size(pages, seqs, shared, with_weights, C.byref(n)), "mukv_paged_shared_workspace_size")
     return n.value
+
+
+def mukv_paged_evict8(pages, scales, seqs, weights, budget, n_sink, n_recent, into_ptr, into_width, kept_ptr, lengths_ptr, stream):
+    _check((_lib or load()).mukv_paged_evict8(pages, scales, seqs, weights, budget, n_sink, n_recent, into_ptr, into_width, kept_ptr, lengths_ptr,
+                                              stream), "mukv_paged_evict8")
 
 
 # ---- convenience object ----------------------------------------------------------------------
@@ -970,17 +976,18 @@ class PagedKV(_Sequences):
         assert kept.dtype is _I32 and lengths_out.dtype is _I32 and kept.shape == shape and lengths_out.shape == lengths.shape
         assert kept.is_contiguous() and lengths_out.is_contiguous() and kept.get_device() == index and lengths_out.get_device() == index
         w = _WEIGHTS.pack(weights.data_ptr(), weights_out.data_ptr(), *st[:3], weights.shape[3], 0.0)
-        mukv_paged_evict(self._pages_at, s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1],
-                         kept.data_ptr(), lengths_out.data_ptr(), _stream_of(index))
+        self._evict(s, w, budget, sink, recent, _ptr(into), 0 if into is None else into.shape[1], kept.data_ptr(), lengths_out.data_ptr(),
+                    _stream_of(index))
         return kept, lengths_out
+
+    def _evict(self, *args):
+        mukv_paged_evict(self._pages_at, *args)
 
 
 class PagedKV8(PagedKV):
     """The conversation's cache in 8 bits: k_pages, v_pages float8_e4m3fn [layer][page][KV head][row][feature], k_scales, v_scales
     float8_e8m0fnu (or their bytes, uint8) [layer][page][KV head][row], any strides but the pages' last.  dtype: that of queries, new rows and
     outputs.  Calls are those of PagedKV, and read()."""
-
-    evict = None   # (that of PagedKV takes the rows for numbers of its dtype)
 
     def __init__(self, k_pages, v_pages, k_scales, v_scales, *, n_q_heads, dtype=torch.bfloat16):
         _Sequences.__init__(self)
@@ -1004,6 +1011,9 @@ class PagedKV8(PagedKV):
         append, attend = lib.mukv_paged_append8, lib.mukv_paged_attend8
         self._c_append = lambda pages, *rest: append(pages, at, *rest)
         self._c_attend = lambda pages, *rest: attend(pages, at, *rest)
+
+    def _evict(self, *args):
+        mukv_paged_evict8(self._pages_at, self._scales_at, *args)
 
     def read(self, layer, table, lengths, offsets, *, n_tokens=None, k_out=None, v_out=None):
         """Rows as they were written, as the cache's dtype: [n_tokens][n_kv_heads][head_dim], those of sequence b at offsets[b] ..

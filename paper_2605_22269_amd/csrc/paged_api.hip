@@ -316,6 +316,46 @@ int attend(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer
     return finished(scales ? mukv::launch_paged_weights8(of_groups, D, bf16, st) : mukv::launch_paged_weights(of_groups, D, bf16, st));
 }
 
+// Eviction from rows as they are or (scales) in 8 bits.
+int evict(const mukv_paged *pages, const mukv_row_scales *scales, bool eight, const mukv_seqs *seqs, const mukv_row_weights *weights,
+          int32_t budget, int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width, int32_t *kept_out,
+          int32_t *lengths_out, void *stream) {
+    if (const int rc = eight ? check_pages8(pages, scales) : check_pages(pages)) return rc;
+    if (const int rc = check_seqs(pages, seqs, false, false)) return rc;
+    if (!weights || !weights->in || !kept_out || !lengths_out) return MUKV_ERR_INVALID_ARG;
+    mukv_row_weights w = *weights;
+    w.decay = 0.f; // not read
+    if (const int rc = check_weights(&w)) return rc;
+    if (budget < 1 || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > budget) return MUKV_ERR_INVALID_ARG;
+    if (into_table && into_width < 1) return MUKV_ERR_INVALID_ARG;
+    const int64_t lists = (int64_t)pages->n_layers * seqs->n_seqs * pages->n_kv_heads;
+    if (lists > 0x7fffffff || (int64_t)into_width * seqs->n_seqs > 0x7fffffff || budget > 1 << 30) return MUKV_ERR_UNSUPPORTED;
+    mukv::EvictArgs a = {};
+    mukv_seqs s = *seqs;
+    s.offsets = nullptr;
+    s.n_tokens = s.max_new = 0;
+    const int esz = eight ? 1 : elem_size(pages->dtype);
+    a.view = view_of(*pages, 0, s, scales);
+    a.stride_layer = in_bytes(pages->stride_layer, pages->n_layers, esz);
+    a.scale_layer = eight ? in_bytes(scales->stride_layer, pages->n_layers, 1) : 0;
+    a.w_in = w.in;
+    a.w_out = w.out;
+    a.w_layer = w.stride_layer;
+    a.w_seq = w.stride_seq;
+    a.w_head = w.stride_head;
+    a.w_rows = w.rows;
+    a.budget = budget;
+    a.n_sink = n_sink;
+    a.n_recent = n_recent;
+    a.into = into_table;
+    a.into_width = into_width;
+    a.kept = kept_out;
+    a.lengths_out = lengths_out;
+    DeviceScope dev(pages->device_id);
+    if (!dev.ok) return MUKV_ERR_HIP;
+    return finished(mukv::launch_paged_evict(a, pages->n_layers, pages->head_dim * esz, pages->device_id, reinterpret_cast<hipStream_t>(stream)));
+}
+
 } // namespace
 
 extern "C" {
@@ -431,39 +471,13 @@ int mukv_paged_attend_shared(const mukv_paged *pages, const mukv_row_scales *sca
 int mukv_paged_evict(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_row_weights *weights, int32_t budget,
                      int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
                      int32_t *kept_out, int32_t *lengths_out, void *stream) {
-    if (const int rc = check_pages(pages)) return rc;
-    if (const int rc = check_seqs(pages, seqs, false, false)) return rc;
-    if (!weights || !weights->in || !kept_out || !lengths_out) return MUKV_ERR_INVALID_ARG;
-    mukv_row_weights w = *weights;
-    w.decay = 0.f; // not read
-    if (const int rc = check_weights(&w)) return rc;
-    if (budget < 1 || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > budget) return MUKV_ERR_INVALID_ARG;
-    if (into_table && into_width < 1) return MUKV_ERR_INVALID_ARG;
-    const int64_t lists = (int64_t)pages->n_layers * seqs->n_seqs * pages->n_kv_heads;
-    if (lists > 0x7fffffff || (int64_t)into_width * seqs->n_seqs > 0x7fffffff || budget > 1 << 30) return MUKV_ERR_UNSUPPORTED;
-    mukv::EvictArgs a = {};
-    mukv_seqs s = *seqs;
-    s.offsets = nullptr;
-    s.n_tokens = s.max_new = 0;
-    const int esz = elem_size(pages->dtype);
-    a.view = view_of(*pages, 0, s);
-    a.stride_layer = in_bytes(pages->stride_layer, pages->n_layers, esz);
-    a.w_in = w.in;
-    a.w_out = w.out;
-    a.w_layer = w.stride_layer;
-    a.w_seq = w.stride_seq;
-    a.w_head = w.stride_head;
-    a.w_rows = w.rows;
-    a.budget = budget;
-    a.n_sink = n_sink;
-    a.n_recent = n_recent;
-    a.into = into_table;
-    a.into_width = into_width;
-    a.kept = kept_out;
-    a.lengths_out = lengths_out;
-    DeviceScope dev(pages->device_id);
-    if (!dev.ok) return MUKV_ERR_HIP;
-    return finished(mukv::launch_paged_evict(a, pages->n_layers, pages->head_dim * esz, pages->device_id, reinterpret_cast<hipStream_t>(stream)));
+    return evict(pages, nullptr, false, seqs, weights, budget, n_sink, n_recent, into_table, into_width, kept_out, lengths_out, stream);
+}
+
+int mukv_paged_evict8(const mukv_paged *pages, const mukv_row_scales *scales, const mukv_seqs *seqs, const mukv_row_weights *weights,
+                      int32_t budget, int32_t n_sink, int32_t n_recent, const int32_t *into_table, int32_t into_width,
+                      int32_t *kept_out, int32_t *lengths_out, void *stream) {
+    return evict(pages, scales, true, seqs, weights, budget, n_sink, n_recent, into_table, into_width, kept_out, lengths_out, stream);
 }
 
 } // extern "C"

@@ -213,7 +213,9 @@ __device__ __forceinline__ void write_length(const EvictArgs &a, const int32_t *
     if (threadIdx.x == 0) a.lengths_out[b] = lo;
 }
 
-// Onto other pages: every row on its own.  Grid (layer x sequence x KV head, n_rows rows).
+// Onto other pages: every row on its own.  Grid (layer x sequence x KV head, n_rows rows).  EIGHT: rows in 8 bits, each with a byte of its own
+// elsewhere.
+template <bool EIGHT>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, int row_bytes, int n_rows) {
     __shared__ int64_t s_from[kMoveRows], s_to[kMoveRows]; // byte offsets in the layer's pages, -1: nothing to move
     const PagedView &v = a.view;
@@ -232,6 +234,13 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
                 if (is_page(v, page) && is_page(v, dst)) {
                     from = offset_of(v, page, row);
                     to = offset_of(v, dst, i);
+                    if constexpr (EIGHT) {
+                        const int64_t head = layer * a.scale_layer + g * v.scales.stride_head;
+                        const int64_t s0 = head + scale_offset_of(v, page, row), s1 = head + scale_offset_of(v, dst, i);
+                        const unsigned char ks = v.scales.k[s0], vs = v.scales.v[s0];
+                        v.scales.k[s1] = ks;
+                        v.scales.v[s1] = vs;
+                    }
                 }
             }
             s_from[tid] = from;
@@ -262,7 +271,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
 
 // In place: row i of the result is row kept[i] >= i, so whatever is overwritten in ascending order has been read.  A workgroup takes all
 // rows of one tensor in turn, but only 64 bytes of each: the slices of a row do not meet, so there are several workgroups to a list.
-// Grid (list, slice, keys or values).
+// Grid (list, slice, keys or values).  EIGHT: the rows' bytes go with the first slice.
+template <bool EIGHT>
 __global__ __launch_bounds__(kMoveThreads) void evict_pack_kernel(EvictArgs a, int row_bytes) {
     const PagedView &v = a.view;
     const int tid = threadIdx.x, list = blockIdx.x;
@@ -273,7 +283,13 @@ __global__ __launch_bounds__(kMoveThreads) void evict_pack_kernel(EvictArgs a, i
     constexpr int kAhead = 4;
     raw16 x[2][kAhead];
     int64_t to[2][kAhead]; // -1: nothing to move
-    auto request = [&](int i0, raw16(&y)[kAhead], int64_t(&dst)[kAhead]) __attribute__((always_inline)) {
+    const bool has_scale = EIGHT && blockIdx.y == 0 && tid % pieces == 0;
+    unsigned char *const scales = !EIGHT ? nullptr : (blockIdx.z ? v.scales.v : v.scales.k) + layer * a.scale_layer + g * v.scales.stride_head;
+    unsigned char sx[2][kAhead];
+    int64_t s_to[2][kAhead];
+    auto request = [&](int i0, int which) __attribute__((always_inline)) {
+        raw16(&y)[kAhead] = x[which];
+        int64_t(&dst)[kAhead] = to[which];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int i = i0 + u * rows_at_once + r0, row = i < a.budget ? kept[i] : -1;
@@ -283,26 +299,33 @@ __global__ __launch_bounds__(kMoveThreads) void evict_pack_kernel(EvictArgs a, i
             if (!is_page(v, page) || !is_page(v, d)) continue;
             dst[u] = offset_of(v, d, i);
             y[u] = *reinterpret_cast<const raw16 *>(base + offset_of(v, page, row));
+            if (has_scale) {
+                s_to[which][u] = scale_offset_of(v, d, i);
+                sx[which][u] = scales[scale_offset_of(v, page, row)];
+            }
         }
     };
-    auto put = [&](const raw16(&y)[kAhead], const int64_t(&dst)[kAhead]) __attribute__((always_inline)) {
+    auto put = [&](int which) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (dst[u] >= 0) *reinterpret_cast<raw16 *>(base + dst[u]) = y[u];
+        for (int u = 0; u < kAhead; ++u) {
+            if (to[which][u] < 0) continue;
+            *reinterpret_cast<raw16 *>(base + to[which][u]) = x[which][u];
+            if (has_scale) scales[s_to[which][u]] = sx[which][u];
+        }
     };
     const int step = kAhead * rows_at_once;
     auto landed = [] { // every wave's rows are in registers before any is overwritten
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
-    request(0, x[0], to[0]);
+    request(0, 0);
     for (int i0 = 0; i0 < a.budget; i0 += 2 * step) {
         landed();
-        request(i0 + step, x[1], to[1]); // (rows after all that is overwritten now)
-        put(x[0], to[0]);
+        request(i0 + step, 1); // (rows after all that is overwritten now)
+        put(0);
         landed();
-        request(i0 + 2 * step, x[0], to[0]);
-        put(x[1], to[1]);
+        request(i0 + 2 * step, 0);
+        put(1);
     }
     if (blockIdx.y == 0 && blockIdx.z == 0 && layer == 0 && g == 0) write_length(a, kept, b);
 }
@@ -320,6 +343,19 @@ hipError_t launch_select(const EvictArgs &a, int lists, int keys, int device, hi
 
 } // namespace
 
+template <bool EIGHT>
+static hipError_t launch_move(const EvictArgs &a, int lists, int row_bytes, hipStream_t st) {
+    if (a.into) {
+        // (a workgroup's threads ask for four pieces each, together)
+        const int rows = 1024 / (row_bytes / 16) < 64 ? 64 : 1024 / (row_bytes / 16) > kMoveRows ? kMoveRows : 1024 / (row_bytes / 16);
+        const int chunks = (a.budget + rows - 1) / rows;
+        hipLaunchKernelGGL(evict_move_kernel<EIGHT>, dim3(lists, chunks < 65535 ? chunks : 65535), dim3(kMoveThreads), 0, st, a, row_bytes, rows);
+    } else {
+        hipLaunchKernelGGL(evict_pack_kernel<EIGHT>, dim3(lists, row_bytes < 64 ? 1 : row_bytes / 64, 2), dim3(kMoveThreads), 0, st, a, row_bytes);
+    }
+    return hipGetLastError();
+}
+
 hipError_t launch_paged_evict(const EvictArgs &a, int n_layers, int row_bytes, int device, hipStream_t st) {
     const int lists = n_layers * a.view.n_seqs * a.view.Hkv;
     const int64_t room = room_of(a.view);
@@ -328,15 +364,7 @@ hipError_t launch_paged_evict(const EvictArgs &a, int n_layers, int row_bytes, i
     // to 6000 rows 45 / 28.)
     hipError_t e = lists <= 256 ? launch_select<1024>(a, lists, keys, device, st) : launch_select<512>(a, lists, keys, device, st);
     if (e != hipSuccess) return e;
-    if (a.into) {
-        // (a workgroup's threads ask for four pieces each, together)
-        const int rows = 1024 / (row_bytes / 16) < 64 ? 64 : 1024 / (row_bytes / 16) > kMoveRows ? kMoveRows : 1024 / (row_bytes / 16);
-        const int chunks = (a.budget + rows - 1) / rows;
-        hipLaunchKernelGGL(evict_move_kernel, dim3(lists, chunks < 65535 ? chunks : 65535), dim3(kMoveThreads), 0, st, a, row_bytes, rows);
-    } else {
-        hipLaunchKernelGGL(evict_pack_kernel, dim3(lists, row_bytes < 64 ? 1 : row_bytes / 64, 2), dim3(kMoveThreads), 0, st, a, row_bytes);
-    }
-    return hipGetLastError();
+    return a.view.scales.k ? launch_move<true>(a, lists, row_bytes, st) : launch_move<false>(a, lists, row_bytes, st);
 }
 
 } // namespace mukv

@@ -92,7 +92,7 @@ hipError_t launch_shared_flash8(const PagedAttendArgs &a, int D, hipStream_t st)
 
 struct EvictArgs {
     PagedView view; // of layer 0
-    int64_t stride_layer; // bytes
+    int64_t stride_layer, scale_layer; // bytes; of the scales, where rows are in 8 bits
     const float *w_in;
     float *w_out;
     int64_t w_layer, w_seq, w_head; // elements

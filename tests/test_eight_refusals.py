@@ -237,3 +237,40 @@ def test_groups_are_packed_as_they_are_declared():
                 dict(table=Stand(3, 7, dtype=torch.int32, strides=(8, 1)))):
         with pytest.raises(AssertionError):
             mk.Shared(*{**t, **bad}.values())
+
+
+# ---- eviction ----
+def evict(p=None, sc=scales(), s=None, w=None, budget=50, sink=4, recent=10, into=P, width=5, kept=P, lengths=P):
+    w = weights() if w is None else w
+    return mk.load().mukv_paged_evict8(ref(p or pages()), ref(sc), ref(s or seqs()), ref(w) if w else None, budget, sink, recent, into, width, kept,
+                                       lengths, None)
+
+
+def test_evict_refuses():
+    for kw, status in PAGES8:
+        assert evict(p=pages(**kw)) == status, kw
+    for kw, status in SCALES:
+        assert evict(sc=of(kw)) == status, kw
+    for kw, status in [x for x in WEIGHTS if "decay" not in x[0]] + [({"in_": None}, BAD)]:
+        assert evict(w=weights(**kw)) == status, kw
+    for kw, status in [({"n_seqs": 0}, BAD), ({"table": None}, BAD), ({"lengths": None}, BAD), ({"table_width": 0}, BAD), ({"table_width": 1 << 28}, UNSUP)]:
+        assert evict(s=seqs(**kw)) == status, kw
+    for kw, status in [({"budget": 0}, BAD), ({"sink": -1}, BAD), ({"recent": -1}, BAD), ({"sink": 41}, BAD), ({"width": 0}, BAD), ({"kept": None}, BAD),
+                       ({"lengths": None}, BAD), ({"w": 0}, BAD), ({"budget": (1 << 30) + 1}, UNSUP)]:
+        assert evict(**kw) == status, kw
+
+
+@pytest.mark.parametrize("place", PLACES)
+def test_eviction_refuses_tensors_that_lie_elsewhere(place, monkeypatch):
+    c, reached = cache8(), []
+    monkeypatch.setattr(mk, "mukv_paged_evict8", lambda *a: reached.append(a))
+    monkeypatch.setattr(mk, "mukv_paged_evict", lambda *a: pytest.fail("rows of 16 bits"))
+    monkeypatch.setattr(mk, "_stream_of", lambda index: 0)
+    rest = dict(table=("i", 2, 5), lengths=("i", 2), weights=("f", 1, 2, 2, 80), weights_out=("f", 1, 2, 2, 80), into=("i", 2, 5),
+                kept=("i", 1, 2, 2, 40), lengths_out=("i", 2))
+    c.evict(budget=40, **tensors({}, **rest))
+    assert len(reached) == 1 and reached[0][1] == c._scales_at
+    for name in rest:
+        with pytest.raises(AssertionError):
+            c.evict(budget=40, **tensors({name: place}, **rest))
+    assert len(reached) == 1
