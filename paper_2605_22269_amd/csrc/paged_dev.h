@@ -72,6 +72,7 @@ __device__ __forceinline__ bool find_share(const PagedView &v, const PlanShape &
     float least;
     const int per = chunk_by_cost(p, sums, true, &least);
     bool even = tiles >= 1 && tiles + workers <= p.records && tiles * x->s.blocks <= kMostSteps;
+    even = even && shares_fit(p, (uint32_t)tiles, workers);
     even = even && cost_of_shares(p, sums.tiles, sums.seen, (float)workers) < least;
     if (even) {
         int head = 0;

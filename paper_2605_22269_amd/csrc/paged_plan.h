@@ -182,6 +182,9 @@ MUKV_HD int record_of(uint32_t first_worker, int tile) { return (int)first_worke
 MUKV_HD float cost_of_shares(const PlanShape &p, float tiles, float line, float workers) {
     return ceilf(line / workers) + (float)p.start * (1.f + tiles / workers) + p.join * (1.f + workers / tiles) + p.record * (workers + tiles);
 }
+// Whether a tile is in no more than p.most stretches, where that matters (what is left of shared rows is read again by their number): a tile of a
+// line of equal ones meets the starts of workers / tiles stretches, rounded up, and one more, and may begin inside another.
+MUKV_HD bool shares_fit(const PlanShape &p, uint32_t tiles, uint32_t workers) { return !p.units || tiles * (uint32_t)(p.most - 2) >= workers; }
 // Workgroups that cover every unit.
 MUKV_HD int64_t tiles_bound(const PagedView &v, const PlanShape &p) {
     const int64_t with = v.n_seqs < v.n_tokens ? v.n_seqs : v.n_tokens;

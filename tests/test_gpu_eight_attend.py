@@ -147,3 +147,35 @@ def test_captured_and_replayed_beside_eager_calls():
         call(eager)
         torch.cuda.synchronize()
         assert torch.equal(out, eager), i
+
+
+@pytest.mark.parametrize("new", [2, 300])
+def test_offsets_far_past_32_bits(new):
+    """Pages, and their scales, that lie past 4 GiB: written, attended to alone and as what others share."""
+    D, R, n = 128, 1024, 34000
+    kp, vp = (torch.zeros(1, n, 1, R, D, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in "kv")
+    big = torch.zeros(n, 130 * 1024, dtype=torch.uint8, device="cuda")
+    scales = [big.as_strided((1, n, 1, R), (0, 130 * 1024, 0, 1), storage_offset=x) for x in (0, 2048)]
+    far = mk.PagedKV8(kp, vp, *scales, n_q_heads=8)
+    near_by = Batch([(new, 1500)], None, D, 8, 1, R, BF16, True, seed=4, layers=1, layer=0)
+    table, lengths, off = i32([[n - 1, n - 2]]), i32([1500]), i32([0, new])
+    k, v = (torch.randn(1500, 1, D, device="cuda").bfloat16() for _ in "kv")
+    far.append(0, table, lengths, k, v)
+    near_by.cache.append(0, i32(near_by.table), lengths, k, v)
+    assert torch.equal(far.attend(0, table, lengths, near_by.q, offsets=off), near_by.attend())
+    own = torch.randn(new, 1, D, device="cuda").bfloat16()
+    far.append(0, i32([[n - 5]]), i32([new]), own, own)
+    spare = i32([[p for p in range(near_by.n_pages) if p not in near_by.table][:1]])
+    near_by.cache.append(0, spare, i32([new]), own, own)
+    a = far.attend(0, i32([[n - 5]]), i32([new]), near_by.q, offsets=off, shared=mk.Shared(table, lengths))
+    b = near_by.cache.attend(0, spare, i32([new]), near_by.q, offsets=off, shared=mk.Shared(i32(near_by.table), lengths))
+    assert torch.equal(a, b)
+
+
+def test_no_new_tokens():
+    c = Batch([(0, 30), (0, 5)], None, 64, 4, 2, 8, BF16, True, seed=1)
+    assert c.attend().shape == (0, 4, 64)
+    w = torch.ones(2, 2, 30, device="cuda")
+    out = torch.zeros_like(w)
+    c.attend(weights=w, weights_out=out, decay=0.25)
+    assert (out[0] == 0.25).all() and (out[1, :, :5] == 0.25).all() and (out[1, :, 5:] == 0).all()

@@ -94,6 +94,15 @@ def test_tokens_of_no_group_and_pages_that_are_none(dtype, eight):
     c.check(c.attend())
 
 
+@pytest.mark.parametrize("users,hq,hkv,rows", [(16, 64, 1, 110000), (20, 56, 1, 64 * 1600), (3, 5, 1, 70000)])
+def test_few_tiles_of_long_rows(users, hq, hkv, rows):
+    """As many chunks of a tile as there can be."""
+    c = Batch([(1, 3)] * users, [(users, rows)], 128, hq, hkv, 64, BF16, True, seed=3, layers=1, layer=0)
+    first = c.attend()
+    c.check(first)
+    assert torch.equal(c.attend(), first)
+
+
 @pytest.mark.parametrize("n", [70, 200])
 def test_many_groups(n):
     rng = np.random.default_rng(n)
