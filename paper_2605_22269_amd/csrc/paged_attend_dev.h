@@ -572,7 +572,8 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
 // Grid (rows, sequence, KV head).  A wave keeps the keys of kTiles times 16 rows (the A operand) in registers and the sequence's queries
 // stream past it, 16 at a time and requested one tile ahead, with what their weights subtract and the sum they are divided by: S^T
 // leaves a lane one query and four rows of every 16, so the sums over the queries run in the lane until the end, where 16 lanes join.
-template <typename T, int D, bool EIGHT, int kTiles>
+// SPLIT: the four waves have the same rows and a quarter of the queries each, where there are few rows and many queries, as groups have them.
+template <typename T, int D, bool EIGHT, int kTiles, bool SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void paged_weights_kernel(PagedAttendArgs a, int n_groups) {
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
@@ -588,7 +589,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
     const bool has_piece = kPieces >= 4 || lg < kPieces;
     const int my_piece = kPieces >= 4 ? lg : lg & (kPieces - 1);
     constexpr int kRows = 16 * kTiles; // of a wave
-    for (int r0 = kRows * ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)); r0 < n_w; r0 += 4 * kRows * n_groups) {
+    constexpr int kApart = SPLIT ? 1 : 4; // rows of the workgroup, in those of a wave
+    __shared__ float s_sum[SPLIT ? 4 : 1][SPLIT ? kRows : 1];
+    for (int r0 = kRows * ((int)blockIdx.x * kApart + (SPLIT ? 0 : (int)(threadIdx.x >> 6))); r0 < n_w; r0 += kApart * kRows * n_groups) {
         raw16 kx[kTiles][KK];
         typename Keys::Codes kc[EIGHT ? kTiles : 1];
         uint32_t k_scale[EIGHT ? kTiles : 1];
@@ -692,11 +695,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
         };
         // queries before the first row's first token see none of these rows
         int q0 = a.causal && r0 - past > 0 ? (r0 - past < s.n_new ? (r0 - past) * G & ~15 : n_queries) : 0;
+        constexpr int kStep = SPLIT ? 128 : 32;
+        if constexpr (SPLIT) q0 += 32 * (int)(threadIdx.x >> 6);
         if (q0 < n_queries) request(q0, 0);
-        for (; q0 < n_queries; q0 += 32) {
+        for (; q0 < n_queries; q0 += kStep) {
             if (q0 + 16 < n_queries) request(q0 + 16, 1);
             add(0, q0);
-            if (q0 + 32 < n_queries) request(q0 + 32, 0);
+            if (q0 + kStep < n_queries) request(q0 + kStep, 0);
             if (q0 + 16 < n_queries) add(1, q0 + 16);
         }
 #pragma unroll
@@ -704,24 +709,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[t][e] = row16_sum(sum[t][e]);
             const int row = r0 + 16 * t + 4 * lg + (lr & 3);
-            if (lr < 4 && row < n_w) {
+            if constexpr (SPLIT) {
+                if (lr < 4) s_sum[threadIdx.x >> 6][row - r0] = lr == 0 ? sum[t][0] : lr == 1 ? sum[t][1] : lr == 2 ? sum[t][2] : sum[t][3];
+            } else if (lr < 4 && row < n_w) {
                 const int64_t at = b * a.weights_seq + g * a.weights_head + row;
                 const float got = lr == 0 ? sum[t][0] : lr == 1 ? sum[t][1] : lr == 2 ? sum[t][2] : sum[t][3];
                 a.weights_out[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], got) : got;
             }
         }
+        if constexpr (SPLIT) {
+            __syncthreads();
+            const int row = r0 + (int)threadIdx.x;
+            if (threadIdx.x < kRows && row < n_w) {
+                const int64_t at = b * a.weights_seq + g * a.weights_head + row;
+                const float got = (s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x]) + (s_sum[2][threadIdx.x] + s_sum[3][threadIdx.x]);
+                a.weights_out[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], got) : got;
+            }
+            __syncthreads(); // the next rows' sums take their place
+        }
     }
 }
 
-template <typename T, int D, bool EIGHT, int kTiles>
+template <typename T, int D, bool EIGHT, int kTiles, bool SPLIT = false>
 hipError_t launch_weights(const PagedAttendArgs &a, hipStream_t st) {
-    constexpr int kRows = 4 * 16 * kTiles; // of a workgroup
+    constexpr int kRows = (SPLIT ? 1 : 4) * 16 * kTiles; // of a workgroup
     const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
     int64_t groups = (rows + kRows - 1) / kRows, most = 8192 / ((int64_t)a.view.Hkv * a.view.n_seqs);
     if (most < 16) most = 16;
     if (groups > most) groups = most; // (a workgroup goes round: a table is often wider than its sequences)
     if (groups < 1) return hipSuccess;
-    hipLaunchKernelGGL((paged_weights_kernel<T, D, EIGHT, kTiles>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, (int)groups);
+    hipLaunchKernelGGL((paged_weights_kernel<T, D, EIGHT, kTiles, SPLIT>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, (int)groups);
     return hipGetLastError();
 }
 
@@ -750,6 +767,13 @@ hipError_t launch_weights_typed(const PagedAttendArgs &a, hipStream_t st) {
     // Queries that stream past are shared by the rows a wave holds; where there are few of them it is more waves that count (us a
     // launch, 16 / 64 rows a wave: 64 users, one token, 2000 rows, 64/8 heads 61 / 70; 6 users, 16 tokens, 36000 rows in all, 28/4 heads 38 / 29).
     if ((int64_t)a.view.n_tokens * a.view.G <= 32 * (int64_t)a.view.n_seqs) return launch_weights<T, D, EIGHT, 1>(a, st);
+    if (EIGHT || a.shared.mode != SharedResults::kNone) { // (other calls' sums stay in the order that they have been in)
+        const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
+        // (us a call, without / with: 64/8 heads of 128 over 6272 shared rows in bf16, 256 tokens 222 / 188, 16 tokens 53 / 57; 128 tokens over 1548, heads
+        // of 64, 93 / 62; 16 tokens over 20000 rows in 8 bits, 28/4 heads, 53.5 / 56.5)
+        const int64_t groups = div_up(rows, 64) * a.view.n_seqs * a.view.Hkv, queries = (int64_t)a.view.n_tokens * a.view.G / a.view.n_seqs;
+        if (groups < 512 || (groups < 2048 && queries >= 512)) return launch_weights<T, D, EIGHT, sizeof(T) == 2 ? 4 : 2, true>(a, st);
+    }
     return launch_weights<T, D, EIGHT, sizeof(T) == 2 ? 4 : 2>(a, st);
 }
 
