@@ -806,6 +806,7 @@ int mukv_paged_evict8(const mukv_paged *pages, const mukv_row_scales *scales, co
  *                   each other.  Tokens before the first and behind the last see no
  *                   shared rows.  n_tokens as in seqs, max_new: most new tokens of a group
  *                   (0: not known).  Where offsets do not ascend, out is left as it is
+ *                   and weights are undefined
  *   weights, shared_weights   NULL, or where the weights of the sequences' own rows, of the
  *                   shared rows of every group go: the sum over all that see them
  *   workspace       at least mukv_paged_shared_workspace_size() bytes, otherwise as there

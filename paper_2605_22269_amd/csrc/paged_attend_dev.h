@@ -454,8 +454,8 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         for (; blk + W < b_hi; blk += W) step(std::true_type{}, blk + W);
         step(std::false_type{}, 0);
     }
-    // What the other launch left, but for the values: to LDS, by the wave that has the fewest rows.  (Before its rows the wave waits for three loads
-    // one after the other: 48 users' tokens in three rooms 44.9 us, so 43.x.)
+    // What the other launch left, but for the values: to LDS, by the wave that has the fewest rows.  (Asked for before its rows, three loads one
+    // after the other hold them up: 48 users' tokens in three rooms 44.9 us a call, so 43.5.)
     __shared__ Taken s_taken[SHARED ? kPQ : 1];
     __shared__ float s_by[SHARED ? kPlanChunks : 1][kPQ];
     __shared__ int s_fit;
