@@ -164,15 +164,16 @@ struct Space {
 };
 int64_t hint_of(const mukv_seqs &s) { return s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs); } // new tokens of a sequence
 int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
-mukv::PlanShape plan_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool *prompts) {
+mukv::PlanShape plan_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool eight, bool *prompts) {
     const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint_of(s));
     *prompts = tile != 0;
-    return mukv::paged_plan(p.dtype, tile, causal);
+    return mukv::paged_plan(p.dtype, tile, causal, eight);
 }
-Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights) {
+// eight: rows in 8 bits, which takes the same space
+Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights, bool eight = false) {
     Space x = {};
     bool prompts;
-    x.plan = plan_of(p, s, causal, &prompts);
+    x.plan = plan_of(p, s, causal, eight, &prompts);
     const int64_t rows = (int64_t)x.plan.records * x.plan.queries, sums = prompts ? rows : 0;
     x.stats = 4 * mukv::kPlanRecords;
     x.values = x.stats + 8 * rows;
@@ -181,7 +182,7 @@ Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared,
     const int64_t queries = (int64_t)s.n_tokens * p.n_q_heads;
     x.bytes = x.pairs + (with_weights ? 8 * queries : 0);
     if (shared) { // places for the queries of as many chunks as there can be, then for those of tiles with one
-        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype, p.head_dim, hint_of(*shared));
+        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype, p.head_dim, hint_of(*shared), eight);
         x.single = x.shared_plan.records * x.shared_plan.queries;
         x.fit = up_to_16(x.bytes);
         x.left_heads = x.fit + 16;
@@ -265,7 +266,7 @@ int attend(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer
         if (!aligned(out)) return MUKV_ERR_UNSUPPORTED;
     }
     if (!workspace) return MUKV_ERR_INVALID_ARG;
-    const Space x = space_of(*pages, *seqs, shared, causal != 0, any_weights);
+    const Space x = space_of(*pages, *seqs, shared, causal != 0, any_weights, scales != nullptr);
     if (workspace_bytes < x.bytes) return MUKV_ERR_CAPACITY;
     if (!aligned(workspace)) return MUKV_ERR_UNSUPPORTED;
     mukv::PagedAttendArgs a = {};

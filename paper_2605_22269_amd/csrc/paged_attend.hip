@@ -21,7 +21,7 @@ int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint) {
     return queries <= 128 || (tiles <= 256 && room <= 4096) ? 128 : 256;
 }
 
-PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
+PlanShape paged_plan(int dtype, int prompt_tile, bool causal, bool eight) {
     PlanShape p;
     p.causal = causal;
     p.most = kPlanChunks;
@@ -35,7 +35,7 @@ PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
         p.record = 0.06f;
     } else {
         p.queries = kPQ;
-        p.rows = dtype == MUKV_BF16 ? 128 : 64; // a block of every wave
+        p.rows = dtype == MUKV_BF16 || eight ? 128 : 64; // a block of every wave
         p.records = 2048;
         p.places = 512;
         p.start = 0;
@@ -52,12 +52,12 @@ PlanShape paged_plan(int dtype, int prompt_tile, bool causal) {
 // over 10000 rows in 8 bits 111 / 57* / 65, over 40000 408 / 175 / 171*; 718 tokens over 6272, 28/4 heads, 303 / 127 / 118*.
 // Workgroups without a unit still have to start, after all that have one.  Few tiles: no more units than places, or one group's tiles
 // shared out step by step, which leaves no place without work either (the last two cases above: 171.6 and 121.8 with 704 units).
-PlanShape shared_plan(const PagedView &groups, int dtype, int D, int64_t new_hint) {
+PlanShape shared_plan(const PagedView &groups, int dtype, int D, int64_t new_hint, bool eight) {
     const int64_t queries = new_hint * groups.G, tiles256 = div_up(queries, 256) * groups.n_seqs * groups.Hkv;
     int tile = 0;
     if (dtype == MUKV_BF16 && D >= 64 && queries >= 48 && (int64_t)groups.n_tokens * groups.Hq >= 1000)
         tile = queries > 128 && tiles256 * div_up(room_of(groups), 64) > 24 * 256 ? 256 : 128;
-    PlanShape p = paged_plan(dtype, tile, false);
+    PlanShape p = paged_plan(dtype, tile, false, eight);
     if (!tile) return p;
     p.join = 0.2f; // (the other launch's, shared by more workgroups)
     p.record = 0.02f;

@@ -80,14 +80,36 @@ __device__ __forceinline__ f32x4 scores_f32(const raw16 (&k)[KK], Q q) {
     return x;
 }
 
-// The rows of a tile, in blocks of 32 (bf16) or 16 (fp32), dealt to the waves in turn; nothing crosses the waves until the end.
+// Eight fp32 numbers as three bf16 each, which add up to it: 8 of its 24 bits after the other, cut off, so that nothing can overflow.
+// (An infinity is the first part; NaN stays NaN in one of them.)
+__device__ __forceinline__ void three_parts(const raw16 (&x)[2], raw16 (&part)[3]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t a = x[e / 2][2 * e % 4], b = x[e / 2][2 * e % 4 + 1];
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            part[j][e] = a >> 16 | (b & 0xFFFF0000u);
+            auto rest = [](uint32_t y) {
+                const float f = __uint_as_float(y);
+                return fabsf(f) == INFINITY ? 0u : __float_as_uint(f - __uint_as_float(y & 0xFFFF0000u));
+            };
+            a = rest(a);
+            b = rest(b);
+        }
+    }
+}
+
+// The rows of a tile, in blocks of 32 (bf16, EIGHT) or 16 (fp32), dealt to the waves in turn; nothing crosses the waves until the end.
 //   rows     a lane works out where one row lives, from a table entry that was requested a block earlier; the others fetch that by
 //            lane permutes.  Keys and values go straight to registers, the next block's requested as soon as this one's are used up.
 //   scores   S^T = K Q^T (16x16x32 bf16, 16x16x4 fp32): a lane holds ONE query (lane % 16) and the rows 4 (lane / 16) + r of every 16.
 //   values   O^T += V^T P^T: the weights are the B operand as they stand in the lane.  bf16: pairs hi + lo, 16 of the fp32
 //            weight's 24 bits; the value rows pass through LDS the wave has to itself and the transpose read.  fp32: no transpose needed.
-// EIGHT: rows of 8 bits (eight_dev.h) become the payload type's as they are used, which changes no bit of them: keys in registers, where a
+// EIGHT: rows of 8 bits (eight_dev.h) become bf16 as they are used, which changes no bit of them: keys in registers, where a
 // lane's codes are neighbours, so an operand's features are others than without (the queries' are, too); values on their way to LDS.
+// fp32 payloads go the same way: queries and weights are three bf16 each, all 24 bits, whose products with a row are exact and are
+// added in fp32.  Three matrix instructions so take the place of eight that are twice as long (us a call: 64 users over 200 to 12000
+// rows, 64/8 heads of 128, 236, in fp32 522; 12 users, 5 tokens, 28/4 heads of 64, 42 for 90; prompts of 700 to 1500 tokens 698 for 1632).
 // As many workgroups to a compute unit as the registers allow (us a launch, two / as now: 100 users of 3 rows, 12 heads of 64 bf16, 13.7 / 10.2;
 // 12 users, 5 tokens over 1000 to 9000 rows, 28/4 heads of 64 bf16, 26.5 / 22.3; 6 prompts of 700 to 1500 tokens, 28/4 heads of 32 bf16, 148 / 94;
 // of fp32 252 / 218; 1500 tokens, 16/4 heads of 64 fp32, 103 / 92).
@@ -96,26 +118,28 @@ template <typename T, int D, bool EIGHT, bool SHARED>
 __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D <= 32 ? 4 : D == 64 ? 3 : 2, D <= 32 ? 5 : D == 64 ? 3 : 2))) void paged_attend_kernel(PagedAttendArgs a) {
     constexpr int W = kPWaves;
     constexpr bool kBf16 = sizeof(T) == 2;
-    constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
-    constexpr int kRows = kBf16 ? 32 : 16;             // rows of a block
+    constexpr bool kNarrow = kBf16 || EIGHT; // rows are multiplied as bf16, queries and weights perhaps in parts
+    constexpr int kQParts = kBf16 ? 1 : 3, kWParts = kBf16 ? 2 : 3;
+    constexpr int kRowB = D * (kNarrow ? 2 : 4), kPieces = kRowB / 16;
+    constexpr int kRows = kNarrow ? 32 : 16;             // rows of a block
     constexpr int kTiles = kRows / 16;                 // 16-row tiles of the scores
-    constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16; // 16-byte pieces of a key row (and of a query) per lane
+    constexpr int KK = kNarrow ? (D + 31) / 32 : D / 16; // 16-byte pieces of a key row (and of a query) per lane
     constexpr int NF = D / 16;                         // 16-feature tiles of the output
     // bf16: value pieces per lane, each load of the wave kRowsPerLoad whole rows.  fp32: per 4-row step D / 16 floats.  (EIGHT, bf16: a
     // load is two pieces, where a row has more than two)
-    constexpr int kVH = kBf16 ? (EIGHT && D > 16 ? 2 : 1) : (D == 128 ? 2 : 1); // pieces, or loads, per row
-    constexpr int kRowsPerLoad = 64 * (kBf16 ? kVH : 1) / kPieces, NV = kBf16 ? kRows / kRowsPerLoad : 4;
-    constexpr int kVW = kBf16 ? 4 : (D >= 64 ? 4 : D / 16); // dwords of a piece
-    constexpr int kValueLanes = kBf16 ? kPieces / kVH : 16; // of a row
+    constexpr int kVH = kNarrow ? (EIGHT && D > 16 ? 2 : 1) : (D == 128 ? 2 : 1); // pieces, or loads, per row
+    constexpr int kRowsPerLoad = 64 * (kNarrow ? kVH : 1) / kPieces, NV = kNarrow ? kRows / kRowsPerLoad : 4;
+    constexpr int kVW = kNarrow ? 4 : (D >= 64 ? 4 : D / 16); // dwords of a piece
+    constexpr int kValueLanes = kNarrow ? kPieces / kVH : 16; // of a row
     typedef __attribute__((ext_vector_type(kVW))) unsigned int raw_v;
-    using Keys = KeyCodes<T, D>;
-    // codes of values: bf16, words of a load; fp32, kVW bytes of each
-    constexpr int kVC = kBf16 ? 2 * kVH : kVH;
+    using Keys = KeyCodes<std::conditional_t<kNarrow, uint16_t, T>, D>;
+    // words of codes of a load of values
+    constexpr int kVC = kNarrow ? 2 * kVH : kVH;
     // per wave: staged value rows (bf16), at the end its outputs [16 queries][D]
     __shared__ __align__(1024) unsigned char s_buf[W][64 * D];
     __shared__ float s_m[W][kPQ], s_l[W][kPQ];
     constexpr bool kQueryLds = !kBf16 && D == 128; // fp32, 128 features: the queries' operands wait in LDS
-    __shared__ raw16 s_q[kQueryLds ? KK : 1][kQueryLds ? 64 : 1];
+    __shared__ raw16 s_q[!kQueryLds ? 1 : EIGHT ? KK * kQParts : KK][kQueryLds ? 64 : 1];
     const PagedView &v = a.view;
     if (SHARED && a.shared.mode == SharedResults::kLeave) tell_fit(v, a.shared);
     Unit u;
@@ -128,7 +152,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     const int my_q = u.tile * kPQ + lr;
     const bool q_ok = my_q < n_queries;
     const int my_tok = q_ok ? my_q / G : 0;
-    raw16 qb[kQueryLds ? 1 : KK];
+    raw16 qb[kQueryLds ? 1 : EIGHT ? KK * kQParts : KK];
     const bool has_piece = kPieces >= 4 || lg < kPieces; // (rows of 32 bytes have two pieces)
     const int my_piece = kPieces >= 4 ? lg : lg & (kPieces - 1);
     {
@@ -136,6 +160,20 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             if (kQueryLds && wave != 0) break; // the same in all waves
+            if constexpr (EIGHT && !kBf16) {
+                const raw16 *const at = reinterpret_cast<const raw16 *>(qp + 32 * Keys::piece_of(my_piece, kk));
+                raw16 x[2] = {brought_down<T, D>(at[0]), brought_down<T, D>(at[1])}, part[kQParts];
+                if (!q_ok || !has_piece) x[0] = x[1] = raw16{0u, 0u, 0u, 0u};
+                three_parts(x, part);
+#pragma unroll
+                for (int j = 0; j < kQParts; ++j) {
+                    if constexpr (kQueryLds)
+                        s_q[kk * kQParts + j][lane] = part[j];
+                    else
+                        qb[kk * kQParts + j] = part[j];
+                }
+                continue;
+            }
             raw16 x = *reinterpret_cast<const raw16 *>(qp + 16 * (EIGHT ? Keys::piece_of(my_piece, kk) : my_piece + 4 * kk));
             x = q_ok && has_piece ? brought_down<T, D>(x) : raw16{0u, 0u, 0u, 0u};
             if constexpr (kQueryLds)
@@ -176,7 +214,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     auto from_lane = [&](int64_t x, int from) __attribute__((always_inline)) {
         return (int64_t)((uint64_t)(unsigned)__shfl((int)(x >> 32), from) << 32 | (unsigned)__shfl((int)x, from));
     };
-    auto value_row = [&](int i) { return kBf16 ? i * kRowsPerLoad + lane / kValueLanes : 4 * lg + i; }; // of the lane's load i
+    auto value_row = [&](int i) { return kNarrow ? i * kRowsPerLoad + lane / kValueLanes : 4 * lg + i; }; // of the lane's load i
     raw16 kx[kTiles][KK];
     raw_v vx[NV][kVH];
     typename Keys::Codes kc[EIGHT ? kTiles : 1]; // EIGHT: as they come from memory
@@ -203,16 +241,10 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const unsigned char *p = vb + from_lane(off, value_row(i));
-                if constexpr (kBf16) {
-                    typedef __attribute__((ext_vector_type(kVC))) unsigned int raw_c;
-                    const raw_c x = *reinterpret_cast<const raw_c *>(p + (lane % kValueLanes) * 4 * kVC);
+                typedef __attribute__((ext_vector_type(kVC))) unsigned int raw_c;
+                const raw_c x = *reinterpret_cast<const raw_c *>(p + (lane % kValueLanes) * 4 * kVC);
 #pragma unroll
-                    for (int w = 0; w < kVC; ++w) vc[i][w] = x[w];
-                } else {
-                    using Word = std::conditional_t<kVW == 4, uint32_t, std::conditional_t<kVW == 2, uint16_t, uint8_t>>;
-#pragma unroll
-                    for (int h = 0; h < kVH; ++h) vc[i][h] = *reinterpret_cast<const Word *>(p + lr * kVW + 64 * h);
-                }
+                for (int w = 0; w < kVC; ++w) vc[i][w] = x[w];
             }
             return;
         }
@@ -225,7 +257,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     };
 
     float m_run = -INFINITY, l_run = 0.f; // of query lr; l_run: over the rows this lane holds
-    f32x4 acc[NF]; // of query lr.  bf16: tile f, features 16 f + 4 lg + r.  fp32: tile (h, e), features 64 h + kVW (4 lg + r) + e
+    f32x4 acc[NF]; // of query lr.  kNarrow: tile f, features 16 f + 4 lg + r.  fp32: tile (h, e), features 64 h + kVW (4 lg + r) + e
 #pragma unroll
     for (int f = 0; f < NF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
     unsigned char *const buf = s_buf[wave];
@@ -237,7 +269,33 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
         // ---- scores S^T = K Q^T: query lr, rows 16 t + 4 lg + r ----
         f32x4 sc[kTiles];
         if constexpr (kQueryLds) asm volatile("" ::: "memory"); // (the queries are read again, not held)
-        if constexpr (kBf16) {
+        if constexpr (EIGHT && !kBf16) { // sums of 32 terms, of the queries' parts the least first, joined pair by pair
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                kc[t].spread(scale_of((uint32_t)__shfl((int)k_scale, 16 * t + lr)), kx[t]);
+                if (!has_piece) kx[t][0] = raw16{0u, 0u, 0u, 0u}; // (16 features: KK is 1)
+            }
+            f32x4 pair[kTiles];
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                f32x4 c[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = kQParts - 1; j >= 0; --j) {
+                    const raw16 z = kQueryLds ? s_q[kQueryLds ? kk * kQParts + j : 0][kQueryLds ? lane : 0] : qb[kQueryLds ? 0 : kk * kQParts + j];
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[t][kk]), __builtin_bit_cast(bf16x8, z), c[t], 0, 0, 0);
+                }
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    pair[t] = kk % 2 ? pair[t] + c[t] : c[t];
+                    if (kk == (KK > 1 ? 1 : 0)) sc[t] = pair[t];
+                    if (kk == 3) sc[t] += pair[t];
+                }
+            }
+        } else if constexpr (kBf16) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -253,7 +311,6 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                 }
             }
         } else {
-            if constexpr (EIGHT) kc[0].spread(scale_of((uint32_t)__shfl((int)k_scale, lr)), kx[0]);
             sc[0] = scores_f32<KK>(kx[0], [&](int kk) { return kQueryLds ? s_q[kk][lane] : qb[kQueryLds ? 0 : kk]; });
         }
         int64_t off_next = 0;
@@ -314,7 +371,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
             const float s = scale_of((uint32_t)__shfl((int)v_scale, value_row(i)));
 #pragma unroll
             for (int h = 0; h < kVH; ++h) {
-                const raw16 x = kBf16 ? bf16_piece(vc[i][kBf16 ? 2 * h : 0], vc[i][kBf16 ? 2 * h + 1 : 0], s) : f32_piece(vc[i][kBf16 ? 0 : h], s);
+                const raw16 x = bf16_piece(vc[i][EIGHT ? 2 * h : 0], vc[i][EIGHT ? 2 * h + 1 : 0], s);
 #pragma unroll
                 for (int e = 0; e < kVW; ++e) vx[i][h][e] = x[e];
             }
@@ -355,12 +412,22 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
             apart = first_tok != last_tok && __builtin_amdgcn_ballot_w64(worst == 0x7F800000u) != 0;
         }
         // ---- O^T += V^T P^T: the weights are the B operand as they stand in the lane ----
-        if constexpr (kBf16) {
-            raw16 hi, lo;
+        if constexpr (kNarrow) {
+            raw16 hi, lo, least;
+            if constexpr (kBf16) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                hi[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
-                lo[e] = bf16_pair(p[2 * e] - __uint_as_float(hi[e] << 16), p[2 * e + 1] - __uint_as_float(hi[e] & 0xFFFF0000u));
+                for (int e = 0; e < 4; ++e) {
+                    hi[e] = bf16_pair(p[2 * e], p[2 * e + 1]);
+                    lo[e] = bf16_pair(p[2 * e] - __uint_as_float(hi[e] << 16), p[2 * e + 1] - __uint_as_float(hi[e] & 0xFFFF0000u));
+                }
+            } else {
+                raw16 x[2], part[kWParts];
+#pragma unroll
+                for (int e = 0; e < 4 * kTiles; ++e) x[e / 4][e % 4] = __float_as_uint(p[e]);
+                three_parts(x, part);
+                hi = part[0];
+                lo = part[1];
+                least = part[2];
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -379,10 +446,19 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                 const i16x4 v1 = lds_read_tr16(buf + r1 * kRowB + 16 * ((2 * f + piece) ^ row_swizzle<D>(r1)) + sub);
                 return i16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
             };
+            auto product_of_parts = [&](bf16x8 x) __attribute__((always_inline)) { // the least first
+                f32x4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8, least), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
+                return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
+            };
             if (__builtin_expect(!apart, 1)) {
 #pragma unroll
                 for (int f = 0; f < NF; ++f) {
                     const bf16x8 av = __builtin_bit_cast(bf16x8, values_of(f));
+                    if constexpr (kWParts == 3) {
+                        acc[f] += product_of_parts(av);
+                        continue;
+                    }
                     acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, hi), acc[f], 0, 0, 0);
                     acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, lo), acc[f], 0, 0, 0);
                 }
@@ -395,17 +471,18 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = tok >= first_to_see(e) ? x[e] : (short)0;
                         f32x4 c = acc[f];
-                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
-                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
+                        if constexpr (kWParts == 3) {
+                            c += product_of_parts(__builtin_bit_cast(bf16x8, x));
+                        } else {
+                            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, hi), c, 0, 0, 0);
+                            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, lo), c, 0, 0, 0);
+                        }
 #pragma unroll
                         for (int r = 0; r < 4; ++r) acc[f][r] = tok == my_tok ? c[r] : acc[f][r];
                     }
             }
             asm volatile("" ::: "memory"); // the next block's rows take their place
         } else {
-            if constexpr (EIGHT)
-#pragma unroll
-                for (int i = 0; i < NV; ++i) spread_values(i);
             __builtin_amdgcn_sched_barrier(0);
             auto product = [&](int h, int e, auto seen) __attribute__((always_inline)) { // four rows at a time, joined pair by pair
                 f32x4 d[4];
@@ -476,7 +553,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
     f32x4(*const s_o)[kQuads] = reinterpret_cast<f32x4(*)[kQuads]>(buf);
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-        if constexpr (kBf16) {
+        if constexpr (kNarrow) {
             s_o[lr][(4 * f + lg) ^ (lr & (kQuads - 1))] = acc[f];
         } else if constexpr (kVW == 4) { // register r of the four tiles of h: features 64 h + 16 lg + 4 r ..
             const int h = f / 4, r = f % 4;

@@ -27,9 +27,9 @@ hipError_t launch_rows8(const RopeArgs &a, int dtype, bool read, hipStream_t st)
 // Which kernel takes an attention call follows from types and sizes that the host knows (paged_attend.hip): 0 that for any shape, otherwise
 // the one for prompts, with tiles of so many queries.  new_hint: new tokens of a sequence, as far as that is known.
 int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint);
-PlanShape paged_plan(int dtype, int prompt_tile, bool causal);
+PlanShape paged_plan(int dtype, int prompt_tile, bool causal, bool eight);
 // The same for rows that groups share, where chunks are left, not joined.
-PlanShape shared_plan(const PagedView &groups, int dtype, int D, int64_t new_hint);
+PlanShape shared_plan(const PagedView &groups, int dtype, int D, int64_t new_hint, bool eight);
 constexpr int kPlanChunks = 64;     // most chunks of a sequence
 constexpr int kPlanRecords = 2048;  // most that any plan has: the counts at a workspace's start
 

@@ -109,13 +109,20 @@ class Batch:
         n = max(min(int(self.lengths.max()), self.table.shape[1] * self.R), 1)   # (no more than a table has room for)
         return n + (min(max(int(self.shared_lengths.max()), 0), self.shared_table.shape[1] * self.R) if self.grouped else 0)
 
+    def of_parts(self, reach):
+        """fp32 over rows in 8 bits, relative, on top of attention_error: queries and weights are three bf16, of at most 1, 2^-7 and 2^-15 of
+        them, and 32 products of each add up in the matrix core: 32 (1 + 2^-7 + 2^-15) + 3 < 36 roundings and two where four such sums are
+        joined, for the 12 of a score there, in numerator and denominator; 36 and one where a block of 32 rows joins the rest, for the
+        20 of sums over rows."""
+        return (2 * (38 - 12) * reach / np.sqrt(self.D) + (37 - 20)) * 2.0**-24 if self.eight and self.dtype == F32 else 0.0
+
     def error(self, amean, reach):
         """paged_testlib.attention_error, and for the join of own rows with shared ones: the difference of two references (each at most as
         large as a score) and a multiplication and an addition more."""
         G = self.hq // self.hkv
         most = max(self.T // max(len(self.news), 1), int(self.news.max()), int(np.diff(self.shared_off).max()) if self.grouped else 0)
         single = self.dtype == BF16 and self.D >= 64 and most * G >= 48
-        err = attention_error(amean, reach, self.rows_seen(), self.D, self.dtype, single)
+        err = attention_error(amean, reach, self.rows_seen(), self.D, self.dtype, single) + amean * self.of_parts(reach)
         return err + amean * (8 + 4 * 1.4427 * reach / np.sqrt(self.D)) * 2.0**-24 if self.grouped else err
 
     def check(self, got, causal=True):
@@ -127,4 +134,5 @@ class Batch:
         """Of a row's weight, relative: each of those that add up is off as in error() (of values of 1), and they are added up."""
         worst = reach.max() if reach.size else 0.0
         rel = attention_error(1.0, worst, self.rows_seen(), self.D, F32) + (2 * (self.D + 4) * 2.0**-24 * worst / np.sqrt(self.D) if self.dtype == BF16 else 0)
+        rel = rel + self.of_parts(worst)
         return rel + (8 + 4 * 1.4427 * worst / np.sqrt(self.D)) * 2.0**-24 + 2.0**-23 * max(1, tokens * (self.hq // self.hkv)) / 16
