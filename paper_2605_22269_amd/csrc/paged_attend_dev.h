@@ -99,6 +99,22 @@ __device__ __forceinline__ void three_parts(const raw16 (&x)[2], raw16 (&part)[3
     }
 }
 
+// Scores of 16 bf16 rows and 16 queries in three parts: sums of 32 terms of each part, the least first, joined pair by pair.
+template <int KK>
+__device__ __forceinline__ f32x4 scores_of_parts(const raw16 (&k)[KK], const raw16 (&part)[KK][3]) {
+    f32x4 c[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+        c[kk] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 2; j >= 0; --j)
+            c[kk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[kk]), __builtin_bit_cast(bf16x8, part[kk][j]), c[kk], 0, 0, 0);
+    }
+    if constexpr (KK == 4) return (c[0] + c[1]) + (c[2] + c[3]);
+    if constexpr (KK == 2) return c[0] + c[1];
+    return c[0];
+}
+
 // The rows of a tile, in blocks of 32 (bf16, EIGHT) or 16 (fp32), dealt to the waves in turn; nothing crosses the waves until the end.
 //   rows     a lane works out where one row lives, from a table entry that was requested a block earlier; the others fetch that by
 //            lane permutes.  Keys and values go straight to registers, the next block's requested as soon as this one's are used up.
@@ -653,9 +669,10 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
 template <typename T, int D, bool EIGHT, int kTiles, bool SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void paged_weights_kernel(PagedAttendArgs a, int n_groups) {
     constexpr bool kBf16 = sizeof(T) == 2;
-    constexpr int kRowB = D * (int)sizeof(T), kPieces = kRowB / 16;
-    constexpr int KK = kBf16 ? (D + 31) / 32 : D / 16;
-    using Keys = KeyCodes<T, D>;
+    constexpr bool kNarrow = kBf16 || EIGHT, kInParts = EIGHT && !kBf16; // as in paged_attend_kernel
+    constexpr int kRowB = D * (kNarrow ? 2 : 4), kPieces = kRowB / 16;
+    constexpr int KK = kNarrow ? (D + 31) / 32 : D / 16;
+    using Keys = KeyCodes<std::conditional_t<kNarrow, uint16_t, T>, D>;
     const PagedView &v = a.view;
     const int g = blockIdx.z, b = blockIdx.y;
     const SeqShape s = shape_of(v, a.plan, b);
@@ -707,7 +724,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[t][e] = 0.f;
-        raw16 qx[2][KK];
+        raw16 qx[2][kInParts ? 2 * KK : KK];
         f32x2 pair[2];
         int tok[2];
         auto request = [&](int q0, int at) __attribute__((always_inline)) {
@@ -716,7 +733,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
             const unsigned char *qp = a.q + (int64_t)(s.first + tok[at]) * a.q_token + (int64_t)h * a.q_head;
             pair[at] = *reinterpret_cast<const f32x2 *>(a.pairs + 2 * ((int64_t)(s.first + tok[at]) * v.Hq + h));
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) qx[at][kk] = *reinterpret_cast<const raw16 *>(qp + 16 * (EIGHT ? Keys::piece_of(my_piece, kk) : my_piece + 4 * kk));
+            for (int kk = 0; kk < KK; ++kk) {
+                if constexpr (kInParts) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) qx[at][2 * kk + i] = reinterpret_cast<const raw16 *>(qp + 32 * Keys::piece_of(my_piece, kk))[i];
+                    continue;
+                }
+                qx[at][kk] = *reinterpret_cast<const raw16 *>(qp + 16 * (EIGHT ? Keys::piece_of(my_piece, kk) : my_piece + 4 * kk));
+            }
             if (q0 + lr >= n_queries) tok[at] = -1; // sees nothing
         };
         // EIGHT: most rows are seen by all tokens, where nothing has to be looked at
@@ -730,9 +754,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
             late = __builtin_amdgcn_ballot_w64(last > 0) != 0;
         }
         auto add = [&](int at, int q0) __attribute__((always_inline)) {
-            raw16 q[KK];
+            raw16 q[kInParts ? 1 : KK], part[kInParts ? KK : 1][3];
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) q[kk] = has_piece ? brought_down<T, D>(qx[at][kk]) : raw16{0u, 0u, 0u, 0u};
+            for (int kk = 0; kk < KK; ++kk) {
+                if constexpr (kInParts) {
+                    raw16 x[2] = {brought_down<T, D>(qx[at][2 * kk]), brought_down<T, D>(qx[at][2 * kk + 1])};
+                    if (!has_piece) x[0] = x[1] = raw16{0u, 0u, 0u, 0u};
+                    three_parts(x, part[kk]);
+                    continue;
+                }
+                q[kInParts ? 0 : kk] = has_piece ? brought_down<T, D>(qx[at][kk]) : raw16{0u, 0u, 0u, 0u};
+            }
             const float ref = pair[at][0], inv = pair[at][1];
             const bool large = __builtin_amdgcn_ballot_w64(fabsf(ref) > kLargeRef) != 0; // (its rounding shows)
             if (EIGHT && kBf16 && !late && !large && q0 + 16 <= n_queries) {
@@ -750,7 +782,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 f32x4 sc = {0.f, 0.f, 0.f, 0.f};
-                if constexpr (kBf16) {
+                if constexpr (kInParts) {
+                    sc = scores_of_parts<KK>(kx[t], part);
+                } else if constexpr (kBf16) {
 #pragma unroll
                     for (int kk = 0; kk < KK; ++kk)
                         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kx[t][kk]), __builtin_bit_cast(bf16x8, q[kk]), sc, 0, 0, 0);
@@ -849,9 +883,9 @@ hipError_t launch_weights_typed(const PagedAttendArgs &a, hipStream_t st) {
         // (us a call, without / with: 64/8 heads of 128 over 6272 shared rows in bf16, 256 tokens 222 / 188, 16 tokens 53 / 57; 128 tokens over 1548, heads
         // of 64, 93 / 62; 16 tokens over 20000 rows in 8 bits, 28/4 heads, 53.5 / 56.5)
         const int64_t groups = div_up(rows, 64) * a.view.n_seqs * a.view.Hkv, queries = (int64_t)a.view.n_tokens * a.view.G / a.view.n_seqs;
-        if (groups < 512 || (groups < 2048 && queries >= 512)) return launch_weights<T, D, EIGHT, sizeof(T) == 2 ? 4 : 2, true>(a, st);
+        if (groups < 512 || (groups < 2048 && queries >= 512)) return launch_weights<T, D, EIGHT, EIGHT || sizeof(T) == 2 ? 4 : 2, true>(a, st);
     }
-    return launch_weights<T, D, EIGHT, sizeof(T) == 2 ? 4 : 2>(a, st);
+    return launch_weights<T, D, EIGHT, EIGHT || sizeof(T) == 2 ? 4 : 2>(a, st);
 }
 
 template <typename T, bool EIGHT>
