@@ -30,7 +30,8 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
 // halves of a step in flight: so a half is worked through in order (kPlain), in half the registers.  A step of 64 rows takes 4100
 // clocks of the compute unit for 4470, 2048 of them products (us a call: 1568 tokens over 7840 rows in 8 bits 185 for 197, 8192 over themselves 514 for 543).
 // EIGHT: rows of 8 bits (eight_dev.h) come through registers, where they become bf16, and lie in LDS as the others do: a step's codes are
-// requested where its rows would be, and put down half a step later, between the products of the step before.
+// requested where its rows would be, and put down between the products of the half in which they have to be there (half a step earlier they are
+// waited for: 8 users, 16 tokens over 8000 rows, 46.0 us a call for 45.1; 1568 tokens over 7840 rows, 28/4 heads of 64, 136 for 131).
 // SHARED: one of two launches, as in paged_attend_dev.h.
 template <int D, int kQB, int W, bool PAIRS, bool EIGHT, bool SHARED>
 __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit &u) {
@@ -40,8 +41,9 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     constexpr int KK = D / 16, NF = D / 32; // 16-feature steps of the scores, 32-feature blocks of the output
     constexpr int kBuf = kFRows * kRowB;
     constexpr bool kPlain = W == 8;
+    constexpr int kValues = kPlain ? 2 : 3; // steps whose values are there
     constexpr int kFQ = 32 * kQB * W; // queries of the workgroup, kQB blocks of 32 a wave
-    __shared__ __align__(1024) unsigned char s_kv[5 * kBuf]; // keys of two steps, values of three
+    __shared__ __align__(1024) unsigned char s_kv[(2 + kValues) * kBuf]; // keys of two steps, and values
     __shared__ int64_t s_off[kRing][kFRows];                 // byte offset of a row
     __shared__ int64_t s_scale_off[EIGHT ? kRing : 1][EIGHT ? kFRows : 1]; // and of its scales
     __shared__ __align__(16) int s_ft[kRing][kFRows];        // first token that sees it
@@ -134,7 +136,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
     const int c_row = kWaveRows * wave + lane / kCodeLanes, c_piece = lane % kCodeLanes;
     auto put_down = [&](int t, const Codes &x) __attribute__((always_inline)) { // the rows of step t, requested before
         if (!EIGHT || t >= n_steps) return;
-        unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % 3) * kBuf;
+        unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % kValues) * kBuf;
 #pragma unroll
         for (int i = 0; i < kCodeLoads; ++i) {
             const int row = c_row + i * kCodeRows;
@@ -163,7 +165,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             request_codes(t, next);
             return;
         }
-        unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % 3) * kBuf;
+        unsigned char *const dk = s_kv + (t & 1) * kBuf, *const dv = s_kv + (2 + t % kValues) * kBuf;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int64_t off = s_off[t & (kRing - 1)][ld_row + i * kRowsPerLoad];
@@ -199,7 +201,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         for (int kk = 0; kk < KK; ++kk) k_at[kk] ^= kBuf;
     };
     auto next_values = [&](int t) __attribute__((always_inline)) { // from those of step t
-        const unsigned by = t % 3 == 2 ? 0u - 2u * kBuf : (unsigned)kBuf;
+        const unsigned by = t % kValues == kValues - 1 ? 0u - (kValues - 1u) * kBuf : (unsigned)kBuf;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             v_at[f][0] += by;
@@ -212,7 +214,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
         const i16x4 x = lds_read_tr16(s_kv + v_at[f][0] + at), y = lds_read_tr16(s_kv + v_at[f][1] + at);
         return __builtin_bit_cast(bf16x8, i16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
     };
-    auto values_of = [&](int h) { return s_kv + (2 + (h >> 1) % 3) * kBuf + (h & 1) * 32 * kRowB; };
+    auto values_of = [&](int h) { return s_kv + (2 + (h >> 1) % kValues) * kBuf + (h & 1) * 32 * kRowB; };
     // weights of query block i and 16 rows as a matrix operand
     auto weights_of = [&](const f32x16 &s, int i, int grp) __attribute__((always_inline)) {
         raw16 w;
@@ -397,6 +399,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             __builtin_amdgcn_sched_group_barrier(0x402, D == 128 ? 5 : 10, 0); // vector instructions beside it
         }
         __builtin_amdgcn_sched_barrier(0);
+        if (P == 0 && h > 0) put_down((h >> 1) + 1, next); // (requested a step before)
         // ---- the rest of the scores; values of the first 16 rows, weights of the others ----
 #pragma unroll
         for (int kk = K1; kk < KK; ++kk)
@@ -421,7 +424,6 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
             next_keys();
         } else {
             next_values(h >> 1);
-            put_down((h >> 1) + 2, next);
         }
         // ---- values of the other 16 rows; the scores go to where vector instructions reach them ----
         load_ahead(There{});
