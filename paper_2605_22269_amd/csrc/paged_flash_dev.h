@@ -1,7 +1,7 @@
 // Attention of many new tokens a sequence over a paged cache, or over packed sequences, on the matrix cores: bf16 rows of 64 or 128
-// features.  How rows are shared out and joined is as in paged_attend.hip.  The softmax differs in two things: what exponents subtract (the
+// features.  How rows are shared out and joined is as in paged_attend_dev.h.  The softmax differs in two things: what exponents subtract (the
 // largest score of a unit's first rows, see below), and the weights, which enter the product rounded to bf16, as the matrix cores take
-// them: as the pairs that paged_attend.hip multiplies by they would be twice the products.  Each weight is off by 2^-9 of itself at
+// them: as the pairs that paged_attend_dev.h multiplies by they would be twice the products.  Each weight is off by 2^-9 of itself at
 // most, no more than an output is by its own rounding: outputs are 0.0019-0.0023 off (2-norm, normal numbers), 0.0017 with that rounding alone.
 #pragma once
 
