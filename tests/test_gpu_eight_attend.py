@@ -179,3 +179,17 @@ def test_no_new_tokens():
     out = torch.zeros_like(w)
     c.attend(weights=w, weights_out=out, decay=0.25)
     assert (out[0] == 0.25).all() and (out[1, :, :5] == 0.25).all() and (out[1, :, 5:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("power", [-100, -60, 60, 100])
+def test_queries_and_rows_of_far_sizes(power, dtype):
+    """Queries times 2^power, keys times 2^-power: scores, and with them outputs, stay what they are.  (Of an fp32 query of 2^-100 the last part
+    may be less than the least normal number: 2^-126 2^100 of a key's size, 2^-2 of a rounding of a score, may be lost.)"""
+    c = Batch([(1, 500), (5, 60)], None, 128, 8, 2, 16, dtype, True, seed=9)
+    first = c.attend()
+    c.q *= 2.0**power
+    c.ks.view(torch.uint8)[:] -= power if power > 0 else power + 256
+    got = c.attend()
+    c.check(got)
+    assert torch.equal(got, first) or (dtype == F32 and power == -100)
