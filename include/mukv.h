@@ -808,7 +808,8 @@ int mukv_paged_evict8(const mukv_paged *pages, const mukv_row_scales *scales, co
  *                   (0: not known).  Where offsets do not ascend, out is left as it is
  *                   and weights are undefined
  *   weights, shared_weights   NULL, or where the weights of the sequences' own rows, of the
- *                   shared rows of every group go: the sum over all that see them
+ *                   shared rows of every group go: the sum over all that see them.  A group's
+ *                   tokens that are no sequence's (padding) see nothing
  *   workspace       at least mukv_paged_shared_workspace_size() bytes, otherwise as there
  *
  * What is shared is added up apart and joined to the rest in fp32 before the one rounding.

@@ -646,6 +646,7 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
             if (c == 0) {
                 *reinterpret_cast<f32x4 *>(a.shared.stats + 4 * place) = f32x4{m, l, l, 0.f};
                 leave_head(a.shared, u, kPQ, n, row);
+                if (a.pairs) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = f32x2{0.f, 0.f}; // (stays so if it is no sequence's)
             }
         } else if (u.chunks > 1) {
             if (c == 0) store_far(a.records.stats + ((int64_t)(u.record + u.chunk) * kPQ + n) * 2, m, l);
@@ -766,8 +767,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
                 q[kInParts ? 0 : kk] = has_piece ? brought_down<T, D>(qx[at][kk]) : raw16{0u, 0u, 0u, 0u};
             }
             const float ref = pair[at][0], inv = pair[at][1];
+            const int seer = inv == 0.f ? -1 : tok[at]; // (zero: sees no row, or is a group's token and no sequence's)
             const bool large = __builtin_amdgcn_ballot_w64(fabsf(ref) > kLargeRef) != 0; // (its rounding shows)
-            if (EIGHT && kBf16 && !late && !large && q0 + 16 <= n_queries) {
+            if (EIGHT && kBf16 && !late && !large && q0 + 16 <= n_queries && __builtin_amdgcn_ballot_w64(seer < 0) == 0) {
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -800,7 +802,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
                         w = __builtin_amdgcn_exp2f(large && fabsf(ref) > kLargeRef ? scaled_apart(sc[e], scale, ref) : fmaf(sc[e], scale, -ref));
                     else
                         w = large ? weight_of_any(sc[e], scale, ref) : weight_of(sc[e], scale, ref);
-                    sum[t][e] += tok[at] >= from[t][e] && tok[at] >= 0 ? w * inv : 0.f;
+                    sum[t][e] += seer >= from[t][e] && seer >= 0 ? w * inv : 0.f;
                 }
             }
         };

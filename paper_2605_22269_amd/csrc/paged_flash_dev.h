@@ -679,6 +679,7 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                 if (half == 0) {
                     *reinterpret_cast<f32x4 *>(a.shared.stats + 4 * place) = f32x4{at[i], l_sum[i], PAIRS ? l_all[i] : l_sum[i], 0.f};
                     leave_head(a.shared, u, kFQ, qq - u.tile * kFQ, row);
+                    if (PAIRS) *reinterpret_cast<f32x2 *>(a.pairs + 2 * row) = f32x2{0.f, 0.f}; // (stays so if it is no sequence's)
                 }
             }
         } else if (u.chunks > 1) {

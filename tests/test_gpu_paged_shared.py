@@ -209,3 +209,26 @@ def test_equal_shares_need_no_offsets():
     plain = c.cache.attend(1, i32(c.table), i32(c.lengths), c.q, shared=mk.Shared(i32(c.shared_table), i32(c.shared_lengths)))
     c.check(plain)
     assert torch.equal(plain, c.attend())
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS, ids=IDS)
+@pytest.mark.parametrize("D,new", [(64, 2), (128, 70), (64, 300)])
+def test_padding_behind_the_sequences(D, new, dtype, eight):
+    """Tokens of a group that are no sequence's are left as they are and count for no row's weight, whatever stands there."""
+    c = Batch([(new, new + 70), (1, 40), (new, new + 5)], [(new, 90), (1 + new, 200)], D, 8, 2, 16, dtype, eight, seed=new + D)
+    c.off[3] = c.off[2]                                             # the last sequence has none of its tokens
+    n = int(c.off[2])
+    for bad in (1e30, float("nan")):
+        c.q[n:] = bad
+        out = torch.full_like(c.q, 7.0)
+        own = torch.zeros(3, 2, c.table.shape[1] * 16, device="cuda")
+        common = torch.zeros(2, 2, c.shared_table.shape[1] * 16, device="cuda")
+        c.attend(out=out, weights_out=own, shared_weights_out=common)
+        assert (out[n:] == 7.0).all()
+        c.q[n:] = 0
+        want, received, shared, amean, reach = c.wanted()
+        near(f64(out)[:n], want[:n], c.error(amean, reach)[:n], dtype)
+        tol = c.weights_error(reach, c.T)
+        for got, want, lengths in ((own, received, c.lengths), (common, shared, c.shared_lengths)):
+            for b, m in enumerate(lengths):
+                near(f64(got)[b][:, :m], want[b], (1 + want[b]) * tol, F32)
