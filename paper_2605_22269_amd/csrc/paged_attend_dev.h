@@ -681,6 +681,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
     const int n_w = s.rows < a.weights_rows ? s.rows : a.weights_rows; // rows that have a weight
     const int past = s.length - s.n_new, n_queries = s.n_new * G;
     const float scale = a.scale_log2e * (1.f / query_factor<T, D>());
+    const bool padded = a.shared.mode == SharedResults::kLeave; // a group's tokens may be no sequence's: see no row, whatever stands there
     const bool has_piece = kPieces >= 4 || lg < kPieces;
     const int my_piece = kPieces >= 4 ? lg : lg & (kPieces - 1);
     constexpr int kRows = 16 * kTiles; // of a wave
@@ -767,9 +768,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
                 q[kInParts ? 0 : kk] = has_piece ? brought_down<T, D>(qx[at][kk]) : raw16{0u, 0u, 0u, 0u};
             }
             const float ref = pair[at][0], inv = pair[at][1];
-            const int seer = inv == 0.f ? -1 : tok[at]; // (zero: sees no row, or is a group's token and no sequence's)
-            const bool large = __builtin_amdgcn_ballot_w64(fabsf(ref) > kLargeRef) != 0; // (its rounding shows)
-            if (EIGHT && kBf16 && !late && !large && q0 + 16 <= n_queries && __builtin_amdgcn_ballot_w64(seer < 0) == 0) {
+            const bool none = padded && inv == 0.f;
+            const bool large = __builtin_amdgcn_ballot_w64(none || fabsf(ref) > kLargeRef) != 0; // (its rounding shows)
+            if (EIGHT && kBf16 && !late && !large && q0 + 16 <= n_queries) {
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -802,7 +803,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
                         w = __builtin_amdgcn_exp2f(large && fabsf(ref) > kLargeRef ? scaled_apart(sc[e], scale, ref) : fmaf(sc[e], scale, -ref));
                     else
                         w = large ? weight_of_any(sc[e], scale, ref) : weight_of(sc[e], scale, ref);
-                    sum[t][e] += seer >= from[t][e] && seer >= 0 ? w * inv : 0.f;
+                    sum[t][e] += tok[at] >= from[t][e] && tok[at] >= 0 && !none ? w * inv : 0.f;
                 }
             }
         };
