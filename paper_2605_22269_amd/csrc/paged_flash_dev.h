@@ -484,19 +484,30 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
                     for (int jj = 0; jj < 4; ++jj) x[f][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+                constexpr int kTogether = W == 8 ? 1 : 2; // chunks requested together, where there are registers (718 tokens of 16 users 106.2 us a call, one by one 110.3)
 #pragma unroll 1
-                for (int c = 0; c < t.chunks; ++c) {
-                    const float *const vp = a.shared.values + ((int64_t)t.place + (int64_t)c * t.stride) * D + 4 * half;
-                    const f32x2 st = *reinterpret_cast<const f32x2 *>(a.shared.stats + 4 * ((int64_t)t.place + (int64_t)c * t.stride));
-                    const float by = st[1] != 0.f ? __builtin_amdgcn_exp2f(st[0] - t.at) : -1.f;
+                for (int c0 = 0; c0 < t.chunks; c0 += kTogether) {
+                    f32x4 y[kTogether][NF][4];
+                    f32x2 st[kTogether];
 #pragma unroll
-                    for (int f = 0; f < NF; ++f)
+                    for (int n = 0; n < kTogether; ++n) {
+                        const int64_t place = t.place + (int64_t)(c0 + n < t.chunks ? c0 + n : c0) * t.stride;
+                        st[n] = *reinterpret_cast<const f32x2 *>(a.shared.stats + 4 * place);
 #pragma unroll
-                        for (int jj = 0; jj < 4; ++jj) {
-                            const f32x4 y = *reinterpret_cast<const f32x4 *>(vp + 32 * f + 8 * jj);
+                        for (int f = 0; f < NF; ++f)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[f][jj][e] = by < 0.f ? x[f][jj][e] : fmaf(y[e], by, x[f][jj][e]);
-                        }
+                            for (int jj = 0; jj < 4; ++jj) y[n][f][jj] = *reinterpret_cast<const f32x4 *>(a.shared.values + place * D + 4 * half + 32 * f + 8 * jj);
+                    }
+#pragma unroll
+                    for (int n = 0; n < kTogether; ++n) {
+                        const float by = c0 + n < t.chunks && st[n][1] != 0.f ? __builtin_amdgcn_exp2f(st[n][0] - t.at) : -1.f;
+#pragma unroll
+                        for (int f = 0; f < NF; ++f)
+#pragma unroll
+                            for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) x[f][jj][e] = by < 0.f ? x[f][jj][e] : fmaf(y[n][f][jj][e], by, x[f][jj][e]);
+                    }
                 }
                 const JoinBy by = join_by(at[i], l_sum[i], t.at, t.sum);
                 if (by.other == 0.f) continue;
