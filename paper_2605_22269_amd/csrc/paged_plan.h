@@ -195,8 +195,9 @@ MUKV_HD int64_t units_bound(const PagedView &v, const PlanShape &p) {
     const int64_t room = v.table ? room_of(v) : v.n_tokens; // (packed: a sequence has no more rows than there are tokens)
     int64_t chunks = div_up(room, p.rows);
     chunks = chunks > p.most ? p.most : chunks < 1 ? 1 : chunks;
-    // with start: all units are within the records if any tile has two chunks; without: tiles of one chunk come on top
-    const int64_t split = p.start ? (tiles > most_units(p) ? tiles : most_units(p)) : tiles + p.records;
+    // with start: all units are within the records if any tile has two chunks; without: a tile's chunks are less than one more than its blocks by
+    // those of a chunk, of which there are at most records / 2.002 (chunk_by_room)
+    const int64_t split = p.start ? (tiles > most_units(p) ? tiles : most_units(p)) : tiles + p.records / 2 + 1;
     return tiles * chunks < split ? tiles * chunks : split;
 }
 
