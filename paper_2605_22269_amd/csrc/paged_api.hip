@@ -165,9 +165,9 @@ struct Space {
 int64_t hint_of(const mukv_seqs &s) { return s.max_new > 0 ? s.max_new : mukv::div_up(s.n_tokens, s.n_seqs); } // new tokens of a sequence
 int64_t up_to_16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 mukv::PlanShape plan_of(const mukv_paged &p, const mukv_seqs &s, bool causal, bool eight, bool *prompts) {
-    const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype, p.head_dim, hint_of(s));
+    const int tile = mukv::paged_prompt_tile(view_of(p, 0, s), p.dtype == MUKV_BF16, p.head_dim, hint_of(s));
     *prompts = tile != 0;
-    return mukv::paged_plan(p.dtype, tile, causal, eight);
+    return mukv::paged_plan(p.dtype == MUKV_BF16, tile, causal, eight);
 }
 // eight: rows in 8 bits, which takes the same space
 Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared, bool causal, bool with_weights, bool eight = false) {
@@ -182,7 +182,7 @@ Space space_of(const mukv_paged &p, const mukv_seqs &s, const mukv_seqs *shared,
     const int64_t queries = (int64_t)s.n_tokens * p.n_q_heads;
     x.bytes = x.pairs + (with_weights ? 8 * queries : 0);
     if (shared) { // places for the queries of as many chunks as there can be, then for those of tiles with one
-        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype, p.head_dim, hint_of(*shared), eight);
+        x.shared_plan = mukv::shared_plan(view_of(p, 0, *shared), p.dtype == MUKV_BF16, p.head_dim, hint_of(*shared), eight);
         x.single = x.shared_plan.records * x.shared_plan.queries;
         x.fit = up_to_16(x.bytes);
         x.left_heads = x.fit + 16;

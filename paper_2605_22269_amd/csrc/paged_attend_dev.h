@@ -17,7 +17,7 @@ namespace mukv {
 
 namespace {
 
-constexpr int kPQ = 16, kPWaves = 4; // queries and waves of a workgroup
+constexpr int kPWaves = 4; // of a workgroup, which has kPQ queries
 
 // Keys of 8 bits as the rows of a score: a lane of four has D / 4 neighbouring codes (or two such runs of 16), which are one operand after
 // the other.

@@ -794,14 +794,6 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
 
 } // namespace
 
-// Whether one sequence's tiles may be shared out evenly: to look at that takes the kernel a microsecond, so not where it gains nothing:
-// few tiles, which come out even in chunks, more than twice the compute units, or few rows (us a launch without / with, 28/4 heads of 128:
-// 200 tokens over 20000 rows 89 / 93, 300 alone 14.5 / 15.6, 1000 29.8 / 31.0, 2000 55.0 / 57.3; the gains are at the kernel).
-static bool may_share(const PagedView &v, const PlanShape &p) {
-    if (p.units) return v.n_seqs == 1; // shared rows of one group
-    const int64_t tiles = div_up((int64_t)v.n_tokens * v.G, p.queries) * v.Hkv, room = v.table ? room_of(v) : v.n_tokens;
-    return v.n_seqs == 1 && tiles > 64 && tiles <= p.records - p.places && room >= 4096;
-}
 template <int D, int kQB, int W, bool PAIRS, bool EIGHT, bool SHARED>
 static void start_flash(const PagedAttendArgs &a, unsigned grid, hipStream_t st) {
     if (may_share(a.view, a.plan))

@@ -24,15 +24,6 @@ hipError_t launch_rope(const RopeArgs &a, int dtype, hipStream_t st);
 // k and v to pages of 8 bits; read: from them to k.out and v.out
 hipError_t launch_rows8(const RopeArgs &a, int dtype, bool read, hipStream_t st);
 
-// Which kernel takes an attention call follows from types and sizes that the host knows (paged_attend.hip): 0 that for any shape, otherwise
-// the one for prompts, with tiles of so many queries.  new_hint: new tokens of a sequence, as far as that is known.
-int paged_prompt_tile(const PagedView &v, int dtype, int D, int64_t new_hint);
-PlanShape paged_plan(int dtype, int prompt_tile, bool causal, bool eight);
-// The same for rows that groups share, where chunks are left, not joined.
-PlanShape shared_plan(const PagedView &groups, int dtype, int D, int64_t new_hint, bool eight);
-constexpr int kPlanChunks = 64;     // most chunks of a sequence
-constexpr int kPlanRecords = 2048;  // most that any plan has: the counts at a workspace's start
-
 // What a chunk of a tile's rows leaves for whoever joins them: per query, what its exponents subtracted and the sum of its weights, and its
 // unnormalised output.
 struct ChunkRecords {
@@ -51,7 +42,7 @@ struct SharedResults {
     int mode;
     int n_groups;
     const int32_t *offsets; // of the groups' tokens; tokens before the first and behind the last are no group's.  Null: all are some group's
-    int32_t *heads;         // [n_tokens * Hq][4]: chunks, the first one's place, places from one to the next
+    int32_t *heads;         // [n_tokens * Hq][4]: chunks (kPlanChunks at most: PlanShape::left), the first one's place, places from one to the next
     float *values;          // [place][D]
     float *stats;           // [place][4]
     int single;             // place of query 0 of tiles with one chunk
