@@ -452,7 +452,8 @@ int mukv_paged_attend8(const mukv_paged *pages, const mukv_row_scales *scales, i
 int mukv_paged_shared_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_seqs *shared, int32_t with_weights,
                                      int64_t *bytes_out) {
     if (!bytes_out || (with_weights != 0 && with_weights != 1)) return MUKV_ERR_INVALID_ARG;
-    if (const int rc = check_pages(pages, false, true)) return rc; // (either kind of pages: only counts are read)
+    // (only counts are read, of either kind of pages: strides that suit bytes suit elements of the payload dtype, but not the other way round)
+    if (const int rc = check_pages(pages)) return rc;
     if (const int rc = check_seqs(pages, seqs, false, true)) return rc;
     if (const int rc = check_seqs(pages, shared, false, true)) return rc;
     if (shared->n_tokens != seqs->n_tokens) return MUKV_ERR_SHAPE;
