@@ -608,9 +608,9 @@ __global__ __launch_bounds__(64 * kPWaves) __attribute__((amdgpu_waves_per_eu(D 
                 }
                 const JoinBy by = join_by(m, l, t.at, t.sum);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = by.other == 0.f ? o[e] : fmaf(x[e], by.other, by.own == 0.f ? 0.f : o[e] * by.own);
-                l_all = (by.own == 0.f ? 0.f : l * by.own) + (by.other == 0.f ? 0.f : t.sum_all * by.other);
-                l = (by.own == 0.f ? 0.f : l * by.own) + (by.other == 0.f ? 0.f : t.sum * by.other);
+                for (int e = 0; e < 4; ++e) o[e] = by.other < 0.f ? o[e] : fmaf(x[e], by.other, counted(o[e], by.own));
+                l_all = counted(l, by.own) + counted(t.sum_all, by.other);
+                l = counted(l, by.own) + counted(t.sum, by.other);
                 m = by.at;
             }
         }

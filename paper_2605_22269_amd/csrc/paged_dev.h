@@ -201,7 +201,8 @@ __device__ __forceinline__ bool in_a_group(const SharedResults &r, int token) {
     return !r.offsets || (token >= r.offsets[0] && token < r.offsets[r.n_groups]);
 }
 // How two parts of a row's softmax become one: what each is multiplied by, and what weights are relative to then.  A part without
-// weights (their sum is zero; a NaN is not) counts for nothing.
+// weights (their sum is zero; a NaN is not) counts for nothing: -1.  One that weighs so little that its factor is zero is multiplied by that all
+// the same, so that what is no number in it still reaches the output, as in a sum over all rows.
 struct JoinBy {
     float at, own, other;
 };
@@ -209,10 +210,12 @@ __device__ __forceinline__ JoinBy join_by(float at, float sum, float other_at, f
     const bool some = sum != 0.f, others = other_sum != 0.f;
     JoinBy j;
     j.at = some && others ? fmaxf(at, other_at) : others ? other_at : at;
-    j.own = some ? (others ? __builtin_amdgcn_exp2f(at - j.at) : 1.f) : 0.f;
-    j.other = others ? (some ? __builtin_amdgcn_exp2f(other_at - j.at) : 1.f) : 0.f;
+    j.own = some ? (others ? __builtin_amdgcn_exp2f(at - j.at) : 1.f) : -1.f;
+    j.other = others ? (some ? __builtin_amdgcn_exp2f(other_at - j.at) : 1.f) : -1.f;
     return j;
 }
+// x, which is zero where by, a factor of one of the two, is -1
+__device__ __forceinline__ float counted(float x, float by) { return by < 0.f ? 0.f : x * by; }
 
 // What a lane leaves of a unit's query n (query `row` among the outputs): where.
 __device__ __forceinline__ int place_left(const SharedResults &r, const Unit &u, int queries, int n, int64_t row) {

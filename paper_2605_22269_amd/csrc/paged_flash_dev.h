@@ -511,14 +511,13 @@ __device__ __forceinline__ void flash_unit(const PagedAttendArgs &a, const Unit 
                     }
                 }
                 const JoinBy by = join_by(at[i], l_sum[i], t.at, t.sum);
-                if (by.other == 0.f) continue;
-                const bool some = by.own != 0.f;
+                if (by.other < 0.f) continue;
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[i][f][j] = fmaf(x[f][j / 4][j % 4], by.other, some ? o[i][f][j] * by.own : 0.f);
-                l_sum[i] = fmaf(t.sum, by.other, some ? l_sum[i] * by.own : 0.f);
-                if (PAIRS) l_all[i] = fmaf(t.sum_all, by.other, some ? l_all[i] * by.own : 0.f);
+                    for (int j = 0; j < 16; ++j) o[i][f][j] = fmaf(x[f][j / 4][j % 4], by.other, counted(o[i][f][j], by.own));
+                l_sum[i] = fmaf(t.sum, by.other, counted(l_sum[i], by.own));
+                if (PAIRS) l_all[i] = fmaf(t.sum_all, by.other, counted(l_all[i], by.own));
                 at[i] = by.at;
             }
         }
