@@ -848,11 +848,9 @@ template <typename T, int D, bool EIGHT, int kTiles, bool SPLIT = false>
 hipError_t launch_weights(const PagedAttendArgs &a, hipStream_t st) {
     constexpr int kRows = (SPLIT ? 1 : 4) * 16 * kTiles; // of a workgroup
     const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
-    int64_t groups = (rows + kRows - 1) / kRows, most = 8192 / ((int64_t)a.view.Hkv * a.view.n_seqs);
-    if (most < 16) most = 16;
-    if (groups > most) groups = most; // (a workgroup goes round: a table is often wider than its sequences)
+    const int groups = weight_groups(rows, kRows, (int64_t)a.view.Hkv * a.view.n_seqs);
     if (groups < 1) return hipSuccess;
-    hipLaunchKernelGGL((paged_weights_kernel<T, D, EIGHT, kTiles, SPLIT>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, (int)groups);
+    hipLaunchKernelGGL((paged_weights_kernel<T, D, EIGHT, kTiles, SPLIT>), dim3((unsigned)groups, a.view.n_seqs, a.view.Hkv), dim3(256), 0, st, a, groups);
     return hipGetLastError();
 }
 

@@ -277,6 +277,16 @@ inline PlanShape shared_plan(const PagedView &groups, bool bf16, int D, int64_t 
     p.records = p.places + 8 + (int)tiles;
     return p;
 }
+// Workgroups that share a list's rows, `per` at a time, where weights of rows are worked out.  They go round: a table is often wider than its
+// sequences.  A round is at most 2^20 rows, so that the number of a workgroup's next row behind a sequence of 2^31 - 2^20 of them, the most there are,
+// is still one of 32 bits.
+MUKV_HD int weight_groups(int64_t rows, int per, int64_t lists) {
+    int64_t most = 8192 / lists;
+    if (most < 16) most = 16;
+    if (most > (1 << 20) / per) most = (1 << 20) / per;
+    const int64_t groups = div_up(rows, per);
+    return (int)(groups < most ? groups : most);
+}
 // Whether one sequence's tiles may be shared out evenly: to look at that takes the kernel a microsecond, so not where it gains nothing:
 // few tiles, which come out even in chunks, more than twice the compute units, or few rows (us a launch without / with, 28/4 heads of 128:
 // 200 tokens over 20000 rows 89 / 93, 300 alone 14.5 / 15.6, 1000 29.8 / 31.0, 2000 55.0 / 57.3; the gains are at the kernel).
