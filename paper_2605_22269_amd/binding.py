@@ -801,8 +801,32 @@ class _Sequences:
             weights_in = weights.data_ptr()
         return _WEIGHTS.pack(weights_in, weights_out.data_ptr(), 0, st[0], st[1], weights_out.shape[2], decay)
 
-    def _space(self, need, index, stream, device):
-        """Address and size of scratch for a call on this stream."""
+    def _attend(self, pages, s, index, heads, key, layer, q, causal, out, weights, weights_out, decay, shared=None, shared_weights=None,
+                shared_weights_out=None):
+        """heads: sequences and KV heads; key: all that the scratch's size follows from, but for shared rows.  (One function: what is passed through
+        on the way shows where a launch takes a few microseconds.)"""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
+        assert q.get_device() == index
+        w = sw = None
+        if weights_out is not None or weights is not None:
+            w = self._weights(weights, weights_out, heads, index, decay)
+        stream = _stream_of(index)
+        if shared is None:
+            need = self._need
+            if need[0] != key:
+                need = self._need = key, mukv_paged_workspace_size(pages, s, int(w is not None))
+        else:
+            assert shared.index == index
+            if shared_weights_out is not None or shared_weights is not None:
+                sw = self._weights(shared_weights, shared_weights_out, (shared.n, heads[1]), index, decay)
+            groups, need = shared.pack(q.shape[0]), self._shared_need
+            key = *key, sw is None, shared.n, shared.width, shared.max_tokens
+            if need[0] != key:
+                need = self._shared_need = key, mukv_paged_shared_workspace_size(pages, s, groups, int(w is not None or sw is not None))
+        need = need[1]
         capture = C.c_uint64()
         rc = self._c_capture(stream, C.byref(capture))
         if rc:
@@ -811,28 +835,17 @@ class _Sequences:
         place = index, stream, capture != 0
         ws = self._scratch.get(place)
         if ws is None or ws[1] < need or ws[3] != capture:
-            t = torch.empty(need, dtype=torch.uint8, device=device)
+            t = torch.empty(need, dtype=torch.uint8, device=q.device)
             t[:MUKV_PAGED_CLEAR].zero_()   # every call finds and leaves it so
             ws = self._scratch[place] = t.data_ptr(), need, t, capture
-        return ws
-
-    def _attend(self, pages, s, index, heads, key, layer, q, causal, out, weights, weights_out, decay):
-        """heads: sequences and KV heads; key: all that the scratch's size follows from."""
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        strides = _STRIDES.get(q.stride()) or _rows(q)
+        if shared is None:
+            rc = self._c_attend(pages, layer, s, q.data_ptr(), strides, 1 if causal else 0, out.data_ptr(), w, ws[0], ws[1], stream)
         else:
-            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
-        assert q.get_device() == index
-        w = self._weights(weights, weights_out, heads, index, decay)
-        stream = _stream_of(index)
-        need = self._need
-        if need[0] != key:
-            need = self._need = key, mukv_paged_workspace_size(pages, s, int(w is not None))
-        ws = self._space(need[1], index, stream, q.device)
-        rc = self._c_attend(pages, layer, s, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q), 1 if causal else 0, out.data_ptr(),
-                            w, ws[0], ws[1], stream)
+            rc = self._c_shared(pages, self._scales_at, layer, s, groups, q.data_ptr(), strides, 1 if causal else 0, out.data_ptr(), w, sw, ws[0],
+                                ws[1], stream)
         if rc:
-            _check(rc, "mukv_paged_attend")
+            _check(rc, "mukv_paged_attend" if shared is None else "mukv_paged_attend_shared")
         return out
 
 
@@ -931,25 +944,8 @@ class PagedKV(_Sequences):
         if shared is None:
             assert shared_weights is None and shared_weights_out is None
             return self._attend(self._pages_at, s, self._index, (n, self._heads), key, layer, q, causal, out, weights, weights_out, decay)
-        index = self._index
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        else:
-            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
-        assert q.get_device() == index and shared.index == index
-        w = self._weights(weights, weights_out, (n, self._heads), index, decay)
-        sw = self._weights(shared_weights, shared_weights_out, (shared.n, self._heads), index, decay)
-        groups = shared.pack(T)
-        stream, need = _stream_of(index), self._shared_need
-        key = *key, sw is None, shared.n, shared.width, shared.max_tokens
-        if need[0] != key:
-            need = self._shared_need = key, mukv_paged_shared_workspace_size(self._pages_at, s, groups, int(w is not None or sw is not None))
-        ws = self._space(need[1], index, stream, q.device)
-        rc = self._c_shared(self._pages_at, self._scales_at, layer, s, groups, q.data_ptr(), _STRIDES.get(q.stride()) or _rows(q),
-                            1 if causal else 0, out.data_ptr(), w, sw, ws[0], ws[1], stream)
-        if rc:
-            _check(rc, "mukv_paged_attend_shared")
-        return out
+        return self._attend(self._pages_at, s, self._index, (n, self._heads), key, layer, q, causal, out, weights, weights_out, decay, shared,
+                            shared_weights, shared_weights_out)
 
     def evict(self, table, lengths, weights, budget, *, sink=0, recent=0, into=None, weights_out=None, kept=None, lengths_out=None):
         """Brings every sequence down to `budget` rows per layer and KV head: the first `sink`, the last `recent`, and the others

@@ -36,9 +36,10 @@ def test_others_are_refused(kw, status):
 def test_the_python_call_takes_them(dtype, row, monkeypatch):
     at = lambda: Stand(1, 9, 2, 16, 64, dtype=dtype, strides=(row * 16 * 18, row * 32, row * 16, row, 1))  # noqa: E731
     c, reached = mk.PagedKV(at(), at(), n_q_heads=4), []
+    real = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: real(*a, **kw))
     monkeypatch.setattr(mk, "_stream_of", lambda index: 0)
-    monkeypatch.setattr(c, "_space", lambda need, *rest: reached.append(need) or (1 << 20, need))
-    c._c_shared = lambda *a: 0
+    c._c_shared, c._c_capture = (lambda *a: reached.append(a[-2]) or 0), lambda stream, at: 0   # bytes of scratch
     kind = "b" if dtype is torch.bfloat16 else "f"
     t = tensors({}, **SEQUENCES, q=(kind, 3, 4, 64), out=(kind, 3, 4, 64))
     group = mk.Shared(*tensors({}, table=("i", 1, 6), lengths=("i", 1), offsets=("i", 2)).values())
