@@ -778,7 +778,8 @@ int mukv_paged_read8(const mukv_paged *pages, const mukv_row_scales *scales, int
 /*
  * mukv_paged_attend over a cache in 8 bits (seqs->table is not NULL), with the same
  * workspace: rows count for what mukv_paged_read8 gives, and everything that is said
- * there holds.
+ * there holds.  fp32 queries are multiplied in three parts of 8 bits each: of a feature
+ * below 2^-107 the last ones may be lost.
  */
 int mukv_paged_attend8(const mukv_paged *pages, const mukv_row_scales *scales, int32_t layer, const mukv_seqs *seqs,
                        const void *q, const mukv_strides *q_strides, int32_t causal, void *out, const mukv_row_weights *weights,
@@ -794,7 +795,7 @@ int mukv_paged_evict8(const mukv_paged *pages, const mukv_row_scales *scales, co
 /*
  * Attention where groups of sequences share rows (a video that several users ask
  * about, instructions before every conversation): the shared rows lie in the pages once
- * and are read once for all of a group's tokens.  A token sees all rows that its group
+ * and are read for many of a group's tokens at a time.  A token sees all rows that its group
  * shares and, as in mukv_paged_attend, those of its sequence (causal: up to its own); one
  * softmax goes over both.
  *
@@ -813,6 +814,12 @@ int mukv_paged_evict8(const mukv_paged *pages, const mukv_row_scales *scales, co
  *   workspace       at least mukv_paged_shared_workspace_size() bytes, otherwise as there
  *
  * What is shared is added up apart and joined to the rest in fp32 before the one rounding.
+ * A group's new tokens are to its rows what a prompt's are to a sequence's.  With bf16 payloads,
+ * heads of 64 or 128, 48 or more queries of a group to a KV head (a query is a token and a head;
+ * by shared->max_new, or else n_tokens / n_seqs) and 1000 in all, the kernel for many tokens takes
+ * them: shared rows are read once for 128 or 256 of these queries, and weighed by weights
+ * rounded to bf16 -- those of single tokens too, whose weights over rows of their own have
+ * 16 bits.  Other calls read shared rows once for 16 queries and weigh them as own ones.
  * Errors: as mukv_paged_attend; SHAPE (n_tokens differ).
  */
 int mukv_paged_shared_workspace_size(const mukv_paged *pages, const mukv_seqs *seqs, const mukv_seqs *shared, int32_t with_weights,

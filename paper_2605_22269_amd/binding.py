@@ -851,7 +851,8 @@ class _Sequences:
 
 class Shared:
     """Rows that groups of sequences share: table int32 [group][page], lengths int32 [group], offsets int32 [group+1] -- group g's new
-    tokens are offsets[g] .. offsets[g+1]-1 of a call's (None: as many each).  max_tokens: most of a group, as a hint."""
+    tokens are offsets[g] .. offsets[g+1]-1 of a call's (None: as many each).  max_tokens: most of a group, as a hint.  To shared rows a
+    group's tokens are as one prompt: in bf16, many of them weigh these rows by weights rounded to bf16, single tokens too."""
 
     def __init__(self, table, lengths, offsets=None, *, max_tokens=0):
         n, width = table.shape

@@ -882,7 +882,8 @@ hipError_t launch_weights_typed(const PagedAttendArgs &a, hipStream_t st) {
     if (EIGHT || a.shared.mode != SharedResults::kNone) { // (other calls' sums stay in the order that they have been in)
         const int64_t room = a.view.table ? room_of(a.view) : a.view.page_rows, rows = room < a.weights_rows ? room : a.weights_rows;
         // (us a call, without / with: 64/8 heads of 128 over 6272 shared rows in bf16, 256 tokens 222 / 188, 16 tokens 53 / 57; 128 tokens over 1548, heads
-        // of 64, 93 / 62; 16 tokens over 20000 rows in 8 bits, 28/4 heads, 53.5 / 56.5)
+        // of 64, 93 / 62; 16 tokens over 20000 rows in 8 bits, 28/4 heads, 53.5 / 56.5.  With few queries not all four waves have some: 5 tokens,
+        // 35 queries to a KV head, over 1500, 4000 and 8000 rows 19.6 / 18.0, 21.7 / 20.1 and 25.7 / 25.7; 16 tokens 22.9 / 19.8, 26.5 / 23.1, 32.0 / 29.6)
         const int64_t groups = div_up(rows, 64) * a.view.n_seqs * a.view.Hkv, queries = (int64_t)a.view.n_tokens * a.view.G / a.view.n_seqs;
         if (groups < 512 || (groups < 2048 && queries >= 512)) return launch_weights<T, D, EIGHT, EIGHT || sizeof(T) == 2 ? 4 : 2, true>(a, st);
     }

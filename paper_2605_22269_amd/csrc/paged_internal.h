@@ -29,7 +29,7 @@ hipError_t launch_rows8(const RopeArgs &a, int dtype, bool read, hipStream_t st)
 struct ChunkRecords {
     float *stats;  // [record][queries][2]
     float *values; // [record][queries][D]
-    float *sums;   // [record][queries]: of weights that the values were not multiplied by as they are, before their rounding (paged_flash.hip,
+    float *sums;   // [record][queries]: of weights that the values were not multiplied by as they are, before their rounding (paged_flash_dev.h,
                    // where the weights of rows are asked for)
 };
 

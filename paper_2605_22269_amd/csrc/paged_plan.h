@@ -256,11 +256,12 @@ inline PlanShape paged_plan(bool bf16, int prompt_tile, bool causal, bool eight)
 }
 
 // Which kernel takes rows that groups share, and its plan: chunks are left, not joined, so that tiles are better small and many units cheap.
-// us a call, what the rule takes marked (any / prompts in tiles of 128 / of 256): 8 users over 6272 rows, 28/4 heads of 128, 27.3* / 31.8 / 41.6; 16 over
-// 500 18.1* / 20.9 / 27.1; 48 users in three rooms of 2113 to 6272 45.7 / 40.5* / 55.2; 64 in eight rooms 57.3 / 42.7* / 60.5; 64 users, 64/8 heads,
-// over 10000 rows in 8 bits 111 / 57* / 65, over 40000 408 / 175 / 171*; 718 tokens over 6272, 28/4 heads, 303 / 127 / 118*.
+// us a call, single tokens over 20 to 900 rows of their own too, what the rule takes marked (any / prompts in tiles of 128 / of 256): 8 users over
+// 6272 rows, 28/4 heads of 128, 27.1* / 32.1 / 37.7; 16 over 500 20.7* / 26.1 / 29.6; 48 users in three rooms of 2113 to 6272 44.9 / 39.9* / 46.7;
+// 64 in eight rooms 62.5 / 46.7* / 57.2; 64 users of 100 to 3000 rows, 64/8 heads, over 10000 rows in 8 bits 153 / 86.7* / 90.9, over 40000
+// 470 / 173 / 151*; 718 tokens of prompts over 6272, 28/4 heads, 305 / 126 / 106*.
 // Workgroups without a unit still have to start, after all that have one.  Few tiles: no more units than places, or one group's tiles
-// shared out step by step, which leaves no place without work either (the last two cases above: 171.6 and 121.8 with 704 units).
+// shared out step by step, which leaves no place without work either (the last two cases above: 153 and 110 with 704 units).
 inline PlanShape shared_plan(const PagedView &groups, bool bf16, int D, int64_t new_hint, bool eight) {
     const int64_t queries = new_hint * groups.G, tiles256 = div_up(queries, 256) * groups.n_seqs * groups.Hkv;
     int tile = 0;
